@@ -302,6 +302,108 @@ int cg_net_tensor(const cg_net *net, int layer, int which, void *ws, float **ptr
  * with respect to the rectifier's output is not materialised.) */
 long long cg_net_tensor_image_stride(const cg_net *net, int layer);
 
+/* ---- the operators of an attention sublayer -------------------------------
+ *
+ * Dropout without a stored mask, layer norm, and attention over packed sequences,
+ * each with its backward pass.  They take tensors in fp32 or bf16 (one type for
+ * all the tensors of a call that are typed `void *`); gains, shifts, statistics,
+ * bias tables and their gradients are fp32.  Sums, statistics and softmax are
+ * held in fp32; a bf16 result is rounded once (nearest even).  Apart from what
+ * follows, the conventions at the top of this file hold:
+ *  - Rows may lie in wider tensors: a row stride or a token stride is given in
+ *    elements, the elements of a row (of a head) lie next to each other.  Nothing
+ *    but the type's own size is asked of a pointer's or a stride's alignment;
+ *    fp32 statistics, tables and gradients of weights are dense.
+ *  - Every sum is taken in a fixed order: results are the same bits run to run. */
+enum { CG_TYPE_FP32 = 0, CG_TYPE_BF16 = 1 };
+
+/* Dropout whose mask is a function of (seed, offset, element) and is never stored.
+ * Element e (row * cols + column) belongs to block e / 8 of Philox4x32-10 with the
+ * key `seed` and the counter (e / 8, offset), low words first; it takes the 16 bits
+ * e % 8 of the block's four words (low halves first) and is kept if they are at
+ * least t = min(65535, floor(65536 p + 1/2)).  What is kept is multiplied by
+ * 65536 / (65536 - t), what is not is 0 whatever it was.  0 <= p < 1.  Two calls
+ * with the same numbers drop the same elements: forward and backward of a layer
+ * pass the same, another layer or step another seed or offset. */
+typedef struct { double p; uint64_t seed, offset; } cg_drop;
+
+/* y = drop(x) + add, rows x cols elements of `type`; add may be NULL.  *_ld: elements
+ * from a row to the next.  rows = 0 and cols = 0 are no-ops.
+ * rows * cols < 2^31. */
+int cg_dropout_fwd(const cg_drop *drop, int type, int64_t rows, int64_t cols, const void *x, int64_t x_ld,
+                   const void *add, int64_t add_ld, void *y, int64_t y_ld, void *stream);
+/* dx = drop(dy), the same elements (the gradient of add is dy itself). */
+int cg_dropout_bwd(const cg_drop *drop, int type, int64_t rows, int64_t cols, const void *dy, int64_t dy_ld,
+                   void *dx, int64_t dx_ld, void *stream);
+
+/* Layer norm over the rows of x [rows][cols]:  y = (x - mean) * rstd * gamma + beta,
+ * rstd = 1 / sqrt(mean((x - mean)^2) + eps).  cols >= 1; rows = 0 gives empty outputs
+ * and zero gradients of the weights.  rows * cols < 2^31. */
+typedef struct { int type; int64_t rows, cols; float eps; } cg_layernorm_desc;
+
+/* mean, rstd [rows]: kept for the backward pass; both NULL where there is none.
+ * beta and gamma: [cols] fp32. */
+int cg_layernorm_fwd(const cg_layernorm_desc *d, const void *x, int64_t x_ld, const float *gamma, const float *beta,
+                     void *y, int64_t y_ld, float *mean, float *rstd, void *stream);
+/* Bytes of workspace of either backward pass below. */
+size_t cg_layernorm_workspace_bytes(const cg_layernorm_desc *d);
+/* dx = gradient through the norm (+ dsum, the gradient that reaches x past the norm; NULL: none),
+ * dgamma = sum over rows of dy * (x - mean) * rstd, dbeta = sum over rows of dy. */
+int cg_layernorm_bwd(const cg_layernorm_desc *d, const void *dy, int64_t dy_ld, const void *x, int64_t x_ld,
+                     const float *gamma, const float *mean, const float *rstd, const void *dsum, int64_t dsum_ld,
+                     void *dx, int64_t dx_ld, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream);
+
+/* The end of a sublayer and the beginning of the next in one pass:
+ *     sum = x + drop(branch)   (rounded to `type`: a tensor of the net),   y = layer norm of sum. */
+int cg_dropout_add_layernorm_fwd(const cg_layernorm_desc *d, const cg_drop *drop, const void *branch, int64_t branch_ld,
+                                 const void *x, int64_t x_ld, const float *gamma, const float *beta, void *sum,
+                                 int64_t sum_ld, void *y, int64_t y_ld, float *mean, float *rstd, void *stream);
+/* dx = the gradient of sum: through the norm, + dsum (NULL: none); dbranch = drop(dx). */
+int cg_dropout_add_layernorm_bwd(const cg_layernorm_desc *d, const cg_drop *drop, const void *dy, int64_t dy_ld,
+                                 const void *dsum, int64_t dsum_ld, const void *sum, int64_t sum_ld, const float *gamma,
+                                 const float *mean, const float *rstd, void *dx, int64_t dx_ld, void *dbranch,
+                                 int64_t dbranch_ld, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream);
+
+/* Attention over B packed sequences.  Queries [Tq][Hq][D], keys and values [Tk][Hkv][D];
+ * sequence b has the query tokens cu_q[b] .. cu_q[b+1]-1 and the key tokens cu_k[b] .. cu_k[b+1]-1
+ * (device arrays of B + 1 ascending int32; lengths, zero among them, are read on the device, so
+ * nothing is waited for).  Query head h reads key-value head h / (Hq / Hkv).  With n queries and
+ * m keys, query i of a sequence stands at position i + m - n of its keys: the last query beside the last key.
+ *     s_ij = scale * <q_i, k_j> + bias[h][bucket(j - (i + m - n))],   o_i = sum_j softmax_j(s_ij) v_j,
+ *     lse_i = log sum_j exp(s_ij),    causal: only keys j <= i + m - n.
+ * A row that sees no key has o = 0, lse = -inf and passes no gradient on.  scale > 0, finite.
+ * bias (buckets > 0): a table [Hq][buckets] fp32, -inf allowed.  With n = buckets / 2 if `both`, else buckets,
+ * and E = n / 2, a distance dist = max(0, -delta) (both: |delta|) below E has its own bucket, the
+ * others have min(n - 1, E + floor(log(dist / E) / log(max_distance / E) * (n - E))); both: keys behind the query
+ * (delta > 0) have the buckets n .. 2n - 1.  n >= 2, buckets <= 256, n / 2 < max_distance <= 65536.
+ * *_tok, *_head: elements from a token and from a head to the next.  The strides of o are also those of o_rest and
+ * do; those of q, k and v also those of dq, dk and dv.
+ * 1 <= D <= 128; Tq * Hq, Tk * Hkv < 2^31; tensors may exceed 2^31 bytes.
+ * Arithmetic: bf16 tensors are multiplied as they are, the probabilities and the gradients of the scores
+ * rounded to bf16 for their products; fp32 tensors as three bf16 numbers in six products (CG_MATH_FP32 above).
+ * Sequences that overlap or reach past Tq, Tk are cut there; rows of no sequence are neither read nor written. */
+typedef struct {
+    int type, B, Hq, Hkv, D;
+    int64_t Tq, Tk;
+    int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
+    float scale;
+    int causal;
+    int buckets, max_distance, both;
+} cg_attn_desc;
+
+/* pass: CG_PASS_FWD or CG_PASS_BWD_DATA (0 for an invalid descriptor or pass). */
+size_t cg_attn_workspace_bytes(const cg_attn_desc *d, int pass);
+/* lse [Hq][Tq] fp32.  o_rest (bf16 tensors in a training step; else NULL): what o lost when it was rounded, kept for the
+ * backward pass.  With a bias it also has the probabilities multiplied in two bf16 numbers, at half the forward
+ * product's time again: the gradient of the bias is a sum of differences that a rounded o would spoil. */
+int cg_attn_fwd(const cg_attn_desc *d, const void *q, const void *k, const void *v, const int32_t *cu_q,
+                const int32_t *cu_k, const float *bias, void *o, float *lse, void *o_rest, void *ws, size_t ws_bytes,
+                void *stream);
+/* dbias [Hq][buckets] fp32 (NULL: none wanted).  o_rest may be NULL. */
+int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q, const void *k, const void *v, const int32_t *cu_q,
+                const int32_t *cu_k, const float *bias, const void *o, const void *o_rest, const float *lse, void *dq,
+                void *dk, void *dv, float *dbias, void *ws, size_t ws_bytes, void *stream);
+
 const char *cg_strerror(int code);
 const char *cg_version(void);
 int cg_last_hip_error(void);   /* hipError_t of the most recent CG_EHIP on this thread */

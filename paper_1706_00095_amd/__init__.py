@@ -17,6 +17,7 @@ CG_OK, CG_EINVAL, CG_ENOSPC, CG_EUNSUPPORTED, CG_EHIP = 0, -1, -2, -3, -4
 CG_PASS_FWD, CG_PASS_BWD_DATA, CG_PASS_BWD_WEIGHT = 0, 1, 2
 CG_STEP_OVERLAP, CG_STEP_SERIAL, CG_STEP_JOIN, CG_STEP_TREE_SUM, CG_STEP_BF16, CG_STEP_BF16X3 = 0, 1, 2, 4, 8, 16
 CG_MATH_FP32, CG_MATH_BF16, CG_MATH_BF16X3 = 0, 1, 2
+CG_TYPE_FP32, CG_TYPE_BF16 = 0, 1
 CG_MAX_PEERS = 64
 CG_NOALLOC_SCRATCH_BYTES = 64 << 20
 LAYER_KINDS = {"conv": 0, "relu": 1, "lrn": 2, "maxpool": 3, "avgpool": 4, "fc": 5, "dropout": 6,
@@ -28,6 +29,9 @@ EXPORTS = [
     "cg_grad_reduce_sgd", "cg_grad_reduce_sgd_multi", "cg_grad_reduce_sgd_tree", "cg_grad_reduce_sgd_tree_multi", "cg_net_create", "cg_net_destroy", "cg_net_param_count", "cg_net_layer_fused", "cg_net_bind",
     "cg_net_workspace_bytes", "cg_train_step", "cg_net_tensor", "cg_net_tensor_image_stride", "cg_strerror", "cg_version", "cg_last_hip_error", "cg_debug_conv_operand", "cg_debug_copy", "cg_debug_stream", "cg_debug_mfma_loop", "cg_debug_launch_count", "cg_debug_fuse_lrn_pool", "cg_debug_patch_min_tiles", "cg_debug_resident_blocks", "cg_debug_band_kernel", "cg_debug_direct_kernel",
     "cg_profile_enable", "cg_profile_count", "cg_profile_get",
+    "cg_dropout_fwd", "cg_dropout_bwd", "cg_layernorm_fwd", "cg_layernorm_workspace_bytes", "cg_layernorm_bwd",
+    "cg_dropout_add_layernorm_fwd", "cg_dropout_add_layernorm_bwd",
+    "cg_attn_workspace_bytes", "cg_attn_fwd", "cg_attn_bwd",
 ]
 
 
@@ -51,6 +55,22 @@ class cg_layer_desc(C.Structure):
                 ("k", C.c_int), ("stride", C.c_int), ("pad", C.c_int), ("lrn_size", C.c_int),
                 ("lrn_alpha", C.c_float), ("lrn_beta", C.c_float), ("lrn_kappa", C.c_float),
                 ("fc_out", C.c_int), ("drop_p", C.c_float)]
+
+
+class cg_drop(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64)]
+
+
+class cg_layernorm_desc(C.Structure):
+    _fields_ = [("type", C.c_int), ("rows", C.c_int64), ("cols", C.c_int64), ("eps", C.c_float)]
+
+
+class cg_attn_desc(C.Structure):
+    _fields_ = [("type", C.c_int), ("B", C.c_int), ("Hq", C.c_int), ("Hkv", C.c_int), ("D", C.c_int),
+                ("Tq", C.c_int64), ("Tk", C.c_int64),
+                ("q_tok", C.c_int64), ("q_head", C.c_int64), ("k_tok", C.c_int64), ("k_head", C.c_int64),
+                ("v_tok", C.c_int64), ("v_head", C.c_int64), ("o_tok", C.c_int64), ("o_head", C.c_int64),
+                ("scale", C.c_float), ("causal", C.c_int), ("buckets", C.c_int), ("max_distance", C.c_int), ("both", C.c_int)]
 
 
 class cg_profile_record(C.Structure):
@@ -107,6 +127,20 @@ def lib():
                                             C.POINTER(C.c_longlong), ip]
         L.cg_profile_enable.argtypes = [C.c_int]
         L.cg_profile_get.argtypes = [C.c_int, C.POINTER(cg_profile_record)]
+        i64, rp, np_ = C.c_int64, C.POINTER(cg_drop), C.POINTER(cg_layernorm_desc)
+        L.cg_dropout_fwd.argtypes = [rp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, vp]
+        L.cg_dropout_bwd.argtypes = [rp, C.c_int, i64, i64, vp, i64, vp, i64, vp]
+        L.cg_layernorm_workspace_bytes.argtypes = [np_]
+        L.cg_layernorm_workspace_bytes.restype = sz
+        L.cg_layernorm_fwd.argtypes = [np_, vp, i64, vp, vp, vp, i64, vp, vp, vp]
+        L.cg_layernorm_bwd.argtypes = [np_, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.cg_dropout_add_layernorm_fwd.argtypes = [np_, rp, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, vp]
+        L.cg_dropout_add_layernorm_bwd.argtypes = [np_, rp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        ap = C.POINTER(cg_attn_desc)
+        L.cg_attn_workspace_bytes.argtypes = [ap, C.c_int]
+        L.cg_attn_workspace_bytes.restype = sz
+        L.cg_attn_fwd.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.cg_attn_bwd.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.cg_strerror.argtypes = [C.c_int]
         L.cg_strerror.restype = C.c_char_p
         L.cg_version.restype = C.c_char_p
@@ -236,6 +270,168 @@ def cg_grad_reduce_sgd_multi(ws, vs, gs, peers, ns, sgd, stream=None, _name="cg_
     counts = (C.c_size_t * max(nb, 1))(*ns)
     _check(getattr(lib(), _name)(nb, _ptr_array(ws), _ptr_array(vs), _ptr_array(gs), table, K, counts,
                                  C.byref(sgd), _stream(stream)), _name)
+
+
+# ---- the operators of an attention sublayer ----
+
+_TYPES = {torch.float32: CG_TYPE_FP32, torch.bfloat16: CG_TYPE_BF16}
+
+
+def drop(p, seed, offset=0):
+    """The numbers that say which elements a dropout drops: the same for a layer's forward and backward pass."""
+    return cg_drop(p, seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF)
+
+
+def _type_of(t):
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"expected a tensor of torch.float32 or torch.bfloat16, got {t.dtype}") from None
+
+
+def _shape_of_rows(t):
+    """(rows, columns) of a tensor of any number of dimensions: the last one is a row's."""
+    if t.dim() < 1:
+        raise ValueError("expected a tensor of rows")
+    cols = t.shape[-1]
+    return (t.shape[0] if t.dim() == 2 else t.numel() // cols if cols else 0), cols
+
+
+def _row_args(t, like, what):
+    """(pointer, elements from a row to the next) of a tensor of `like`'s shape and type; its rows may lie in wider ones."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dtype != like.dtype:
+        raise TypeError(f"{what}: expected a device tensor of {like.dtype}")
+    if t.shape != like.shape:
+        raise ValueError(f"{what}: expected the shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    cols = t.shape[-1]
+    if t.dim() == 2:
+        if t.stride(1) != 1 and cols > 1:
+            raise ValueError(f"{what}: the elements of a row have to lie next to each other")
+        return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else cols)
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: tensors of other than two dimensions have to be contiguous")
+    return t.data_ptr(), cols
+
+
+def _weights(t, n, what):
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n:
+        raise TypeError(f"{what}: expected a contiguous device tensor of {n} float32")
+    return t.data_ptr()
+
+
+def cg_dropout_fwd(drop, x, add, y, stream=None):
+    """y = drop(x) + add (None: nothing is added)."""
+    _check(lib().cg_dropout_fwd(drop, _type_of(x), *_shape_of_rows(x), *_row_args(x, x, "x"), *_row_args(add, x, "add"),
+                                *_row_args(y, x, "y"), _stream(stream)), "cg_dropout_fwd")
+
+
+def cg_dropout_bwd(drop, dy, dx, stream=None):
+    _check(lib().cg_dropout_bwd(drop, _type_of(dy), *_shape_of_rows(dy), *_row_args(dy, dy, "dy"), *_row_args(dx, dy, "dx"),
+                                _stream(stream)), "cg_dropout_bwd")
+
+
+def layernorm_desc(x, eps=1e-5):
+    """Descriptor for tensors of x's type and shape."""
+    return cg_layernorm_desc(_type_of(x), *_shape_of_rows(x), eps)
+
+
+def cg_layernorm_workspace_bytes(d):
+    return int(lib().cg_layernorm_workspace_bytes(d))
+
+
+def _norm_tensor(d, x, what):
+    if _type_of(x) != d.type or _shape_of_rows(x) != (d.rows, d.cols):
+        raise ValueError(f"{what}: not of the descriptor's type and shape")
+
+
+def cg_layernorm_fwd(d, x, gamma, beta, y, mean=None, rstd=None, stream=None):
+    _norm_tensor(d, x, "x")
+    n, r = d.cols, d.rows
+    _check(lib().cg_layernorm_fwd(d, *_row_args(x, x, "x"), _weights(gamma, n, "gamma"), _weights(beta, n, "beta"), *_row_args(y, x, "y"),
+                                  _weights(mean, r, "mean"), _weights(rstd, r, "rstd"), _stream(stream)), "cg_layernorm_fwd")
+
+
+def cg_layernorm_bwd(d, dy, x, gamma, mean, rstd, dsum, dx, dgamma, dbeta, ws, stream=None):
+    _norm_tensor(d, x, "x")
+    n, r = d.cols, d.rows
+    _check(lib().cg_layernorm_bwd(d, *_row_args(dy, x, "dy"), *_row_args(x, x, "x"), _weights(gamma, n, "gamma"), _weights(mean, r, "mean"),
+                                  _weights(rstd, r, "rstd"), *_row_args(dsum, x, "dsum"), *_row_args(dx, x, "dx"), _weights(dgamma, n, "dgamma"),
+                                  _weights(dbeta, n, "dbeta"), *_ws_args(ws), _stream(stream)), "cg_layernorm_bwd")
+
+
+def cg_dropout_add_layernorm_fwd(d, drop, branch, x, gamma, beta, total, y, mean=None, rstd=None, stream=None):
+    """total = x + drop(branch); y = layer norm of total."""
+    _norm_tensor(d, x, "x")
+    n, r = d.cols, d.rows
+    _check(lib().cg_dropout_add_layernorm_fwd(d, drop, *_row_args(branch, x, "branch"), *_row_args(x, x, "x"), _weights(gamma, n, "gamma"),
+                                              _weights(beta, n, "beta"), *_row_args(total, x, "total"), *_row_args(y, x, "y"),
+                                              _weights(mean, r, "mean"), _weights(rstd, r, "rstd"), _stream(stream)),
+           "cg_dropout_add_layernorm_fwd")
+
+
+def cg_dropout_add_layernorm_bwd(d, drop, dy, dsum, total, gamma, mean, rstd, dx, dbranch, dgamma, dbeta, ws, stream=None):
+    _norm_tensor(d, total, "total")
+    n, r = d.cols, d.rows
+    _check(lib().cg_dropout_add_layernorm_bwd(d, drop, *_row_args(dy, total, "dy"), *_row_args(dsum, total, "dsum"), *_row_args(total, total, "total"),
+                                              _weights(gamma, n, "gamma"), _weights(mean, r, "mean"), _weights(rstd, r, "rstd"),
+                                              *_row_args(dx, total, "dx"), *_row_args(dbranch, total, "dbranch"), _weights(dgamma, n, "dgamma"),
+                                              _weights(dbeta, n, "dbeta"), *_ws_args(ws), _stream(stream)), "cg_dropout_add_layernorm_bwd")
+
+
+def attn_desc(q, k, v, o, B, scale, causal=False, buckets=0, max_distance=0, both=False):
+    """Descriptor of attention over B packed sequences: q, o [Tq][Hq][D], k, v [Tk][Hkv][D], of any token and head strides."""
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or q.shape != o.shape or q.shape[2] != k.shape[2]:
+        raise ValueError("expected q and o of one shape [tokens][heads][D], k and v of another with the same D")
+    if not (q.dtype == k.dtype == v.dtype == o.dtype):
+        raise TypeError("q, k, v and o have to be of one type")
+    if q.shape[2] > 1 and not (q.stride(2) == k.stride(2) == v.stride(2) == o.stride(2) == 1):
+        raise ValueError("the elements of a head have to lie next to each other")
+    Tq, Hq, D = q.shape
+    Tk, Hkv, _ = k.shape
+    return cg_attn_desc(_type_of(q), B, Hq, Hkv, D, Tq, Tk, *q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *o.stride()[:2],
+                        scale, causal, buckets, max_distance, both)
+
+
+def cg_attn_workspace_bytes(d, which):
+    return int(lib().cg_attn_workspace_bytes(d, which))
+
+
+def _heads(t, d, T, H, tok, head, what):
+    """The pointer of a tensor [T][H][D] with the descriptor's type and strides."""
+    if t is None:
+        return None
+    if not t.is_cuda or _type_of(t) != d.type:
+        raise TypeError(f"{what}: expected a device tensor of the descriptor's type")
+    if t.shape != (T, H, d.D) or (t.stride() != (tok, head, 1) and t.numel() > 0 and any(
+            n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), (tok, head, 1)))):
+        raise ValueError(f"{what}: not of the descriptor's shape and strides")
+    return t.data_ptr()
+
+
+def _lengths(t, d, what):
+    if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != d.B + 1:
+        raise TypeError(f"{what}: expected a contiguous device tensor of {d.B + 1} int32")
+    return t.data_ptr()
+
+
+def cg_attn_fwd(d, q, k, v, cu_q, cu_k, bias, o, lse, o_rest=None, ws=None, stream=None):
+    Q, K, V, O = (d.Tq, d.Hq, d.q_tok, d.q_head), (d.Tk, d.Hkv, d.k_tok, d.k_head), (d.Tk, d.Hkv, d.v_tok, d.v_head), (d.Tq, d.Hq, d.o_tok, d.o_head)
+    _check(lib().cg_attn_fwd(d, _heads(q, d, *Q, "q"), _heads(k, d, *K, "k"), _heads(v, d, *V, "v"), _lengths(cu_q, d, "cu_q"),
+                             _lengths(cu_k, d, "cu_k"), _weights(bias, d.Hq * d.buckets, "bias"), _heads(o, d, *O, "o"),
+                             _weights(lse, d.Hq * d.Tq, "lse"), _heads(o_rest, d, *O, "o_rest"), *_ws_args(ws), _stream(stream)), "cg_attn_fwd")
+
+
+def cg_attn_bwd(d, d_o, q, k, v, cu_q, cu_k, bias, o, o_rest, lse, dq, dk, dv, dbias, ws, stream=None):
+    Q, K, V, O = (d.Tq, d.Hq, d.q_tok, d.q_head), (d.Tk, d.Hkv, d.k_tok, d.k_head), (d.Tk, d.Hkv, d.v_tok, d.v_head), (d.Tq, d.Hq, d.o_tok, d.o_head)
+    _check(lib().cg_attn_bwd(d, _heads(d_o, d, *O, "d_o"), _heads(q, d, *Q, "q"), _heads(k, d, *K, "k"), _heads(v, d, *V, "v"),
+                             _lengths(cu_q, d, "cu_q"), _lengths(cu_k, d, "cu_k"), _weights(bias, d.Hq * d.buckets, "bias"),
+                             _heads(o, d, *O, "o"), _heads(o_rest, d, *O, "o_rest"), _weights(lse, d.Hq * d.Tq, "lse"),
+                             _heads(dq, d, *Q, "dq"), _heads(dk, d, *K, "dk"), _heads(dv, d, *V, "dv"),
+                             _weights(dbias, d.Hq * d.buckets, "dbias"), *_ws_args(ws), _stream(stream)), "cg_attn_bwd")
 
 
 def cg_debug_patch_min_tiles(tiles):
