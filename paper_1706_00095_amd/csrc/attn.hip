@@ -1,4 +1,224 @@
-#include "cg_internal.h"
-extern "C" size_t cg_attn_workspace_bytes(const cg_attn_desc *, int) { return 0; }
-extern "C" int cg_attn_fwd(const cg_attn_desc *, const void *, const void *, const void *, const int32_t *, const int32_t *, const float *, void *, float *, void *, void *, size_t, void *) { return CG_EUNSUPPORTED; }
-extern "C" int cg_attn_bwd(const cg_attn_desc *, const void *, const void *, const void *, const void *, const int32_t *, const int32_t *, const float *, const void *, const void *, const float *, void *, void *, void *, float *, void *, size_t, void *) { return CG_EUNSUPPORTED; }
+// Attention: descriptors, workspaces, the table of the bias by distance, and the order of the launches.
+#include <cmath>
+#include "attn_device.h"
+
+namespace cg {
+namespace {
+
+constexpr int kMaxBuckets = 256, kMaxDistance = 65536;
+
+// From which distance on the buckets E + 1 .. n - 1 apply: bucket(dist) = dist below E, else E + (how many are <= dist).
+struct Thresholds {
+    int n, E, both;
+    int from[kMaxBuckets / 2 + 1];
+};
+
+// Bias and bucket by distance, for the heads' tables [2 W + 1] in the workspace: a kernel of a few microseconds, so that the
+// attention kernels look a distance up instead of taking its logarithm for every pair.
+__global__ __launch_bounds__(256) void bias_table_kernel(Thresholds th, const float *bias, int buckets, int W, float *tab, uint8_t *bid)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y;
+    if (i > 2 * W) return;
+    const int delta = i - W, dist = th.both ? abs(delta) : max(-delta, 0);
+    int b = dist;
+    if (dist >= th.E) {
+        int lo = 0, hi = th.n - 1 - th.E;       // thresholds there are
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (th.from[mid] <= dist) lo = mid + 1;
+            else hi = mid;
+        }
+        b = th.E + lo;
+    }
+    if (th.both && delta > 0) b += th.n;
+    tab[(int64_t)h * (2 * W + 1) + i] = bias[(int64_t)h * buckets + b];
+    if (h == 0) bid[i] = (uint8_t)b;
+}
+
+// dist >= E reaches bucket E + t where log(dist / E) / log(max / E) * (n - E) + 1e-9 >= t, that is
+// dist >= E (max / E)^((t - 1e-9) / (n - E)); the 1e-9 keeps distances that reach it exactly from falling short in their last place.
+Thresholds thresholds(const cg_attn_desc &d)
+{
+    Thresholds th{};
+    th.both = d.both != 0;
+    th.n = d.both ? d.buckets / 2 : d.buckets;
+    th.E = th.n / 2;
+    const double ratio = (double)d.max_distance / th.E;
+    for (int t = 1; t < th.n - th.E; ++t)
+        th.from[t - 1] = (int)std::ceil(th.E * std::pow(ratio, (t - 1e-9) / (th.n - th.E)));
+    return th;
+}
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+int check(const cg_attn_desc *d)
+{
+    if (!d || (d->type != CG_TYPE_FP32 && d->type != CG_TYPE_BF16)) return CG_EINVAL;
+    if (d->B < 0 || d->Hq < 1 || d->Hkv < 1 || d->D < 1 || d->Hq % d->Hkv || d->Tq < 0 || d->Tk < 0) return CG_EINVAL;
+    if (!(d->scale > 0.f) || !std::isfinite(d->scale) || d->buckets < 0) return CG_EINVAL;
+    if (d->q_tok < 0 || d->q_head < 0 || d->k_tok < 0 || d->k_head < 0 || d->v_tok < 0 || d->v_head < 0 || d->o_tok < 0 || d->o_head < 0) return CG_EINVAL;
+    if (d->buckets > 0) {
+        const int n = d->both ? d->buckets / 2 : d->buckets;
+        if (n < 2 || (d->both && d->buckets % 2) || d->max_distance <= n / 2) return CG_EINVAL;
+        if (d->buckets > kMaxBuckets || d->max_distance > kMaxDistance) return CG_EUNSUPPORTED;
+    }
+    if (d->D > kAttnMaxD || d->Tq * d->Hq > INT32_MAX || d->Tk * d->Hkv > INT32_MAX || d->Tq > INT32_MAX || d->Tk > INT32_MAX) return CG_EUNSUPPORTED;
+    if ((d->Tq * d->Hq / kAttnRows + d->B) * (int64_t)d->Hq > (1 << 30) || (d->Tk / kAttnRows + d->B) * (int64_t)d->Hkv > (1 << 30)) return CG_EUNSUPPORTED;
+    return CG_OK;
+}
+
+// How the pass is laid out and what it keeps in the workspace.
+struct Plan {
+    int Gp, tiles_q, tiles_k, W, splits, chunk;
+    size_t tab, bid, part_o, part_ml, delta, dbias, bytes;       // offsets; bytes in all
+};
+
+// Few query tiles leave most of the chip idle, and a long axis of keys is walked tile by tile: the keys are then cut into chunks, a
+// block each, and joined by a second kernel.  kSplitBelow blocks: fewer than one a compute unit.  A chunk is at least kMinChunk keys, and
+// as many as share all the keys out to about kSplitBlocks blocks.
+constexpr int kSplitBelow = 256, kSplitBlocks = 512, kMinChunk = 256;
+constexpr int64_t kSplitBytes = 256ll << 20;
+
+Plan plan_of(const cg_attn_desc &d, int pass)
+{
+    Plan p{};
+    p.Gp = d.buckets ? 1 : d.Hq / d.Hkv;
+    p.tiles_q = (int)(d.Tq * p.Gp / kAttnRows + d.B);
+    p.tiles_k = (int)(d.Tk / kAttnRows + d.B);
+    p.W = d.buckets ? d.max_distance : 0;
+    p.splits = 1;
+    const int64_t Hr = d.Hq / p.Gp, blocks = Hr * p.tiles_q;
+    int64_t at = 0;
+    if (d.buckets) {
+        p.tab = 0;
+        p.bid = (size_t)up(d.Hq * (2ll * p.W + 1) * 4, 256);
+        at = (int64_t)p.bid + up(2ll * p.W + 1, 256);
+    }
+    if (pass == CG_PASS_FWD) {
+        const int64_t row_bytes = (up(d.D, 32) + 2) * 4;
+        if (blocks > 0 && blocks < kSplitBelow && d.Tk >= 4 * kMinChunk) {
+            int64_t chunk = up(d.Tk * Hr / kSplitBlocks, 64);
+            if (chunk < kMinChunk) chunk = kMinChunk;
+            while (blocks * ((d.Tk + chunk - 1) / chunk) * kAttnRows * row_bytes > kSplitBytes) chunk *= 2;
+            p.chunk = (int)chunk;
+            p.splits = (int)((d.Tk + chunk - 1) / chunk);
+        }
+        if (p.splits > 1) {
+            p.part_o = (size_t)at;
+            at += up(blocks * p.splits * kAttnRows * up(d.D, 32) * 4, 256);
+            p.part_ml = (size_t)at;
+            at += up(blocks * p.splits * kAttnRows * 2 * 4, 256);
+        }
+    } else {
+        p.delta = (size_t)at;
+        at += up(d.Tq * d.Hq * 4, 256);
+        p.dbias = (size_t)at;
+        if (d.buckets) at += up((int64_t)d.Hq * p.tiles_q * d.buckets * 4, 256);
+    }
+    p.bytes = (size_t)at;
+    return p;
+}
+
+bool tensor_ok(const void *p, int type, int64_t n)
+{
+    return n == 0 || (p && (reinterpret_cast<uintptr_t>(p) & (type == CG_TYPE_FP32 ? 3 : 1)) == 0);
+}
+bool words_ok(const void *p, int64_t n) { return n == 0 || (p && (reinterpret_cast<uintptr_t>(p) & 3) == 0); }
+
+AttnArgs args_of(const cg_attn_desc &d, const Plan &p, const void *q, const void *k, const void *v, const int32_t *cu_q, const int32_t *cu_k, char *ws)
+{
+    AttnArgs a{};
+    a.q = q, a.k = k, a.v = v, a.cu_q = cu_q, a.cu_k = cu_k;
+    a.q_tok = d.q_tok, a.q_head = d.q_head, a.k_tok = d.k_tok, a.k_head = d.k_head;
+    a.v_tok = d.v_tok, a.v_head = d.v_head, a.o_tok = d.o_tok, a.o_head = d.o_head;
+    a.B = d.B, a.Tq = (int)d.Tq, a.Tk = (int)d.Tk, a.Hq = d.Hq, a.Hkv = d.Hkv, a.G = d.Hq / d.Hkv, a.Gp = p.Gp, a.D = d.D;
+    a.by_gp = make_fastdiv((uint32_t)p.Gp);
+    a.scale = d.scale;
+    a.causal = d.causal != 0;
+    a.buckets = d.buckets;
+    a.W = p.W;
+    a.tiles = p.tiles_q;
+    a.splits = p.splits, a.chunk = p.chunk;
+    if (d.buckets) {
+        a.btab = reinterpret_cast<const float *>(ws + p.tab);
+        a.bid = reinterpret_cast<const uint8_t *>(ws + p.bid);
+    }
+    return a;
+}
+int table_launch(const cg_attn_desc &d, const Plan &p, const float *bias, char *ws, hipStream_t s)
+{
+    if (!d.buckets) return CG_OK;
+    hipLaunchKernelGGL(bias_table_kernel, dim3((unsigned)(2 * p.W + 1 + 255) / 256, (unsigned)d.Hq), dim3(256), 0, s, thresholds(d), bias, d.buckets, p.W,
+                       reinterpret_cast<float *>(ws + p.tab), reinterpret_cast<uint8_t *>(ws + p.bid));
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+int ws_check(const Plan &p, const void *ws, size_t ws_bytes)
+{
+    if (p.bytes && (!ws || !aligned16(ws))) return CG_EINVAL;
+    return ws_bytes < p.bytes ? CG_ENOSPC : CG_OK;
+}
+
+}  // namespace
+}  // namespace cg
+
+using namespace cg;
+
+extern "C" size_t cg_attn_workspace_bytes(const cg_attn_desc *d, int pass)
+{
+    if (check(d) != CG_OK || (pass != CG_PASS_FWD && pass != CG_PASS_BWD_DATA)) return 0;
+    return plan_of(*d, pass).bytes;
+}
+
+extern "C" int cg_attn_fwd(const cg_attn_desc *d, const void *q, const void *k, const void *v, const int32_t *cu_q, const int32_t *cu_k,
+                           const float *bias, void *o, float *lse, void *o_rest, void *ws, size_t ws_bytes, void *stream)
+{
+    if (int rc = check(d)) return rc;
+    if (d->B == 0 || d->Tq == 0) return CG_OK;
+    if (!tensor_ok(q, d->type, 1) || !tensor_ok(k, d->type, d->Tk) || !tensor_ok(v, d->type, d->Tk) || !tensor_ok(o, d->type, 1) || !words_ok(lse, 1) ||
+        !words_ok(cu_q, 1) || !words_ok(cu_k, 1) || !words_ok(bias, d->buckets)) return CG_EINVAL;
+    if (o_rest && (d->type != CG_TYPE_BF16 || !tensor_ok(o_rest, d->type, 1))) return CG_EINVAL;
+    const Plan p = plan_of(*d, CG_PASS_FWD);
+    if (int rc = ws_check(p, ws, ws_bytes)) return rc;
+    char *w = static_cast<char *>(ws);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (int rc = table_launch(*d, p, bias, w, s)) return rc;
+    AttnArgs a = args_of(*d, p, q, k, v, cu_q, cu_k, w);
+    a.o = o, a.o_rest = o_rest, a.lse = lse;
+    if (p.splits > 1) {
+        a.part_o = reinterpret_cast<float *>(w + p.part_o);
+        a.part_ml = reinterpret_cast<float *>(w + p.part_ml);
+    }
+    if (int rc = attn_fwd_launch(a, d->type, s)) return rc;
+    return p.splits > 1 ? attn_combine_launch(a, d->type, s) : CG_OK;
+}
+
+extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q, const void *k, const void *v, const int32_t *cu_q,
+                           const int32_t *cu_k, const float *bias, const void *o, const void *o_rest, const float *lse, void *dq,
+                           void *dk, void *dv, float *dbias, void *ws, size_t ws_bytes, void *stream)
+{
+    if (int rc = check(d)) return rc;
+    if (!tensor_ok(q, d->type, d->Tq) || !tensor_ok(k, d->type, d->Tk) || !tensor_ok(v, d->type, d->Tk) || !tensor_ok(o, d->type, d->Tq) ||
+        !tensor_ok(d_o, d->type, d->Tq) || !tensor_ok(dq, d->type, d->Tq) || !tensor_ok(dk, d->type, d->Tk) || !tensor_ok(dv, d->type, d->Tk) ||
+        !words_ok(lse, d->Tq) || !words_ok(cu_q, d->B) || !words_ok(cu_k, d->B) || !words_ok(bias, d->buckets)) return CG_EINVAL;
+    if ((o_rest && (d->type != CG_TYPE_BF16 || !tensor_ok(o_rest, d->type, 1))) || (dbias && (!d->buckets || !words_ok(dbias, 1)))) return CG_EINVAL;
+    const Plan p = plan_of(*d, CG_PASS_BWD_DATA);
+    if (int rc = ws_check(p, ws, ws_bytes)) return rc;
+    char *w = static_cast<char *>(ws);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (int rc = table_launch(*d, p, bias, w, s)) return rc;
+    AttnArgs a = args_of(*d, p, q, k, v, cu_q, cu_k, w);
+    a.d_o = d_o, a.o_in = o, a.o_rest_in = o_rest, a.lse = const_cast<float *>(lse);
+    a.dq = dq, a.dk = dk, a.dv = dv;
+    a.delta = reinterpret_cast<float *>(w + p.delta);
+    if (dbias) a.dbias_part = reinterpret_cast<float *>(w + p.dbias);
+    if (d->B > 0 && d->Tq > 0)
+        if (int rc = attn_dq_launch(a, d->type, s)) return rc;
+    if (dbias)
+        if (int rc = attn_dbias_launch(a.dbias_part, d->Tq > 0 ? p.tiles_q : 0, d->Hq, d->buckets, dbias, s)) return rc;
+    if (d->B > 0 && d->Tk > 0) {
+        a.tiles = p.tiles_k;
+        return attn_dkdv_launch(a, d->type, s);
+    }
+    return CG_OK;
+}

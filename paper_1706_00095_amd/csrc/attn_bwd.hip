@@ -1,0 +1,409 @@
+// Attention, backward.  The scores are computed again from lse, once with the queries as X (dq, the bias's gradient and delta)
+// and once with the keys as X (dk, dv): seven products instead of five, but every sum stays in one block's registers, so no
+// gradient is added with atomics and results repeat bit for bit.
+#include "attn_device.h"
+
+namespace cg {
+namespace {
+
+constexpr int kDiag = 33;          // a wave's 32 x 32 scores' gradients in LDS, rows of 33
+
+// Sums of a wave's 32 x 32 tile along its diagonals (equal distances), then over the diagonals of a bucket, into this wave's
+// own `acc` [buckets].  Buckets of neighbouring distances are the same or neighbours, so equal ones are runs of lanes.
+__device__ __forceinline__ void add_diagonals(const float (&ds)[16], int delta0, const AttnArgs &a, float *sq, float *acc, int lane)
+{
+    const int c = lane & 31, h32 = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sq[c * kDiag + 8 * (i / 4) + 4 * h32 + i % 4] = ds[i];
+    // the wave's own accesses to LDS: in order, but the compiler has to be told
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    float v = 0.f;
+#pragma unroll 8
+    for (int x = 0; x < 32; ++x) {
+        const int y = lane + x - 31;
+        if (y >= 0 && y < 32) v += sq[x * kDiag + y];
+    }
+    const int delta = delta0 + lane - 31;
+    const int bucket = lane < 63 ? (int)a.bid[min(max(delta, -a.W), a.W) + a.W] : -1;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const float u = __shfl_up(v, d);
+        const int ub = __shfl_up(bucket, d);
+        if (lane >= d && ub == bucket) v += u;
+    }
+    const int next = __shfl_down(bucket, 1);
+    if (lane < 63 && next != bucket) acc[bucket] += v;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+template <class T, int DP, bool BIAS>
+__global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel(AttnArgs a)
+{
+    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
+    using TileY = Tile<DP, YT, NP>;
+    __shared__ __align__(16) char ldsK[TileY::BYTES], ldsV[TileY::BYTES];
+    __shared__ float window[BIAS ? kAttnRows + YT : 1], square[BIAS ? 4 : 1][BIAS ? 32 * kDiag : 1], bsum[BIAS ? 4 : 1][BIAS ? 256 : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h32 = lane >> 5;
+    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, tile = a.tiles - 1 - blockIdx.x / Hr;
+    const bool want_bias = BIAS && a.dbias_part;
+    int b, t;
+    const bool any = find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t);
+    if (want_bias) {
+        if (!any) {
+            for (int i = threadIdx.x; i < a.buckets; i += 256) a.dbias_part[((int64_t)hr * a.tiles + tile) * a.buckets + i] = 0.f;
+        } else
+            for (int i = threadIdx.x; i < 4 * 256; i += 256) bsum[i / 256][i % 256] = 0.f;
+        __syncthreads();
+    }
+    if (!any) return;
+    const Seq s = seq_of(a, b);
+    const int row0 = t * kAttnRows, rows = s.n * a.Gp, off = s.m - s.n;
+    const int h0 = hr * a.Gp, hkv = h0 / a.G;
+    const int row = row0 + 32 * wave + (lane & 31);
+    const bool here = row < rows;
+    const int tok = (int)fdiv((uint32_t)min(row, rows - 1), a.by_gp), head = h0 + (here ? row - tok * a.Gp : 0);
+    const int limit = a.causal ? min(max(tok + 1 + off, 0), s.m) : s.m;
+    const int first_tok = (int)fdiv((uint32_t)min(row0 + 32 * wave, rows - 1), a.by_gp);
+    const int wave_limit = a.causal ? min(max(first_tok + 1 + off, 0), s.m) : s.m;
+    const int last_tok = (int)fdiv((uint32_t)min(row0 + kAttnRows, rows) - 1, a.by_gp);
+    const int kend = a.causal ? min(max(last_tok + 1 + off, 0), s.m) : s.m;
+
+    const FastDiv one = {1, 1, 0};
+    const Rows<T> K{static_cast<const T *>(a.k) + (int64_t)s.k0 * a.k_tok + (int64_t)hkv * a.k_head, a.k_tok, 0, s.m, a.D, one};
+    const Rows<T> V{static_cast<const T *>(a.v) + (int64_t)s.k0 * a.v_tok + (int64_t)hkv * a.v_head, a.v_tok, 0, s.m, a.D, one};
+    const Rows<T> Q{static_cast<const T *>(a.q) + (int64_t)s.q0 * a.q_tok + (int64_t)h0 * a.q_head, a.q_tok, a.q_head, rows, a.D, a.by_gp};
+    const int64_t o_at = (int64_t)s.q0 * a.o_tok + (int64_t)h0 * a.o_head;
+    const Rows<T> dO{static_cast<const T *>(a.d_o) + o_at, a.o_tok, a.o_head, rows, a.D, a.by_gp};
+    const Rows<T> O{static_cast<const T *>(a.o_in) + o_at, a.o_tok, a.o_head, rows, a.D, a.by_gp};
+    const Rows<T> R{static_cast<const T *>(a.o_rest_in) + o_at, a.o_tok, a.o_head, rows, a.D, a.by_gp};
+    Frag<NP> fq[KS], fdo[KS];
+    float delta = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int d = 16 * ks + 8 * h32;
+        fq[ks] = frag_of(Q.load(row, d));
+        const Raw8<T> g = dO.load(row, d), o = O.load(row, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) delta = fmaf(elem(g, i), elem(o, i), delta);
+        if (NP == 1 && a.o_rest_in) {
+            const Raw8<T> r = R.load(row, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) delta = fmaf(elem(g, i), elem(r, i), delta);
+        }
+        fdo[ks] = frag_of(g);
+    }
+    delta += other_half(delta);
+    const int64_t stat = (int64_t)head * a.Tq + s.q0 + tok;
+    float lse = here ? a.lse[stat] : -INFINITY;
+    if (here && h32 == 0) a.delta[stat] = delta;
+    if (lse == -INFINITY) lse = INFINITY;      // a row that sees nothing (or is none): probabilities 0
+    const float c = a.scale * kLog2e, lse2 = lse * kLog2e;
+
+    v16f dQ[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) dQ[dt] = v16f{};
+    float far_past = 0.f, far_future = 0.f;
+
+    Stage<T, DP, YT, 256> sk, sv;
+    if (kend > 0) {
+        sk.load(K, 0);
+        sv.load(V, 0);
+    }
+    for (int k0 = 0; k0 < kend; k0 += YT) {
+        __syncthreads();
+        sk.put(ldsK);
+        sv.put(ldsV);
+        if constexpr (BIAS) bias_window(window, a, h0, k0 - (row0 + kAttnRows - 1) - off, kAttnRows + YT - 1, 256);
+        __syncthreads();
+        if (k0 + YT < kend) {
+            sk.load(K, k0 + YT);
+            sv.load(V, k0 + YT);
+        }
+        Frag<NP> fds[SUB][2];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            Acc<NP> S, P;
+            S.zero();
+            P.zero();
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                S.mma(TileY::rows(ldsK, 32 * u, ks, lane), fq[ks]);
+                P.mma(TileY::rows(ldsV, 32 * u, ks, lane), fdo[ks]);
+            }
+            float ds[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int y = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4;
+                float p;
+                if constexpr (BIAS) {
+                    const float x = fmaf(S.get(i), a.scale, window[y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
+                    p = __builtin_amdgcn_exp2f((x - lse) * kLog2e);
+                } else p = __builtin_amdgcn_exp2f(fmaf(S.get(i), c, -lse2));
+                ds[i] = p * (P.get(i) - delta);
+            }
+            if (k0 + 32 * u + 32 > wave_limit)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (k0 + 32 * u + 8 * (i / 4) + 4 * h32 + i % 4 >= limit) ds[i] = 0.f;
+            if constexpr (BIAS) {
+                if (want_bias) {
+                    // distances of this 32 x 32 part: first .. first + 62
+                    const int delta0 = k0 + 32 * u - (row0 + 32 * wave) - off;
+                    if (delta0 + 31 <= -a.W || delta0 - 31 >= a.W) {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum += here ? ds[i] : 0.f;
+                        (delta0 < 0 ? far_past : far_future) += sum;
+                    } else {
+                        if (!here)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) ds[i] = 0.f;
+                        add_diagonals(ds, delta0, a, square[wave], bsum[wave], lane);
+                    }
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < 2; ++g) fds[u][g] = cut8<NP>(&ds[8 * g]);
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            if constexpr (NP == 1) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) dQ[dt] = mfma(TileY::cols(ldsK, 32 * u + 16 * g, dt, lane).p[0], fds[u][g].p[0], dQ[dt]);
+            } else {
+                Acc<NP> S;
+                S.zero();
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsK, 32 * u + 16 * g, dt, lane), fds[u][g]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) dQ[dt][i] += S.get(i);
+            }
+        }
+    }
+    if (want_bias) {
+#pragma unroll
+        for (int m = 32; m; m >>= 1) {
+            far_past += __shfl_xor(far_past, m);
+            far_future += __shfl_xor(far_future, m);
+        }
+        if (lane == 0) {
+            bsum[wave][a.bid[0]] += far_past;
+            bsum[wave][a.bid[2 * a.W]] += far_future;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.buckets; i += 256)
+            a.dbias_part[((int64_t)hr * a.tiles + tile) * a.buckets + i] = (bsum[0][i] + bsum[1][i]) + (bsum[2][i] + bsum[3][i]);
+    }
+    if (!here) return;
+    T *to = static_cast<T *>(a.dq) + (int64_t)(s.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = 32 * dt + 8 * j + 4 * h32;
+            float f[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = dQ[dt][4 * j + i] * a.scale;
+            store4(to + d, f, a.D - d);
+        }
+}
+
+// dbias[h][bucket]: the blocks' sums in order, in 64 bits.  A block a head, a thread a bucket.
+__global__ __launch_bounds__(256) void attn_dbias_kernel(const float *part, int tiles, int buckets, float *dbias)
+{
+    const int h = blockIdx.x, i = threadIdx.x;
+    if (i >= buckets) return;
+    double s = 0;
+    for (int t = 0; t < tiles; ++t) s += part[((int64_t)h * tiles + t) * buckets + i];
+    dbias[(int64_t)h * buckets + i] = (float)s;
+}
+
+// X: 128 keys of a key-value head; Y: the query rows that see them, of all Gp heads.  With a bias Gp = 1, and the G heads
+// are walked one after the other.
+template <class T, int DP, bool BIAS>
+__global__ __launch_bounds__(256, 1) void attn_dkdv_kernel(AttnArgs a)
+{
+    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = 32;
+    using TileY = Tile<DP, YT, NP>;
+    __shared__ __align__(16) char ldsQ[TileY::BYTES], ldsO[TileY::BYTES];
+    __shared__ __align__(16) float yl[YT], yd[YT];       // lse, delta of the tile's rows
+    __shared__ __align__(16) int ylim[YT];               // keys the row sees: below this
+    __shared__ float window[BIAS ? kAttnRows + YT : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h32 = lane >> 5;
+    const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
+    int b, t;
+    if (!find_tile(a.cu_k, a.Tk, a.B, kAttnRows, 1, tile, b, t)) return;
+    const Seq s = seq_of(a, b);
+    const int key0 = t * kAttnRows, rows = s.n * a.Gp, off = s.m - s.n;
+    const int key = key0 + 32 * wave + (lane & 31);
+
+    const FastDiv one = {1, 1, 0};
+    const Rows<T> K{static_cast<const T *>(a.k) + (int64_t)s.k0 * a.k_tok + (int64_t)hkv * a.k_head, a.k_tok, 0, s.m, a.D, one};
+    const Rows<T> V{static_cast<const T *>(a.v) + (int64_t)s.k0 * a.v_tok + (int64_t)hkv * a.v_head, a.v_tok, 0, s.m, a.D, one};
+    Frag<NP> fk[KS], fv[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        fk[ks] = frag_of(K.load(key, 16 * ks + 8 * h32));
+        fv[ks] = frag_of(V.load(key, 16 * ks + 8 * h32));
+    }
+    v16f dK[DT], dV[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) dK[dt] = v16f{}, dV[dt] = v16f{};
+    const float c = a.scale * kLog2e;
+    // the first row that sees the block's first key
+    const int first = a.causal ? max(key0 - off, 0) : 0;
+    const int begin = (int)min((int64_t)first * a.Gp, (int64_t)rows) / YT * YT;
+
+    for (int g = 0; g < a.G / a.Gp; ++g) {
+        const int h0 = hkv * a.G + g * a.Gp;
+        const Rows<T> Q{static_cast<const T *>(a.q) + (int64_t)s.q0 * a.q_tok + (int64_t)h0 * a.q_head, a.q_tok, a.q_head, rows, a.D, a.by_gp};
+        const Rows<T> dO{static_cast<const T *>(a.d_o) + (int64_t)s.q0 * a.o_tok + (int64_t)h0 * a.o_head, a.o_tok, a.o_head, rows, a.D, a.by_gp};
+        Stage<T, DP, YT, 256> sq, so;
+        if (begin < rows) {
+            sq.load(Q, begin);
+            so.load(dO, begin);
+        }
+        for (int y0 = begin; y0 < rows; y0 += YT) {
+            __syncthreads();
+            sq.put(ldsQ);
+            so.put(ldsO);
+            if (threadIdx.x < YT) {
+                const int r = y0 + threadIdx.x, tok = (int)fdiv((uint32_t)min(r, rows - 1), a.by_gp);
+                const int64_t stat = (int64_t)(h0 + r - tok * a.Gp) * a.Tq + s.q0 + tok;
+                const bool here = r < rows;
+                float l = here ? a.lse[stat] : -INFINITY;
+                if (l == -INFINITY) l = INFINITY;
+                yl[threadIdx.x] = BIAS ? l : l * kLog2e;
+                yd[threadIdx.x] = here ? a.delta[stat] : 0.f;
+                ylim[threadIdx.x] = a.causal ? tok + 1 + off : s.m;
+            }
+            if constexpr (BIAS) bias_window(window, a, h0, key0 - (y0 + YT - 1) - off, kAttnRows + YT - 1, 256);
+            __syncthreads();
+            if (y0 + YT < rows) {
+                sq.load(Q, y0 + YT);
+                so.load(dO, y0 + YT);
+            }
+            Acc<NP> S, P;
+            S.zero();
+            P.zero();
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                S.mma(TileY::rows(ldsQ, 0, ks, lane), fk[ks]);
+                P.mma(TileY::rows(ldsO, 0, ks, lane), fv[ks]);
+            }
+            float p[16], ds[16];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int y = 8 * j + 4 * h32;
+                const float4 l4 = *reinterpret_cast<const float4 *>(yl + y), d4 = *reinterpret_cast<const float4 *>(yd + y);
+                const int4 m4 = *reinterpret_cast<const int4 *>(ylim + y);
+                const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+                const int lim[4] = {m4.x, m4.y, m4.z, m4.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x;
+                    if constexpr (BIAS) {
+                        x = fmaf(S.get(4 * j + i), a.scale, window[32 * wave + (lane & 31) - (y + i) + YT - 1]);
+                        x = __builtin_amdgcn_exp2f((x - l[i]) * kLog2e);
+                    } else x = __builtin_amdgcn_exp2f(fmaf(S.get(4 * j + i), c, -l[i]));
+                    const bool sees = key < lim[i];
+                    p[4 * j + i] = sees ? x : 0.f;
+                    ds[4 * j + i] = sees ? x * (P.get(4 * j + i) - d[i]) : 0.f;
+                }
+            }
+            Frag<NP> fp[2], fds[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                fp[e] = cut8<NP>(&p[8 * e]);
+                fds[e] = cut8<NP>(&ds[8 * e]);
+            }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                if constexpr (NP == 1) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        dV[dt] = mfma(TileY::cols(ldsO, 16 * e, dt, lane).p[0], fp[e].p[0], dV[dt]);
+                        dK[dt] = mfma(TileY::cols(ldsQ, 16 * e, dt, lane).p[0], fds[e].p[0], dK[dt]);
+                    }
+                } else {
+                    Acc<NP> A;
+                    A.zero();
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsO, 16 * e, dt, lane), fp[e]);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) dV[dt][i] += A.get(i);
+                    A.zero();
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsQ, 16 * e, dt, lane), fds[e]);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) dK[dt][i] += A.get(i);
+                }
+            }
+        }
+    }
+    if (key >= s.m) return;
+    T *tk = static_cast<T *>(a.dk) + (int64_t)(s.k0 + key) * a.k_tok + (int64_t)hkv * a.k_head;
+    T *tv = static_cast<T *>(a.dv) + (int64_t)(s.k0 + key) * a.v_tok + (int64_t)hkv * a.v_head;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = 32 * dt + 8 * j + 4 * h32;
+            const float f[4] = {dV[dt][4 * j], dV[dt][4 * j + 1], dV[dt][4 * j + 2], dV[dt][4 * j + 3]};
+            store4(tv + d, f, a.D - d);
+            const float g[4] = {dK[dt][4 * j] * a.scale, dK[dt][4 * j + 1] * a.scale, dK[dt][4 * j + 2] * a.scale, dK[dt][4 * j + 3] * a.scale};
+            store4(tk + d, g, a.D - d);
+        }
+}
+
+template <class T, int DP> int dq_dp(const AttnArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles);
+    if (a.btab) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false>), grid, dim3(256), 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+template <class T, int DP> int dkdv_dp(const AttnArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)a.Hkv * a.tiles);
+    if (a.btab) hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, false>), grid, dim3(256), 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
+}  // namespace
+
+int attn_dq_launch(const AttnArgs &a, int type, hipStream_t s)
+{
+#define CG_DP(DP) if (a.D <= DP) return type == CG_TYPE_FP32 ? dq_dp<float, DP>(a, s) : dq_dp<bf16raw, DP>(a, s)
+    CG_DP(32);
+    CG_DP(64);
+    CG_DP(96);
+    CG_DP(128);
+#undef CG_DP
+    return CG_EUNSUPPORTED;
+}
+int attn_dkdv_launch(const AttnArgs &a, int type, hipStream_t s)
+{
+#define CG_DP(DP) if (a.D <= DP) return type == CG_TYPE_FP32 ? dkdv_dp<float, DP>(a, s) : dkdv_dp<bf16raw, DP>(a, s)
+    CG_DP(32);
+    CG_DP(64);
+    CG_DP(96);
+    CG_DP(128);
+#undef CG_DP
+    return CG_EUNSUPPORTED;
+}
+int attn_dbias_launch(const float *part, int tiles, int Hq, int buckets, float *dbias, hipStream_t s)
+{
+    hipLaunchKernelGGL(attn_dbias_kernel, dim3((unsigned)Hq), dim3(256), 0, s, part, tiles, buckets, dbias);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
+}  // namespace cg

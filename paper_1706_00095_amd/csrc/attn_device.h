@@ -1,0 +1,290 @@
+// Device code shared by the attention kernels (attn_fwd.hip, attn_bwd.hip) and what their host side passes to them.
+//
+// Common frame.  All products run on v_mfma_f32_32x32x16_bf16: fp32 tensors are cut into three bf16 pieces (NP = 3, six
+// products), bf16 tensors are taken as they are (NP = 1).  Of the two sides of the score matrix one, X, lives in registers: a
+// wave owns 32 of its rows (queries in the forward and the dq kernel, keys in the dk/dv kernel) and holds them as the
+// instruction's second operand.  The other, Y, passes through LDS in tiles all waves share and is the first operand.  A lane
+// then holds 16 scores of ONE X row (C layout: column lane % 32, rows 8 (i / 4) + 4 (lane / 32) + i % 4), so softmax statistics are
+// sums within a lane and one exchange with lane ^ 32, and the scores are in place as the second operand of the next product,
+// whose contraction runs over Y: its slots are filled in the order the C layout has, and the first operand, Y transposed, is read
+// from the same LDS tile by transposing reads (ds_read_b64_tr_b16) in that order.  Scores never pass through LDS.
+//
+// Query rows.  With grouped heads the Gp query heads that share a key-value head are packed into one problem of n Gp rows
+// (row r: token r / Gp, head r % Gp), so that K and V are read once for all of them and their dk, dv need no sum afterwards.
+// With a bias Gp = 1: the table differs from head to head.
+#pragma once
+#include "cg_internal.h"
+#include "igemm_device.h"
+#include "typed_device.h"
+
+namespace cg {
+
+struct AttnArgs {
+    const void *q, *k, *v, *d_o, *o_in, *o_rest_in;
+    void *o, *o_rest, *dq, *dk, *dv;
+    float *lse, *delta;                    // [Hq][Tq]
+    const int32_t *cu_q, *cu_k;
+    int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
+    int B, Tq, Tk, Hq, Hkv, G, Gp, D;      // G: query heads of a key-value head; Gp of them are packed (1 or G)
+    FastDiv by_gp;
+    float scale;
+    int causal;
+    // bias by distance: btab [Hq][2 W + 1], bucket of delta (clamped to -W .. W) bid [2 W + 1]
+    const float *btab;
+    const uint8_t *bid;
+    int W, buckets;
+    float *dbias_part;                     // [Hq][tiles][buckets]
+    int tiles;                             // of X rows over all sequences, an upper bound
+    // keys cut into `splits` chunks of `chunk` (0: one)
+    int splits, chunk;
+    float *part_o, *part_ml;               // [Hr][tiles][splits][rows][DP], [..][2][rows]
+};
+
+constexpr int kAttnRows = 128;             // X rows of a block: four waves of 32
+constexpr int kAttnMaxD = 128;
+
+// attn_fwd.hip, attn_bwd.hip: DP is D rounded up to a multiple of 32
+int attn_fwd_launch(const AttnArgs &a, int type, hipStream_t s);
+int attn_combine_launch(const AttnArgs &a, int type, hipStream_t s);
+int attn_dq_launch(const AttnArgs &a, int type, hipStream_t s);
+int attn_dkdv_launch(const AttnArgs &a, int type, hipStream_t s);
+int attn_dbias_launch(const float *part, int tiles, int Hq, int buckets, float *dbias, hipStream_t s);
+
+namespace {
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+template <class T> struct Pieces { static constexpr int N = sizeof(T) == 4 ? 3 : 1; };
+
+// ---- operands and accumulators ------------------------------------------------------------------------------------------
+template <int NP> struct Frag { u32x4 p[NP]; };      // eight values, NP bf16 pieces each, most significant first
+
+// Two fp32 values in NP bf16 pieces, each the nearest even of what the ones before it left; three hold 24 bits.
+template <int NP> __device__ __forceinline__ void cut_pair(float x0, float x1, uint32_t (&pc)[NP])
+{
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+        pc[k] = pack_bf16(x0, x1);
+        if (k + 1 < NP) {
+            uint32_t h = pc[k];
+            asm("" : "+v"(h));             // both values from the pair, not each converted once more on its own
+            x0 -= __uint_as_float(h << 16);
+            x1 -= __uint_as_float(h & 0xffff0000u);
+        }
+    }
+}
+template <int NP> __device__ __forceinline__ Frag<NP> cut8(const float *f)
+{
+    Frag<NP> r;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        uint32_t pc[NP];
+        cut_pair<NP>(f[2 * t], f[2 * t + 1], pc);
+#pragma unroll
+        for (int k = 0; k < NP; ++k) r.p[k][t] = pc[k];
+    }
+    return r;
+}
+__device__ __forceinline__ Frag<1> frag_of(const Raw8<bf16raw> &r) { return {{u32x4{r.w[0], r.w[1], r.w[2], r.w[3]}}}; }
+__device__ __forceinline__ Frag<3> frag_of(const Raw8<float> &r)
+{
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = elem(r, i);
+    return cut8<3>(f);
+}
+
+__device__ __forceinline__ v16f mfma(u32x4 a, u32x4 b, v16f c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// Three pieces: the products below the first are added up on their own, because an instruction drops what lies below the
+// last place of the sum it adds to; the two sums meet in one rounded addition.
+template <int NP> struct Acc;
+template <> struct Acc<1> {
+    v16f big;
+    __device__ __forceinline__ void zero() { big = v16f{}; }
+    __device__ __forceinline__ void mma(const Frag<1> &a, const Frag<1> &b) { big = mfma(a.p[0], b.p[0], big); }
+    __device__ __forceinline__ float get(int i) const { return big[i]; }
+};
+template <> struct Acc<3> {
+    v16f big, small;
+    __device__ __forceinline__ void zero() { big = v16f{}, small = v16f{}; }
+    __device__ __forceinline__ void mma(const Frag<3> &a, const Frag<3> &b)
+    {
+        small = mfma(a.p[2], b.p[0], small);
+        small = mfma(a.p[0], b.p[2], small);
+        small = mfma(a.p[1], b.p[1], small);
+        small = mfma(a.p[1], b.p[0], small);
+        small = mfma(a.p[0], b.p[1], small);
+        big = mfma(a.p[0], b.p[0], big);
+    }
+    __device__ __forceinline__ float get(int i) const { return big[i] + small[i]; }
+};
+
+// ---- LDS tiles ------------------------------------------------------------------------------------------------------------
+// ROWS x DP bf16, NP planes.  16-byte chunks of a row are exchanged by a function of the row so that neither eight rows'
+// same chunk (row reads) nor four rows' same 64 bytes (transposing reads) fall on the same banks (64 of 4 bytes).
+template <int DP> __device__ __forceinline__ int swizzle(int row)
+{
+    if constexpr (DP == 128) return (row & 3) << 2 | (row >> 2 & 1);
+    else if constexpr (DP == 64) return (row >> 1 & 1) << 2 | (row >> 2 & 1);
+    else return row >> 2 & 1;
+}
+template <int DP, int ROWS, int NP> struct Tile {
+    static constexpr int CH = DP / 8, BYTES = NP * ROWS * DP * 2;
+    static __device__ __forceinline__ int at(int row, int chunk) { return row * DP * 2 + ((chunk ^ swizzle<DP>(row)) << 4); }
+    static __device__ __forceinline__ void put(char *t, int row, int chunk, const Frag<NP> &f)
+    {
+#pragma unroll
+        for (int k = 0; k < NP; ++k) *reinterpret_cast<u32x4 *>(t + k * ROWS * DP * 2 + at(row, chunk)) = f.p[k];
+    }
+    // first operand, rows of the tile: row0 + lane % 32, contraction 16 ks ..
+    static __device__ __forceinline__ Frag<NP> rows(const char *t, int row0, int ks, int lane)
+    {
+        Frag<NP> f;
+#pragma unroll
+        for (int k = 0; k < NP; ++k)
+            f.p[k] = *reinterpret_cast<const u32x4 *>(t + k * ROWS * DP * 2 + at(row0 + (lane & 31), 2 * ks + (lane >> 5)));
+        return f;
+    }
+    // first operand, columns of the tile: 32 dt + lane % 32, contraction over the rows row0 .. row0 + 15 in the order of the C layout.
+    // A transposing read gives lane i of 16 column i of the 4 x 16 values that the 16 lanes' addresses name, four lanes a row.
+    static __device__ __forceinline__ Frag<NP> cols(const char *t, int row0, int dt, int lane)
+    {
+        const int row = row0 + 4 * (lane >> 5) + (lane >> 2 & 3), chunk = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        Frag<NP> f;
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            const char *base = t + k * ROWS * DP * 2 + 8 * (lane & 1);
+            const s16x4 lo = tr(base + at(row, chunk)), hi = tr(base + at(row + 8, chunk));
+            const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+            f.p[k] = u32x4{a.x, a.y, b.x, b.y};
+        }
+        return f;
+    }
+    static __device__ __forceinline__ s16x4 tr(const char *p)
+    {
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p));
+    }
+};
+
+// ---- where rows lie -------------------------------------------------------------------------------------------------------
+struct Seq { int b, q0, n, k0, m; };        // query tokens q0 .. q0 + n - 1, key tokens k0 .. k0 + m - 1 (cut to the tensors)
+
+__device__ __forceinline__ void bounds_of(const int32_t *cu, int T, int b, int &first, int &len)
+{
+    first = min(max(cu[b], 0), T);
+    len = min(max(cu[b + 1], first), T) - first;
+}
+// The sequence that tile `tile` (of `rows` rows, `per` rows a token of cu) belongs to, and its number there.  64 sequences at a
+// time, one a lane.  false: there are fewer tiles.
+__device__ __forceinline__ bool find_tile(const int32_t *cu, int T, int B, int rows, int per, int tile, int &b, int &t)
+{
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < B; b0 += 64) {
+        int first = 0, len = 0;
+        if (b0 + lane < B) bounds_of(cu, T, b0 + lane, first, len);
+        const int mine = (len * per + rows - 1) / rows;
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int u = __shfl_up(upto, d);
+            if (lane >= d) upto += u;
+        }
+        const uint64_t beyond = __ballot(upto > tile);
+        if (beyond) {
+            const int at = __builtin_ctzll(beyond);
+            b = b0 + at;
+            t = __builtin_amdgcn_readfirstlane(tile - (__shfl(upto, at) - __shfl(mine, at)));
+            return true;
+        }
+        tile -= __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+    }
+    return false;
+}
+__device__ __forceinline__ Seq seq_of(const AttnArgs &a, int b)
+{
+    Seq s;
+    s.b = b;
+    bounds_of(a.cu_q, a.Tq, b, s.q0, s.n);
+    bounds_of(a.cu_k, a.Tk, b, s.k0, s.m);
+    return s;
+}
+
+// Rows of one operand of one problem: row r of the sequence lies at base + (r / Gp) tok + (r % Gp) head.
+template <class T> struct Rows {
+    const T *base;
+    int64_t tok, head;
+    int count, D;               // rows there are
+    FastDiv by;                 // d = 1: rows are tokens
+    __device__ __forceinline__ const T *at(int r) const
+    {
+        if (by.d == 1) return base + (int64_t)r * tok;
+        const int t = (int)fdiv((uint32_t)r, by);
+        return base + (int64_t)t * tok + (int64_t)(r - t * (int)by.d) * head;
+    }
+    __device__ __forceinline__ Raw8<T> load(int r, int d) const
+    {
+        const int n = r < count ? D - d : 0;
+        return load8(n > 0 ? at(r) + d : base, n);
+    }
+};
+
+// A tile of Y on its way: loaded into registers while the tile before it is multiplied, then cut and put into LDS.
+template <class T, int DP, int ROWS, int THREADS> struct Stage {
+    static constexpr int NP = Pieces<T>::N, CH = DP / 8, N = (ROWS * CH + THREADS - 1) / THREADS;
+    Raw8<T> r[N];
+    __device__ __forceinline__ void load(const Rows<T> &src, int row0)
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int i = threadIdx.x + j * THREADS;
+            r[j] = src.load(row0 + i / CH, 8 * (i % CH));
+        }
+    }
+    __device__ __forceinline__ void put(char *t) const
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int i = threadIdx.x + j * THREADS;
+            if (ROWS * CH % THREADS == 0 || i < ROWS * CH) Tile<DP, ROWS, NP>::put(t, i / CH, i % CH, frag_of(r[j]));
+        }
+    }
+};
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// 32 dt + 8 j + 4 (lane / 32) ..: four neighbouring columns of an X row
+template <class T> __device__ __forceinline__ void store4(T *p, const float (&f)[4], int n)
+{
+    if (n >= 4) {
+        if constexpr (sizeof(T) == 4) {
+            Loose16<T> q;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q.w[i] = __float_as_uint(f[i]);
+            *reinterpret_cast<Loose16<T> *>(p) = q;
+        } else {
+            struct __attribute__((packed, aligned(2))) Loose8 { uint32_t w[2]; } q = {{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])}};
+            *reinterpret_cast<Loose8 *>(p) = q;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) p[i] = from_f32<T>(f[i]);
+    }
+}
+
+// The bias of a tile: entry e is that of delta = first + e, clamped to the table.
+__device__ __forceinline__ void bias_window(float *w, const AttnArgs &a, int h, int first, int n, int threads)
+{
+    const float *tab = a.btab + (int64_t)h * (2 * a.W + 1) + a.W;
+    for (int e = threadIdx.x; e < n; e += threads) w[e] = tab[min(max(first + e, -a.W), a.W)];
+}
+
+}  // namespace
+}  // namespace cg

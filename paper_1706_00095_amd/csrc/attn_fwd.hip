@@ -1,0 +1,277 @@
+// Attention, forward: one pass over the keys with the running maximum and sum of a softmax.
+#include "attn_device.h"
+
+namespace cg {
+namespace {
+
+// A block takes 128 query rows (X) of one problem and walks the keys (Y) they see in tiles of YT.
+template <class T, int DP, bool BIAS> struct Fwd {
+    static constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
+    using TileY = Tile<DP, YT, NP>;
+};
+
+template <class T, int DP, bool BIAS>
+__global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
+{
+    using F = Fwd<T, DP, BIAS>;
+    using TileY = typename F::TileY;
+    constexpr int NP = F::NP, YT = F::YT;
+    __shared__ __align__(16) char ldsK[TileY::BYTES], ldsV[TileY::BYTES];
+    __shared__ float window[BIAS ? kAttnRows + YT : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h32 = lane >> 5;
+    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, item = blockIdx.x / Hr, split = item % a.splits;
+    // the last tiles of a sequence see most keys under a causal mask: they start first
+    const int tile = a.tiles - 1 - item / a.splits;
+    int b, t;
+    if (!find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t)) return;
+    const Seq s = seq_of(a, b);
+    const int row0 = t * kAttnRows, rows = s.n * a.Gp, off = s.m - s.n;
+    const int h0 = hr * a.Gp, hkv = h0 / a.G;
+    // what this lane's row sees: keys below `limit`
+    const int row = row0 + 32 * wave + (lane & 31);
+    const bool here = row < rows;
+    const int tok = (int)fdiv((uint32_t)min(row, rows - 1), a.by_gp), head = h0 + (here ? row - tok * a.Gp : 0);
+    const int limit = a.causal ? min(max(tok + 1 + off, 0), s.m) : s.m;
+    const int first_tok = (int)fdiv((uint32_t)min(row0 + 32 * wave, rows - 1), a.by_gp);
+    const int wave_limit = a.causal ? min(max(first_tok + 1 + off, 0), s.m) : s.m;       // every row of the wave sees those
+    const int last_tok = (int)fdiv((uint32_t)min(row0 + kAttnRows, rows) - 1, a.by_gp);
+    int kend = a.causal ? min(max(last_tok + 1 + off, 0), s.m) : s.m, kbeg = 0;
+    if (a.splits > 1) {
+        kbeg = split * a.chunk;
+        if (split > 0 && kbeg >= kend) return;
+        kend = min(kend, kbeg + a.chunk);
+    }
+
+    const FastDiv one = {1, 1, 0};
+    const Rows<T> K{static_cast<const T *>(a.k) + (int64_t)s.k0 * a.k_tok + (int64_t)hkv * a.k_head, a.k_tok, 0, s.m, a.D, one};
+    const Rows<T> V{static_cast<const T *>(a.v) + (int64_t)s.k0 * a.v_tok + (int64_t)hkv * a.v_head, a.v_tok, 0, s.m, a.D, one};
+    const Rows<T> Q{static_cast<const T *>(a.q) + (int64_t)s.q0 * a.q_tok + (int64_t)h0 * a.q_head, a.q_tok, a.q_head, rows, a.D, a.by_gp};
+    Frag<NP> fq[F::KS];
+#pragma unroll
+    for (int ks = 0; ks < F::KS; ++ks) fq[ks] = frag_of(Q.load(row, 16 * ks + 8 * h32));
+
+    v16f O[F::DT];
+#pragma unroll
+    for (int dt = 0; dt < F::DT; ++dt) O[dt] = v16f{};
+    float m = -INFINITY, l = 0.f;
+    // without a bias scores stay as the product gives them and the scale enters the exponent: exp2(s c - m c)
+    const float c = a.scale * kLog2e;
+    const bool exact_p = BIAS && NP == 1 && a.o_rest;
+
+    Stage<T, DP, YT, 256> sk, sv;
+    if (kbeg < kend) {
+        sk.load(K, kbeg);
+        sv.load(V, kbeg);
+    }
+    for (int k0 = kbeg; k0 < kend; k0 += YT) {
+        __syncthreads();
+        sk.put(ldsK);
+        sv.put(ldsV);
+        if constexpr (BIAS) bias_window(window, a, h0, k0 - (row0 + kAttnRows - 1) - off, kAttnRows + YT - 1, 256);
+        __syncthreads();
+        if (k0 + YT < kend) {
+            sk.load(K, k0 + YT);
+            sv.load(V, k0 + YT);
+        }
+        float p[F::SUB][16];
+        float mt = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < F::SUB; ++u) {
+            Acc<NP> S;
+            S.zero();
+#pragma unroll
+            for (int ks = 0; ks < F::KS; ++ks) S.mma(TileY::rows(ldsK, 32 * u, ks, lane), fq[ks]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int y = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4;
+                p[u][i] = S.get(i);
+                if constexpr (BIAS) p[u][i] = fmaf(p[u][i], a.scale, window[y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
+            }
+        }
+        if (k0 + YT > wave_limit)
+#pragma unroll
+            for (int u = 0; u < F::SUB; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (k0 + 32 * u + 8 * (i / 4) + 4 * h32 + i % 4 >= limit) p[u][i] = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < F::SUB; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mt = fmaxf(mt, p[u][i]);
+        mt = fmaxf(mt, other_half(mt));
+        const float mn = fmaxf(m, mt), ms = mn == -INFINITY ? 0.f : mn;      // a row that has seen no key yet: exp2(-inf) = 0
+        const float alpha = __builtin_amdgcn_exp2f((m - ms) * (BIAS ? kLog2e : c));
+        m = mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < F::SUB; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[u][i] = __builtin_amdgcn_exp2f(BIAS ? (p[u][i] - ms) * kLog2e : fmaf(p[u][i], c, -ms * c));
+                sum += p[u][i];
+            }
+        l = fmaf(l, alpha, sum);
+        if constexpr (NP == 1) {
+            if (__any(alpha != 1.f))
+#pragma unroll
+                for (int dt = 0; dt < F::DT; ++dt) O[dt] *= alpha;
+#pragma unroll
+            for (int u = 0; u < F::SUB; ++u)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const Frag<1> fp = cut8<1>(&p[u][8 * g]);
+                    Frag<1> rest;
+                    if (exact_p) {
+                        float f[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = p[u][8 * g + i] - __uint_as_float(i & 1 ? fp.p[0][i / 2] & 0xffff0000u : fp.p[0][i / 2] << 16);
+                        rest = cut8<1>(f);
+                    }
+#pragma unroll
+                    for (int dt = 0; dt < F::DT; ++dt) {
+                        const Frag<1> fv = TileY::cols(ldsV, 32 * u + 16 * g, dt, lane);
+                        O[dt] = mfma(fv.p[0], fp.p[0], O[dt]);
+                        if (exact_p) O[dt] = mfma(fv.p[0], rest.p[0], O[dt]);
+                    }
+                }
+        } else {       // a tile's sum from zero, then one rounding into the running one
+            Frag<NP> fp[F::SUB][2];
+#pragma unroll
+            for (int u = 0; u < F::SUB; ++u)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) fp[u][g] = cut8<NP>(&p[u][8 * g]);
+#pragma unroll
+            for (int dt = 0; dt < F::DT; ++dt) {
+                Acc<NP> S;
+                S.zero();
+#pragma unroll
+                for (int u = 0; u < F::SUB; ++u)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsV, 32 * u + 16 * g, dt, lane), fp[u][g]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) O[dt][i] = fmaf(O[dt][i], alpha, S.get(i));
+            }
+        }
+    }
+    l += other_half(l);
+    if (a.splits > 1) {
+        if (!here) return;
+        const int64_t at = ((int64_t)hr * a.tiles + tile) * a.splits + split;
+        float *po = a.part_o + (at * kAttnRows + (row - row0)) * DP, *ml = a.part_ml + at * 2 * kAttnRows;
+        if (h32 == 0) {
+            ml[row - row0] = BIAS ? m : m * a.scale;
+            ml[kAttnRows + row - row0] = l;
+        }
+#pragma unroll
+        for (int dt = 0; dt < F::DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float f[4] = {O[dt][4 * j], O[dt][4 * j + 1], O[dt][4 * j + 2], O[dt][4 * j + 3]};
+                store4(po + 32 * dt + 8 * j + 4 * h32, f, 4);
+            }
+        return;
+    }
+    if (!here) return;
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;      // no key: 0; NaN stays
+    if (h32 == 0) a.lse[(int64_t)head * a.Tq + s.q0 + tok] = l == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), kLn2, BIAS ? m : m * a.scale);
+    const int64_t at = (int64_t)(s.q0 + tok) * a.o_tok + (int64_t)head * a.o_head;
+#pragma unroll
+    for (int dt = 0; dt < F::DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = 32 * dt + 8 * j + 4 * h32;
+            float f[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = O[dt][4 * j + i] * inv;
+            store4(static_cast<T *>(a.o) + at + d, f, a.D - d);
+            if constexpr (NP == 1) {
+                if (a.o_rest) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f[i] -= to_f32(from_f32<T>(f[i]));
+                    store4(static_cast<T *>(a.o_rest) + at + d, f, a.D - d);
+                }
+            }
+        }
+}
+
+// Joins the chunks of the keys: o = sum_s e^(m_s - M) o_s / sum_s e^(m_s - M) l_s.  A wave takes a row.
+template <class T, int DP> __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, item = blockIdx.x / Hr, tile = item / (kAttnRows / 4), part = item % (kAttnRows / 4);
+    int b, t;
+    if (!find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t)) return;
+    const Seq s = seq_of(a, b);
+    const int row0 = t * kAttnRows, rows = s.n * a.Gp, row = row0 + 4 * part + wave, off = s.m - s.n;
+    if (row >= rows) return;
+    const int tok = (int)fdiv((uint32_t)row, a.by_gp), head = hr * a.Gp + row - tok * a.Gp;
+    // the chunks that the tile's block has walked: the first always, the others up to the last key its rows see
+    const int last_tok = (int)fdiv((uint32_t)min(row0 + kAttnRows, rows) - 1, a.by_gp);
+    const int kend = a.causal ? min(max(last_tok + 1 + off, 0), s.m) : s.m;
+    const int n = max(1, (kend + a.chunk - 1) / a.chunk);
+    const int64_t at = ((int64_t)hr * a.tiles + tile) * a.splits;
+    const float *ml = a.part_ml + at * 2 * kAttnRows + (row - row0), *po = a.part_o + (at * kAttnRows + (row - row0)) * DP;
+    float M = -INFINITY;
+    for (int i = 0; i < n; ++i) M = fmaxf(M, ml[(int64_t)i * 2 * kAttnRows]);
+    const float Ms = M == -INFINITY ? 0.f : M;
+    float l = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int i = 0; i < n; ++i) {
+        const float w = __builtin_amdgcn_exp2f((ml[(int64_t)i * 2 * kAttnRows] - Ms) * kLog2e);
+        l = fmaf(w, ml[(int64_t)i * 2 * kAttnRows + kAttnRows], l);
+        const float *p = po + (int64_t)i * kAttnRows * DP;
+        if (lane < DP) o0 = fmaf(w, p[lane], o0);
+        if (lane + 64 < DP) o1 = fmaf(w, p[lane + 64], o1);
+    }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+    if (lane == 0) a.lse[(int64_t)head * a.Tq + s.q0 + tok] = l == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), kLn2, M);
+    const int64_t to = (int64_t)(s.q0 + tok) * a.o_tok + (int64_t)head * a.o_head;
+    const float f[2] = {o0 * inv, o1 * inv};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int d = lane + 64 * i;
+        if (d >= a.D) continue;
+        const T v = from_f32<T>(f[i]);
+        static_cast<T *>(a.o)[to + d] = v;
+        if (sizeof(T) == 2 && a.o_rest) static_cast<T *>(a.o_rest)[to + d] = from_f32<T>(f[i] - to_f32(v));
+    }
+}
+
+template <class T, int DP> int fwd_dp(const AttnArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
+    if (a.btab) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_fwd_kernel<T, DP, false>), grid, dim3(256), 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+template <class T, int DP> int combine_dp(const AttnArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((attn_combine_kernel<T, DP>), dim3((unsigned)(a.Hq / a.Gp) * a.tiles * (kAttnRows / 4)), dim3(256), 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
+}  // namespace
+
+int attn_fwd_launch(const AttnArgs &a, int type, hipStream_t s)
+{
+#define CG_DP(DP) if (a.D <= DP) return type == CG_TYPE_FP32 ? fwd_dp<float, DP>(a, s) : fwd_dp<bf16raw, DP>(a, s)
+    CG_DP(32);
+    CG_DP(64);
+    CG_DP(96);
+    CG_DP(128);
+#undef CG_DP
+    return CG_EUNSUPPORTED;
+}
+int attn_combine_launch(const AttnArgs &a, int type, hipStream_t s)
+{
+#define CG_DP(DP) if (a.D <= DP) return type == CG_TYPE_FP32 ? combine_dp<float, DP>(a, s) : combine_dp<bf16raw, DP>(a, s)
+    CG_DP(32);
+    CG_DP(64);
+    CG_DP(96);
+    CG_DP(128);
+#undef CG_DP
+    return CG_EUNSUPPORTED;
+}
+
+}  // namespace cg
