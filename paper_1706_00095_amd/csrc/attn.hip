@@ -139,6 +139,7 @@ AttnArgs args_of(const cg_attn_desc &d, const Plan &p, const void *q, const void
     a.W = p.W;
     a.tiles = p.tiles_q;
     a.splits = p.splits, a.chunk = p.chunk;
+    a.dma = d.type == CG_TYPE_BF16 && attn_dma_ok(k, d.k_tok, 0, 1, d.D) && attn_dma_ok(v, d.v_tok, 0, 1, d.D) && d.k_head % 8 == 0 && d.v_head % 8 == 0;
     if (d.buckets) {
         a.btab = reinterpret_cast<const float *>(ws + p.tab);
         a.bid = reinterpret_cast<const uint8_t *>(ws + p.bid);
@@ -218,6 +219,7 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
         if (int rc = attn_dbias_launch(a.dbias_part, d->Tq > 0 ? p.tiles_q : 0, d->Hq, d->buckets, dbias, s)) return rc;
     if (d->B > 0 && d->Tk > 0) {
         a.tiles = p.tiles_k;
+        a.dma = d->type == CG_TYPE_BF16 && attn_dma_ok(q, d->q_tok, d->q_head, p.Gp, d->D) && attn_dma_ok(d_o, d->o_tok, d->o_head, p.Gp, d->D);
         return attn_dkdv_launch(a, d->type, s);
     }
     return CG_OK;

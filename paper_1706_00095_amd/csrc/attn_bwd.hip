@@ -36,14 +36,15 @@ __device__ __forceinline__ void add_diagonals(const float (&ds)[16], int delta0,
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-template <class T, int DP, bool BIAS>
+template <class T, int DP, bool BIAS, bool DMA>
 __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel(AttnArgs a)
 {
     constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
     using TileY = Tile<DP, YT, NP>;
-    __shared__ __align__(16) char ldsK[TileY::BYTES], ldsV[TileY::BYTES];
-    __shared__ float window[BIAS ? kAttnRows + YT : 1], square[BIAS ? 4 : 1][BIAS ? 32 * kDiag : 1], bsum[BIAS ? 4 : 1][BIAS ? 256 : 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h32 = lane >> 5;
+    __shared__ __align__(16) char lds[2][2][TileY::BYTES];
+    LdsByte *const ldsK = (LdsByte *)lds[0][0], *const ldsV = (LdsByte *)lds[1][0];
+    __shared__ float window[2][BIAS ? 256 : 1], square[BIAS ? 4 : 1][BIAS ? 32 * kDiag : 1], bsum[BIAS ? 4 : 1][BIAS ? 256 : 1];
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
     const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, tile = a.tiles - 1 - blockIdx.x / Hr;
     const bool want_bias = BIAS && a.dbias_part;
     int b, t;
@@ -66,6 +67,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
     const int first_tok = (int)fdiv((uint32_t)min(row0 + 32 * wave, rows - 1), a.by_gp);
     const int wave_limit = a.causal ? min(max(first_tok + 1 + off, 0), s.m) : s.m;
     const int last_tok = (int)fdiv((uint32_t)min(row0 + kAttnRows, rows) - 1, a.by_gp);
+    const int wave_last = (int)fdiv((uint32_t)(min(max(row0 + 32 * wave + 32, 1), rows) - 1), a.by_gp);
+    const int wave_kend = row0 + 32 * wave >= rows ? 0 : a.causal ? min(max(wave_last + 1 + off, 0), s.m) : s.m;
     const int kend = a.causal ? min(max(last_tok + 1 + off, 0), s.m) : s.m;
 
     const FastDiv one = {1, 1, 0};
@@ -104,21 +107,26 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
     for (int dt = 0; dt < DT; ++dt) dQ[dt] = v16f{};
     float far_past = 0.f, far_future = 0.f;
 
-    Stage<T, DP, YT, 256> sk, sv;
+    Loader<T, DP, YT, DMA> lk(K), lv(V);
+    const int window0 = -(row0 + kAttnRows - 1) - off;
+    float bias_next = 0.f;
     if (kend > 0) {
-        sk.load(K, 0);
-        sv.load(V, 0);
+        lk.start(0, ldsK);
+        lv.start(0, ldsV);
+        if constexpr (BIAS) window[0][threadIdx.x] = window_load(a, h0, window0);
+        lk.finish(ldsK);
+        lv.finish(ldsV);
     }
-    for (int k0 = 0; k0 < kend; k0 += YT) {
-        __syncthreads();
-        sk.put(ldsK);
-        sv.put(ldsV);
-        if constexpr (BIAS) bias_window(window, a, h0, k0 - (row0 + kAttnRows - 1) - off, kAttnRows + YT - 1, 256);
-        __syncthreads();
-        if (k0 + YT < kend) {
-            sk.load(K, k0 + YT);
-            sv.load(V, k0 + YT);
+    int buf = 0;
+    for (int k0 = 0; k0 < kend; k0 += YT, buf ^= 1) {
+        tile_sync();
+        const bool more = k0 + YT < kend;
+        if (more) {
+            lk.start(k0 + YT, ldsK + (buf ^ 1) * TileY::BYTES);
+            lv.start(k0 + YT, ldsV + (buf ^ 1) * TileY::BYTES);
+            if constexpr (BIAS) bias_next = window_load(a, h0, k0 + YT + window0);
         }
+        if (k0 < wave_kend) {
         Frag<NP> fds[SUB][2];
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
@@ -127,8 +135,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
             P.zero();
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                S.mma(TileY::rows(ldsK, 32 * u, ks, lane), fq[ks]);
-                P.mma(TileY::rows(ldsV, 32 * u, ks, lane), fdo[ks]);
+                S.mma(TileY::rows(ldsK + buf * TileY::BYTES, 32 * u, ks, lane), fq[ks]);
+                P.mma(TileY::rows(ldsV + buf * TileY::BYTES, 32 * u, ks, lane), fdo[ks]);
             }
             float ds[16];
 #pragma unroll
@@ -136,7 +144,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
                 const int y = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4;
                 float p;
                 if constexpr (BIAS) {
-                    const float x = fmaf(S.get(i), a.scale, window[y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
+                    const float x = fmaf(S.get(i), a.scale, window[buf][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
                     p = __builtin_amdgcn_exp2f((x - lse) * kLog2e);
                 } else p = __builtin_amdgcn_exp2f(fmaf(S.get(i), c, -lse2));
                 ds[i] = p * (P.get(i) - delta);
@@ -171,17 +179,23 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) dQ[dt] = mfma(TileY::cols(ldsK, 32 * u + 16 * g, dt, lane).p[0], fds[u][g].p[0], dQ[dt]);
+                    for (int g = 0; g < 2; ++g) dQ[dt] = mfma(TileY::cols(ldsK + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane).p[0], fds[u][g].p[0], dQ[dt]);
             } else {
                 Acc<NP> S;
                 S.zero();
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsK, 32 * u + 16 * g, dt, lane), fds[u][g]);
+                    for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsK + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane), fds[u][g]);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) dQ[dt][i] += S.get(i);
             }
+        }
+        }
+        if (more) {
+            lk.finish(ldsK + (buf ^ 1) * TileY::BYTES);
+            lv.finish(ldsV + (buf ^ 1) * TileY::BYTES);
+            if constexpr (BIAS) window[buf ^ 1][threadIdx.x] = bias_next;
         }
     }
     if (want_bias) {
@@ -224,16 +238,17 @@ __global__ __launch_bounds__(256) void attn_dbias_kernel(const float *part, int 
 
 // X: 128 keys of a key-value head; Y: the query rows that see them, of all Gp heads.  With a bias Gp = 1, and the G heads
 // are walked one after the other.
-template <class T, int DP, bool BIAS>
+template <class T, int DP, bool BIAS, bool DMA>
 __global__ __launch_bounds__(256, 1) void attn_dkdv_kernel(AttnArgs a)
 {
-    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = 32;
+    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
     using TileY = Tile<DP, YT, NP>;
-    __shared__ __align__(16) char ldsQ[TileY::BYTES], ldsO[TileY::BYTES];
-    __shared__ __align__(16) float yl[YT], yd[YT];       // lse, delta of the tile's rows
-    __shared__ __align__(16) int ylim[YT];               // keys the row sees: below this
-    __shared__ float window[BIAS ? kAttnRows + YT : 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h32 = lane >> 5;
+    __shared__ __align__(16) char lds[2][2][TileY::BYTES];
+    LdsByte *const ldsQ = (LdsByte *)lds[0][0], *const ldsO = (LdsByte *)lds[1][0];
+    __shared__ __align__(16) float yl[2][YT], yd[2][YT];       // lse, delta of the tile's rows
+    __shared__ __align__(16) int ylim[2][YT];                  // keys the row sees: below this
+    __shared__ float window[2][BIAS ? 256 : 1];
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
     const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
     int b, t;
     if (!find_tile(a.cu_k, a.Tk, a.B, kAttnRows, 1, tile, b, t)) return;
@@ -262,52 +277,72 @@ __global__ __launch_bounds__(256, 1) void attn_dkdv_kernel(AttnArgs a)
         const int h0 = hkv * a.G + g * a.Gp;
         const Rows<T> Q{static_cast<const T *>(a.q) + (int64_t)s.q0 * a.q_tok + (int64_t)h0 * a.q_head, a.q_tok, a.q_head, rows, a.D, a.by_gp};
         const Rows<T> dO{static_cast<const T *>(a.d_o) + (int64_t)s.q0 * a.o_tok + (int64_t)h0 * a.o_head, a.o_tok, a.o_head, rows, a.D, a.by_gp};
-        Stage<T, DP, YT, 256> sq, so;
-        if (begin < rows) {
-            sq.load(Q, begin);
-            so.load(dO, begin);
-        }
-        for (int y0 = begin; y0 < rows; y0 += YT) {
-            __syncthreads();
-            sq.put(ldsQ);
-            so.put(ldsO);
+        Loader<T, DP, YT, DMA> lq(Q), lo(dO);
+        const int window0 = key0 - (YT - 1) - off;
+        float bias_next = 0.f, l_next = 0.f, d_next = 0.f;
+        int lim_next = 0;
+        // what the tile's rows have apart from their elements: a thread a row
+        auto row_start = [&](int y0) {
+            const int r = y0 + (threadIdx.x % YT), tok = (int)fdiv((uint32_t)min(r, rows - 1), a.by_gp);
+            const bool here = r < rows;
+            const int64_t stat = (int64_t)(h0 + (here ? r - tok * a.Gp : 0)) * a.Tq + s.q0 + tok;
+            l_next = here ? a.lse[stat] : -INFINITY;
+            d_next = here ? a.delta[stat] : 0.f;
+            lim_next = a.causal ? tok + 1 + off : s.m;
+            if constexpr (BIAS) bias_next = window_load(a, h0, window0 - y0);
+        };
+        auto row_finish = [&](int to) {
             if (threadIdx.x < YT) {
-                const int r = y0 + threadIdx.x, tok = (int)fdiv((uint32_t)min(r, rows - 1), a.by_gp);
-                const int64_t stat = (int64_t)(h0 + r - tok * a.Gp) * a.Tq + s.q0 + tok;
-                const bool here = r < rows;
-                float l = here ? a.lse[stat] : -INFINITY;
-                if (l == -INFINITY) l = INFINITY;
-                yl[threadIdx.x] = BIAS ? l : l * kLog2e;
-                yd[threadIdx.x] = here ? a.delta[stat] : 0.f;
-                ylim[threadIdx.x] = a.causal ? tok + 1 + off : s.m;
+                const float l = l_next == -INFINITY ? INFINITY : l_next;      // sees nothing: probabilities 0
+                yl[to][threadIdx.x] = BIAS ? l : l * kLog2e;
+                yd[to][threadIdx.x] = d_next;
+                ylim[to][threadIdx.x] = lim_next;
             }
-            if constexpr (BIAS) bias_window(window, a, h0, key0 - (y0 + YT - 1) - off, kAttnRows + YT - 1, 256);
-            __syncthreads();
-            if (y0 + YT < rows) {
-                sq.load(Q, y0 + YT);
-                so.load(dO, y0 + YT);
+            if constexpr (BIAS) window[to][threadIdx.x] = bias_next;
+        };
+        int buf = 0;
+        __syncthreads();      // the head before this one may still be read
+        if (begin < rows) {
+            lq.start(begin, ldsQ);
+            lo.start(begin, ldsO);
+            row_start(begin);
+            lq.finish(ldsQ);
+            lo.finish(ldsO);
+            row_finish(0);
+        }
+        for (int y0 = begin; y0 < rows; y0 += YT, buf ^= 1) {
+            tile_sync();
+            const bool more = y0 + YT < rows;
+            if (more) {
+                lq.start(y0 + YT, ldsQ + (buf ^ 1) * TileY::BYTES);
+                lo.start(y0 + YT, ldsO + (buf ^ 1) * TileY::BYTES);
+                row_start(y0 + YT);
             }
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+            // no row of these sees a key of this wave
+            if (a.causal && key0 + 32 * wave >= (int)__builtin_amdgcn_readfirstlane(ylim[buf][32 * u + 31])) continue;
             Acc<NP> S, P;
             S.zero();
             P.zero();
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                S.mma(TileY::rows(ldsQ, 0, ks, lane), fk[ks]);
-                P.mma(TileY::rows(ldsO, 0, ks, lane), fv[ks]);
+                S.mma(TileY::rows(ldsQ + buf * TileY::BYTES, 32 * u, ks, lane), fk[ks]);
+                P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), fv[ks]);
             }
             float p[16], ds[16];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int y = 8 * j + 4 * h32;
-                const float4 l4 = *reinterpret_cast<const float4 *>(yl + y), d4 = *reinterpret_cast<const float4 *>(yd + y);
-                const int4 m4 = *reinterpret_cast<const int4 *>(ylim + y);
+                const int y = 32 * u + 8 * j + 4 * h32;
+                const float4 l4 = *reinterpret_cast<const float4 *>(yl[buf] + y), d4 = *reinterpret_cast<const float4 *>(yd[buf] + y);
+                const int4 m4 = *reinterpret_cast<const int4 *>(ylim[buf] + y);
                 const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
                 const int lim[4] = {m4.x, m4.y, m4.z, m4.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float x;
                     if constexpr (BIAS) {
-                        x = fmaf(S.get(4 * j + i), a.scale, window[32 * wave + (lane & 31) - (y + i) + YT - 1]);
+                        x = fmaf(S.get(4 * j + i), a.scale, window[buf][32 * wave + (lane & 31) - (y + i) + YT - 1]);
                         x = __builtin_amdgcn_exp2f((x - l[i]) * kLog2e);
                     } else x = __builtin_amdgcn_exp2f(fmaf(S.get(4 * j + i), c, -l[i]));
                     const bool sees = key < lim[i];
@@ -326,22 +361,28 @@ __global__ __launch_bounds__(256, 1) void attn_dkdv_kernel(AttnArgs a)
                 if constexpr (NP == 1) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        dV[dt] = mfma(TileY::cols(ldsO, 16 * e, dt, lane).p[0], fp[e].p[0], dV[dt]);
-                        dK[dt] = mfma(TileY::cols(ldsQ, 16 * e, dt, lane).p[0], fds[e].p[0], dK[dt]);
+                        dV[dt] = mfma(TileY::cols(ldsO + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane).p[0], fp[e].p[0], dV[dt]);
+                        dK[dt] = mfma(TileY::cols(ldsQ + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane).p[0], fds[e].p[0], dK[dt]);
                     }
                 } else {
                     Acc<NP> A;
                     A.zero();
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsO, 16 * e, dt, lane), fp[e]);
+                    for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsO + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane), fp[e]);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) dV[dt][i] += A.get(i);
                     A.zero();
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsQ, 16 * e, dt, lane), fds[e]);
+                    for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsQ + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane), fds[e]);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) dK[dt][i] += A.get(i);
                 }
+            }
+            }
+            if (more) {
+                lq.finish(ldsQ + (buf ^ 1) * TileY::BYTES);
+                lo.finish(ldsO + (buf ^ 1) * TileY::BYTES);
+                row_finish(buf ^ 1);
             }
         }
     }
@@ -360,21 +401,33 @@ __global__ __launch_bounds__(256, 1) void attn_dkdv_kernel(AttnArgs a)
         }
 }
 
-template <class T, int DP> int dq_dp(const AttnArgs &a, hipStream_t s)
+template <class T, int DP, bool DMA> int dq_run(const AttnArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles);
-    if (a.btab) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false>), grid, dim3(256), 0, s, a);
+    if (a.btab) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+template <class T, int DP> int dq_dp(const AttnArgs &a, hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2)
+        if (a.dma) return dq_run<T, DP, true>(a, s);
+    return dq_run<T, DP, false>(a, s);
+}
+template <class T, int DP, bool DMA> int dkdv_run(const AttnArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)a.Hkv * a.tiles);
+    if (a.btab) hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
 }
 template <class T, int DP> int dkdv_dp(const AttnArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)a.Hkv * a.tiles);
-    if (a.btab) hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, false>), grid, dim3(256), 0, s, a);
-    CG_HIP_TRY(hipGetLastError());
-    return CG_OK;
+    if constexpr (sizeof(T) == 2)
+        if (a.dma) return dkdv_run<T, DP, true>(a, s);
+    return dkdv_run<T, DP, false>(a, s);
 }
 
 }  // namespace

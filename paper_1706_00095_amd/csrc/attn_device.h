@@ -37,11 +37,19 @@ struct AttnArgs {
     int tiles;                             // of X rows over all sequences, an upper bound
     // keys cut into `splits` chunks of `chunk` (0: one)
     int splits, chunk;
+    int dma;                               // K and V (forward, dq), Q and dO (dk/dv) may travel without registers
     float *part_o, *part_ml;               // [Hr][tiles][splits][rows][DP], [..][2][rows]
 };
 
 constexpr int kAttnRows = 128;             // X rows of a block: four waves of 32
 constexpr int kAttnMaxD = 128;
+
+// May rows of these strides (elements, bf16) travel without registers?  `per`: heads packed as rows (a tile of 32 begins with
+// a token).  16-byte aligned rows, and rows behind the last one behind the buffer's end.
+inline bool attn_dma_ok(const void *p, int64_t tok, int64_t head, int per, int D)
+{
+    return aligned16(p) && D % 8 == 0 && tok % 8 == 0 && head % 8 == 0 && tok >= (per - 1) * head + D && tok < (1 << 23) && 32 % per == 0;
+}
 
 // attn_fwd.hip, attn_bwd.hip: DP is D rounded up to a multiple of 32
 int attn_fwd_launch(const AttnArgs &a, int type, hipStream_t s);
@@ -55,6 +63,9 @@ namespace {
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+typedef __attribute__((address_space(3))) char LdsByte;      // LDS by its own addresses: 32 bits, no null checks
+#define CG_LDS(type, p) (*reinterpret_cast<__attribute__((address_space(3))) type *>(p))
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
@@ -138,38 +149,38 @@ template <int DP> __device__ __forceinline__ int swizzle(int row)
 template <int DP, int ROWS, int NP> struct Tile {
     static constexpr int CH = DP / 8, BYTES = NP * ROWS * DP * 2;
     static __device__ __forceinline__ int at(int row, int chunk) { return row * DP * 2 + ((chunk ^ swizzle<DP>(row)) << 4); }
-    static __device__ __forceinline__ void put(char *t, int row, int chunk, const Frag<NP> &f)
+    static __device__ __forceinline__ void put(LdsByte *t, int row, int chunk, const Frag<NP> &f)
     {
 #pragma unroll
-        for (int k = 0; k < NP; ++k) *reinterpret_cast<u32x4 *>(t + k * ROWS * DP * 2 + at(row, chunk)) = f.p[k];
+        for (int k = 0; k < NP; ++k) CG_LDS(u32x4, t + k * ROWS * DP * 2 + at(row, chunk)) = f.p[k];
     }
     // first operand, rows of the tile: row0 + lane % 32, contraction 16 ks ..
-    static __device__ __forceinline__ Frag<NP> rows(const char *t, int row0, int ks, int lane)
+    static __device__ __forceinline__ Frag<NP> rows(LdsByte *t, int row0, int ks, int lane)
     {
         Frag<NP> f;
 #pragma unroll
         for (int k = 0; k < NP; ++k)
-            f.p[k] = *reinterpret_cast<const u32x4 *>(t + k * ROWS * DP * 2 + at(row0 + (lane & 31), 2 * ks + (lane >> 5)));
+            f.p[k] = CG_LDS(u32x4, t + k * ROWS * DP * 2 + at(row0 + (lane & 31), 2 * ks + (lane >> 5)));
         return f;
     }
     // first operand, columns of the tile: 32 dt + lane % 32, contraction over the rows row0 .. row0 + 15 in the order of the C layout.
     // A transposing read gives lane i of 16 column i of the 4 x 16 values that the 16 lanes' addresses name, four lanes a row.
-    static __device__ __forceinline__ Frag<NP> cols(const char *t, int row0, int dt, int lane)
+    static __device__ __forceinline__ Frag<NP> cols(LdsByte *t, int row0, int dt, int lane)
     {
         const int row = row0 + 4 * (lane >> 5) + (lane >> 2 & 3), chunk = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
         Frag<NP> f;
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-            const char *base = t + k * ROWS * DP * 2 + 8 * (lane & 1);
+            LdsByte *base = t + k * ROWS * DP * 2 + 8 * (lane & 1);
             const s16x4 lo = tr(base + at(row, chunk)), hi = tr(base + at(row + 8, chunk));
             const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
             f.p[k] = u32x4{a.x, a.y, b.x, b.y};
         }
         return f;
     }
-    static __device__ __forceinline__ s16x4 tr(const char *p)
+    static __device__ __forceinline__ s16x4 tr(LdsByte *p)
     {
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p));
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(p));
     }
 };
 
@@ -235,27 +246,91 @@ template <class T> struct Rows {
     }
 };
 
-// A tile of Y on its way: loaded into registers while the tile before it is multiplied, then cut and put into LDS.
-template <class T, int DP, int ROWS, int THREADS> struct Stage {
-    static constexpr int NP = Pieces<T>::N, CH = DP / 8, N = (ROWS * CH + THREADS - 1) / THREADS;
+// A tile of Y on its way into one of two LDS buffers while the tile before it is multiplied in the other.
+//  start(row0, lds): the loads leave.  finish(lds): after the multiplications, before the barrier.
+// DMA: from memory to LDS without registers (bf16, 16-byte aligned rows; attn_dma_ok).  The buffer's base moves with the
+// tile, so a lane's offsets stay the same for all tiles and 32 bits wide whatever the length of a sequence; what lies behind the
+// last row is out of the buffer's range and arrives as zeros, as do the columns D .. DP - 1.
+// Otherwise: through registers, at any alignment, cut in pieces (fp32) on the way.
+template <class T, int DP, int ROWS, bool DMA> struct Loader;
+
+template <class T, int DP, int ROWS> struct Loader<T, DP, ROWS, false> {
+    static constexpr int NP = Pieces<T>::N, CH = DP / 8, N = (ROWS * CH + 255) / 256;
+    Rows<T> src;
     Raw8<T> r[N];
-    __device__ __forceinline__ void load(const Rows<T> &src, int row0)
+    __device__ __forceinline__ Loader(const Rows<T> &s) : src(s) {}
+    __device__ __forceinline__ void start(int row0, LdsByte *)
     {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int i = threadIdx.x + j * THREADS;
+            const int i = threadIdx.x + j * 256;
             r[j] = src.load(row0 + i / CH, 8 * (i % CH));
         }
     }
-    __device__ __forceinline__ void put(char *t) const
+    __device__ __forceinline__ void finish(LdsByte *t) const
     {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int i = threadIdx.x + j * THREADS;
-            if (ROWS * CH % THREADS == 0 || i < ROWS * CH) Tile<DP, ROWS, NP>::put(t, i / CH, i % CH, frag_of(r[j]));
+            const int i = threadIdx.x + j * 256;
+            if (ROWS * CH % 256 == 0 || i < ROWS * CH) Tile<DP, ROWS, NP>::put(t, i / CH, i % CH, frag_of(r[j]));
         }
     }
 };
+
+// 64 lanes x 16 bytes from memory to LDS: lane l's land at lds + 16 l.  Assembly, so that the waits stay with this file: the
+// compiler would drain every load before each LDS read.  Four wait states, because the descriptor's registers may have been
+// written by a vector instruction just before and nothing looks inside.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma16(BufferRsrc rsrc, LdsByte *lds, uint32_t voff)
+{
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)lds);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(voff), "s"(rsrc) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int DP, int ROWS> struct Loader<bf16raw, DP, ROWS, true> {
+    static constexpr int LOADS = ROWS * DP * 2 / 1024, N = (LOADS + 3) / 4;      // of 64 x 16 bytes; four waves share them
+    const bf16raw *base;
+    int64_t tok;
+    int gp, count;
+    uint32_t tail;          // bytes of the last token's rows
+    uint32_t voff[N];
+    __device__ __forceinline__ Loader(const Rows<bf16raw> &s) : base(s.base), tok(s.tok), gp((int)s.by.d), count(s.count)
+    {
+        const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        tail = (uint32_t)(((gp - 1) * s.head + s.D) * 2);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int at = (4 * j + wave) * 1024 + lane * 16, row = at / (DP * 2), chunk = at % (DP * 2) / 16 ^ swizzle<DP>(row);
+            const int t = row / gp;
+            voff[j] = 8 * chunk < s.D ? (uint32_t)((t * s.tok + (row - t * gp) * s.head) * 2 + chunk * 16) : OOB_ROW;
+        }
+    }
+    __device__ __forceinline__ void start(int row0, LdsByte *lds) const
+    {
+        const int t0 = row0 / gp, left = count / gp - t0;      // tokens; rows are whole tokens' (a tile begins with one)
+        const uint64_t at = (uint64_t)reinterpret_cast<uintptr_t>(base) + (uint64_t)((int64_t)t0 * tok * 2);
+        const uint64_t span = left > 0 ? (uint64_t)(left - 1) * (uint64_t)tok * 2 + tail : 0;
+        BufferRsrc r;
+        r.x = __builtin_amdgcn_readfirstlane((uint32_t)at);
+        r.y = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu);
+        r.z = __builtin_amdgcn_readfirstlane((uint32_t)(span < kMaxBufferBytes ? span : kMaxBufferBytes));
+        r.w = 0x00020000u;
+        const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (LOADS % 4 == 0 || 4 * j + wave < LOADS) dma16(r, lds + (4 * j + wave) * 1024, voff[j]);
+    }
+    __device__ __forceinline__ void finish(LdsByte *) const {}
+};
+
+// Between tiles: this wave's loads into LDS have landed, and everyone's.
+__device__ __forceinline__ void tile_sync()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 
@@ -279,11 +354,10 @@ template <class T> __device__ __forceinline__ void store4(T *p, const float (&f)
     }
 }
 
-// The bias of a tile: entry e is that of delta = first + e, clamped to the table.
-__device__ __forceinline__ void bias_window(float *w, const AttnArgs &a, int h, int first, int n, int threads)
+// The bias of a tile: entry e is that of delta = first + e, clamped to the table.  At most 256 entries, one a thread.
+__device__ __forceinline__ float window_load(const AttnArgs &a, int h, int first)
 {
-    const float *tab = a.btab + (int64_t)h * (2 * a.W + 1) + a.W;
-    for (int e = threadIdx.x; e < n; e += threads) w[e] = tab[min(max(first + e, -a.W), a.W)];
+    return a.btab[(int64_t)h * (2 * a.W + 1) + a.W + min(max(first + (int)threadIdx.x, -a.W), a.W)];
 }
 
 }  // namespace

@@ -5,20 +5,15 @@ namespace cg {
 namespace {
 
 // A block takes 128 query rows (X) of one problem and walks the keys (Y) they see in tiles of YT.
-template <class T, int DP, bool BIAS> struct Fwd {
-    static constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
-    using TileY = Tile<DP, YT, NP>;
-};
-
-template <class T, int DP, bool BIAS>
+template <class T, int DP, bool BIAS, bool DMA>
 __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
 {
-    using F = Fwd<T, DP, BIAS>;
-    using TileY = typename F::TileY;
-    constexpr int NP = F::NP, YT = F::YT;
-    __shared__ __align__(16) char ldsK[TileY::BYTES], ldsV[TileY::BYTES];
-    __shared__ float window[BIAS ? kAttnRows + YT : 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h32 = lane >> 5;
+    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
+    using TileY = Tile<DP, YT, NP>;
+    __shared__ __align__(16) char lds[2][2][TileY::BYTES];
+    LdsByte *const ldsK = (LdsByte *)lds[0][0], *const ldsV = (LdsByte *)lds[1][0];
+    __shared__ float window[2][BIAS ? 256 : 1];
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
     const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, item = blockIdx.x / Hr, split = item % a.splits;
     // the last tiles of a sequence see most keys under a causal mask: they start first
     const int tile = a.tiles - 1 - item / a.splits;
@@ -35,6 +30,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
     const int first_tok = (int)fdiv((uint32_t)min(row0 + 32 * wave, rows - 1), a.by_gp);
     const int wave_limit = a.causal ? min(max(first_tok + 1 + off, 0), s.m) : s.m;       // every row of the wave sees those
     const int last_tok = (int)fdiv((uint32_t)min(row0 + kAttnRows, rows) - 1, a.by_gp);
+    const int wave_last = (int)fdiv((uint32_t)(min(max(row0 + 32 * wave + 32, 1), rows) - 1), a.by_gp);
+    const int wave_kend = row0 + 32 * wave >= rows ? 0 : a.causal ? min(max(wave_last + 1 + off, 0), s.m) : s.m;
     int kend = a.causal ? min(max(last_tok + 1 + off, 0), s.m) : s.m, kbeg = 0;
     if (a.splits > 1) {
         kbeg = split * a.chunk;
@@ -46,56 +43,63 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
     const Rows<T> K{static_cast<const T *>(a.k) + (int64_t)s.k0 * a.k_tok + (int64_t)hkv * a.k_head, a.k_tok, 0, s.m, a.D, one};
     const Rows<T> V{static_cast<const T *>(a.v) + (int64_t)s.k0 * a.v_tok + (int64_t)hkv * a.v_head, a.v_tok, 0, s.m, a.D, one};
     const Rows<T> Q{static_cast<const T *>(a.q) + (int64_t)s.q0 * a.q_tok + (int64_t)h0 * a.q_head, a.q_tok, a.q_head, rows, a.D, a.by_gp};
-    Frag<NP> fq[F::KS];
+    Frag<NP> fq[KS];
 #pragma unroll
-    for (int ks = 0; ks < F::KS; ++ks) fq[ks] = frag_of(Q.load(row, 16 * ks + 8 * h32));
+    for (int ks = 0; ks < KS; ++ks) fq[ks] = frag_of(Q.load(row, 16 * ks + 8 * h32));
 
-    v16f O[F::DT];
+    v16f O[DT];
 #pragma unroll
-    for (int dt = 0; dt < F::DT; ++dt) O[dt] = v16f{};
+    for (int dt = 0; dt < DT; ++dt) O[dt] = v16f{};
     float m = -INFINITY, l = 0.f;
     // without a bias scores stay as the product gives them and the scale enters the exponent: exp2(s c - m c)
     const float c = a.scale * kLog2e;
     const bool exact_p = BIAS && NP == 1 && a.o_rest;
 
-    Stage<T, DP, YT, 256> sk, sv;
+    // Two buffers and one barrier a tile: behind it the tile is there and everyone is done with the one before, whose buffer the
+    // next one's loads then fill while this one is multiplied.
+    Loader<T, DP, YT, DMA> lk(K), lv(V);
+    const int window0 = -(row0 + kAttnRows - 1) - off;
+    float bias_next = 0.f;
     if (kbeg < kend) {
-        sk.load(K, kbeg);
-        sv.load(V, kbeg);
+        lk.start(kbeg, ldsK);
+        lv.start(kbeg, ldsV);
+        if constexpr (BIAS) window[0][threadIdx.x] = window_load(a, h0, kbeg + window0);
+        lk.finish(ldsK);
+        lv.finish(ldsV);
     }
-    for (int k0 = kbeg; k0 < kend; k0 += YT) {
-        __syncthreads();
-        sk.put(ldsK);
-        sv.put(ldsV);
-        if constexpr (BIAS) bias_window(window, a, h0, k0 - (row0 + kAttnRows - 1) - off, kAttnRows + YT - 1, 256);
-        __syncthreads();
-        if (k0 + YT < kend) {
-            sk.load(K, k0 + YT);
-            sv.load(V, k0 + YT);
+    int buf = 0;
+    for (int k0 = kbeg; k0 < kend; k0 += YT, buf ^= 1) {
+        tile_sync();
+        const bool more = k0 + YT < kend;
+        if (more) {
+            lk.start(k0 + YT, ldsK + (buf ^ 1) * TileY::BYTES);
+            lv.start(k0 + YT, ldsV + (buf ^ 1) * TileY::BYTES);
+            if constexpr (BIAS) bias_next = window_load(a, h0, k0 + YT + window0);
         }
-        float p[F::SUB][16];
+        if (k0 < wave_kend) {       // some row of the wave sees some key of the tile
+        float p[SUB][16];
         float mt = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < F::SUB; ++u) {
+        for (int u = 0; u < SUB; ++u) {
             Acc<NP> S;
             S.zero();
 #pragma unroll
-            for (int ks = 0; ks < F::KS; ++ks) S.mma(TileY::rows(ldsK, 32 * u, ks, lane), fq[ks]);
+            for (int ks = 0; ks < KS; ++ks) S.mma(TileY::rows(ldsK + buf * TileY::BYTES, 32 * u, ks, lane), fq[ks]);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int y = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4;
                 p[u][i] = S.get(i);
-                if constexpr (BIAS) p[u][i] = fmaf(p[u][i], a.scale, window[y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
+                if constexpr (BIAS) p[u][i] = fmaf(p[u][i], a.scale, window[buf][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
             }
         }
         if (k0 + YT > wave_limit)
 #pragma unroll
-            for (int u = 0; u < F::SUB; ++u)
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (k0 + 32 * u + 8 * (i / 4) + 4 * h32 + i % 4 >= limit) p[u][i] = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < F::SUB; ++u)
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mt = fmaxf(mt, p[u][i]);
         mt = fmaxf(mt, other_half(mt));
@@ -104,7 +108,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
         m = mn;
         float sum = 0.f;
 #pragma unroll
-        for (int u = 0; u < F::SUB; ++u)
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 p[u][i] = __builtin_amdgcn_exp2f(BIAS ? (p[u][i] - ms) * kLog2e : fmaf(p[u][i], c, -ms * c));
@@ -114,9 +118,9 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
         if constexpr (NP == 1) {
             if (__any(alpha != 1.f))
 #pragma unroll
-                for (int dt = 0; dt < F::DT; ++dt) O[dt] *= alpha;
+                for (int dt = 0; dt < DT; ++dt) O[dt] *= alpha;
 #pragma unroll
-            for (int u = 0; u < F::SUB; ++u)
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     const Frag<1> fp = cut8<1>(&p[u][8 * g]);
@@ -128,29 +132,35 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
                         rest = cut8<1>(f);
                     }
 #pragma unroll
-                    for (int dt = 0; dt < F::DT; ++dt) {
-                        const Frag<1> fv = TileY::cols(ldsV, 32 * u + 16 * g, dt, lane);
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const Frag<1> fv = TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane);
                         O[dt] = mfma(fv.p[0], fp.p[0], O[dt]);
                         if (exact_p) O[dt] = mfma(fv.p[0], rest.p[0], O[dt]);
                     }
                 }
         } else {       // a tile's sum from zero, then one rounding into the running one
-            Frag<NP> fp[F::SUB][2];
+            Frag<NP> fp[SUB][2];
 #pragma unroll
-            for (int u = 0; u < F::SUB; ++u)
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int g = 0; g < 2; ++g) fp[u][g] = cut8<NP>(&p[u][8 * g]);
 #pragma unroll
-            for (int dt = 0; dt < F::DT; ++dt) {
+            for (int dt = 0; dt < DT; ++dt) {
                 Acc<NP> S;
                 S.zero();
 #pragma unroll
-                for (int u = 0; u < F::SUB; ++u)
+                for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsV, 32 * u + 16 * g, dt, lane), fp[u][g]);
+                    for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane), fp[u][g]);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) O[dt][i] = fmaf(O[dt][i], alpha, S.get(i));
             }
+        }
+        }
+        if (more) {
+            lk.finish(ldsK + (buf ^ 1) * TileY::BYTES);
+            lv.finish(ldsV + (buf ^ 1) * TileY::BYTES);
+            if constexpr (BIAS) window[buf ^ 1][threadIdx.x] = bias_next;
         }
     }
     l += other_half(l);
@@ -163,7 +173,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
             ml[kAttnRows + row - row0] = l;
         }
 #pragma unroll
-        for (int dt = 0; dt < F::DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float f[4] = {O[dt][4 * j], O[dt][4 * j + 1], O[dt][4 * j + 2], O[dt][4 * j + 3]};
@@ -176,7 +186,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
     if (h32 == 0) a.lse[(int64_t)head * a.Tq + s.q0 + tok] = l == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), kLn2, BIAS ? m : m * a.scale);
     const int64_t at = (int64_t)(s.q0 + tok) * a.o_tok + (int64_t)head * a.o_head;
 #pragma unroll
-    for (int dt = 0; dt < F::DT; ++dt)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int d = 32 * dt + 8 * j + 4 * h32;
@@ -197,7 +207,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
 // Joins the chunks of the keys: o = sum_s e^(m_s - M) o_s / sum_s e^(m_s - M) l_s.  A wave takes a row.
 template <class T, int DP> __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, item = blockIdx.x / Hr, tile = item / (kAttnRows / 4), part = item % (kAttnRows / 4);
     int b, t;
     if (!find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t)) return;
@@ -236,13 +246,19 @@ template <class T, int DP> __global__ __launch_bounds__(256) void attn_combine_k
     }
 }
 
-template <class T, int DP> int fwd_dp(const AttnArgs &a, hipStream_t s)
+template <class T, int DP, bool DMA> int fwd_run(const AttnArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
-    if (a.btab) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_fwd_kernel<T, DP, false>), grid, dim3(256), 0, s, a);
+    if (a.btab) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_fwd_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
+}
+template <class T, int DP> int fwd_dp(const AttnArgs &a, hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2)
+        if (a.dma) return fwd_run<T, DP, true>(a, s);
+    return fwd_run<T, DP, false>(a, s);
 }
 template <class T, int DP> int combine_dp(const AttnArgs &a, hipStream_t s)
 {
