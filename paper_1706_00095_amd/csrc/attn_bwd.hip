@@ -239,10 +239,16 @@ __global__ __launch_bounds__(256) void attn_dbias_kernel(const float *part, int 
 // X: 128 keys of a key-value head; Y: the query rows that see them, of all Gp heads.  With a bias Gp = 1, and the G heads
 // are walked one after the other.
 template <class T, int DP, bool BIAS, bool DMA>
-__global__ __launch_bounds__(256, 1) void attn_dkdv_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kernel(AttnArgs a)
 {
-    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
+    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 && DP < 128 ? 64 : 32, SUB = YT / 32;
     using TileY = Tile<DP, YT, NP>;
+    // Two waves a SIMD (256 registers each) hide each other's LDS reads and exponentials.  At DP = 128 dK, dV and both operands' fragments
+    // leave no room for anything else: V's fragments are read from LDS each time instead.
+    constexpr bool V_IN_LDS = NP == 1 && DP >= 96;
+    using TileX = Tile<DP, kAttnRows, NP>;
+    __shared__ __align__(16) char lds_v[V_IN_LDS ? TileX::BYTES : 16];
+    LdsByte *const ldsV = (LdsByte *)lds_v;
     __shared__ __align__(16) char lds[2][2][TileY::BYTES];
     LdsByte *const ldsQ = (LdsByte *)lds[0][0], *const ldsO = (LdsByte *)lds[1][0];
     __shared__ __align__(16) float yl[2][YT], yd[2][YT];       // lse, delta of the tile's rows
@@ -259,11 +265,13 @@ __global__ __launch_bounds__(256, 1) void attn_dkdv_kernel(AttnArgs a)
     const FastDiv one = {1, 1, 0};
     const Rows<T> K{static_cast<const T *>(a.k) + (int64_t)s.k0 * a.k_tok + (int64_t)hkv * a.k_head, a.k_tok, 0, s.m, a.D, one};
     const Rows<T> V{static_cast<const T *>(a.v) + (int64_t)s.k0 * a.v_tok + (int64_t)hkv * a.v_head, a.v_tok, 0, s.m, a.D, one};
-    Frag<NP> fk[KS], fv[KS];
+    Frag<NP> fk[KS], fv[V_IN_LDS ? 1 : KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         fk[ks] = frag_of(K.load(key, 16 * ks + 8 * h32));
-        fv[ks] = frag_of(V.load(key, 16 * ks + 8 * h32));
+        const Frag<NP> f = frag_of(V.load(key, 16 * ks + 8 * h32));
+        if constexpr (V_IN_LDS) TileX::put(ldsV, 32 * wave + (lane & 31), 2 * ks + h32, f);      // read by the lane's own wave alone
+        else fv[ks] = f;
     }
     v16f dK[DT], dV[DT];
 #pragma unroll
@@ -328,16 +336,15 @@ __global__ __launch_bounds__(256, 1) void attn_dkdv_kernel(AttnArgs a)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 S.mma(TileY::rows(ldsQ + buf * TileY::BYTES, 32 * u, ks, lane), fk[ks]);
-                P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), fv[ks]);
+                if constexpr (V_IN_LDS) P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), TileX::rows(ldsV, 32 * wave, ks, lane));
+                else P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), fv[ks]);
             }
             float p[16], ds[16];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int y = 32 * u + 8 * j + 4 * h32;
                 const float4 l4 = *reinterpret_cast<const float4 *>(yl[buf] + y), d4 = *reinterpret_cast<const float4 *>(yd[buf] + y);
-                const int4 m4 = *reinterpret_cast<const int4 *>(ylim[buf] + y);
                 const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
-                const int lim[4] = {m4.x, m4.y, m4.z, m4.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float x;
@@ -345,11 +352,20 @@ __global__ __launch_bounds__(256, 1) void attn_dkdv_kernel(AttnArgs a)
                         x = fmaf(S.get(4 * j + i), a.scale, window[buf][32 * wave + (lane & 31) - (y + i) + YT - 1]);
                         x = __builtin_amdgcn_exp2f((x - l[i]) * kLog2e);
                     } else x = __builtin_amdgcn_exp2f(fmaf(S.get(4 * j + i), c, -l[i]));
-                    const bool sees = key < lim[i];
-                    p[4 * j + i] = sees ? x : 0.f;
-                    ds[4 * j + i] = sees ? x * (P.get(4 * j + i) - d[i]) : 0.f;
+                    p[4 * j + i] = x;
+                    ds[4 * j + i] = x * (P.get(4 * j + i) - d[i]);
                 }
             }
+            // the first row does not see all the wave's keys, or some keys are none
+            if (key0 + 32 * wave + 32 > (int)__builtin_amdgcn_readfirstlane(ylim[buf][32 * u]))
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int4 m4 = *reinterpret_cast<const int4 *>(ylim[buf] + 32 * u + 8 * j + 4 * h32);
+                    const int lim[4] = {m4.x, m4.y, m4.z, m4.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (key >= lim[i]) p[4 * j + i] = 0.f, ds[4 * j + i] = 0.f;
+                }
             Frag<NP> fp[2], fds[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
