@@ -95,12 +95,16 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
         }
         fdo[ks] = frag_of(g);
     }
-    delta += other_half(delta);
+    delta = sum_halves(delta);
     const int64_t stat = (int64_t)head * a.Tq + s.q0 + tok;
     float lse = here ? a.lse[stat] : -INFINITY;
     if (here && h32 == 0) a.delta[stat] = delta;
     if (lse == -INFINITY) lse = INFINITY;      // a row that sees nothing (or is none): probabilities 0
     const float c = a.scale * kLog2e, lse2 = lse * kLog2e;
+
+    arrived(fq);
+    arrived(fdo);
+    arrived(lse);
 
     v16f dQ[DT];
 #pragma unroll
@@ -152,7 +156,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
             if (k0 + 32 * u + 32 > wave_limit)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (k0 + 32 * u + 8 * (i / 4) + 4 * h32 + i % 4 >= limit) ds[i] = 0.f;
+                    if (32 * u + 8 * (i / 4) + i % 4 >= limit - k0 - 4 * h32) ds[i] = 0.f;
             if constexpr (BIAS) {
                 if (want_bias) {
                     // distances of this 32 x 32 part: first .. first + 62
@@ -273,6 +277,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
         if constexpr (V_IN_LDS) TileX::put(ldsV, 32 * wave + (lane & 31), 2 * ks + h32, f);      // read by the lane's own wave alone
         else fv[ks] = f;
     }
+    arrived(fk);
+    if constexpr (!V_IN_LDS) arrived(fv);
     v16f dK[DT], dV[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dK[dt] = v16f{}, dV[dt] = v16f{};

@@ -332,7 +332,27 @@ __device__ __forceinline__ void tile_sync()
     __syncthreads();
 }
 
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// Over a lane and lane ^ 32, which hold the two halves of an X row's scores.
+__device__ __forceinline__ float max_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// The fragments are there from here on.  Without it the compiler waits for them at their first use, inside the loop over tiles, and
+// with them, in every turn, for the tile that has just been asked for.
+template <int NP, int N> __device__ __forceinline__ void arrived(Frag<NP> (&f)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int k = 0; k < NP; ++k) asm volatile("" : "+v"(f[i].p[k]));
+}
+__device__ __forceinline__ void arrived(float &x) { asm volatile("" : "+v"(x)); }
 
 // 32 dt + 8 j + 4 (lane / 32) ..: four neighbouring columns of an X row
 template <class T> __device__ __forceinline__ void store4(T *p, const float (&f)[4], int n)

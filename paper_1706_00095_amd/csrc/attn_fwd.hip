@@ -4,6 +4,8 @@
 namespace cg {
 namespace {
 
+constexpr float kSlack = 8.f;
+
 // A block takes 128 query rows (X) of one problem and walks the keys (Y) they see in tiles of YT.
 template <class T, int DP, bool BIAS, bool DMA>
 __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
@@ -46,6 +48,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
     Frag<NP> fq[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) fq[ks] = frag_of(Q.load(row, 16 * ks + 8 * h32));
+
+    arrived(fq);
 
     v16f O[DT];
 #pragma unroll
@@ -97,14 +101,17 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
             for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (k0 + 32 * u + 8 * (i / 4) + 4 * h32 + i % 4 >= limit) p[u][i] = -INFINITY;
+                    if (32 * u + 8 * (i / 4) + i % 4 >= limit - k0 - 4 * h32) p[u][i] = -INFINITY;
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mt = fmaxf(mt, p[u][i]);
-        mt = fmaxf(mt, other_half(mt));
-        const float mn = fmaxf(m, mt), ms = mn == -INFINITY ? 0.f : mn;      // a row that has seen no key yet: exp2(-inf) = 0
-        const float alpha = __builtin_amdgcn_exp2f((m - ms) * (BIAS ? kLog2e : c));
+        mt = max_halves(mt);
+        // The running maximum follows only where it has grown by a factor of 2^kSlack: p stays below that, at the same relative
+        // precision, and the sums are hardly ever scaled again.
+        const bool grows = (mt - m) * (BIAS ? kLog2e : c) > kSlack;
+        const float mn = grows ? mt : m, ms = mn == -INFINITY ? 0.f : mn;      // a row that has seen no key yet: exp2(-inf) = 0
+        const float alpha = grows ? __builtin_amdgcn_exp2f((m - ms) * (BIAS ? kLog2e : c)) : 1.f;
         m = mn;
         float sum = 0.f;
 #pragma unroll
@@ -116,7 +123,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
             }
         l = fmaf(l, alpha, sum);
         if constexpr (NP == 1) {
-            if (__any(alpha != 1.f))
+            if (__any(grows))
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) O[dt] *= alpha;
 #pragma unroll
@@ -163,7 +170,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
             if constexpr (BIAS) window[buf ^ 1][threadIdx.x] = bias_next;
         }
     }
-    l += other_half(l);
+    l = sum_halves(l);
     if (a.splits > 1) {
         if (!here) return;
         const int64_t at = ((int64_t)hr * a.tiles + tile) * a.splits + split;
