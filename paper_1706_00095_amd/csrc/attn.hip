@@ -70,7 +70,7 @@ int check(const cg_attn_desc *d)
 // How the pass is laid out and what it keeps in the workspace.
 struct Plan {
     int Gp, tiles_q, tiles_k, W, splits, chunk;
-    size_t tab, bid, part_o, part_ml, delta, dbias, bytes;       // offsets; bytes in all
+    size_t tab, bid, part_o, part_ml, delta, lse_b, dbias, bytes;       // offsets; bytes in all
 };
 
 // Few query tiles leave most of the chip idle, and a long axis of keys is walked tile by tile: the keys are then cut into chunks, a
@@ -111,6 +111,8 @@ Plan plan_of(const cg_attn_desc &d, int pass)
         }
     } else {
         p.delta = (size_t)at;
+        at += up(d.Tq * d.Hq * 4, 256);
+        p.lse_b = (size_t)at;
         at += up(d.Tq * d.Hq * 4, 256);
         p.dbias = (size_t)at;
         if (d.buckets) at += up((int64_t)d.Hq * p.tiles_q * d.buckets * 4, 256);
@@ -212,6 +214,7 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
     a.d_o = d_o, a.o_in = o, a.o_rest_in = o_rest, a.lse = const_cast<float *>(lse);
     a.dq = dq, a.dk = dk, a.dv = dv;
     a.delta = reinterpret_cast<float *>(w + p.delta);
+    a.lse_b = reinterpret_cast<float *>(w + p.lse_b);
     if (dbias) a.dbias_part = reinterpret_cast<float *>(w + p.dbias);
     if (d->B > 0 && d->Tq > 0)
         if (int rc = attn_dq_launch(a, d->type, s)) return rc;
@@ -219,7 +222,8 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
         if (int rc = attn_dbias_launch(a.dbias_part, d->Tq > 0 ? p.tiles_q : 0, d->Hq, d->buckets, dbias, s)) return rc;
     if (d->B > 0 && d->Tk > 0) {
         a.tiles = p.tiles_k;
-        a.dma = d->type == CG_TYPE_BF16 && attn_dma_ok(q, d->q_tok, d->q_head, p.Gp, d->D) && attn_dma_ok(d_o, d->o_tok, d->o_head, p.Gp, d->D);
+        a.dma = d->type == CG_TYPE_BF16 && attn_dma_ok(q, d->q_tok, d->q_head, p.Gp, d->D) && attn_dma_ok(d_o, d->o_tok, d->o_head, p.Gp, d->D) &&
+                d->Tq * d->Hq < (1 << 29);
         return attn_dkdv_launch(a, d->type, s);
     }
     return CG_OK;

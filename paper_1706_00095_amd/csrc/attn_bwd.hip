@@ -97,14 +97,16 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
     }
     delta = sum_halves(delta);
     const int64_t stat = (int64_t)head * a.Tq + s.q0 + tok;
-    float lse = here ? a.lse[stat] : -INFINITY;
-    if (here && h32 == 0) a.delta[stat] = delta;
-    if (lse == -INFINITY) lse = INFINITY;      // a row that sees nothing (or is none): probabilities 0
-    const float c = a.scale * kLog2e, lse2 = lse * kLog2e;
+    const float lse = here ? a.lse[stat] : -INFINITY;
+    // the exponent takes lse in the scores' own units with a bias, else times log2 e; a row that sees nothing (or is none) has probabilities 0
+    const float c = a.scale * kLog2e, lse_b = lse == -INFINITY ? INFINITY : BIAS ? lse : lse * kLog2e;
+    if (here && h32 == 0) {
+        a.delta[stat] = delta;
+        a.lse_b[stat] = lse_b;
+    }
 
     arrived(fq);
     arrived(fdo);
-    arrived(lse);
 
     v16f dQ[DT];
 #pragma unroll
@@ -149,8 +151,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
                 float p;
                 if constexpr (BIAS) {
                     const float x = fmaf(S.get(i), a.scale, window[buf][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
-                    p = __builtin_amdgcn_exp2f((x - lse) * kLog2e);
-                } else p = __builtin_amdgcn_exp2f(fmaf(S.get(i), c, -lse2));
+                    p = __builtin_amdgcn_exp2f((x - lse_b) * kLog2e);
+                } else p = __builtin_amdgcn_exp2f(fmaf(S.get(i), c, -lse_b));
                 ds[i] = p * (P.get(i) - delta);
             }
             if (k0 + 32 * u + 32 > wave_limit)
@@ -255,8 +257,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
     LdsByte *const ldsV = (LdsByte *)lds_v;
     __shared__ __align__(16) char lds[2][2][TileY::BYTES];
     LdsByte *const ldsQ = (LdsByte *)lds[0][0], *const ldsO = (LdsByte *)lds[1][0];
-    __shared__ __align__(16) float yl[2][YT], yd[2][YT];       // lse, delta of the tile's rows
-    __shared__ __align__(16) int ylim[2][YT];                  // keys the row sees: below this
+    __shared__ __align__(16) float stats[2][2][64];            // lse_b, delta of the tile's rows
     __shared__ float window[2][BIAS ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
     const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
@@ -283,9 +284,11 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dK[dt] = v16f{}, dV[dt] = v16f{};
     const float c = a.scale * kLog2e;
-    // the first row that sees the block's first key
-    const int first = a.causal ? max(key0 - off, 0) : 0;
-    const int begin = (int)min((int64_t)first * a.Gp, (int64_t)rows) / YT * YT;
+    // Row r of token r / Gp sees the key where r >= (key - off) Gp.  Keys behind the last one need no mask: what is added up for them
+    // is not stored.
+    auto row_of = [&](int k) { return a.causal ? (int)min(max((int64_t)(k - off) * a.Gp, (int64_t)0), (int64_t)rows) : 0; };
+    const int first_row = row_of(key), wave_first = row_of(key0 + 32 * wave), wave_all = row_of(key0 + 32 * wave + 31);
+    const int begin = row_of(key0) / YT * YT;
 
     for (int g = 0; g < a.G / a.Gp; ++g) {
         const int h0 = hkv * a.G + g * a.Gp;
@@ -293,25 +296,28 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
         const Rows<T> dO{static_cast<const T *>(a.d_o) + (int64_t)s.q0 * a.o_tok + (int64_t)h0 * a.o_head, a.o_tok, a.o_head, rows, a.D, a.by_gp};
         Loader<T, DP, YT, DMA> lq(Q), lo(dO);
         const int window0 = key0 - (YT - 1) - off;
-        float bias_next = 0.f, l_next = 0.f, d_next = 0.f;
-        int lim_next = 0;
-        // what the tile's rows have apart from their elements: a thread a row
-        auto row_start = [&](int y0) {
-            const int r = y0 + (threadIdx.x % YT), tok = (int)fdiv((uint32_t)min(r, rows - 1), a.by_gp);
-            const bool here = r < rows;
-            const int64_t stat = (int64_t)(h0 + (here ? r - tok * a.Gp : 0)) * a.Tq + s.q0 + tok;
-            l_next = here ? a.lse[stat] : -INFINITY;
-            d_next = here ? a.delta[stat] : 0.f;
-            lim_next = a.causal ? tok + 1 + off : s.m;
+        float bias_next = 0.f, stat_next = 0.f;
+        // What the tile's rows have apart from their elements: threads 0 .. 63 lse_b, 64 .. 127 delta, a row each.  Rows that are none get
+        // zeros: their elements are zeros as well, so that a probability of 1 adds nothing.
+        auto row_start = [&](int y0, int to) {
+            if (wave < 2) {
+                const int r = y0 + lane;
+                const float *from = (wave == 0 ? a.lse_b : a.delta) + (int64_t)h0 * a.Tq + s.q0;
+                const bool here = lane < YT && r < rows;
+                if constexpr (DMA) {
+                    const int tok = (int)fdiv((uint32_t)(here ? r : 0), a.by_gp);
+                    const uint32_t at = (uint32_t)(((here ? r : 0) - tok * a.Gp) * a.Tq + tok) * 4u;      // Hq Tq < 2^29
+                    dma4(raw_buffer((uint64_t)reinterpret_cast<uintptr_t>(from), kMaxBufferBytes), (LdsByte *)stats[to][wave], here ? at : OOB_ROW);
+                } else {
+                    const int tok = (int)fdiv((uint32_t)(here ? r : 0), a.by_gp);
+                    stat_next = here ? from[(int64_t)(r - tok * a.Gp) * a.Tq + tok] : 0.f;
+                }
+            }
             if constexpr (BIAS) bias_next = window_load(a, h0, window0 - y0);
         };
         auto row_finish = [&](int to) {
-            if (threadIdx.x < YT) {
-                const float l = l_next == -INFINITY ? INFINITY : l_next;      // sees nothing: probabilities 0
-                yl[to][threadIdx.x] = BIAS ? l : l * kLog2e;
-                yd[to][threadIdx.x] = d_next;
-                ylim[to][threadIdx.x] = lim_next;
-            }
+            if constexpr (!DMA)
+                if (wave < 2) stats[to][wave][lane] = stat_next;
             if constexpr (BIAS) window[to][threadIdx.x] = bias_next;
         };
         int buf = 0;
@@ -319,7 +325,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
         if (begin < rows) {
             lq.start(begin, ldsQ);
             lo.start(begin, ldsO);
-            row_start(begin);
+            row_start(begin, 0);
             lq.finish(ldsQ);
             lo.finish(ldsO);
             row_finish(0);
@@ -330,12 +336,11 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
             if (more) {
                 lq.start(y0 + YT, ldsQ + (buf ^ 1) * TileY::BYTES);
                 lo.start(y0 + YT, ldsO + (buf ^ 1) * TileY::BYTES);
-                row_start(y0 + YT);
+                row_start(y0 + YT, buf ^ 1);
             }
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
-            // no row of these sees a key of this wave
-            if (a.causal && key0 + 32 * wave >= (int)__builtin_amdgcn_readfirstlane(ylim[buf][32 * u + 31])) continue;
+            if (y0 + 32 * u + 32 <= wave_first) continue;      // no row of these sees a key of this wave
             Acc<NP> S, P;
             S.zero();
             P.zero();
@@ -345,11 +350,12 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
                 if constexpr (V_IN_LDS) P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), TileX::rows(ldsV, 32 * wave, ks, lane));
                 else P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), fv[ks]);
             }
+            if constexpr (NP == 1) reads_ahead<2 * KS, 6, V_IN_LDS ? 2 : 1>();
             float p[16], ds[16];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int y = 32 * u + 8 * j + 4 * h32;
-                const float4 l4 = *reinterpret_cast<const float4 *>(yl[buf] + y), d4 = *reinterpret_cast<const float4 *>(yd[buf] + y);
+                const float4 l4 = *reinterpret_cast<const float4 *>(stats[buf][0] + y), d4 = *reinterpret_cast<const float4 *>(stats[buf][1] + y);
                 const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -362,16 +368,10 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
                     ds[4 * j + i] = x * (P.get(4 * j + i) - d[i]);
                 }
             }
-            // the first row does not see all the wave's keys, or some keys are none
-            if (key0 + 32 * wave + 32 > (int)__builtin_amdgcn_readfirstlane(ylim[buf][32 * u]))
+            if (y0 + 32 * u < wave_all)       // some row does not see some key
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int4 m4 = *reinterpret_cast<const int4 *>(ylim[buf] + 32 * u + 8 * j + 4 * h32);
-                    const int lim[4] = {m4.x, m4.y, m4.z, m4.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (key >= lim[i]) p[4 * j + i] = 0.f, ds[4 * j + i] = 0.f;
-                }
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i / 4) + i % 4 < first_row - y0 - 32 * u - 4 * h32) p[i] = 0.f, ds[i] = 0.f;
             Frag<NP> fp[2], fds[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {

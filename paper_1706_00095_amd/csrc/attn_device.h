@@ -22,7 +22,8 @@ namespace cg {
 struct AttnArgs {
     const void *q, *k, *v, *d_o, *o_in, *o_rest_in;
     void *o, *o_rest, *dq, *dk, *dv;
-    float *lse, *delta;                    // [Hq][Tq]
+    float *lse;                            // [Hq][Tq]
+    float *delta, *lse_b;                  // [Hq][Tq], written by the dq kernel: sums of do o, and lse as the exponent takes it
     const int32_t *cu_q, *cu_k;
     int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
     int B, Tq, Tk, Hq, Hkv, G, Gp, D;      // G: query heads of a key-value head; Gp of them are packed (1 or G)
@@ -282,6 +283,11 @@ template <class T, int DP, int ROWS> struct Loader<T, DP, ROWS, false> {
 // written by a vector instruction just before and nothing looks inside.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma4(BufferRsrc rsrc, LdsByte *lds, uint32_t voff)
+{
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)lds);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(voff), "s"(rsrc) : "memory", "m0");
+}
 __device__ __forceinline__ void dma16(BufferRsrc rsrc, LdsByte *lds, uint32_t voff)
 {
     const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)lds);
@@ -289,34 +295,43 @@ __device__ __forceinline__ void dma16(BufferRsrc rsrc, LdsByte *lds, uint32_t vo
 }
 #pragma clang diagnostic pop
 
+__device__ __forceinline__ BufferRsrc raw_buffer(uint64_t at, uint64_t bytes)
+{
+    BufferRsrc r;
+    r.x = __builtin_amdgcn_readfirstlane((uint32_t)at);
+    r.y = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu);
+    r.z = __builtin_amdgcn_readfirstlane((uint32_t)(bytes < kMaxBufferBytes ? bytes : kMaxBufferBytes));
+    r.w = 0x00020000u;
+    return r;
+}
+
 template <int DP, int ROWS> struct Loader<bf16raw, DP, ROWS, true> {
     static constexpr int LOADS = ROWS * DP * 2 / 1024, N = (LOADS + 3) / 4;      // of 64 x 16 bytes; four waves share them
     const bf16raw *base;
     int64_t tok;
-    int gp, count;
+    int shift, tokens;      // a token's rows: a power of two
     uint32_t tail;          // bytes of the last token's rows
     uint32_t voff[N];
-    __device__ __forceinline__ Loader(const Rows<bf16raw> &s) : base(s.base), tok(s.tok), gp((int)s.by.d), count(s.count)
+    __device__ __forceinline__ Loader(const Rows<bf16raw> &s) : base(s.base), tok(s.tok)
     {
+        const int gp = (int)s.by.d;
+        shift = __builtin_ctz(gp);
+        tokens = s.count >> shift;
         const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         tail = (uint32_t)(((gp - 1) * s.head + s.D) * 2);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const int at = (4 * j + wave) * 1024 + lane * 16, row = at / (DP * 2), chunk = at % (DP * 2) / 16 ^ swizzle<DP>(row);
-            const int t = row / gp;
-            voff[j] = 8 * chunk < s.D ? (uint32_t)((t * s.tok + (row - t * gp) * s.head) * 2 + chunk * 16) : OOB_ROW;
+            const int t = row >> shift;
+            voff[j] = 8 * chunk < s.D ? (uint32_t)((t * s.tok + (row - (t << shift)) * s.head) * 2 + chunk * 16) : OOB_ROW;
         }
     }
     __device__ __forceinline__ void start(int row0, LdsByte *lds) const
     {
-        const int t0 = row0 / gp, left = count / gp - t0;      // tokens; rows are whole tokens' (a tile begins with one)
+        const int t0 = row0 >> shift, left = tokens - t0;      // a tile begins with a token
         const uint64_t at = (uint64_t)reinterpret_cast<uintptr_t>(base) + (uint64_t)((int64_t)t0 * tok * 2);
         const uint64_t span = left > 0 ? (uint64_t)(left - 1) * (uint64_t)tok * 2 + tail : 0;
-        BufferRsrc r;
-        r.x = __builtin_amdgcn_readfirstlane((uint32_t)at);
-        r.y = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu);
-        r.z = __builtin_amdgcn_readfirstlane((uint32_t)(span < kMaxBufferBytes ? span : kMaxBufferBytes));
-        r.w = 0x00020000u;
+        const BufferRsrc r = raw_buffer(at, span);
         const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
         for (int j = 0; j < N; ++j)
@@ -372,6 +387,18 @@ template <class T> __device__ __forceinline__ void store4(T *p, const float (&f)
         for (int i = 0; i < 4; ++i)
             if (i < n) p[i] = from_f32<T>(f[i]);
     }
+}
+
+// The order of a stretch of code without branches: `ahead` LDS reads first, then one more (two for transposing reads) behind each
+// of N matrix instructions.  Left to itself the compiler reads one or two operands ahead, and an LDS read takes as long as
+// four matrix instructions and more.
+template <int N, int AHEAD, int EACH> __device__ __forceinline__ void reads_ahead()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+    static_for<0, N>([](auto) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+    });
 }
 
 // The bias of a tile: entry e is that of delta = first + e, clamped to the table.  At most 256 entries, one a thread.

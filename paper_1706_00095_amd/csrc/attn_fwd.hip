@@ -10,7 +10,7 @@ constexpr float kSlack = 8.f;
 template <class T, int DP, bool BIAS, bool DMA>
 __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
 {
-    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
+    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32, AHEAD = 6;
     using TileY = Tile<DP, YT, NP>;
     __shared__ __align__(16) char lds[2][2][TileY::BYTES];
     LdsByte *const ldsK = (LdsByte *)lds[0][0], *const ldsV = (LdsByte *)lds[1][0];
@@ -96,6 +96,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
                 if constexpr (BIAS) p[u][i] = fmaf(p[u][i], a.scale, window[buf][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
             }
         }
+        if constexpr (NP == 1) reads_ahead<SUB * KS, AHEAD, 1>();
         if (k0 + YT > wave_limit)
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
