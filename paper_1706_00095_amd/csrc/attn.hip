@@ -67,17 +67,35 @@ int check(const cg_attn_desc *d)
     return CG_OK;
 }
 
-// How the pass is laid out and what it keeps in the workspace.
-struct Plan {
-    int Gp, tiles_q, tiles_k, W, splits, chunk;
-    size_t tab, bid, part_o, part_ml, delta, lse_b, dbias, bytes;       // offsets; bytes in all
-};
+// Few X tiles leave most of the chip idle while each walks a long Y axis: the axis is then cut into chunks, a block each, and a
+// second kernel joins what they found.
+struct Split { int splits, chunk; };
 
-// Few query tiles leave most of the chip idle, and a long axis of keys is walked tile by tile: the keys are then cut into chunks, a
-// block each, and joined by a second kernel.  kSplitBelow blocks: fewer than one a compute unit.  A chunk is at least kMinChunk keys, and
-// as many as share all the keys out to about kSplitBlocks blocks.
-constexpr int kSplitBelow = 256, kSplitBlocks = 512, kMinChunk = 256;
-constexpr int64_t kSplitBytes = 256ll << 20;
+// How a kernel over problems x tiles of X (an upper bound) is cut along Y: not at all where there are blocks for the chip (kFull), nor
+// where Y is short (on average over the B sequences, and in all).  Otherwise into as many chunks as bring about kTarget blocks
+// where the sequences are alike, of kMinChunk rows at least: a chunk's set-up and its partial result cost about what 64 rows do.  At most
+// kMaxChunks, because the grid has room for them in every tile, whichever sequence is the long one.
+constexpr int kFull = 256, kTarget = 512, kMinChunk = 128, kMaxChunks = 64;
+constexpr int64_t kPartBytes = 256ll << 20;
+
+Split split_of(int64_t problems, int64_t tiles, int64_t y, int64_t B, int64_t row_bytes)
+{
+    const int64_t blocks = problems * tiles;
+    if (blocks == 0 || blocks >= kFull || (y < 4 * kMinChunk && y < 2 * kMinChunk * B)) return {1, 0};
+    int64_t chunk = kMinChunk;
+    for (const int64_t least : {up(y / B * blocks / kTarget, 64), up((y + kMaxChunks - 1) / kMaxChunks, 64)})
+        if (chunk < least) chunk = least;
+    while (blocks * ((y + chunk - 1) / chunk) * kAttnRows * row_bytes > kPartBytes) chunk *= 2;
+    const int64_t n = (y + chunk - 1) / chunk;
+    return n > 1 ? Split{(int)n, (int)chunk} : Split{1, 0};
+}
+
+// How the pass is laid out and what it keeps in the workspace (offsets; bytes in all).
+struct Plan {
+    int Gp, tiles_q, tiles_k, W, DP;
+    Split q, k;                 // of the kernels whose X are queries (forward, dq) and keys (dk, dv)
+    size_t tab, bid, part[2], part_ml, delta, lse_b, dbias, bytes;
+};
 
 Plan plan_of(const cg_attn_desc &d, int pass)
 {
@@ -86,36 +104,32 @@ Plan plan_of(const cg_attn_desc &d, int pass)
     p.tiles_q = (int)(d.Tq * p.Gp / kAttnRows + d.B);
     p.tiles_k = (int)(d.Tk / kAttnRows + d.B);
     p.W = d.buckets ? d.max_distance : 0;
-    p.splits = 1;
-    const int64_t Hr = d.Hq / p.Gp, blocks = Hr * p.tiles_q;
+    p.DP = (int)up(d.D, 32);
+    const int64_t Hr = d.Hq / p.Gp;
     int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t here = (size_t)at;
+        at += up(bytes, 256);
+        return here;
+    };
     if (d.buckets) {
-        p.tab = 0;
-        p.bid = (size_t)up(d.Hq * (2ll * p.W + 1) * 4, 256);
-        at = (int64_t)p.bid + up(2ll * p.W + 1, 256);
+        p.tab = take(d.Hq * (2ll * p.W + 1) * 4);
+        p.bid = take(2ll * p.W + 1);
     }
+    p.q = split_of(Hr, p.tiles_q, d.Tk, d.B, (p.DP + 2) * 4);
+    const int64_t q_rows = p.q.splits > 1 ? Hr * p.tiles_q * p.q.splits * kAttnRows : 0;
     if (pass == CG_PASS_FWD) {
-        const int64_t row_bytes = (up(d.D, 32) + 2) * 4;
-        if (blocks > 0 && blocks < kSplitBelow && d.Tk >= 4 * kMinChunk) {
-            int64_t chunk = up(d.Tk * Hr / kSplitBlocks, 64);
-            if (chunk < kMinChunk) chunk = kMinChunk;
-            while (blocks * ((d.Tk + chunk - 1) / chunk) * kAttnRows * row_bytes > kSplitBytes) chunk *= 2;
-            p.chunk = (int)chunk;
-            p.splits = (int)((d.Tk + chunk - 1) / chunk);
-        }
-        if (p.splits > 1) {
-            p.part_o = (size_t)at;
-            at += up(blocks * p.splits * kAttnRows * up(d.D, 32) * 4, 256);
-            p.part_ml = (size_t)at;
-            at += up(blocks * p.splits * kAttnRows * 2 * 4, 256);
-        }
+        p.part[0] = take(q_rows * p.DP * 4);
+        p.part_ml = take(q_rows * 2 * 4);
     } else {
-        p.delta = (size_t)at;
-        at += up(d.Tq * d.Hq * 4, 256);
-        p.lse_b = (size_t)at;
-        at += up(d.Tq * d.Hq * 4, 256);
-        p.dbias = (size_t)at;
-        if (d.buckets) at += up((int64_t)d.Hq * p.tiles_q * d.buckets * 4, 256);
+        // the sums over keys and the sums over rows are done one after the other: one room for both
+        p.k = split_of(d.Hkv, p.tiles_k, d.Tq * p.Gp, d.B, 2 * p.DP * 4);
+        const int64_t k_rows = p.k.splits > 1 ? d.Hkv * p.tiles_k * p.k.splits * kAttnRows : 0;
+        p.part[0] = take((q_rows > k_rows ? q_rows : k_rows) * p.DP * 4);
+        p.part[1] = take(k_rows * p.DP * 4);
+        p.delta = take(d.Tq * d.Hq * 4);
+        p.lse_b = take(d.Tq * d.Hq * 4);
+        p.dbias = take((int64_t)d.Hq * p.tiles_q * p.q.splits * d.buckets * 4);
     }
     p.bytes = (size_t)at;
     return p;
@@ -140,7 +154,10 @@ AttnArgs args_of(const cg_attn_desc &d, const Plan &p, const void *q, const void
     a.buckets = d.buckets;
     a.W = p.W;
     a.tiles = p.tiles_q;
-    a.splits = p.splits, a.chunk = p.chunk;
+    a.splits = p.q.splits, a.chunk = p.q.chunk;
+    for (int i = 0; i < 2; ++i) a.part[i] = reinterpret_cast<float *>(ws + p.part[i]);
+    a.part_ml = reinterpret_cast<float *>(ws + p.part_ml);
+    a.yt = attn_dkdv_yt(d.type == CG_TYPE_BF16, p.DP);
     a.dma = d.type == CG_TYPE_BF16 && attn_dma_ok(k, d.k_tok, 0, 1, d.D) && attn_dma_ok(v, d.v_tok, 0, 1, d.D) && d.k_head % 8 == 0 && d.v_head % 8 == 0;
     if (d.buckets) {
         a.btab = reinterpret_cast<const float *>(ws + p.tab);
@@ -188,12 +205,8 @@ extern "C" int cg_attn_fwd(const cg_attn_desc *d, const void *q, const void *k, 
     if (int rc = table_launch(*d, p, bias, w, s)) return rc;
     AttnArgs a = args_of(*d, p, q, k, v, cu_q, cu_k, w);
     a.o = o, a.o_rest = o_rest, a.lse = lse;
-    if (p.splits > 1) {
-        a.part_o = reinterpret_cast<float *>(w + p.part_o);
-        a.part_ml = reinterpret_cast<float *>(w + p.part_ml);
-    }
     if (int rc = attn_fwd_launch(a, d->type, s)) return rc;
-    return p.splits > 1 ? attn_combine_launch(a, d->type, s) : CG_OK;
+    return a.splits > 1 ? attn_join_launch(a, d->type, ATTN_JOIN_O, s) : CG_OK;
 }
 
 extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q, const void *k, const void *v, const int32_t *cu_q,
@@ -216,15 +229,21 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
     a.delta = reinterpret_cast<float *>(w + p.delta);
     a.lse_b = reinterpret_cast<float *>(w + p.lse_b);
     if (dbias) a.dbias_part = reinterpret_cast<float *>(w + p.dbias);
-    if (d->B > 0 && d->Tq > 0)
+    const bool any = d->B > 0 && d->Tq > 0;
+    if (any) {
         if (int rc = attn_dq_launch(a, d->type, s)) return rc;
+        if (a.splits > 1)
+            if (int rc = attn_join_launch(a, d->type, ATTN_JOIN_DQ, s)) return rc;
+    }
     if (dbias)
-        if (int rc = attn_dbias_launch(a.dbias_part, d->Tq > 0 ? p.tiles_q : 0, d->Hq, d->buckets, dbias, s)) return rc;
+        if (int rc = attn_dbias_launch(a.dbias_part, any ? p.tiles_q * p.q.splits : 0, d->Hq, d->buckets, dbias, s)) return rc;
     if (d->B > 0 && d->Tk > 0) {
         a.tiles = p.tiles_k;
         a.dma = d->type == CG_TYPE_BF16 && attn_dma_ok(q, d->q_tok, d->q_head, p.Gp, d->D) && attn_dma_ok(d_o, d->o_tok, d->o_head, p.Gp, d->D) &&
                 d->Tq * d->Hq < (1 << 29);
-        return attn_dkdv_launch(a, d->type, s);
+        a.splits = p.k.splits, a.chunk = p.k.chunk;
+        if (int rc = attn_dkdv_launch(a, d->type, s)) return rc;
+        if (a.splits > 1) return attn_join_launch(a, d->type, ATTN_JOIN_DKDV, s);
     }
     return CG_OK;
 }

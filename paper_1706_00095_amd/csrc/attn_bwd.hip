@@ -45,18 +45,16 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
     LdsByte *const ldsK = (LdsByte *)lds[0][0], *const ldsV = (LdsByte *)lds[1][0];
     __shared__ float window[2][BIAS ? 256 : 1], square[BIAS ? 4 : 1][BIAS ? 32 * kDiag : 1], bsum[BIAS ? 4 : 1][BIAS ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
-    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, tile = a.tiles - 1 - blockIdx.x / Hr;
+    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, item = blockIdx.x / Hr, split = item % a.splits, tile = a.tiles - 1 - item / a.splits;
     const bool want_bias = BIAS && a.dbias_part;
     int b, t;
     const bool any = find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t);
-    if (want_bias) {
-        if (!any) {
-            for (int i = threadIdx.x; i < a.buckets; i += 256) a.dbias_part[((int64_t)hr * a.tiles + tile) * a.buckets + i] = 0.f;
-        } else
-            for (int i = threadIdx.x; i < 4 * 256; i += 256) bsum[i / 256][i % 256] = 0.f;
-        __syncthreads();
-    }
-    if (!any) return;
+    float *const bias_out = want_bias ? a.dbias_part + (((int64_t)hr * a.tiles + tile) * a.splits + split) * a.buckets : nullptr;
+    auto no_bias = [&] {
+        if (want_bias)
+            for (int i = threadIdx.x; i < a.buckets; i += 256) bias_out[i] = 0.f;
+    };
+    if (!any) return no_bias();
     const Seq s = seq_of(a, b);
     const int row0 = t * kAttnRows, rows = s.n * a.Gp, off = s.m - s.n;
     const int h0 = hr * a.Gp, hkv = h0 / a.G;
@@ -66,10 +64,18 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
     const int limit = a.causal ? min(max(tok + 1 + off, 0), s.m) : s.m;
     const int first_tok = (int)fdiv((uint32_t)min(row0 + 32 * wave, rows - 1), a.by_gp);
     const int wave_limit = a.causal ? min(max(first_tok + 1 + off, 0), s.m) : s.m;
-    const int last_tok = (int)fdiv((uint32_t)min(row0 + kAttnRows, rows) - 1, a.by_gp);
-    const int wave_last = (int)fdiv((uint32_t)(min(max(row0 + 32 * wave + 32, 1), rows) - 1), a.by_gp);
-    const int wave_kend = row0 + 32 * wave >= rows ? 0 : a.causal ? min(max(wave_last + 1 + off, 0), s.m) : s.m;
-    const int kend = a.causal ? min(max(last_tok + 1 + off, 0), s.m) : s.m;
+    const int wave_kend = row0 + 32 * wave >= rows ? 0 : keys_seen(a, s, row0 + 32 * wave + 32, rows);
+    int kend = keys_seen(a, s, row0 + kAttnRows, rows), kbeg = 0;
+    const int chunks = chunks_of(a, 0, kend);
+    if (split >= chunks) return no_bias();
+    if (chunks > 1) {
+        kbeg = split * a.chunk;
+        kend = min(kend, kbeg + a.chunk);
+    }
+    if (want_bias) {
+        for (int i = threadIdx.x; i < 4 * 256; i += 256) bsum[i / 256][i % 256] = 0.f;
+        __syncthreads();
+    }
 
     const FastDiv one = {1, 1, 0};
     const Rows<T> K{static_cast<const T *>(a.k) + (int64_t)s.k0 * a.k_tok + (int64_t)hkv * a.k_head, a.k_tok, 0, s.m, a.D, one};
@@ -100,7 +106,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
     const float lse = here ? a.lse[stat] : -INFINITY;
     // the exponent takes lse in the scores' own units with a bias, else times log2 e; a row that sees nothing (or is none) has probabilities 0
     const float c = a.scale * kLog2e, lse_b = lse == -INFINITY ? INFINITY : BIAS ? lse : lse * kLog2e;
-    if (here && h32 == 0) {
+    if (here && h32 == 0 && split == 0) {
         a.delta[stat] = delta;
         a.lse_b[stat] = lse_b;
     }
@@ -116,15 +122,15 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
     Loader<T, DP, YT, DMA> lk(K), lv(V);
     const int window0 = -(row0 + kAttnRows - 1) - off;
     float bias_next = 0.f;
-    if (kend > 0) {
-        lk.start(0, ldsK);
-        lv.start(0, ldsV);
-        if constexpr (BIAS) window[0][threadIdx.x] = window_load(a, h0, window0);
+    if (kbeg < kend) {
+        lk.start(kbeg, ldsK);
+        lv.start(kbeg, ldsV);
+        if constexpr (BIAS) window[0][threadIdx.x] = window_load(a, h0, kbeg + window0);
         lk.finish(ldsK);
         lv.finish(ldsV);
     }
     int buf = 0;
-    for (int k0 = 0; k0 < kend; k0 += YT, buf ^= 1) {
+    for (int k0 = kbeg; k0 < kend; k0 += YT, buf ^= 1) {
         tile_sync();
         const bool more = k0 + YT < kend;
         if (more) {
@@ -216,30 +222,30 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
         }
         __syncthreads();
         for (int i = threadIdx.x; i < a.buckets; i += 256)
-            a.dbias_part[((int64_t)hr * a.tiles + tile) * a.buckets + i] = (bsum[0][i] + bsum[1][i]) + (bsum[2][i] + bsum[3][i]);
+            bias_out[i] = (bsum[0][i] + bsum[1][i]) + (bsum[2][i] + bsum[3][i]);
     }
     if (!here) return;
-    T *to = static_cast<T *>(a.dq) + (int64_t)(s.q0 + tok) * a.q_tok + (int64_t)head * a.q_head;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int d = 32 * dt + 8 * j + 4 * h32;
-            float f[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = dQ[dt][4 * j + i] * a.scale;
-            store4(to + d, f, a.D - d);
-        }
+    if (chunks > 1)
+        store_row(a.part[0] + ((((int64_t)hr * a.tiles + tile) * a.splits + split) * kAttnRows + (row - row0)) * DP, dQ, a.scale, DP, h32);
+    else store_row(static_cast<T *>(a.dq) + (int64_t)(s.q0 + tok) * a.q_tok + (int64_t)head * a.q_head, dQ, a.scale, a.D, h32);
 }
 
-// dbias[h][bucket]: the blocks' sums in order, in 64 bits.  A block a head, a thread a bucket.
-__global__ __launch_bounds__(256) void attn_dbias_kernel(const float *part, int tiles, int buckets, float *dbias)
+// dbias[h][bucket]: the blocks' sums added in a fixed order, in 64 bits.  A block takes a head and 16 buckets, 16 threads a bucket.
+__global__ __launch_bounds__(256) void attn_dbias_kernel(const float *part, int parts, int buckets, float *dbias)
 {
-    const int h = blockIdx.x, i = threadIdx.x;
-    if (i >= buckets) return;
+    __shared__ double lds[16][17];
+    const int h = blockIdx.y, x = threadIdx.x % 16, j = threadIdx.x / 16, i = blockIdx.x * 16 + x;
     double s = 0;
-    for (int t = 0; t < tiles; ++t) s += part[((int64_t)h * tiles + t) * buckets + i];
-    dbias[(int64_t)h * buckets + i] = (float)s;
+    if (i < buckets)
+#pragma unroll 4
+        for (int t = j; t < parts; t += 16) s += part[((int64_t)h * parts + t) * buckets + i];
+    lds[j][x] = s;
+    __syncthreads();
+    if (j == 0 && i < buckets) {
+#pragma unroll
+        for (int k = 1; k < 16; ++k) s += lds[k][x];
+        dbias[(int64_t)h * buckets + i] = (float)s;
+    }
 }
 
 // X: 128 keys of a key-value head; Y: the query rows that see them, of all Gp heads.  With a bias Gp = 1, and the G heads
@@ -247,7 +253,7 @@ __global__ __launch_bounds__(256) void attn_dbias_kernel(const float *part, int 
 template <class T, int DP, bool BIAS, bool DMA>
 __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kernel(AttnArgs a)
 {
-    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 && DP < 128 ? 64 : 32, SUB = YT / 32;
+    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = attn_dkdv_yt(NP == 1, DP), SUB = YT / 32;
     using TileY = Tile<DP, YT, NP>;
     // Two waves a SIMD (256 registers each) hide each other's LDS reads and exponentials.  At DP = 128 dK, dV and both operands' fragments
     // leave no room for anything else: V's fragments are read from LDS each time instead.
@@ -260,12 +266,22 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
     __shared__ __align__(16) float stats[2][2][64];            // lse_b, delta of the tile's rows
     __shared__ float window[2][BIAS ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
-    const int hkv = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv;
+    const int hkv = blockIdx.x % a.Hkv, item = blockIdx.x / a.Hkv, split = item % a.splits, tile = item / a.splits;
     int b, t;
     if (!find_tile(a.cu_k, a.Tk, a.B, kAttnRows, 1, tile, b, t)) return;
     const Seq s = seq_of(a, b);
     const int key0 = t * kAttnRows, rows = s.n * a.Gp, off = s.m - s.n;
     const int key = key0 + 32 * wave + (lane & 31);
+    // Row r of token r / Gp sees the key from first_seeing on.  Keys behind the last one need no mask: what is added up for them is
+    // not stored.
+    const int first_row = first_seeing(a, s, key), wave_first = first_seeing(a, s, key0 + 32 * wave), wave_all = first_seeing(a, s, key0 + 32 * wave + 31);
+    int begin = first_seeing(a, s, key0) / YT * YT, end = rows;
+    const int chunks = chunks_of(a, begin, end);
+    if (split >= chunks) return;
+    if (chunks > 1) {
+        begin += split * a.chunk;
+        end = min(end, begin + a.chunk);
+    }
 
     const FastDiv one = {1, 1, 0};
     const Rows<T> K{static_cast<const T *>(a.k) + (int64_t)s.k0 * a.k_tok + (int64_t)hkv * a.k_head, a.k_tok, 0, s.m, a.D, one};
@@ -284,12 +300,6 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dK[dt] = v16f{}, dV[dt] = v16f{};
     const float c = a.scale * kLog2e;
-    // Row r of token r / Gp sees the key where r >= (key - off) Gp.  Keys behind the last one need no mask: what is added up for them
-    // is not stored.
-    auto row_of = [&](int k) { return a.causal ? (int)min(max((int64_t)(k - off) * a.Gp, (int64_t)0), (int64_t)rows) : 0; };
-    const int first_row = row_of(key), wave_first = row_of(key0 + 32 * wave), wave_all = row_of(key0 + 32 * wave + 31);
-    const int begin = row_of(key0) / YT * YT;
-
     for (int g = 0; g < a.G / a.Gp; ++g) {
         const int h0 = hkv * a.G + g * a.Gp;
         const Rows<T> Q{static_cast<const T *>(a.q) + (int64_t)s.q0 * a.q_tok + (int64_t)h0 * a.q_head, a.q_tok, a.q_head, rows, a.D, a.by_gp};
@@ -322,7 +332,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
         };
         int buf = 0;
         __syncthreads();      // the head before this one may still be read
-        if (begin < rows) {
+        if (begin < end) {
             lq.start(begin, ldsQ);
             lo.start(begin, ldsO);
             row_start(begin, 0);
@@ -330,9 +340,9 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
             lo.finish(ldsO);
             row_finish(0);
         }
-        for (int y0 = begin; y0 < rows; y0 += YT, buf ^= 1) {
+        for (int y0 = begin; y0 < end; y0 += YT, buf ^= 1) {
             tile_sync();
-            const bool more = y0 + YT < rows;
+            const bool more = y0 + YT < end;
             if (more) {
                 lq.start(y0 + YT, ldsQ + (buf ^ 1) * TileY::BYTES);
                 lo.start(y0 + YT, ldsO + (buf ^ 1) * TileY::BYTES);
@@ -409,23 +419,19 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
         }
     }
     if (key >= s.m) return;
-    T *tk = static_cast<T *>(a.dk) + (int64_t)(s.k0 + key) * a.k_tok + (int64_t)hkv * a.k_head;
-    T *tv = static_cast<T *>(a.dv) + (int64_t)(s.k0 + key) * a.v_tok + (int64_t)hkv * a.v_head;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int d = 32 * dt + 8 * j + 4 * h32;
-            const float f[4] = {dV[dt][4 * j], dV[dt][4 * j + 1], dV[dt][4 * j + 2], dV[dt][4 * j + 3]};
-            store4(tv + d, f, a.D - d);
-            const float g[4] = {dK[dt][4 * j] * a.scale, dK[dt][4 * j + 1] * a.scale, dK[dt][4 * j + 2] * a.scale, dK[dt][4 * j + 3] * a.scale};
-            store4(tk + d, g, a.D - d);
-        }
+    if (chunks > 1) {
+        const int64_t at = ((((int64_t)hkv * a.tiles + tile) * a.splits + split) * kAttnRows + (key - key0)) * DP;
+        store_row(a.part[0] + at, dK, a.scale, DP, h32);
+        store_row(a.part[1] + at, dV, 1.f, DP, h32);
+    } else {
+        store_row(static_cast<T *>(a.dk) + (int64_t)(s.k0 + key) * a.k_tok + (int64_t)hkv * a.k_head, dK, a.scale, a.D, h32);
+        store_row(static_cast<T *>(a.dv) + (int64_t)(s.k0 + key) * a.v_tok + (int64_t)hkv * a.v_head, dV, 1.f, a.D, h32);
+    }
 }
 
 template <class T, int DP, bool DMA> int dq_run(const AttnArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles);
+    const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
     if (a.btab) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
@@ -439,7 +445,7 @@ template <class T, int DP> int dq_dp(const AttnArgs &a, hipStream_t s)
 }
 template <class T, int DP, bool DMA> int dkdv_run(const AttnArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)a.Hkv * a.tiles);
+    const dim3 grid((unsigned)a.Hkv * a.tiles * a.splits);
     if (a.btab) hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
@@ -474,9 +480,9 @@ int attn_dkdv_launch(const AttnArgs &a, int type, hipStream_t s)
 #undef CG_DP
     return CG_EUNSUPPORTED;
 }
-int attn_dbias_launch(const float *part, int tiles, int Hq, int buckets, float *dbias, hipStream_t s)
+int attn_dbias_launch(const float *part, int parts, int Hq, int buckets, float *dbias, hipStream_t s)
 {
-    hipLaunchKernelGGL(attn_dbias_kernel, dim3((unsigned)Hq), dim3(256), 0, s, part, tiles, buckets, dbias);
+    hipLaunchKernelGGL(attn_dbias_kernel, dim3((unsigned)(buckets + 15) / 16, (unsigned)Hq), dim3(256), 0, s, part, parts, buckets, dbias);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
 }

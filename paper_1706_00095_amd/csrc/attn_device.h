@@ -36,14 +36,16 @@ struct AttnArgs {
     int W, buckets;
     float *dbias_part;                     // [Hq][tiles][buckets]
     int tiles;                             // of X rows over all sequences, an upper bound
-    // keys cut into `splits` chunks of `chunk` (0: one)
+    // Y cut into at most `splits` chunks of `chunk` rows, a block each; a tile with several leaves partial results for attn_join_kernel
     int splits, chunk;
+    int yt;                                // rows of a Y tile in the dk/dv kernel (attn_dkdv_yt)
     int dma;                               // K and V (forward, dq), Q and dO (dk/dv) may travel without registers
-    float *part_o, *part_ml;               // [Hr][tiles][splits][rows][DP], [..][2][rows]
+    float *part[2], *part_ml;              // [problem][tiles][splits][128][DP] (forward: o; dq; dk, dv), [..][2][128]
 };
 
 constexpr int kAttnRows = 128;             // X rows of a block: four waves of 32
 constexpr int kAttnMaxD = 128;
+constexpr int attn_dkdv_yt(bool bf16, int DP) { return bf16 && DP < 128 ? 64 : 32; }
 
 // May rows of these strides (elements, bf16) travel without registers?  `per`: heads packed as rows (a tile of 32 begins with
 // a token).  16-byte aligned rows, and rows behind the last one behind the buffer's end.
@@ -54,10 +56,11 @@ inline bool attn_dma_ok(const void *p, int64_t tok, int64_t head, int per, int D
 
 // attn_fwd.hip, attn_bwd.hip: DP is D rounded up to a multiple of 32
 int attn_fwd_launch(const AttnArgs &a, int type, hipStream_t s);
-int attn_combine_launch(const AttnArgs &a, int type, hipStream_t s);
 int attn_dq_launch(const AttnArgs &a, int type, hipStream_t s);
 int attn_dkdv_launch(const AttnArgs &a, int type, hipStream_t s);
-int attn_dbias_launch(const float *part, int tiles, int Hq, int buckets, float *dbias, hipStream_t s);
+enum { ATTN_JOIN_O = 0, ATTN_JOIN_DQ, ATTN_JOIN_DKDV };
+int attn_join_launch(const AttnArgs &a, int type, int what, hipStream_t s);
+int attn_dbias_launch(const float *part, int parts, int Hq, int buckets, float *dbias, hipStream_t s);
 
 namespace {
 
@@ -399,6 +402,36 @@ template <int N, int AHEAD, int EACH> __device__ __forceinline__ void reads_ahea
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
     });
+}
+
+// An X row's accumulators, times `factor`, to a row of T: four neighbouring columns at a time.
+template <class T, int DT> __device__ __forceinline__ void store_row(T *to, const v16f (&acc)[DT], float factor, int D, int h32)
+{
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = 32 * dt + 8 * j + 4 * h32;
+            const float f[4] = {acc[dt][4 * j] * factor, acc[dt][4 * j + 1] * factor, acc[dt][4 * j + 2] * factor, acc[dt][4 * j + 3] * factor};
+            store4(to + d, f, D - d);
+        }
+}
+
+// Chunks that Y rows [begin, end) of a tile are cut into (at least one, which may be empty).
+__device__ __forceinline__ int chunks_of(const AttnArgs &a, int begin, int end)
+{
+    return a.splits == 1 ? 1 : max(1, (end - begin + a.chunk - 1) / a.chunk);
+}
+// What the rows of a tile see, row0 .. of `rows`: keys 0 .. the return value - 1.
+__device__ __forceinline__ int keys_seen(const AttnArgs &a, const Seq &s, int row_end, int rows)
+{
+    const int last = (int)fdiv((uint32_t)(min(max(row_end, 1), rows) - 1), a.by_gp);
+    return a.causal ? min(max(last + 1 + s.m - s.n, 0), s.m) : s.m;
+}
+// The first row, of Gp to a token, that sees key k.
+__device__ __forceinline__ int first_seeing(const AttnArgs &a, const Seq &s, int k)
+{
+    return a.causal ? (int)min(max((int64_t)(k - (s.m - s.n)) * a.Gp, (int64_t)0), (int64_t)s.n * a.Gp) : 0;
 }
 
 // The bias of a tile: entry e is that of delta = first + e, clamped to the table.  At most 256 entries, one a thread.

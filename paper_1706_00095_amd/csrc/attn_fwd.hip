@@ -31,13 +31,12 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
     const int limit = a.causal ? min(max(tok + 1 + off, 0), s.m) : s.m;
     const int first_tok = (int)fdiv((uint32_t)min(row0 + 32 * wave, rows - 1), a.by_gp);
     const int wave_limit = a.causal ? min(max(first_tok + 1 + off, 0), s.m) : s.m;       // every row of the wave sees those
-    const int last_tok = (int)fdiv((uint32_t)min(row0 + kAttnRows, rows) - 1, a.by_gp);
-    const int wave_last = (int)fdiv((uint32_t)(min(max(row0 + 32 * wave + 32, 1), rows) - 1), a.by_gp);
-    const int wave_kend = row0 + 32 * wave >= rows ? 0 : a.causal ? min(max(wave_last + 1 + off, 0), s.m) : s.m;
-    int kend = a.causal ? min(max(last_tok + 1 + off, 0), s.m) : s.m, kbeg = 0;
-    if (a.splits > 1) {
+    const int wave_kend = row0 + 32 * wave >= rows ? 0 : keys_seen(a, s, row0 + 32 * wave + 32, rows);
+    int kend = keys_seen(a, s, row0 + kAttnRows, rows), kbeg = 0;
+    const int chunks = chunks_of(a, 0, kend);
+    if (split >= chunks) return;
+    if (chunks > 1) {
         kbeg = split * a.chunk;
-        if (split > 0 && kbeg >= kend) return;
         kend = min(kend, kbeg + a.chunk);
     }
 
@@ -172,21 +171,15 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
         }
     }
     l = sum_halves(l);
-    if (a.splits > 1) {
+    if (chunks > 1) {
         if (!here) return;
         const int64_t at = ((int64_t)hr * a.tiles + tile) * a.splits + split;
-        float *po = a.part_o + (at * kAttnRows + (row - row0)) * DP, *ml = a.part_ml + at * 2 * kAttnRows;
+        float *ml = a.part_ml + at * 2 * kAttnRows;
         if (h32 == 0) {
             ml[row - row0] = BIAS ? m : m * a.scale;
             ml[kAttnRows + row - row0] = l;
         }
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float f[4] = {O[dt][4 * j], O[dt][4 * j + 1], O[dt][4 * j + 2], O[dt][4 * j + 3]};
-                store4(po + 32 * dt + 8 * j + 4 * h32, f, 4);
-            }
+        store_row(a.part[0] + (at * kAttnRows + (row - row0)) * DP, O, 1.f, DP, h32);
         return;
     }
     if (!here) return;
@@ -212,48 +205,6 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kerne
         }
 }
 
-// Joins the chunks of the keys: o = sum_s e^(m_s - M) o_s / sum_s e^(m_s - M) l_s.  A wave takes a row.
-template <class T, int DP> __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a)
-{
-    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, item = blockIdx.x / Hr, tile = item / (kAttnRows / 4), part = item % (kAttnRows / 4);
-    int b, t;
-    if (!find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t)) return;
-    const Seq s = seq_of(a, b);
-    const int row0 = t * kAttnRows, rows = s.n * a.Gp, row = row0 + 4 * part + wave, off = s.m - s.n;
-    if (row >= rows) return;
-    const int tok = (int)fdiv((uint32_t)row, a.by_gp), head = hr * a.Gp + row - tok * a.Gp;
-    // the chunks that the tile's block has walked: the first always, the others up to the last key its rows see
-    const int last_tok = (int)fdiv((uint32_t)min(row0 + kAttnRows, rows) - 1, a.by_gp);
-    const int kend = a.causal ? min(max(last_tok + 1 + off, 0), s.m) : s.m;
-    const int n = max(1, (kend + a.chunk - 1) / a.chunk);
-    const int64_t at = ((int64_t)hr * a.tiles + tile) * a.splits;
-    const float *ml = a.part_ml + at * 2 * kAttnRows + (row - row0), *po = a.part_o + (at * kAttnRows + (row - row0)) * DP;
-    float M = -INFINITY;
-    for (int i = 0; i < n; ++i) M = fmaxf(M, ml[(int64_t)i * 2 * kAttnRows]);
-    const float Ms = M == -INFINITY ? 0.f : M;
-    float l = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int i = 0; i < n; ++i) {
-        const float w = __builtin_amdgcn_exp2f((ml[(int64_t)i * 2 * kAttnRows] - Ms) * kLog2e);
-        l = fmaf(w, ml[(int64_t)i * 2 * kAttnRows + kAttnRows], l);
-        const float *p = po + (int64_t)i * kAttnRows * DP;
-        if (lane < DP) o0 = fmaf(w, p[lane], o0);
-        if (lane + 64 < DP) o1 = fmaf(w, p[lane + 64], o1);
-    }
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-    if (lane == 0) a.lse[(int64_t)head * a.Tq + s.q0 + tok] = l == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), kLn2, M);
-    const int64_t to = (int64_t)(s.q0 + tok) * a.o_tok + (int64_t)head * a.o_head;
-    const float f[2] = {o0 * inv, o1 * inv};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int d = lane + 64 * i;
-        if (d >= a.D) continue;
-        const T v = from_f32<T>(f[i]);
-        static_cast<T *>(a.o)[to + d] = v;
-        if (sizeof(T) == 2 && a.o_rest) static_cast<T *>(a.o_rest)[to + d] = from_f32<T>(f[i] - to_f32(v));
-    }
-}
-
 template <class T, int DP, bool DMA> int fwd_run(const AttnArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
@@ -268,13 +219,6 @@ template <class T, int DP> int fwd_dp(const AttnArgs &a, hipStream_t s)
         if (a.dma) return fwd_run<T, DP, true>(a, s);
     return fwd_run<T, DP, false>(a, s);
 }
-template <class T, int DP> int combine_dp(const AttnArgs &a, hipStream_t s)
-{
-    hipLaunchKernelGGL((attn_combine_kernel<T, DP>), dim3((unsigned)(a.Hq / a.Gp) * a.tiles * (kAttnRows / 4)), dim3(256), 0, s, a);
-    CG_HIP_TRY(hipGetLastError());
-    return CG_OK;
-}
-
 }  // namespace
 
 int attn_fwd_launch(const AttnArgs &a, int type, hipStream_t s)
@@ -287,15 +231,4 @@ int attn_fwd_launch(const AttnArgs &a, int type, hipStream_t s)
 #undef CG_DP
     return CG_EUNSUPPORTED;
 }
-int attn_combine_launch(const AttnArgs &a, int type, hipStream_t s)
-{
-#define CG_DP(DP) if (a.D <= DP) return type == CG_TYPE_FP32 ? combine_dp<float, DP>(a, s) : combine_dp<bf16raw, DP>(a, s)
-    CG_DP(32);
-    CG_DP(64);
-    CG_DP(96);
-    CG_DP(128);
-#undef CG_DP
-    return CG_EUNSUPPORTED;
-}
-
 }  // namespace cg
