@@ -6,25 +6,33 @@
 namespace cg {
 namespace {
 
-constexpr int kDiag = 33;          // a wave's 32 x 32 scores' gradients in LDS, rows of 33
+// The bias's gradient.  A wave's 32 x 32 part of dS is summed along its 63 diagonals (equal distances): column c of row r goes to row
+// r - c + 31 of a square in LDS, at place c; the places of a row that no (r, c) has stay zero, so a lane adds up one whole row
+// in eight wide reads.  Rows of kDiag words put eight lanes' reads on different banks.
+// Sums over a wave's parts are kept by distance (W <= kNear: a word a distance, which each lane has to itself), else by bucket.
+constexpr int kDiag = 36, kNear = 512;
+__host__ __device__ inline int near_words(int W) { return W <= kNear ? 2 * W + 1 : 256; }
 
-// Sums of a wave's 32 x 32 tile along its diagonals (equal distances), then over the diagonals of a bucket, into this wave's
-// own `acc` [buckets].  Buckets of neighbouring distances are the same or neighbours, so equal ones are runs of lanes.
-__device__ __forceinline__ void add_diagonals(const float (&ds)[16], int delta0, const AttnArgs &a, float *sq, float *acc, int lane)
+__device__ __forceinline__ float diagonal_sum(const float (&ds)[16], float *sq, int lane)
 {
     const int c = lane & 31, h32 = lane >> 5;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sq[c * kDiag + 8 * (i / 4) + 4 * h32 + i % 4] = ds[i];
-    // the wave's own accesses to LDS: in order, but the compiler has to be told
+    for (int i = 0; i < 16; ++i) sq[(8 * (i / 4) + 4 * h32 + i % 4 - c + 31) * kDiag + c] = ds[i];
+    // a wave's LDS accesses keep their order; the compiler has to be told to
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    float v = 0.f;
-#pragma unroll 8
-    for (int x = 0; x < 32; ++x) {
-        const int y = lane + x - 31;
-        if (y >= 0 && y < 32) v += sq[x * kDiag + y];
+    float v[4] = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float4 x = *reinterpret_cast<const float4 *>(sq + min(lane, 62) * kDiag + 4 * j);
+        v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
     }
-    const int delta = delta0 + lane - 31;
-    const int bucket = lane < 63 ? (int)a.bid[min(max(delta, -a.W), a.W) + a.W] : -1;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    return (v[0] + v[1]) + (v[2] + v[3]);
+}
+// Adds a lane's v, whose bucket is `bucket` (-1: none), to acc [buckets].  Neighbouring distances have the same bucket or neighbours, so
+// a bucket's lanes are a run: its last lane gets the run's sum.
+__device__ __forceinline__ void add_runs(float v, int bucket, float *acc, int lane)
+{
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const float u = __shfl_up(v, d);
@@ -32,21 +40,24 @@ __device__ __forceinline__ void add_diagonals(const float (&ds)[16], int delta0,
         if (lane >= d && ub == bucket) v += u;
     }
     const int next = __shfl_down(bucket, 1);
-    if (lane < 63 && next != bucket) acc[bucket] += v;
+    if (bucket >= 0 && (lane == 63 || next != bucket)) acc[bucket] += v;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 template <class T, int DP, bool BIAS, bool DMA>
-__global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void attn_dq_kernel(AttnArgs a)
 {
     constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
     using TileY = Tile<DP, YT, NP>;
     __shared__ __align__(16) char lds[2][2][TileY::BYTES];
     LdsByte *const ldsK = (LdsByte *)lds[0][0], *const ldsV = (LdsByte *)lds[1][0];
-    __shared__ float window[2][BIAS ? 256 : 1], square[BIAS ? 4 : 1][BIAS ? 32 * kDiag : 1], bsum[BIAS ? 4 : 1][BIAS ? 256 : 1];
+    __shared__ float window[2][BIAS ? 256 : 1];
+    __shared__ __align__(16) float square[BIAS ? 4 : 1][BIAS ? 63 * kDiag : 4];
+    extern __shared__ float by_wave[];          // [4][near_words(W)]
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
     const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, item = blockIdx.x / Hr, split = item % a.splits, tile = a.tiles - 1 - item / a.splits;
     const bool want_bias = BIAS && a.dbias_part;
+    float *const mine = by_wave + wave * near_words(a.W);
     int b, t;
     const bool any = find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t);
     float *const bias_out = want_bias ? a.dbias_part + (((int64_t)hr * a.tiles + tile) * a.splits + split) * a.buckets : nullptr;
@@ -73,7 +84,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
         kend = min(kend, kbeg + a.chunk);
     }
     if (want_bias) {
-        for (int i = threadIdx.x; i < 4 * 256; i += 256) bsum[i / 256][i % 256] = 0.f;
+        for (int i = threadIdx.x; i < 4 * 63 * kDiag; i += 256) square[0][i] = 0.f;
+        for (int i = threadIdx.x; i < 4 * near_words(a.W); i += 256) by_wave[i] = 0.f;
         __syncthreads();
     }
 
@@ -178,7 +190,14 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
                         if (!here)
 #pragma unroll
                             for (int i = 0; i < 16; ++i) ds[i] = 0.f;
-                        add_diagonals(ds, delta0, a, square[wave], bsum[wave], lane);
+                        const float v = diagonal_sum(ds, square[wave], lane);
+                        const int delta = delta0 + lane - 31;
+                        if (a.W > kNear) add_runs(v, lane < 63 ? (int)a.bid[min(max(delta, -a.W), a.W) + a.W] : -1, mine, lane);
+                        else if (lane < 63) {
+                            if (delta <= -a.W) far_past += v;
+                            else if (delta >= a.W) far_future += v;
+                            else mine[delta + a.W] += v;
+                        }
                     }
                 }
             }
@@ -216,13 +235,22 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dq_kernel
             far_past += __shfl_xor(far_past, m);
             far_future += __shfl_xor(far_future, m);
         }
+        float *const sums = a.W <= kNear ? square[wave] : mine;       // [buckets] of this wave
+        if (a.W <= kNear) {
+#pragma unroll
+            for (int i = 0; i < 256; i += 64) sums[i + lane] = 0.f;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (int i = 0; i <= 2 * a.W; i += 64)       // 64 distances at a time, in order
+                add_runs(i + lane <= 2 * a.W ? mine[i + lane] : 0.f, i + lane <= 2 * a.W ? (int)a.bid[i + lane] : -1, sums, lane);
+        }
         if (lane == 0) {
-            bsum[wave][a.bid[0]] += far_past;
-            bsum[wave][a.bid[2 * a.W]] += far_future;
+            sums[a.bid[0]] += far_past;
+            sums[a.bid[2 * a.W]] += far_future;
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < a.buckets; i += 256)
-            bias_out[i] = (bsum[0][i] + bsum[1][i]) + (bsum[2][i] + bsum[3][i]);
+        const float *const all = a.W <= kNear ? square[0] : by_wave;
+        const int apart = a.W <= kNear ? 63 * kDiag : near_words(a.W);
+        for (int i = threadIdx.x; i < a.buckets; i += 256) bias_out[i] = (all[i] + all[apart + i]) + (all[2 * apart + i] + all[3 * apart + i]);
     }
     if (!here) return;
     if (chunks > 1)
@@ -251,7 +279,7 @@ __global__ __launch_bounds__(256) void attn_dbias_kernel(const float *part, int 
 // X: 128 keys of a key-value head; Y: the query rows that see them, of all Gp heads.  With a bias Gp = 1, and the G heads
 // are walked one after the other.
 template <class T, int DP, bool BIAS, bool DMA>
-__global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void attn_dkdv_kernel(AttnArgs a)
 {
     constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = attn_dkdv_yt(NP == 1, DP), SUB = YT / 32;
     using TileY = Tile<DP, YT, NP>;
@@ -432,7 +460,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_dkdv_kern
 template <class T, int DP, bool DMA> int dq_run(const AttnArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
-    if (a.btab) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
+    if (a.btab) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true, DMA>), grid, dim3(256), a.dbias_part ? 16 * near_words(a.W) : 0, s, a);
     else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;

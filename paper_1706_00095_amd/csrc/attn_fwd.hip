@@ -8,7 +8,7 @@ constexpr float kSlack = 8.f;
 
 // A block takes 128 query rows (X) of one problem and walks the keys (Y) they see in tiles of YT.
 template <class T, int DP, bool BIAS, bool DMA>
-__global__ __launch_bounds__(256, Pieces<T>::N == 1 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
 {
     constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32, AHEAD = 6;
     using TileY = Tile<DP, YT, NP>;
