@@ -17,7 +17,10 @@ struct Thresholds {
 // attention kernels look a distance up instead of taking its logarithm for every pair.
 __global__ __launch_bounds__(256) void bias_table_kernel(Thresholds th, const float *bias, int buckets, int W, float *tab, uint8_t *bid)
 {
+    __shared__ int from[kMaxBuckets / 2 + 1];
     const int i = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y;
+    if (threadIdx.x < sizeof(from) / sizeof(int)) from[threadIdx.x] = th.from[threadIdx.x];
+    __syncthreads();
     if (i > 2 * W) return;
     const int delta = i - W, dist = th.both ? abs(delta) : max(-delta, 0);
     int b = dist;
@@ -25,7 +28,7 @@ __global__ __launch_bounds__(256) void bias_table_kernel(Thresholds th, const fl
         int lo = 0, hi = th.n - 1 - th.E;       // thresholds there are
         while (lo < hi) {
             const int mid = (lo + hi) / 2;
-            if (th.from[mid] <= dist) lo = mid + 1;
+            if (from[mid] <= dist) lo = mid + 1;
             else hi = mid;
         }
         b = th.E + lo;
@@ -78,11 +81,11 @@ struct Split { int splits, chunk; };
 constexpr int kFull = 256, kTarget = 512, kMinChunk = 128, kMaxChunks = 64;
 constexpr int64_t kPartBytes = 256ll << 20;
 
-Split split_of(int64_t problems, int64_t tiles, int64_t y, int64_t B, int64_t row_bytes)
+Split split_of(int64_t problems, int64_t tiles, int64_t y, int64_t B, int64_t row_bytes, int type)
 {
     const int64_t blocks = problems * tiles;
-    if (blocks == 0 || blocks >= kFull || (y < 4 * kMinChunk && y < 2 * kMinChunk * B)) return {1, 0};
-    int64_t chunk = kMinChunk;
+    int64_t chunk = type == CG_TYPE_FP32 ? kMinChunk / 2 : kMinChunk;
+    if (blocks == 0 || blocks >= kFull || (y < 4 * chunk && y < 2 * chunk * B)) return {1, 0};
     for (const int64_t least : {up(y / B * blocks / kTarget, 64), up((y + kMaxChunks - 1) / kMaxChunks, 64)})
         if (chunk < least) chunk = least;
     while (blocks * ((y + chunk - 1) / chunk) * kAttnRows * row_bytes > kPartBytes) chunk *= 2;
@@ -93,6 +96,7 @@ Split split_of(int64_t problems, int64_t tiles, int64_t y, int64_t B, int64_t ro
 // How the pass is laid out and what it keeps in the workspace (offsets; bytes in all).
 struct Plan {
     int Gp, tiles_q, tiles_k, W, DP;
+    int gsplit;
     Split q, k;                 // of the kernels whose X are queries (forward, dq) and keys (dk, dv)
     size_t tab, bid, part[2], part_ml, delta, lse_b, dbias, bytes;
 };
@@ -116,15 +120,18 @@ Plan plan_of(const cg_attn_desc &d, int pass)
         p.tab = take(d.Hq * (2ll * p.W + 1) * 4);
         p.bid = take(2ll * p.W + 1);
     }
-    p.q = split_of(Hr, p.tiles_q, d.Tk, d.B, (p.DP + 2) * 4);
+    p.q = split_of(Hr, p.tiles_q, d.Tk, d.B, (p.DP + 2) * 4, d.type);
     const int64_t q_rows = p.q.splits > 1 ? Hr * p.tiles_q * p.q.splits * kAttnRows : 0;
     if (pass == CG_PASS_FWD) {
         p.part[0] = take(q_rows * p.DP * 4);
         p.part_ml = take(q_rows * 2 * 4);
     } else {
         // the sums over keys and the sums over rows are done one after the other: one room for both
-        p.k = split_of(d.Hkv, p.tiles_k, d.Tq * p.Gp, d.B, 2 * p.DP * 4);
-        const int64_t k_rows = p.k.splits > 1 ? d.Hkv * p.tiles_k * p.k.splits * kAttnRows : 0;
+        // with a bias a block walks the heads of its keys one after the other; where blocks are few each gets blocks of its own
+        const int64_t G = d.Hq / d.Hkv, blocks_k = (int64_t)d.Hkv * p.tiles_k;
+        p.gsplit = d.buckets && G > 1 && blocks_k < kFull && blocks_k * G * kAttnRows * 2 * p.DP * 4 <= kPartBytes ? (int)G : 1;
+        p.k = split_of((int64_t)d.Hkv * p.gsplit, p.tiles_k, d.Tq * p.Gp, d.B, 2 * p.DP * 4, d.type);
+        const int64_t k_rows = p.k.splits * p.gsplit > 1 ? blocks_k * p.gsplit * p.k.splits * kAttnRows : 0;
         p.part[0] = take((q_rows > k_rows ? q_rows : k_rows) * p.DP * 4);
         p.part[1] = take(k_rows * p.DP * 4);
         p.delta = take(d.Tq * d.Hq * 4);
@@ -154,7 +161,7 @@ AttnArgs args_of(const cg_attn_desc &d, const Plan &p, const void *q, const void
     a.buckets = d.buckets;
     a.W = p.W;
     a.tiles = p.tiles_q;
-    a.splits = p.q.splits, a.chunk = p.q.chunk;
+    a.splits = p.q.splits, a.chunk = p.q.chunk, a.gsplit = 1;
     for (int i = 0; i < 2; ++i) a.part[i] = reinterpret_cast<float *>(ws + p.part[i]);
     a.part_ml = reinterpret_cast<float *>(ws + p.part_ml);
     a.yt = attn_dkdv_yt(d.type == CG_TYPE_BF16, p.DP);
@@ -241,9 +248,9 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
         a.tiles = p.tiles_k;
         a.dma = d->type == CG_TYPE_BF16 && attn_dma_ok(q, d->q_tok, d->q_head, p.Gp, d->D) && attn_dma_ok(d_o, d->o_tok, d->o_head, p.Gp, d->D) &&
                 d->Tq * d->Hq < (1 << 29);
-        a.splits = p.k.splits, a.chunk = p.k.chunk;
+        a.splits = p.k.splits, a.chunk = p.k.chunk, a.gsplit = p.gsplit;
         if (int rc = attn_dkdv_launch(a, d->type, s)) return rc;
-        if (a.splits > 1) return attn_join_launch(a, d->type, ATTN_JOIN_DKDV, s);
+        if (a.splits * a.gsplit > 1) return attn_join_launch(a, d->type, ATTN_JOIN_DKDV, s);
     }
     return CG_OK;
 }

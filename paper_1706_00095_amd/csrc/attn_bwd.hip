@@ -10,7 +10,7 @@ namespace {
 // r - c + 31 of a square in LDS, at place c; the places of a row that no (r, c) has stay zero, so a lane adds up one whole row
 // in eight wide reads.  Rows of kDiag words put eight lanes' reads on different banks.
 // Sums over a wave's parts are kept by distance (W <= kNear: a word a distance, which each lane has to itself), else by bucket.
-constexpr int kDiag = 36, kNear = 512;
+constexpr int kDiag = 36, kNear = 1024;
 __host__ __device__ inline int near_words(int W) { return W <= kNear ? 2 * W + 1 : 256; }
 
 __device__ __forceinline__ float diagonal_sum(const float (&ds)[16], float *sq, int lane)
@@ -294,7 +294,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
     __shared__ __align__(16) float stats[2][2][64];            // lse_b, delta of the tile's rows
     __shared__ float window[2][BIAS ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
-    const int hkv = blockIdx.x % a.Hkv, item = blockIdx.x / a.Hkv, split = item % a.splits, tile = item / a.splits;
+    const int hkv = blockIdx.x % a.Hkv, item = blockIdx.x / a.Hkv, slots = a.splits * a.gsplit, slot = item % slots, tile = item / slots;
+    const int split = slot / a.gsplit;
     int b, t;
     if (!find_tile(a.cu_k, a.Tk, a.B, kAttnRows, 1, tile, b, t)) return;
     const Seq s = seq_of(a, b);
@@ -328,7 +329,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dK[dt] = v16f{}, dV[dt] = v16f{};
     const float c = a.scale * kLog2e;
-    for (int g = 0; g < a.G / a.Gp; ++g) {
+    const int heads = a.G / a.Gp, one_head = slot % a.gsplit;
+    for (int g = a.gsplit > 1 ? one_head : 0; g < (a.gsplit > 1 ? one_head + 1 : heads); ++g) {
         const int h0 = hkv * a.G + g * a.Gp;
         const Rows<T> Q{static_cast<const T *>(a.q) + (int64_t)s.q0 * a.q_tok + (int64_t)h0 * a.q_head, a.q_tok, a.q_head, rows, a.D, a.by_gp};
         const Rows<T> dO{static_cast<const T *>(a.d_o) + (int64_t)s.q0 * a.o_tok + (int64_t)h0 * a.o_head, a.o_tok, a.o_head, rows, a.D, a.by_gp};
@@ -447,8 +449,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
         }
     }
     if (key >= s.m) return;
-    if (chunks > 1) {
-        const int64_t at = ((((int64_t)hkv * a.tiles + tile) * a.splits + split) * kAttnRows + (key - key0)) * DP;
+    if (chunks * a.gsplit > 1) {
+        const int64_t at = ((((int64_t)hkv * a.tiles + tile) * slots + slot) * kAttnRows + (key - key0)) * DP;
         store_row(a.part[0] + at, dK, a.scale, DP, h32);
         store_row(a.part[1] + at, dV, 1.f, DP, h32);
     } else {
@@ -473,7 +475,7 @@ template <class T, int DP> int dq_dp(const AttnArgs &a, hipStream_t s)
 }
 template <class T, int DP, bool DMA> int dkdv_run(const AttnArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)a.Hkv * a.tiles * a.splits);
+    const dim3 grid((unsigned)a.Hkv * a.tiles * a.splits * a.gsplit);
     if (a.btab) hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());

@@ -38,9 +38,10 @@ struct AttnArgs {
     int tiles;                             // of X rows over all sequences, an upper bound
     // Y cut into at most `splits` chunks of `chunk` rows, a block each; a tile with several leaves partial results for attn_join_kernel
     int splits, chunk;
+    int gsplit;                            // dk/dv kernel with a bias: chunks are of one head each (G), or of all (1)
     int yt;                                // rows of a Y tile in the dk/dv kernel (attn_dkdv_yt)
     int dma;                               // K and V (forward, dq), Q and dO (dk/dv) may travel without registers
-    float *part[2], *part_ml;              // [problem][tiles][splits][128][DP] (forward: o; dq; dk, dv), [..][2][128]
+    float *part[2], *part_ml;              // [problem][tiles][splits gsplit][128][DP] (forward: o; dq; dk, dv), [..][2][128]
 };
 
 constexpr int kAttnRows = 128;             // X rows of a block: four waves of 32

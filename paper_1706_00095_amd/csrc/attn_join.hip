@@ -4,16 +4,20 @@
 namespace cg {
 namespace {
 
-// A wave takes an X row, kJoinRows waves' turns a block; DP / 4 lanes hold the row, the other lanes of the wave take other chunks, and the
-// groups are added in order.  o: sum_s e^(m_s - M) o_s / sum_s e^(m_s - M) l_s; gradients: sums.  Tiles of one chunk are done already.
-constexpr int kJoinRows = 8;
+// o: sum_s e^(m_s - M) o_s / sum_s e^(m_s - M) l_s; gradients: sums.  Tiles of one chunk are done already.
+// DP / 4 lanes hold a row, so a wave has 2 to 8 such groups.  ROWS: a group takes a row, and its chunks one after the other (many tiles of
+// few chunks: 1.8 us a wave, and four times fewer waves); else the groups share a row's chunks and are added in order (few tiles of many).
+template <int DP, bool ROWS> struct Join {
+    static constexpr int L = DP / 4, GROUPS = 64 / L, PER_BLOCK = ROWS ? 4 * GROUPS : 4;
+};
 
-template <class T, int DP, int WHAT> __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
+template <class T, int DP, int WHAT, bool ROWS> __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
-    constexpr int L = DP / 4, GROUPS = 64 / L;
+    using J = Join<DP, ROWS>;
+    constexpr int L = J::L, GROUPS = J::GROUPS, AT_ONCE = 4, STEP = ROWS ? 1 : GROUPS;
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int problems = WHAT == ATTN_JOIN_DKDV ? a.Hkv : a.Hq / a.Gp, pr = blockIdx.x % problems, item = blockIdx.x / problems;
-    const int tile = item / (kAttnRows / kJoinRows), part = item % (kAttnRows / kJoinRows);
+    const int tile = item / (kAttnRows / J::PER_BLOCK), part = item % (kAttnRows / J::PER_BLOCK);
     int b, t;
     if (WHAT == ATTN_JOIN_DKDV ? !find_tile(a.cu_k, a.Tk, a.B, kAttnRows, 1, tile, b, t) : !find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t)) return;
     const Seq s = seq_of(a, b);
@@ -21,48 +25,73 @@ template <class T, int DP, int WHAT> __global__ __launch_bounds__(256) void attn
     int n, rows;
     if constexpr (WHAT == ATTN_JOIN_DKDV) {
         rows = s.m;
-        n = chunks_of(a, first_seeing(a, s, row0) / yt * yt, s.n * a.Gp);
+        n = chunks_of(a, first_seeing(a, s, row0) / yt * yt, s.n * a.Gp) * a.gsplit;
     } else {
         rows = s.n * a.Gp;
         n = chunks_of(a, 0, keys_seen(a, s, row0 + kAttnRows, rows));
     }
     if (n == 1) return;
-    const int64_t at = ((int64_t)pr * a.tiles + tile) * a.splits;
+    const int64_t at = ((int64_t)pr * a.tiles + tile) * a.splits * a.gsplit;
     const int group = lane / L, d = 4 * (lane % L);
-    for (int i = wave; i < kJoinRows; i += 4) {
-        const int row = row0 + part * kJoinRows + i;
+    {
+        const int row = row0 + part * J::PER_BLOCK + (ROWS ? wave * GROUPS + min(group, GROUPS - 1) : wave);
         if (row >= rows) return;
-        float M = 0.f, l = 0.f;
-        const float *ml = WHAT == ATTN_JOIN_O ? a.part_ml + at * 2 * kAttnRows + (row - row0) : nullptr;
-        if constexpr (WHAT == ATTN_JOIN_O) {
-            M = -INFINITY;
-            for (int k = lane; k < n; k += 64) M = fmaxf(M, ml[(int64_t)k * 2 * kAttnRows]);
-#pragma unroll
-            for (int x = 32; x; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
-            const float Ms = M == -INFINITY ? 0.f : M;
-            for (int k = lane; k < n; k += 64)
-                l = fmaf(__builtin_amdgcn_exp2f((ml[(int64_t)k * 2 * kAttnRows] - Ms) * kLog2e), ml[(int64_t)k * 2 * kAttnRows + kAttnRows], l);
-#pragma unroll
-            for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
-            M = Ms;
-        }
+        float M = -INFINITY, l = 0.f;
 #pragma unroll
         for (int which = 0; which < (WHAT == ATTN_JOIN_DKDV ? 2 : 1); ++which) {
-            const float *p = a.part[which] + (at * kAttnRows + (row - row0)) * DP + d;
-            float f[4] = {};
+            // a chunk's statistics and its values are asked for together: one wait for a few chunks
+            const float *ml = a.part_ml + at * 2 * kAttnRows + (row - row0), *p = a.part[which] + (at * kAttnRows + (row - row0)) * DP + d;
+            float r[4] = {};
             if (group < GROUPS)
-#pragma unroll 4
-                for (int k = group; k < n; k += GROUPS) {
-                    const float4 v = *reinterpret_cast<const float4 *>(p + (int64_t)k * kAttnRows * DP);
-                    const float w = WHAT == ATTN_JOIN_O ? __builtin_amdgcn_exp2f((ml[(int64_t)k * 2 * kAttnRows] - M) * kLog2e) : 1.f;
-                    f[0] = fmaf(w, v.x, f[0]), f[1] = fmaf(w, v.y, f[1]), f[2] = fmaf(w, v.z, f[2]), f[3] = fmaf(w, v.w, f[3]);
+                for (int k0 = ROWS ? 0 : group; k0 < n; k0 += AT_ONCE * STEP) {
+                    float4 v[AT_ONCE];
+                    float mk[AT_ONCE], lk[AT_ONCE];
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        const int k = k0 + u * STEP;
+                        v[u] = k < n ? *reinterpret_cast<const float4 *>(p + (int64_t)k * kAttnRows * DP) : float4{0.f, 0.f, 0.f, 0.f};
+                        if constexpr (WHAT == ATTN_JOIN_O) {
+                            mk[u] = k < n ? ml[(int64_t)k * 2 * kAttnRows] : -INFINITY;
+                            lk[u] = k < n ? ml[(int64_t)k * 2 * kAttnRows + kAttnRows] : 0.f;
+                        }
+                    }
+                    if constexpr (WHAT == ATTN_JOIN_O) {
+                        float mn = M;
+#pragma unroll
+                        for (int u = 0; u < AT_ONCE; ++u) mn = fmaxf(mn, mk[u]);
+                        const float ms = mn == -INFINITY ? 0.f : mn, keep = __builtin_amdgcn_exp2f((M - ms) * kLog2e);
+                        M = mn, l *= keep;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) r[e] *= keep;
+#pragma unroll
+                        for (int u = 0; u < AT_ONCE; ++u) {
+                            const float w = __builtin_amdgcn_exp2f((mk[u] - ms) * kLog2e);
+                            l = fmaf(w, lk[u], l);
+                            r[0] = fmaf(w, v[u].x, r[0]), r[1] = fmaf(w, v[u].y, r[1]), r[2] = fmaf(w, v[u].z, r[2]), r[3] = fmaf(w, v[u].w, r[3]);
+                        }
+                    } else
+#pragma unroll
+                        for (int u = 0; u < AT_ONCE; ++u) r[0] += v[u].x, r[1] += v[u].y, r[2] += v[u].z, r[3] += v[u].w;
                 }
-            float r[4] = {f[0], f[1], f[2], f[3]};
+            if constexpr (!ROWS) {       // the groups, in order; each knows its own M
+                const float mine[4] = {r[0], r[1], r[2], r[3]}, m_mine = M, l_mine = l;
+                float w = 1.f;
+                if constexpr (WHAT == ATTN_JOIN_O) {
 #pragma unroll
-            for (int g = 1; g < GROUPS; ++g)
+                    for (int g = 0; g < GROUPS; ++g) M = fmaxf(M, __shfl(m_mine, lane % L + g * L));
+                    w = __builtin_amdgcn_exp2f((m_mine - (M == -INFINITY ? 0.f : M)) * kLog2e);
+                    l = 0.f;
+                }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) r[e] += __shfl(f[e], lane % L + g * L);
-            if (group != 0) continue;
+                for (int e = 0; e < 4; ++e) r[e] = 0.f;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) r[e] += __shfl(mine[e] * w, lane % L + g * L);
+                    if constexpr (WHAT == ATTN_JOIN_O) l += __shfl(l_mine * w, lane % L + g * L);
+                }
+            }
+            if (ROWS ? group >= GROUPS : group != 0) continue;
             if constexpr (WHAT == ATTN_JOIN_DKDV) {
                 T *to = which == 0 ? static_cast<T *>(a.dk) + (int64_t)(s.k0 + row) * a.k_tok + (int64_t)pr * a.k_head
                                    : static_cast<T *>(a.dv) + (int64_t)(s.k0 + row) * a.v_tok + (int64_t)pr * a.v_head;
@@ -73,7 +102,7 @@ template <class T, int DP, int WHAT> __global__ __launch_bounds__(256) void attn
                     store4(static_cast<T *>(a.dq) + (int64_t)(s.q0 + tok) * a.q_tok + (int64_t)head * a.q_head + d, r, a.D - d);
                 } else {
                     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-                    if (lane == 0) a.lse[(int64_t)head * a.Tq + s.q0 + tok] = l == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), kLn2, M);
+                    if (d == 0) a.lse[(int64_t)head * a.Tq + s.q0 + tok] = l == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), kLn2, M);
                     const int64_t to = (int64_t)(s.q0 + tok) * a.o_tok + (int64_t)head * a.o_head + d;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) r[e] *= inv;
@@ -90,14 +119,20 @@ template <class T, int DP, int WHAT> __global__ __launch_bounds__(256) void attn
     }
 }
 
-template <class T, int DP> int join_dp(const AttnArgs &a, int what, hipStream_t s)
+template <class T, int DP, bool ROWS> int join_run(const AttnArgs &a, int what, hipStream_t s)
 {
-    const dim3 grid((unsigned)(what == ATTN_JOIN_DKDV ? a.Hkv : a.Hq / a.Gp) * a.tiles * (kAttnRows / kJoinRows));
-    if (what == ATTN_JOIN_O) hipLaunchKernelGGL((attn_join_kernel<T, DP, ATTN_JOIN_O>), grid, dim3(256), 0, s, a);
-    else if (what == ATTN_JOIN_DQ) hipLaunchKernelGGL((attn_join_kernel<T, DP, ATTN_JOIN_DQ>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_join_kernel<T, DP, ATTN_JOIN_DKDV>), grid, dim3(256), 0, s, a);
+    const dim3 grid((unsigned)(what == ATTN_JOIN_DKDV ? a.Hkv : a.Hq / a.Gp) * a.tiles * (kAttnRows / Join<DP, ROWS>::PER_BLOCK));
+    if (what == ATTN_JOIN_O) hipLaunchKernelGGL((attn_join_kernel<T, DP, ATTN_JOIN_O, ROWS>), grid, dim3(256), 0, s, a);
+    else if (what == ATTN_JOIN_DQ) hipLaunchKernelGGL((attn_join_kernel<T, DP, ATTN_JOIN_DQ, ROWS>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_join_kernel<T, DP, ATTN_JOIN_DKDV, ROWS>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
+}
+// A row a wave while the chip has room for all the waves at once (8192)
+template <class T, int DP> int join_dp(const AttnArgs &a, int what, hipStream_t s)
+{
+    const int64_t rows = (int64_t)(what == ATTN_JOIN_DKDV ? a.Hkv : a.Hq / a.Gp) * a.tiles * kAttnRows;
+    return rows > 8192 ? join_run<T, DP, true>(a, what, s) : join_run<T, DP, false>(a, what, s);
 }
 
 }  // namespace
