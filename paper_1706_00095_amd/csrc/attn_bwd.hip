@@ -104,13 +104,13 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
         const int d = 16 * ks + 8 * h32;
         fq[ks] = frag_of(Q.load(row, d));
         const Raw8<T> g = dO.load(row, d), o = O.load(row, d);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) delta = fmaf(elem(g, i), elem(o, i), delta);
         if (NP == 1 && a.o_rest_in) {
             const Raw8<T> r = R.load(row, d);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) delta = fmaf(elem(g, i), elem(r, i), delta);
-        }
+            for (int i = 0; i < 8; ++i) delta = fmaf(elem(g, i), with_rest(elem(o, i), r.w[i / 2 % (sizeof(r.w) / 4)] >> (16 * (i & 1))), delta);
+        } else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) delta = fmaf(elem(g, i), elem(o, i), delta);
         fdo[ks] = frag_of(g);
     }
     delta = sum_halves(delta);

@@ -405,6 +405,30 @@ template <int N, int AHEAD, int EACH> __device__ __forceinline__ void reads_ahea
     });
 }
 
+// What o loses when it is rounded to bf16, in the 16 bits an element of o_rest has: a whole number of 2^-16 of o's last place, which
+// makes 24 bits of o together (a second bf16 number would make 17, and delta, a sum of o times do, is taken from others nearly
+// as large in the gradient of the bias).
+__device__ __forceinline__ uint32_t rest_exponent(float o) { return min(max(__float_as_uint(o) & 0x7f800000u, 0x20000000u), 0x7e800000u); }
+__device__ __forceinline__ float with_rest(float o, uint32_t rest) { return fmaf((float)(int16_t)rest * 0x1p-23f, __uint_as_float(rest_exponent(o)), o); }
+// of four neighbouring elements of an X row, stored like o's
+__device__ __forceinline__ void store_rest4(bf16raw *p, const float (&f)[4], int n)
+{
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float o = to_f32(from_f32<bf16raw>(f[i]));
+        r[i] = (uint32_t)(int)fminf(rintf((f[i] - o) * __uint_as_float(0x7f000000u - rest_exponent(o)) * 0x1p23f), 32767.f) & 0xffffu;
+    }
+    if (n >= 4) {
+        struct __attribute__((packed, aligned(2))) Loose8 { uint32_t w[2]; } q = {{r[0] | r[1] << 16, r[2] | r[3] << 16}};
+        *reinterpret_cast<Loose8 *>(p) = q;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) p[i] = (bf16raw)r[i];
+    }
+}
+
 // An X row's accumulators, times `factor`, to a row of T: four neighbouring columns at a time.
 template <class T, int DT> __device__ __forceinline__ void store_row(T *to, const v16f (&acc)[DT], float factor, int D, int h32)
 {

@@ -7,10 +7,14 @@ namespace {
 constexpr float kSlack = 8.f;
 
 // A block takes 128 query rows (X) of one problem and walks the keys (Y) they see in tiles of YT.
-template <class T, int DP, bool BIAS, bool DMA>
+// EXACT (bf16 in a training step): the probabilities that o is made of keep 24 bits, in three pieces.  The backward pass subtracts
+// delta, a sum of o times do, from dP; where the differences are added up (the bias's gradient) or rows see a few keys only (sequences
+// of kFewKeys on average), dP is as near to delta as a rounded o is to o.
+constexpr int kFewKeys = 64;
+template <class T, int DP, bool BIAS, bool DMA, bool EXACT>
 __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
 {
-    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32, AHEAD = 6;
+    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 && !(EXACT && DP > 64) ? 64 : 32, SUB = YT / 32, AHEAD = 6;
     using TileY = Tile<DP, YT, NP>;
     __shared__ __align__(16) char lds[2][2][TileY::BYTES];
     LdsByte *const ldsK = (LdsByte *)lds[0][0], *const ldsV = (LdsByte *)lds[1][0];
@@ -56,8 +60,6 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
     float m = -INFINITY, l = 0.f;
     // without a bias scores stay as the product gives them and the scale enters the exponent: exp2(s c - m c)
     const float c = a.scale * kLog2e;
-    const bool exact_p = BIAS && NP == 1 && a.o_rest;
-
     // Two buffers and one barrier a tile: behind it the tile is there and everyone is done with the one before, whose buffer the
     // next one's loads then fill while this one is multiplied.
     Loader<T, DP, YT, DMA> lk(K), lv(V);
@@ -122,7 +124,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
                 sum += p[u][i];
             }
         l = fmaf(l, alpha, sum);
-        if constexpr (NP == 1) {
+        if constexpr (NP == 1 && !EXACT) {
             if (__any(grows))
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) O[dt] *= alpha;
@@ -131,20 +133,27 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     const Frag<1> fp = cut8<1>(&p[u][8 * g]);
-                    Frag<1> rest;
-                    if (exact_p) {
-                        float f[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] = p[u][8 * g + i] - __uint_as_float(i & 1 ? fp.p[0][i / 2] & 0xffff0000u : fp.p[0][i / 2] << 16);
-                        rest = cut8<1>(f);
-                    }
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        const Frag<1> fv = TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane);
-                        O[dt] = mfma(fv.p[0], fp.p[0], O[dt]);
-                        if (exact_p) O[dt] = mfma(fv.p[0], rest.p[0], O[dt]);
-                    }
+                    for (int dt = 0; dt < DT; ++dt) O[dt] = mfma(TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane).p[0], fp.p[0], O[dt]);
                 }
+        } else if constexpr (EXACT) {       // probabilities in three pieces, the least first; a tile's sum from zero as below
+            Frag<3> fp[SUB][2];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) fp[u][g] = cut8<3>(&p[u][8 * g]);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                v16f S = v16f{};
+#pragma unroll
+                for (int k = 2; k >= 0; --k)
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) S = mfma(TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane).p[0], fp[u][g].p[k], S);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) O[dt][i] = fmaf(O[dt][i], alpha, S[i]);
+            }
         } else {       // a tile's sum from zero, then one rounding into the running one
             Frag<NP> fp[SUB][2];
 #pragma unroll
@@ -186,30 +195,28 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;      // no key: 0; NaN stays
     if (h32 == 0) a.lse[(int64_t)head * a.Tq + s.q0 + tok] = l == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), kLn2, BIAS ? m : m * a.scale);
     const int64_t at = (int64_t)(s.q0 + tok) * a.o_tok + (int64_t)head * a.o_head;
+    store_row(static_cast<T *>(a.o) + at, O, inv, a.D, h32);
+    if constexpr (NP == 1)
+        if (a.o_rest)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+            for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int d = 32 * dt + 8 * j + 4 * h32;
-            float f[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = O[dt][4 * j + i] * inv;
-            store4(static_cast<T *>(a.o) + at + d, f, a.D - d);
-            if constexpr (NP == 1) {
-                if (a.o_rest) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) f[i] -= to_f32(from_f32<T>(f[i]));
-                    store4(static_cast<T *>(a.o_rest) + at + d, f, a.D - d);
+                for (int j = 0; j < 4; ++j) {
+                    const int d = 32 * dt + 8 * j + 4 * h32;
+                    const float f[4] = {O[dt][4 * j] * inv, O[dt][4 * j + 1] * inv, O[dt][4 * j + 2] * inv, O[dt][4 * j + 3] * inv};
+                    store_rest4(static_cast<bf16raw *>(a.o_rest) + at + d, f, a.D - d);
                 }
-            }
-        }
 }
 
 template <class T, int DP, bool DMA> int fwd_run(const AttnArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
-    if (a.btab) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_fwd_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
+    constexpr bool can = sizeof(T) == 2;
+    const bool exact = can && a.o_rest && (a.btab || a.Tk <= (int64_t)kFewKeys * a.B);
+    if (exact && a.btab) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, true, DMA, can>), grid, dim3(256), 0, s, a);
+    else if (exact) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, false, DMA, can>), grid, dim3(256), 0, s, a);
+    else if (!a.btab) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, false, DMA, false>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_fwd_kernel<T, DP, true, DMA, false>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
 }
@@ -219,6 +226,7 @@ template <class T, int DP> int fwd_dp(const AttnArgs &a, hipStream_t s)
         if (a.dma) return fwd_run<T, DP, true>(a, s);
     return fwd_run<T, DP, false>(a, s);
 }
+
 }  // namespace
 
 int attn_fwd_launch(const AttnArgs &a, int type, hipStream_t s)

@@ -108,11 +108,7 @@ template <class T, int DP, int WHAT, bool ROWS> __global__ __launch_bounds__(256
                     for (int e = 0; e < 4; ++e) r[e] *= inv;
                     store4(static_cast<T *>(a.o) + to, r, a.D - d);
                     if constexpr (sizeof(T) == 2)
-                        if (a.o_rest) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) r[e] -= to_f32(from_f32<T>(r[e]));
-                            store4(static_cast<T *>(a.o_rest) + to, r, a.D - d);
-                        }
+                        if (a.o_rest) store_rest4(static_cast<bf16raw *>(a.o_rest) + to, r, a.D - d);
                 }
             }
         }
