@@ -289,10 +289,10 @@ def drop(p, seed, offset=0):
 
 
 def _type_of(t):
-    try:
-        return _TYPES[t.dtype]
-    except KeyError:
-        raise TypeError(f"expected a tensor of torch.float32 or torch.bfloat16, got {t.dtype}") from None
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"expected a tensor of torch.float32 or torch.bfloat16, got {t.dtype}")
+    return code
 
 
 def _shape_of_rows(t):
@@ -307,24 +307,25 @@ def _row_args(t, like, what):
     """(pointer, elements from a row to the next) of a tensor of `like`'s shape and type; its rows may lie in wider ones."""
     if t is None:
         return None, 0
-    if not t.is_cuda or t.dtype != like.dtype:
-        raise TypeError(f"{what}: expected a device tensor of {like.dtype}")
-    if t.shape != like.shape:
+    if t is not like and t.shape != like.shape:
         raise ValueError(f"{what}: expected the shape {tuple(like.shape)}, got {tuple(t.shape)}")
-    cols = t.shape[-1]
-    if t.dim() == 2:
-        if t.stride(1) != 1 and cols > 1:
+    if t.dtype is not like.dtype or not t.is_cuda:
+        raise TypeError(f"{what}: expected a device tensor of {like.dtype}")
+    steps = t.stride()
+    if len(steps) == 2:
+        rows, cols = t.shape
+        if steps[1] != 1 and cols > 1:
             raise ValueError(f"{what}: the elements of a row have to lie next to each other")
-        return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else cols)
+        return t.data_ptr(), (steps[0] if rows > 1 else cols)
     if not t.is_contiguous():
         raise ValueError(f"{what}: tensors of other than two dimensions have to be contiguous")
-    return t.data_ptr(), cols
+    return t.data_ptr(), t.shape[-1]
 
 
 def _weights(t, n, what):
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n:
+    if t.numel() != n or t.dtype is not torch.float32 or not t.is_contiguous() or not t.is_cuda:
         raise TypeError(f"{what}: expected a contiguous device tensor of {n} float32")
     return t.data_ptr()
 
@@ -410,7 +411,7 @@ def _heads(t, d, T, H, tok, head, what):
     """The pointer of a tensor [T][H][D] with the descriptor's type and strides."""
     if t is None:
         return None
-    if not t.is_cuda or _type_of(t) != d.type:
+    if _TYPES.get(t.dtype) != d.type or not t.is_cuda:
         raise TypeError(f"{what}: expected a device tensor of the descriptor's type")
     if t.shape != (T, H, d.D) or (t.stride() != (tok, head, 1) and t.numel() > 0 and any(
             n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), (tok, head, 1)))):

@@ -159,6 +159,7 @@ struct NormBwdArgs {
     const float *gamma, *mean, *rstd;
     void *dx, *dbranch;               // dbranch: joined only
     float *part;                      // [gridDim.x][2][cols]: sums over a block's rows
+    float *dgamma, *dbeta;            // of a single block: its sums are the result; else NULL
     int64_t dy_ld, x_ld, dsum_ld, dx_ld, dbranch_ld;
     int rows, cols;
     DropArgs drop;
@@ -248,16 +249,20 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
     __shared__ float join[ROWS > 1 ? ROWS - 1 : 1][ROWS > 1 ? LANES * 8 : 1];
     const int slot = threadIdx.x / LANES, t = threadIdx.x % LANES;
     const float inv = 1.f / (float)a.cols;
-    float gam[CPT][8], dg[CPT][8], db[CPT][8];
+    // gains, and what else a row needs, in registers from row to row and ahead of the sums, where there is room: four chunks a
+    // thread read them again (out of the caches) and later
+    constexpr bool ROOM = CPT < 4;
+    float dg[CPT][8], db[CPT][8];
+    Raw8<float> gam[CPT];
+    auto gains = [&](int k) {
+        const int c = 8 * (k * LANES + t);
+        gam[k] = load8(a.gamma + c, a.cols - c);
+    };
 #pragma unroll
     for (int k = 0; k < CPT; ++k) {
-        const int c = 8 * (k * LANES + t);
-        const Raw8<float> g = load8(a.gamma + c, a.cols - c);
+        if (ROOM) gains(k);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            gam[k][i] = elem(g, i);
-            dg[k][i] = db[k][i] = 0.f;
-        }
+        for (int i = 0; i < 8; ++i) dg[k][i] = db[k][i] = 0.f;
     }
     int turn = 0;
     for (int r0 = blockIdx.x * ROWS; r0 < a.rows; r0 += gridDim.x * ROWS, turn ^= 1) {
@@ -269,16 +274,17 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
             const int c = 8 * (k * LANES + t), n = here ? a.cols - c : 0;
             vx[k] = load8(static_cast<const T *>(a.x) + (int64_t)r * a.x_ld + c, n);
             vd[k] = load8(static_cast<const T *>(a.dy) + (int64_t)r * a.dy_ld + c, n);
-            if (a.dsum) vs[k] = load8(static_cast<const T *>(a.dsum) + (int64_t)r * a.dsum_ld + c, n);
+            if (ROOM && a.dsum) vs[k] = load8(static_cast<const T *>(a.dsum) + (int64_t)r * a.dsum_ld + c, n);
         }
         const float mean = here ? a.mean[r] : 0.f, rstd = here ? a.rstd[r] : 0.f;
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < CPT; ++k) {
             const int n = a.cols - 8 * (k * LANES + t);
+            if (!ROOM) gains(k);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float dy = elem(vd[k], i), xh = i < n ? (elem(vx[k], i) - mean) * rstd : 0.f, g = dy * gam[k][i];
+                const float dy = elem(vd[k], i), xh = i < n ? (elem(vx[k], i) - mean) * rstd : 0.f, g = dy * elem(gam[k], i);
                 s[0] += g;
                 s[1] = fmaf(g, xh, s[1]);
                 dg[k][i] = fmaf(dy, xh, dg[k][i]);
@@ -291,9 +297,13 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
         for (int k = 0; k < CPT; ++k) {
             const int c = 8 * (k * LANES + t), n = here ? a.cols - c : 0;
             float f[8];
+            if (!ROOM) {
+                gains(k);
+                if (a.dsum) vs[k] = load8(static_cast<const T *>(a.dsum) + (int64_t)r * a.dsum_ld + c, n);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float xh = (elem(vx[k], i) - mean) * rstd, g = elem(vd[k], i) * gam[k][i];
+                const float xh = (elem(vx[k], i) - mean) * rstd, g = elem(vd[k], i) * elem(gam[k], i);
                 f[i] = rstd * (g - c1 - xh * c2);
                 if (a.dsum) f[i] += elem(vs[k], i);
             }
@@ -308,7 +318,8 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
         }
     }
     // the block's rows joined, then one row of sums a block
-    float *out = a.part + (int64_t)blockIdx.x * 2 * a.cols;
+    float *const out[2] = {a.dgamma ? a.dgamma : a.part + (int64_t)blockIdx.x * 2 * a.cols,
+                           a.dbeta ? a.dbeta : a.part + ((int64_t)blockIdx.x * 2 + 1) * a.cols};
 #pragma unroll
     for (int k = 0; k < CPT; ++k)
 #pragma unroll
@@ -326,7 +337,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
                     for (int i = 0; i < 8; ++i) v[i] += join[j][i * LANES + t];
             }
             const int c = 8 * (k * LANES + t);
-            store8(out + which * a.cols + c, to_raw<float>(v), a.cols - c);
+            store8(out[which] + c, to_raw<float>(v), a.cols - c);
         }
 }
 
@@ -529,13 +540,15 @@ int dropout_run(const cg_drop *drop, int type, int64_t rows, int64_t cols, const
 // Which kernel takes rows of `cols` columns.
 constexpr int SHORT_COLS = 512, MID_COLS = 4096, WIDE_COLS = 16384;
 // Blocks of the backward kernel: each writes a row of column sums, so no more of them than keep the memory busy.
-constexpr int BWD_BLOCKS = 512, LONG_SLICES = 64;
+// A single block takes ONE_BLOCK turns and writes the sums itself: a turn more costs 2 us at most, a second launch 7.
+constexpr int BWD_BLOCKS = 512, LONG_SLICES = 64, ONE_BLOCK = 4;
 
 int bwd_rows_at_once(int64_t cols) { return cols <= 2 * SHORT_COLS ? 8 : cols <= MID_COLS ? 2 : 1; }
 int bwd_parts(int64_t rows, int64_t cols)
 {
     if (cols > WIDE_COLS) return (int)(rows < LONG_SLICES ? rows : LONG_SLICES);
     const int64_t n = (rows + bwd_rows_at_once(cols) - 1) / bwd_rows_at_once(cols);
+    if (n <= ONE_BLOCK) return n > 0;
     return (int)(n < BWD_BLOCKS ? n : BWD_BLOCKS);
 }
 
@@ -556,9 +569,11 @@ template <class T, int JOIN> int norm_fwd_typed(const NormArgs &a, hipStream_t s
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
 }
-template <class T, int JOIN> int norm_bwd_typed(const NormBwdArgs &a, float *dgamma, float *dbeta, hipStream_t s)
+template <class T, int JOIN> int norm_bwd_typed(NormBwdArgs &a, float *dgamma, float *dbeta, hipStream_t s)
 {
     const int n = a.cols, parts = bwd_parts(a.rows, n);
+    const bool whole = parts == 1 && n <= WIDE_COLS;
+    if (whole) a.dgamma = dgamma, a.dbeta = dbeta;
     if (parts > 0) {
         const dim3 grid((unsigned)parts);
         if (n <= SHORT_COLS) hipLaunchKernelGGL((norm_bwd_kernel<T, 1, 1, JOIN, 512>), grid, dim3(512), 0, s, a);
@@ -572,6 +587,7 @@ template <class T, int JOIN> int norm_bwd_typed(const NormBwdArgs &a, float *dga
             hipLaunchKernelGGL((norm_columns_kernel<T>), dim3((unsigned)((n + 511) / 512), (unsigned)parts), dim3(64), 0, s, a);
         }
         CG_HIP_TRY(hipGetLastError());
+        if (whole) return CG_OK;
     }
     hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)((2 * (int64_t)n + 15) / 16)), dim3(256), 0, s, a.part, parts, n, dgamma, dbeta);
     CG_HIP_TRY(hipGetLastError());
