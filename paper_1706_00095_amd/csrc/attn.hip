@@ -165,7 +165,8 @@ AttnArgs args_of(const cg_attn_desc &d, const Plan &p, const void *q, const void
     for (int i = 0; i < 2; ++i) a.part[i] = reinterpret_cast<float *>(ws + p.part[i]);
     a.part_ml = reinterpret_cast<float *>(ws + p.part_ml);
     a.yt = attn_dkdv_yt(d.type == CG_TYPE_BF16, p.DP);
-    a.dma = d.type == CG_TYPE_BF16 && attn_dma_ok(k, d.k_tok, 0, 1, d.D) && attn_dma_ok(v, d.v_tok, 0, 1, d.D) && d.k_head % 8 == 0 && d.v_head % 8 == 0;
+    a.dma = attn_dma_ok(d.type, k, d.k_tok, 0, 1, d.D) && attn_dma_ok(d.type, v, d.v_tok, 0, 1, d.D) &&
+            (d.type == CG_TYPE_FP32 || (d.k_head % 8 == 0 && d.v_head % 8 == 0));
     if (d.buckets) {
         a.btab = reinterpret_cast<const float *>(ws + p.tab);
         a.bid = reinterpret_cast<const uint8_t *>(ws + p.bid);
@@ -246,7 +247,7 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
         if (int rc = attn_dbias_launch(a.dbias_part, any ? p.tiles_q * p.q.splits : 0, d->Hq, d->buckets, dbias, s)) return rc;
     if (d->B > 0 && d->Tk > 0) {
         a.tiles = p.tiles_k;
-        a.dma = d->type == CG_TYPE_BF16 && attn_dma_ok(q, d->q_tok, d->q_head, p.Gp, d->D) && attn_dma_ok(d_o, d->o_tok, d->o_head, p.Gp, d->D) &&
+        a.dma = attn_dma_ok(d->type, q, d->q_tok, d->q_head, p.Gp, d->D) && attn_dma_ok(d->type, d_o, d->o_tok, d->o_head, p.Gp, d->D) &&
                 d->Tq * d->Hq < (1 << 29);
         a.splits = p.k.splits, a.chunk = p.k.chunk, a.gsplit = p.gsplit;
         if (int rc = attn_dkdv_launch(a, d->type, s)) return rc;

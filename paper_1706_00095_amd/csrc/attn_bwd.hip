@@ -469,8 +469,7 @@ template <class T, int DP, bool DMA> int dq_run(const AttnArgs &a, hipStream_t s
 }
 template <class T, int DP> int dq_dp(const AttnArgs &a, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2)
-        if (a.dma) return dq_run<T, DP, true>(a, s);
+    if (a.dma) return dq_run<T, DP, true>(a, s);
     return dq_run<T, DP, false>(a, s);
 }
 template <class T, int DP, bool DMA> int dkdv_run(const AttnArgs &a, hipStream_t s)
@@ -483,8 +482,7 @@ template <class T, int DP, bool DMA> int dkdv_run(const AttnArgs &a, hipStream_t
 }
 template <class T, int DP> int dkdv_dp(const AttnArgs &a, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2)
-        if (a.dma) return dkdv_run<T, DP, true>(a, s);
+    if (a.dma) return dkdv_run<T, DP, true>(a, s);
     return dkdv_run<T, DP, false>(a, s);
 }
 

@@ -48,11 +48,13 @@ constexpr int kAttnRows = 128;             // X rows of a block: four waves of 3
 constexpr int kAttnMaxD = 128;
 constexpr int attn_dkdv_yt(bool bf16, int DP) { return bf16 && DP < 128 ? 64 : 32; }
 
-// May rows of these strides (elements, bf16) travel without registers?  `per`: heads packed as rows (a tile of 32 begins with
-// a token).  16-byte aligned rows, and rows behind the last one behind the buffer's end.
-inline bool attn_dma_ok(const void *p, int64_t tok, int64_t head, int per, int D)
+// May the loaders that go by buffers take rows of these strides (elements)?  `per`: heads packed as rows (a tile of 32 begins with
+// a token).  Rows behind the last one have to lie behind the buffer's end.  bf16 goes to LDS directly: whole and 16-byte aligned
+// chunks of eight; fp32 goes through registers: whole chunks of four.
+inline bool attn_dma_ok(int type, const void *p, int64_t tok, int64_t head, int per, int D)
 {
-    return aligned16(p) && D % 8 == 0 && tok % 8 == 0 && head % 8 == 0 && tok >= (per - 1) * head + D && tok < (1 << 23) && 32 % per == 0;
+    if (!(tok >= (per - 1) * head + D && tok < (1 << 22) && 32 % per == 0)) return false;
+    return type == CG_TYPE_FP32 ? D % 4 == 0 : aligned16(p) && D % 8 == 0 && tok % 8 == 0 && head % 8 == 0;
 }
 
 // attn_fwd.hip, attn_bwd.hip: DP is D rounded up to a multiple of 32
@@ -86,10 +88,9 @@ template <int NP> __device__ __forceinline__ void cut_pair(float x0, float x1, u
     for (int k = 0; k < NP; ++k) {
         pc[k] = pack_bf16(x0, x1);
         if (k + 1 < NP) {
-            uint32_t h = pc[k];
-            asm("" : "+v"(h));             // both values from the pair, not each converted once more on its own
-            x0 -= __uint_as_float(h << 16);
-            x1 -= __uint_as_float(h & 0xffff0000u);
+            asm("" : "+v"(pc[k]));         // both values from the pair, not each converted once more on its own
+            x0 -= __uint_as_float(pc[k] << 16);
+            x1 -= __uint_as_float(pc[k] & 0xffff0000u);
         }
     }
 }
@@ -342,6 +343,55 @@ template <int DP, int ROWS> struct Loader<bf16raw, DP, ROWS, true> {
             if (LOADS % 4 == 0 || 4 * j + wave < LOADS) dma16(r, lds + (4 * j + wave) * 1024, voff[j]);
     }
     __device__ __forceinline__ void finish(LdsByte *) const {}
+};
+
+// fp32 with rows of whole 16 bytes: through registers, by loads from such a moving buffer, which need no bounds checks.
+template <int DP, int ROWS> struct Loader<float, DP, ROWS, true> {
+    static constexpr int CH = DP / 8, N = (ROWS * CH + 255) / 256;
+    const float *base;
+    int64_t tok;
+    int shift, tokens;
+    uint32_t tail;
+    uint32_t voff[N][2];
+    u32x4 r[N][2];
+    __device__ __forceinline__ Loader(const Rows<float> &s) : base(s.base), tok(s.tok)
+    {
+        const int gp = (int)s.by.d;
+        shift = __builtin_ctz(gp);
+        tokens = s.count >> shift;
+        tail = (uint32_t)(((gp - 1) * s.head + s.D) * 4);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int i = threadIdx.x + j * 256, row = i / CH, d = 8 * (i % CH), t = row >> shift;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                voff[j][h] = row < ROWS && d + 4 * h < s.D ? (uint32_t)((t * s.tok + (row - (t << shift)) * s.head + d + 4 * h) * 4) : OOB_ROW;
+        }
+    }
+    __device__ __forceinline__ void start(int row0, LdsByte *)
+    {
+        const int t0 = row0 >> shift, left = tokens - t0;
+        const uint64_t at = (uint64_t)reinterpret_cast<uintptr_t>(base) + (uint64_t)((int64_t)t0 * tok * 4);
+        const uint64_t span = left > 0 ? (uint64_t)(left - 1) * (uint64_t)tok * 4 + tail : 0;
+        const uint64_t u = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>((uintptr_t)u), 0,
+                                                            (int)__builtin_amdgcn_readfirstlane((uint32_t)(span < kMaxBufferBytes ? span : kMaxBufferBytes)), 0x00020000);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) r[j][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff[j][h], 0, 0));
+    }
+    __device__ __forceinline__ void finish(LdsByte *t) const
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int i = threadIdx.x + j * 256;
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(r[j][e / 4][e % 4]);
+            if (ROWS * CH % 256 == 0 || i < ROWS * CH) Tile<DP, ROWS, 3>::put(t, i / CH, i % CH, cut8<3>(f));
+        }
+    }
 };
 
 // Between tiles: this wave's loads into LDS have landed, and everyone's.

@@ -222,8 +222,7 @@ template <class T, int DP, bool DMA> int fwd_run(const AttnArgs &a, hipStream_t 
 }
 template <class T, int DP> int fwd_dp(const AttnArgs &a, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2)
-        if (a.dma) return fwd_run<T, DP, true>(a, s);
+    if (a.dma) return fwd_run<T, DP, true>(a, s);
     return fwd_run<T, DP, false>(a, s);
 }
 
