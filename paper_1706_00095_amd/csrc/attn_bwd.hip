@@ -97,6 +97,15 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
     const Rows<T> dO{static_cast<const T *>(a.d_o) + o_at, a.o_tok, a.o_head, rows, a.D, a.by_gp};
     const Rows<T> O{static_cast<const T *>(a.o_in) + o_at, a.o_tok, a.o_head, rows, a.D, a.by_gp};
     const Rows<T> R{static_cast<const T *>(a.o_rest_in) + o_at, a.o_tok, a.o_head, rows, a.D, a.by_gp};
+    Loader<T, DP, YT, DMA> lk(K), lv(V);
+    const int window0 = -(row0 + kAttnRows - 1) - off;
+    float bias_next = 0.f;
+    if (kbeg < kend) {
+        lk.start(kbeg, ldsK);
+        lv.start(kbeg, ldsV);
+        if constexpr (BIAS) window[0][threadIdx.x] = window_load(a, h0, kbeg + window0);
+    }
+
     Frag<NP> fq[KS], fdo[KS];
     float delta = 0.f;
 #pragma unroll
@@ -131,13 +140,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
     for (int dt = 0; dt < DT; ++dt) dQ[dt] = v16f{};
     float far_past = 0.f, far_future = 0.f;
 
-    Loader<T, DP, YT, DMA> lk(K), lv(V);
-    const int window0 = -(row0 + kAttnRows - 1) - off;
-    float bias_next = 0.f;
     if (kbeg < kend) {
-        lk.start(kbeg, ldsK);
-        lv.start(kbeg, ldsV);
-        if constexpr (BIAS) window[0][threadIdx.x] = window_load(a, h0, kbeg + window0);
         lk.finish(ldsK);
         lv.finish(ldsV);
     }

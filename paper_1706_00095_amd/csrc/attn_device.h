@@ -144,13 +144,13 @@ template <> struct Acc<3> {
 };
 
 // ---- LDS tiles ------------------------------------------------------------------------------------------------------------
-// ROWS x DP bf16, NP planes.  16-byte chunks of a row are exchanged by a function of the row so that neither eight rows'
-// same chunk (row reads) nor four rows' same 64 bytes (transposing reads) fall on the same banks (64 of 4 bytes).
+// ROWS x DP bf16, NP planes.  16-byte chunks of a row are exchanged by a function of the row so that neither sixteen rows' same chunk
+// (a row read takes 16 lanes at a time) nor four rows' same 64 bytes (transposing reads) fall on the same banks (64 of 4 bytes).
 template <int DP> __device__ __forceinline__ int swizzle(int row)
 {
-    if constexpr (DP == 128) return (row & 3) << 2 | (row >> 2 & 1);
-    else if constexpr (DP == 64) return (row >> 1 & 1) << 2 | (row >> 2 & 1);
-    else return row >> 2 & 1;
+    if constexpr (DP == 128) return (row & 3) << 2 | (row >> 2 & 3);
+    else if constexpr (DP == 64) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    else return row >> 2 & 3;
 }
 template <int DP, int ROWS, int NP> struct Tile {
     static constexpr int CH = DP / 8, BYTES = NP * ROWS * DP * 2;

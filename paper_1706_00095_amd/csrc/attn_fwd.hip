@@ -48,6 +48,17 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
     const Rows<T> K{static_cast<const T *>(a.k) + (int64_t)s.k0 * a.k_tok + (int64_t)hkv * a.k_head, a.k_tok, 0, s.m, a.D, one};
     const Rows<T> V{static_cast<const T *>(a.v) + (int64_t)s.k0 * a.v_tok + (int64_t)hkv * a.v_head, a.v_tok, 0, s.m, a.D, one};
     const Rows<T> Q{static_cast<const T *>(a.q) + (int64_t)s.q0 * a.q_tok + (int64_t)h0 * a.q_head, a.q_tok, a.q_head, rows, a.D, a.by_gp};
+    // Two buffers and one barrier a tile: behind it the tile is there and everyone is done with the one before, whose buffer the
+    // next one's loads then fill while this one is multiplied.
+    Loader<T, DP, YT, DMA> lk(K), lv(V);
+    const int window0 = -(row0 + kAttnRows - 1) - off;
+    float bias_next = 0.f;
+    if (kbeg < kend) {
+        lk.start(kbeg, ldsK);
+        lv.start(kbeg, ldsV);
+        if constexpr (BIAS) window[0][threadIdx.x] = window_load(a, h0, kbeg + window0);
+    }
+
     Frag<NP> fq[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) fq[ks] = frag_of(Q.load(row, 16 * ks + 8 * h32));
@@ -60,15 +71,8 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
     float m = -INFINITY, l = 0.f;
     // without a bias scores stay as the product gives them and the scale enters the exponent: exp2(s c - m c)
     const float c = a.scale * kLog2e;
-    // Two buffers and one barrier a tile: behind it the tile is there and everyone is done with the one before, whose buffer the
-    // next one's loads then fill while this one is multiplied.
-    Loader<T, DP, YT, DMA> lk(K), lv(V);
-    const int window0 = -(row0 + kAttnRows - 1) - off;
-    float bias_next = 0.f;
+
     if (kbeg < kend) {
-        lk.start(kbeg, ldsK);
-        lv.start(kbeg, ldsV);
-        if constexpr (BIAS) window[0][threadIdx.x] = window_load(a, h0, kbeg + window0);
         lk.finish(ldsK);
         lv.finish(ldsV);
     }
