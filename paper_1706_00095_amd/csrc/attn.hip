@@ -98,7 +98,7 @@ struct Plan {
     int Gp, tiles_q, tiles_k, W, DP;
     int gsplit;
     Split q, k;                 // of the kernels whose X are queries (forward, dq) and keys (dk, dv)
-    size_t tab, bid, part[2], part_ml, delta, lse_b, dbias, bytes;
+    size_t tab, bid, part_q, part_ml, part_k[2], delta, lse_b, dbias, bytes;
 };
 
 Plan plan_of(const cg_attn_desc &d, int pass)
@@ -123,17 +123,17 @@ Plan plan_of(const cg_attn_desc &d, int pass)
     p.q = split_of(Hr, p.tiles_q, d.Tk, d.B, (p.DP + 2) * 4, d.type);
     const int64_t q_rows = p.q.splits > 1 ? Hr * p.tiles_q * p.q.splits * kAttnRows : 0;
     if (pass == CG_PASS_FWD) {
-        p.part[0] = take(q_rows * p.DP * 4);
+        p.part_q = take(q_rows * p.DP * 4);
         p.part_ml = take(q_rows * 2 * 4);
     } else {
-        // the sums over keys and the sums over rows are done one after the other: one room for both
         // with a bias a block walks the heads of its keys one after the other; where blocks are few each gets blocks of its own
         const int64_t G = d.Hq / d.Hkv, blocks_k = (int64_t)d.Hkv * p.tiles_k;
         p.gsplit = d.buckets && G > 1 && blocks_k < kFull && blocks_k * G * kAttnRows * 2 * p.DP * 4 <= kPartBytes ? (int)G : 1;
         p.k = split_of((int64_t)d.Hkv * p.gsplit, p.tiles_k, d.Tq * p.Gp, d.B, 2 * p.DP * 4, d.type);
         const int64_t k_rows = p.k.splits * p.gsplit > 1 ? blocks_k * p.gsplit * p.k.splits * kAttnRows : 0;
-        p.part[0] = take((q_rows > k_rows ? q_rows : k_rows) * p.DP * 4);
-        p.part[1] = take(k_rows * p.DP * 4);
+        p.part_q = take(q_rows * p.DP * 4);
+        p.part_k[0] = take(k_rows * p.DP * 4);
+        p.part_k[1] = take(k_rows * p.DP * 4);
         p.delta = take(d.Tq * d.Hq * 4);
         p.lse_b = take(d.Tq * d.Hq * 4);
         p.dbias = take((int64_t)d.Hq * p.tiles_q * p.q.splits * d.buckets * 4);
@@ -162,7 +162,7 @@ AttnArgs args_of(const cg_attn_desc &d, const Plan &p, const void *q, const void
     a.W = p.W;
     a.tiles = p.tiles_q;
     a.splits = p.q.splits, a.chunk = p.q.chunk, a.gsplit = 1;
-    for (int i = 0; i < 2; ++i) a.part[i] = reinterpret_cast<float *>(ws + p.part[i]);
+    a.part[0] = reinterpret_cast<float *>(ws + p.part_q);
     a.part_ml = reinterpret_cast<float *>(ws + p.part_ml);
     a.yt = attn_dkdv_yt(d.type == CG_TYPE_BF16, p.DP);
     a.dma = attn_dma_ok(d.type, k, d.k_tok, 0, 1, d.D) && attn_dma_ok(d.type, v, d.v_tok, 0, 1, d.D) &&
@@ -214,7 +214,7 @@ extern "C" int cg_attn_fwd(const cg_attn_desc *d, const void *q, const void *k, 
     AttnArgs a = args_of(*d, p, q, k, v, cu_q, cu_k, w);
     a.o = o, a.o_rest = o_rest, a.lse = lse;
     if (int rc = attn_fwd_launch(a, d->type, s)) return rc;
-    return a.splits > 1 ? attn_join_launch(a, d->type, ATTN_JOIN_O, s) : CG_OK;
+    return a.splits > 1 ? attn_join_launch(a, d->type, s) : CG_OK;
 }
 
 extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q, const void *k, const void *v, const int32_t *cu_q,
@@ -236,22 +236,21 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
     a.dq = dq, a.dk = dk, a.dv = dv;
     a.delta = reinterpret_cast<float *>(w + p.delta);
     a.lse_b = reinterpret_cast<float *>(w + p.lse_b);
-    if (dbias) a.dbias_part = reinterpret_cast<float *>(w + p.dbias);
-    const bool any = d->B > 0 && d->Tq > 0;
-    if (any) {
+    const bool any_q = d->B > 0 && d->Tq > 0, any_k = d->B > 0 && d->Tk > 0;
+    if (dbias) {
+        a.dbias = dbias;
+        a.dbias_part = reinterpret_cast<float *>(w + p.dbias);
+        a.dbias_parts = any_q ? p.tiles_q * p.q.splits : 0;
+    }
+    AttnArgs k_side = a;       // the dk/dv kernel's, which also adds up dbias
+    if (any_q)
         if (int rc = attn_dq_launch(a, d->type, s)) return rc;
-        if (a.splits > 1)
-            if (int rc = attn_join_launch(a, d->type, ATTN_JOIN_DQ, s)) return rc;
-    }
-    if (dbias)
-        if (int rc = attn_dbias_launch(a.dbias_part, any ? p.tiles_q * p.q.splits : 0, d->Hq, d->buckets, dbias, s)) return rc;
-    if (d->B > 0 && d->Tk > 0) {
-        a.tiles = p.tiles_k;
-        a.dma = attn_dma_ok(d->type, q, d->q_tok, d->q_head, p.Gp, d->D) && attn_dma_ok(d->type, d_o, d->o_tok, d->o_head, p.Gp, d->D) &&
-                d->Tq * d->Hq < (1 << 29);
-        a.splits = p.k.splits, a.chunk = p.k.chunk, a.gsplit = p.gsplit;
-        if (int rc = attn_dkdv_launch(a, d->type, s)) return rc;
-        if (a.splits * a.gsplit > 1) return attn_join_launch(a, d->type, ATTN_JOIN_DKDV, s);
-    }
-    return CG_OK;
+    k_side.tiles = any_k ? p.tiles_k : 0;
+    k_side.dma = attn_dma_ok(d->type, q, d->q_tok, d->q_head, p.Gp, d->D) && attn_dma_ok(d->type, d_o, d->o_tok, d->o_head, p.Gp, d->D) &&
+                 d->Tq * d->Hq < (1 << 29);
+    k_side.splits = p.k.splits, k_side.chunk = p.k.chunk, k_side.gsplit = p.gsplit;
+    k_side.part[0] = reinterpret_cast<float *>(w + p.part_k[0]), k_side.part[1] = reinterpret_cast<float *>(w + p.part_k[1]);
+    if (any_k || dbias)
+        if (int rc = attn_dkdv_launch(k_side, d->type, s)) return rc;
+    return attn_join_bwd_launch(any_q && a.splits > 1 ? &a : nullptr, any_k && p.k.splits * p.gsplit > 1 ? &k_side : nullptr, d->type, s);
 }

@@ -261,21 +261,21 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
     else store_row(static_cast<T *>(a.dq) + (int64_t)(s.q0 + tok) * a.q_tok + (int64_t)head * a.q_head, dQ, a.scale, a.D, h32);
 }
 
-// dbias[h][bucket]: the blocks' sums added in a fixed order, in 64 bits.  A block takes a head and 16 buckets, 16 threads a bucket.
-__global__ __launch_bounds__(256) void attn_dbias_kernel(const float *part, int parts, int buckets, float *dbias)
+// dbias[h][bucket]: the dq kernel's blocks' sums added in a fixed order, in 64 bits.  A block takes a head and 16 buckets, 16 threads a
+// bucket.  It rides in the dk/dv launch, behind the blocks of that.
+__device__ __forceinline__ void sum_dbias(const AttnArgs &a, int item, double *lds)
 {
-    __shared__ double lds[16][17];
-    const int h = blockIdx.y, x = threadIdx.x % 16, j = threadIdx.x / 16, i = blockIdx.x * 16 + x;
+    const int groups = (a.buckets + 15) / 16, h = item / groups, x = threadIdx.x % 16, j = threadIdx.x / 16, i = item % groups * 16 + x;
     double s = 0;
-    if (i < buckets)
+    if (i < a.buckets)
 #pragma unroll 4
-        for (int t = j; t < parts; t += 16) s += part[((int64_t)h * parts + t) * buckets + i];
-    lds[j][x] = s;
+        for (int t = j; t < a.dbias_parts; t += 16) s += a.dbias_part[((int64_t)h * a.dbias_parts + t) * a.buckets + i];
+    lds[j * 17 + x] = s;
     __syncthreads();
-    if (j == 0 && i < buckets) {
+    if (j == 0 && i < a.buckets) {
 #pragma unroll
-        for (int k = 1; k < 16; ++k) s += lds[k][x];
-        dbias[(int64_t)h * buckets + i] = (float)s;
+        for (int k = 1; k < 16; ++k) s += lds[k * 17 + x];
+        a.dbias[(int64_t)h * a.buckets + i] = (float)s;
     }
 }
 
@@ -297,6 +297,14 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
     __shared__ __align__(16) float stats[2][2][64];            // lse_b, delta of the tile's rows
     __shared__ float window[2][BIAS ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
+    if constexpr (BIAS) {
+        const int mine = a.Hkv * a.tiles * a.splits * a.gsplit;
+        if ((int)blockIdx.x >= mine) {
+            __shared__ double sums[16 * 17];
+            sum_dbias(a, blockIdx.x - mine, sums);
+            return;
+        }
+    }
     const int hkv = blockIdx.x % a.Hkv, item = blockIdx.x / a.Hkv, slots = a.splits * a.gsplit, slot = item % slots, tile = item / slots;
     const int split = slot / a.gsplit;
     int b, t;
@@ -477,7 +485,7 @@ template <class T, int DP> int dq_dp(const AttnArgs &a, hipStream_t s)
 }
 template <class T, int DP, bool DMA> int dkdv_run(const AttnArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)a.Hkv * a.tiles * a.splits * a.gsplit);
+    const dim3 grid((unsigned)a.Hkv * a.tiles * a.splits * a.gsplit + (a.dbias ? (unsigned)a.Hq * ((a.buckets + 15) / 16) : 0u));
     if (a.btab) hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
@@ -511,11 +519,4 @@ int attn_dkdv_launch(const AttnArgs &a, int type, hipStream_t s)
 #undef CG_DP
     return CG_EUNSUPPORTED;
 }
-int attn_dbias_launch(const float *part, int parts, int Hq, int buckets, float *dbias, hipStream_t s)
-{
-    hipLaunchKernelGGL(attn_dbias_kernel, dim3((unsigned)(buckets + 15) / 16, (unsigned)Hq), dim3(256), 0, s, part, parts, buckets, dbias);
-    CG_HIP_TRY(hipGetLastError());
-    return CG_OK;
-}
-
 }  // namespace cg

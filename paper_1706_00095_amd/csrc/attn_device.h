@@ -34,7 +34,8 @@ struct AttnArgs {
     const float *btab;
     const uint8_t *bid;
     int W, buckets;
-    float *dbias_part;                     // [Hq][tiles][buckets]
+    float *dbias_part, *dbias;             // [Hq][dbias_parts][buckets] of the dq kernel's blocks, tiles x splits; [Hq][buckets]
+    int dbias_parts;
     int tiles;                             // of X rows over all sequences, an upper bound
     // Y cut into at most `splits` chunks of `chunk` rows, a block each; a tile with several leaves partial results for attn_join_kernel
     int splits, chunk;
@@ -61,9 +62,9 @@ inline bool attn_dma_ok(int type, const void *p, int64_t tok, int64_t head, int 
 int attn_fwd_launch(const AttnArgs &a, int type, hipStream_t s);
 int attn_dq_launch(const AttnArgs &a, int type, hipStream_t s);
 int attn_dkdv_launch(const AttnArgs &a, int type, hipStream_t s);
-enum { ATTN_JOIN_O = 0, ATTN_JOIN_DQ, ATTN_JOIN_DKDV };
-int attn_join_launch(const AttnArgs &a, int type, int what, hipStream_t s);
-int attn_dbias_launch(const float *part, int parts, int Hq, int buckets, float *dbias, hipStream_t s);
+// The join of the forward pass; of the backward pass, dq and dk, dv in one launch (either NULL: nothing to join).
+int attn_join_launch(const AttnArgs &a, int type, hipStream_t s);
+int attn_join_bwd_launch(const AttnArgs *dq, const AttnArgs *dkdv, int type, hipStream_t s);
 
 namespace {
 

@@ -11,12 +11,14 @@ template <int DP, bool ROWS> struct Join {
     static constexpr int L = DP / 4, GROUPS = 64 / L, PER_BLOCK = ROWS ? 4 * GROUPS : 4;
 };
 
-template <class T, int DP, int WHAT, bool ROWS> __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
+enum { ATTN_JOIN_O = 0, ATTN_JOIN_DQ, ATTN_JOIN_DKDV };
+
+template <class T, int DP, int WHAT, bool ROWS> __device__ __forceinline__ void join_block(const AttnArgs &a, int block)
 {
     using J = Join<DP, ROWS>;
     constexpr int L = J::L, GROUPS = J::GROUPS, AT_ONCE = 4, STEP = ROWS ? 1 : GROUPS;
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int problems = WHAT == ATTN_JOIN_DKDV ? a.Hkv : a.Hq / a.Gp, pr = blockIdx.x % problems, item = blockIdx.x / problems;
+    const int problems = WHAT == ATTN_JOIN_DKDV ? a.Hkv : a.Hq / a.Gp, pr = block % problems, item = block / problems;
     const int tile = item / (kAttnRows / J::PER_BLOCK), part = item % (kAttnRows / J::PER_BLOCK);
     int b, t;
     if (WHAT == ATTN_JOIN_DKDV ? !find_tile(a.cu_k, a.Tk, a.B, kAttnRows, 1, tile, b, t) : !find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t)) return;
@@ -115,27 +117,61 @@ template <class T, int DP, int WHAT, bool ROWS> __global__ __launch_bounds__(256
     }
 }
 
-template <class T, int DP, bool ROWS> int join_run(const AttnArgs &a, int what, hipStream_t s)
+template <class T, int DP, bool ROWS> __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
-    const dim3 grid((unsigned)(what == ATTN_JOIN_DKDV ? a.Hkv : a.Hq / a.Gp) * a.tiles * (kAttnRows / Join<DP, ROWS>::PER_BLOCK));
-    if (what == ATTN_JOIN_O) hipLaunchKernelGGL((attn_join_kernel<T, DP, ATTN_JOIN_O, ROWS>), grid, dim3(256), 0, s, a);
-    else if (what == ATTN_JOIN_DQ) hipLaunchKernelGGL((attn_join_kernel<T, DP, ATTN_JOIN_DQ, ROWS>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_join_kernel<T, DP, ATTN_JOIN_DKDV, ROWS>), grid, dim3(256), 0, s, a);
+    join_block<T, DP, ATTN_JOIN_O, ROWS>(a, blockIdx.x);
+}
+// blocks 0 .. blocks_q - 1: dq
+template <class T, int DP, bool ROWS> __global__ __launch_bounds__(256) void attn_join_bwd_kernel(AttnArgs q, AttnArgs k, int blocks_q)
+{
+    if ((int)blockIdx.x < blocks_q) join_block<T, DP, ATTN_JOIN_DQ, ROWS>(q, blockIdx.x);
+    else join_block<T, DP, ATTN_JOIN_DKDV, ROWS>(k, blockIdx.x - blocks_q);
+}
+
+// A row a wave while the chip has room for all the waves at once (8192)
+constexpr int64_t kJoinWaves = 8192;
+
+template <class T, int DP, bool ROWS> int join_fwd(const AttnArgs &a, int64_t rows, hipStream_t s)
+{
+    hipLaunchKernelGGL((attn_join_kernel<T, DP, ROWS>), dim3((unsigned)(rows / Join<DP, ROWS>::PER_BLOCK)), dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
 }
-// A row a wave while the chip has room for all the waves at once (8192)
-template <class T, int DP> int join_dp(const AttnArgs &a, int what, hipStream_t s)
+template <class T, int DP> int fwd_dp(const AttnArgs &a, hipStream_t s)
 {
-    const int64_t rows = (int64_t)(what == ATTN_JOIN_DKDV ? a.Hkv : a.Hq / a.Gp) * a.tiles * kAttnRows;
-    return rows > 8192 ? join_run<T, DP, true>(a, what, s) : join_run<T, DP, false>(a, what, s);
+    const int64_t rows = (int64_t)(a.Hq / a.Gp) * a.tiles * kAttnRows;
+    return rows > kJoinWaves ? join_fwd<T, DP, true>(a, rows, s) : join_fwd<T, DP, false>(a, rows, s);
+}
+template <class T, int DP, bool ROWS> int join_bwd(const AttnArgs *q, const AttnArgs *k, int64_t rows_q, int64_t rows_k, hipStream_t s)
+{
+    const int bq = (int)(rows_q / Join<DP, ROWS>::PER_BLOCK), bk = (int)(rows_k / Join<DP, ROWS>::PER_BLOCK);
+    hipLaunchKernelGGL((attn_join_bwd_kernel<T, DP, ROWS>), dim3((unsigned)(bq + bk)), dim3(256), 0, s, q ? *q : *k, k ? *k : *q, bq);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+template <class T, int DP> int bwd_dp(const AttnArgs *q, const AttnArgs *k, hipStream_t s)
+{
+    const int64_t rows_q = q ? (int64_t)(q->Hq / q->Gp) * q->tiles * kAttnRows : 0, rows_k = k ? (int64_t)k->Hkv * k->tiles * kAttnRows : 0;
+    return rows_q + rows_k > kJoinWaves ? join_bwd<T, DP, true>(q, k, rows_q, rows_k, s) : join_bwd<T, DP, false>(q, k, rows_q, rows_k, s);
 }
 
 }  // namespace
 
-int attn_join_launch(const AttnArgs &a, int type, int what, hipStream_t s)
+int attn_join_launch(const AttnArgs &a, int type, hipStream_t s)
 {
-#define CG_DP(DP) if (a.D <= DP) return type == CG_TYPE_FP32 ? join_dp<float, DP>(a, what, s) : join_dp<bf16raw, DP>(a, what, s)
+#define CG_DP(DP) if (a.D <= DP) return type == CG_TYPE_FP32 ? fwd_dp<float, DP>(a, s) : fwd_dp<bf16raw, DP>(a, s)
+    CG_DP(32);
+    CG_DP(64);
+    CG_DP(96);
+    CG_DP(128);
+#undef CG_DP
+    return CG_EUNSUPPORTED;
+}
+int attn_join_bwd_launch(const AttnArgs *dq, const AttnArgs *dkdv, int type, hipStream_t s)
+{
+    if (!dq && !dkdv) return CG_OK;
+    const int D = dq ? dq->D : dkdv->D;
+#define CG_DP(DP) if (D <= DP) return type == CG_TYPE_FP32 ? bwd_dp<float, DP>(dq, dkdv, s) : bwd_dp<bf16raw, DP>(dq, dkdv, s)
     CG_DP(32);
     CG_DP(64);
     CG_DP(96);
