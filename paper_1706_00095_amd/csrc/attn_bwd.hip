@@ -239,12 +239,16 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
             far_future += __shfl_xor(far_future, m);
         }
         float *const sums = a.W <= kNear ? square[wave] : mine;       // [buckets] of this wave
-        if (a.W <= kNear) {
+        if (a.W <= kNear) {       // the waves' sums by distance, in order, then by bucket: a quarter of the distances a wave
 #pragma unroll
             for (int i = 0; i < 256; i += 64) sums[i + lane] = 0.f;
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            for (int i = 0; i <= 2 * a.W; i += 64)       // 64 distances at a time, in order
-                add_runs(i + lane <= 2 * a.W ? mine[i + lane] : 0.f, i + lane <= 2 * a.W ? (int)a.bid[i + lane] : -1, sums, lane);
+            __syncthreads();
+            const int words = near_words(a.W);
+            for (int i = 64 * wave; i < words; i += 256) {
+                const bool there = i + lane < words;
+                const float *w = by_wave + (there ? i + lane : 0);
+                add_runs(there ? (w[0] + w[words]) + (w[2 * words] + w[3 * words]) : 0.f, there ? (int)a.bid[i + lane] : -1, sums, lane);
+            }
         }
         if (lane == 0) {
             sums[a.bid[0]] += far_past;
