@@ -269,3 +269,68 @@ def test_gradients_against_differences():
         a = Attention(q, k, v, vals[3], lens, lens, 0.25, True, table.double() + e * dirs[3], 16, 40, False, torch.float32, False)
         return float((a.o * vals[3]).sum())
     assert abs(along - (value(h) - value(-h)) / (2 * h)) < 1e-3 * size
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_cache_longer_than_32_bits_of_bytes(dtype):
+    """Keys and values as slices of one tensor of over 4 GiB, the last tokens beyond 2^32 bytes."""
+    dt, D, Tk, tok, Tq = DTYPES[dtype], 64, 36000, 1 << (16 if dtype == "bf16" else 15), 3
+    wide = torch.empty(Tk, tok, dtype=dt, device="cuda")
+    assert wide.numel() * wide.element_size() > 1 << 32
+    g = torch.Generator().manual_seed(1)
+    vals = [torch.empty(T, 1, D, dtype=torch.float64).normal_(0, s, generator=g).to(dt) for T, s in ((Tq, 1), (Tk, 1), (Tk, 1), (Tq, 0.02))]
+    q, do = vals[0].cuda(), vals[3].cuda()
+    k, v = wide[:, None, :D], wide[:, None, 4096:4096 + D]
+    k.copy_(vals[1].cuda())
+    v.copy_(vals[2].cuda())
+    dwide = torch.full_like(wide, float("nan"))
+    dk, dv = dwide[:, None, :D], dwide[:, None, 4096:4096 + D]
+    o, dq, rest = torch.empty_like(q), torch.empty_like(q), torch.empty_like(q) if dtype == "bf16" else None
+    d = cg.attn_desc(q, k, v, o, 1, 0.125, True)
+    lse = torch.empty(1, Tq, device="cuda")
+    ws = [torch.empty(cg.cg_attn_workspace_bytes(d, p) + 16, dtype=torch.uint8, device="cuda") for p in (cg.CG_PASS_FWD, cg.CG_PASS_BWD_DATA)]
+    cq, ck = lengths([Tq]), lengths([Tk])
+    cg.cg_attn_fwd(d, q, k, v, cq, ck, None, o, lse, rest, ws[0])
+    cg.cg_attn_bwd(d, do, q, k, v, cq, ck, None, o, rest, lse, dq, dk, dv, None, ws[1])
+    a = Attention(*[t.double() for t in vals], [Tq], [Tk], 0.125, True, None, 0, 0, False, dt, dtype == "bf16")
+    check({"o": o, "lse": lse, "dq": dq, "dk": dk, "dv": dv}, a, dt)
+    assert torch.isnan(dwide[:, D:4096].float()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_strides_wider_than_a_buffer_of_a_tile(dtype):
+    """Tokens more than 2^22 elements apart, and heads outside tokens (all tokens of a head together)."""
+    dt, T, H, D = DTYPES[dtype], 20, 2, 32
+    x, vals = inputs(dtype, [T], [T], H, H, D)
+    far = torch.zeros(T * ((1 << 22) + 8), dtype=dt, device="cuda")
+    q, k, v, do = x
+    k2 = far.as_strided((T, H, D), ((1 << 22) + 8, D, 1))
+    k2.copy_(k)
+    by_head = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (q, v, do)]
+    a = Attention(*vals, [T], [T], 0.25, False, None, 0, 0, False, dt, False)
+    check(call((by_head[0], k2, by_head[1], by_head[2]), 1, lengths([T]), lengths([T]), 0.25, False, None, 0, False, False), a, dt)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bias", [0, 32])
+def test_heads_packed_in_memory_orders_of_their_own(dtype, bias):
+    """Grouped heads whose query heads lie outside the tokens: packed rows are then not in the order of their addresses."""
+    dt, lens, Hq, Hkv, D = DTYPES[dtype], [70, 9], 4, 2, 64
+    x, vals = inputs(dtype, lens, lens, Hq, Hkv, D)
+    q, k, v, do = (t.transpose(0, 1).contiguous().transpose(0, 1) for t in x)
+    table = torch.randn(Hq, bias, generator=torch.Generator().manual_seed(2)).cuda() if bias else None
+    a = Attention(*vals, lens, lens, 0.125, True, table.double().cpu() if bias else None, bias, 100, False, dt, dtype == "bf16")
+    check(call((q, k, v, do), 2, lengths(lens), lengths(lens), 0.125, True, table, 100 if bias else 0, False, dtype == "bf16"), a, dt)
+
+
+@pytest.mark.parametrize("far", [1024, 1025, 3000])
+def test_bias_of_far_distances(far):
+    """On both sides of the number of distances whose sums a wave keeps one by one."""
+    run("bf16", [900, 130], [1400, 130], 2, 1, 64, False, bias=32, far=far, both=True)
+
+
+def test_many_sequences():
+    """More sequences than a wave looks through at once, some of them empty."""
+    lens = [(7 * i) % 13 for i in range(150)]
+    run("bf16", lens, lens, 2, 1, 32, True)
+    run("fp32", lens, [n + 3 for n in lens], 1, 1, 32, False, bias=8, far=9)
