@@ -381,7 +381,9 @@ int cg_dropout_add_layernorm_bwd(const cg_layernorm_desc *d, const cg_drop *drop
  * 1 <= D <= 128; Tq * Hq, Tk * Hkv < 2^31; tensors may exceed 2^31 bytes.
  * Arithmetic: bf16 tensors are multiplied as they are, the probabilities and the gradients of the scores
  * rounded to bf16 for their products; fp32 tensors as three bf16 numbers in six products (CG_MATH_FP32 above).
- * Sequences that overlap or reach past Tq, Tk are cut there; rows of no sequence are neither read nor written. */
+ * Sequences that overlap or reach past Tq, Tk are cut there; rows of no sequence are neither read nor written.
+ * A q, k or v that is not finite makes what sees it not finite; within its own sequence it may do so to rows that a causal mask
+ * or a bias of -inf keeps from it as well (0 times it), never in another sequence. */
 typedef struct {
     int type, B, Hq, Hkv, D;
     int64_t Tq, Tk;

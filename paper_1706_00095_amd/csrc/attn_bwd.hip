@@ -154,77 +154,77 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
             if constexpr (BIAS) bias_next = window_load(a, h0, k0 + YT + window0);
         }
         if (k0 < wave_kend) {
-        Frag<NP> fds[SUB][2];
+            Frag<NP> fds[SUB][2];
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            Acc<NP> S, P;
-            S.zero();
-            P.zero();
+            for (int u = 0; u < SUB; ++u) {
+                Acc<NP> S, P;
+                S.zero();
+                P.zero();
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                S.mma(TileY::rows(ldsK + buf * TileY::BYTES, 32 * u, ks, lane), fq[ks]);
-                P.mma(TileY::rows(ldsV + buf * TileY::BYTES, 32 * u, ks, lane), fdo[ks]);
-            }
-            float ds[16];
+                for (int ks = 0; ks < KS; ++ks) {
+                    S.mma(TileY::rows(ldsK + buf * TileY::BYTES, 32 * u, ks, lane), fq[ks]);
+                    P.mma(TileY::rows(ldsV + buf * TileY::BYTES, 32 * u, ks, lane), fdo[ks]);
+                }
+                float ds[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int y = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4;
-                float p;
+                for (int i = 0; i < 16; ++i) {
+                    const int y = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4;
+                    float p;
+                    if constexpr (BIAS) {
+                        const float x = fmaf(S.get(i), a.scale, window[buf][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
+                        p = __builtin_amdgcn_exp2f((x - lse_b) * kLog2e);
+                    } else p = __builtin_amdgcn_exp2f(fmaf(S.get(i), c, -lse_b));
+                    ds[i] = p * (P.get(i) - delta);
+                }
+                if (k0 + 32 * u + 32 > wave_limit)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (32 * u + 8 * (i / 4) + i % 4 >= limit - k0 - 4 * h32) ds[i] = 0.f;
                 if constexpr (BIAS) {
-                    const float x = fmaf(S.get(i), a.scale, window[buf][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
-                    p = __builtin_amdgcn_exp2f((x - lse_b) * kLog2e);
-                } else p = __builtin_amdgcn_exp2f(fmaf(S.get(i), c, -lse_b));
-                ds[i] = p * (P.get(i) - delta);
-            }
-            if (k0 + 32 * u + 32 > wave_limit)
+                    if (want_bias) {
+                        // distances of this 32 x 32 part: first .. first + 62
+                        const int delta0 = k0 + 32 * u - (row0 + 32 * wave) - off;
+                        if (delta0 + 31 <= -a.W || delta0 - 31 >= a.W) {
+                            float sum = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (32 * u + 8 * (i / 4) + i % 4 >= limit - k0 - 4 * h32) ds[i] = 0.f;
-            if constexpr (BIAS) {
-                if (want_bias) {
-                    // distances of this 32 x 32 part: first .. first + 62
-                    const int delta0 = k0 + 32 * u - (row0 + 32 * wave) - off;
-                    if (delta0 + 31 <= -a.W || delta0 - 31 >= a.W) {
-                        float sum = 0.f;
+                            for (int i = 0; i < 16; ++i) sum += here ? ds[i] : 0.f;
+                            (delta0 < 0 ? far_past : far_future) += sum;
+                        } else {
+                            if (!here)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) sum += here ? ds[i] : 0.f;
-                        (delta0 < 0 ? far_past : far_future) += sum;
-                    } else {
-                        if (!here)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) ds[i] = 0.f;
-                        const float v = diagonal_sum(ds, square[wave], lane);
-                        const int delta = delta0 + lane - 31;
-                        if (a.W > kNear) add_runs(v, lane < 63 ? (int)a.bid[min(max(delta, -a.W), a.W) + a.W] : -1, mine, lane);
-                        else if (lane < 63) {
-                            if (delta <= -a.W) far_past += v;
-                            else if (delta >= a.W) far_future += v;
-                            else mine[delta + a.W] += v;
+                                for (int i = 0; i < 16; ++i) ds[i] = 0.f;
+                            const float v = diagonal_sum(ds, square[wave], lane);
+                            const int delta = delta0 + lane - 31;
+                            if (a.W > kNear) add_runs(v, lane < 63 ? (int)a.bid[min(max(delta, -a.W), a.W) + a.W] : -1, mine, lane);
+                            else if (lane < 63) {
+                                if (delta <= -a.W) far_past += v;
+                                else if (delta >= a.W) far_future += v;
+                                else mine[delta + a.W] += v;
+                            }
                         }
                     }
                 }
+#pragma unroll
+                for (int g = 0; g < 2; ++g) fds[u][g] = cut8<NP>(&ds[8 * g]);
             }
 #pragma unroll
-            for (int g = 0; g < 2; ++g) fds[u][g] = cut8<NP>(&ds[8 * g]);
-        }
+            for (int dt = 0; dt < DT; ++dt) {
+                if constexpr (NP == 1) {
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            if constexpr (NP == 1) {
+                    for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int u = 0; u < SUB; ++u)
+                        for (int g = 0; g < 2; ++g) dQ[dt] = mfma(TileY::cols(ldsK + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane).p[0], fds[u][g].p[0], dQ[dt]);
+                } else {
+                    Acc<NP> S;
+                    S.zero();
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) dQ[dt] = mfma(TileY::cols(ldsK + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane).p[0], fds[u][g].p[0], dQ[dt]);
-            } else {
-                Acc<NP> S;
-                S.zero();
+                    for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int u = 0; u < SUB; ++u)
+                        for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsK + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane), fds[u][g]);
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsK + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane), fds[u][g]);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) dQ[dt][i] += S.get(i);
+                    for (int i = 0; i < 16; ++i) dQ[dt][i] += S.get(i);
+                }
             }
-        }
         }
         if (more) {
             lk.finish(ldsK + (buf ^ 1) * TileY::BYTES);
@@ -395,66 +395,70 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
             }
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
-            if (y0 + 32 * u + 32 <= wave_first) continue;      // no row of these sees a key of this wave
-            Acc<NP> S, P;
-            S.zero();
-            P.zero();
+                if (y0 + 32 * u + 32 <= wave_first) continue;      // no row of these sees a key of this wave
+                Acc<NP> S, P;
+                S.zero();
+                P.zero();
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                S.mma(TileY::rows(ldsQ + buf * TileY::BYTES, 32 * u, ks, lane), fk[ks]);
-                if constexpr (V_IN_LDS) P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), TileX::rows(ldsV, 32 * wave, ks, lane));
-                else P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), fv[ks]);
-            }
-            if constexpr (NP == 1) reads_ahead<2 * KS, 6, V_IN_LDS ? 2 : 1>();
-            float p[16], ds[16];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int y = 32 * u + 8 * j + 4 * h32;
-                const float4 l4 = *reinterpret_cast<const float4 *>(stats[buf][0] + y), d4 = *reinterpret_cast<const float4 *>(stats[buf][1] + y);
-                const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x;
-                    if constexpr (BIAS) {
-                        x = fmaf(S.get(4 * j + i), a.scale, window[buf][32 * wave + (lane & 31) - (y + i) + YT - 1]);
-                        x = __builtin_amdgcn_exp2f((x - l[i]) * kLog2e);
-                    } else x = __builtin_amdgcn_exp2f(fmaf(S.get(4 * j + i), c, -l[i]));
-                    p[4 * j + i] = x;
-                    ds[4 * j + i] = x * (P.get(4 * j + i) - d[i]);
+                for (int ks = 0; ks < KS; ++ks) {
+                    S.mma(TileY::rows(ldsQ + buf * TileY::BYTES, 32 * u, ks, lane), fk[ks]);
+                    if constexpr (V_IN_LDS) P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), TileX::rows(ldsV, 32 * wave, ks, lane));
+                    else P.mma(TileY::rows(ldsO + buf * TileY::BYTES, 32 * u, ks, lane), fv[ks]);
                 }
-            }
-            if (y0 + 32 * u < wave_all)       // some row does not see some key
+                if constexpr (NP == 1) reads_ahead<2 * KS, 6, V_IN_LDS ? 2 : 1>();
+                float p[16], ds[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (8 * (i / 4) + i % 4 < first_row - y0 - 32 * u - 4 * h32) p[i] = 0.f, ds[i] = 0.f;
-            Frag<NP> fp[2], fds[2];
+                for (int j = 0; j < 4; ++j) {
+                    const int at = 32 * u + 8 * j + 4 * h32;
+                    const float4 l4 = *reinterpret_cast<const float4 *>(stats[buf][0] + at), d4 = *reinterpret_cast<const float4 *>(stats[buf][1] + at);
+                    const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                fp[e] = cut8<NP>(&p[8 * e]);
-                fds[e] = cut8<NP>(&ds[8 * e]);
-            }
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                if constexpr (NP == 1) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        dV[dt] = mfma(TileY::cols(ldsO + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane).p[0], fp[e].p[0], dV[dt]);
-                        dK[dt] = mfma(TileY::cols(ldsQ + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane).p[0], fds[e].p[0], dK[dt]);
+                    for (int i = 0; i < 4; ++i) {
+                        float x;
+                        if constexpr (BIAS) {
+                            x = fmaf(S.get(4 * j + i), a.scale, window[buf][32 * wave + (lane & 31) - (at + i) + YT - 1]);
+                            x = __builtin_amdgcn_exp2f((x - l[i]) * kLog2e);
+                        } else x = __builtin_amdgcn_exp2f(fmaf(S.get(4 * j + i), c, -l[i]));
+                        p[4 * j + i] = x;
+                        ds[4 * j + i] = x * (P.get(4 * j + i) - d[i]);
                     }
-                } else {
-                    Acc<NP> A;
-                    A.zero();
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsO + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane), fp[e]);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) dV[dt][i] += A.get(i);
-                    A.zero();
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsQ + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane), fds[e]);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) dK[dt][i] += A.get(i);
                 }
-            }
+                const int y = y0 + 32 * u;
+                // some row does not see some key; or, with a bias, whose exponential may be an infinity, some row is none
+                if (y < wave_all || (BIAS && y + 32 > rows))
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int r = 8 * (i / 4) + i % 4;
+                        if (r < first_row - y - 4 * h32 || (BIAS && r >= rows - y - 4 * h32)) p[i] = 0.f, ds[i] = 0.f;
+                    }
+                Frag<NP> fp[2], fds[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    fp[e] = cut8<NP>(&p[8 * e]);
+                    fds[e] = cut8<NP>(&ds[8 * e]);
+                }
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    if constexpr (NP == 1) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            dV[dt] = mfma(TileY::cols(ldsO + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane).p[0], fp[e].p[0], dV[dt]);
+                            dK[dt] = mfma(TileY::cols(ldsQ + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane).p[0], fds[e].p[0], dK[dt]);
+                        }
+                    } else {
+                        Acc<NP> A;
+                        A.zero();
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsO + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane), fp[e]);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) dV[dt][i] += A.get(i);
+                        A.zero();
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) A.mma(TileY::cols(ldsQ + buf * TileY::BYTES, 32 * u + 16 * e, dt, lane), fds[e]);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) dK[dt][i] += A.get(i);
+                    }
+                }
             }
             if (more) {
                 lq.finish(ldsQ + (buf ^ 1) * TileY::BYTES);

@@ -86,96 +86,96 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
             if constexpr (BIAS) bias_next = window_load(a, h0, k0 + YT + window0);
         }
         if (k0 < wave_kend) {       // some row of the wave sees some key of the tile
-        float p[SUB][16];
-        float mt = -INFINITY;
+            float p[SUB][16];
+            float mt = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            Acc<NP> S;
-            S.zero();
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) S.mma(TileY::rows(ldsK + buf * TileY::BYTES, 32 * u, ks, lane), fq[ks]);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int y = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4;
-                p[u][i] = S.get(i);
-                if constexpr (BIAS) p[u][i] = fmaf(p[u][i], a.scale, window[buf][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
-            }
-        }
-        if constexpr (NP == 1) reads_ahead<SUB * KS, AHEAD, 1>();
-        if (k0 + YT > wave_limit)
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (32 * u + 8 * (i / 4) + i % 4 >= limit - k0 - 4 * h32) p[u][i] = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mt = fmaxf(mt, p[u][i]);
-        mt = max_halves(mt);
-        // The running maximum follows only where it has grown by a factor of 2^kSlack: p stays below that, at the same relative
-        // precision, and the sums are hardly ever scaled again.
-        const bool grows = (mt - m) * (BIAS ? kLog2e : c) > kSlack;
-        const float mn = grows ? mt : m, ms = mn == -INFINITY ? 0.f : mn;      // a row that has seen no key yet: exp2(-inf) = 0
-        const float alpha = grows ? __builtin_amdgcn_exp2f((m - ms) * (BIAS ? kLog2e : c)) : 1.f;
-        m = mn;
-        float sum = 0.f;
-#pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[u][i] = __builtin_amdgcn_exp2f(BIAS ? (p[u][i] - ms) * kLog2e : fmaf(p[u][i], c, -ms * c));
-                sum += p[u][i];
-            }
-        l = fmaf(l, alpha, sum);
-        if constexpr (NP == 1 && !EXACT) {
-            if (__any(grows))
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) O[dt] *= alpha;
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const Frag<1> fp = cut8<1>(&p[u][8 * g]);
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) O[dt] = mfma(TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane).p[0], fp.p[0], O[dt]);
-                }
-        } else if constexpr (EXACT) {       // probabilities in three pieces, the least first; a tile's sum from zero as below
-            Frag<3> fp[SUB][2];
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int g = 0; g < 2; ++g) fp[u][g] = cut8<3>(&p[u][8 * g]);
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                v16f S = v16f{};
-#pragma unroll
-                for (int k = 2; k >= 0; --k)
-#pragma unroll
-                    for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                        for (int g = 0; g < 2; ++g) S = mfma(TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane).p[0], fp[u][g].p[k], S);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) O[dt][i] = fmaf(O[dt][i], alpha, S[i]);
-            }
-        } else {       // a tile's sum from zero, then one rounding into the running one
-            Frag<NP> fp[SUB][2];
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int g = 0; g < 2; ++g) fp[u][g] = cut8<NP>(&p[u][8 * g]);
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
+            for (int u = 0; u < SUB; ++u) {
                 Acc<NP> S;
                 S.zero();
 #pragma unroll
+                for (int ks = 0; ks < KS; ++ks) S.mma(TileY::rows(ldsK + buf * TileY::BYTES, 32 * u, ks, lane), fq[ks]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int y = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4;
+                    p[u][i] = S.get(i);
+                    if constexpr (BIAS) p[u][i] = fmaf(p[u][i], a.scale, window[buf][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
+                }
+            }
+            if constexpr (NP == 1) reads_ahead<SUB * KS, AHEAD, 1>();
+            if (k0 + YT > wave_limit)
+#pragma unroll
                 for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane), fp[u][g]);
+                    for (int i = 0; i < 16; ++i)
+                        if (32 * u + 8 * (i / 4) + i % 4 >= limit - k0 - 4 * h32) p[u][i] = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) O[dt][i] = fmaf(O[dt][i], alpha, S.get(i));
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mt = fmaxf(mt, p[u][i]);
+            mt = max_halves(mt);
+            // The running maximum follows only where it has grown by a factor of 2^kSlack: p stays below that, at the same relative
+            // precision, and the sums are hardly ever scaled again.
+            const bool grows = (mt - m) * (BIAS ? kLog2e : c) > kSlack;
+            const float mn = grows ? mt : m, ms = mn == -INFINITY ? 0.f : mn;      // a row that has seen no key yet: exp2(-inf) = 0
+            const float alpha = grows ? __builtin_amdgcn_exp2f((m - ms) * (BIAS ? kLog2e : c)) : 1.f;
+            m = mn;
+            float sum = 0.f;
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    p[u][i] = __builtin_amdgcn_exp2f(BIAS ? (p[u][i] - ms) * kLog2e : fmaf(p[u][i], c, -ms * c));
+                    sum += p[u][i];
+                }
+            l = fmaf(l, alpha, sum);
+            if constexpr (NP == 1 && !EXACT) {
+                if (__any(grows))
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) O[dt] *= alpha;
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const Frag<1> fp = cut8<1>(&p[u][8 * g]);
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) O[dt] = mfma(TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane).p[0], fp.p[0], O[dt]);
+                    }
+            } else if constexpr (EXACT) {       // probabilities in three pieces, the least first; a tile's sum from zero as below
+                Frag<3> fp[SUB][2];
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) fp[u][g] = cut8<3>(&p[u][8 * g]);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    v16f S = v16f{};
+#pragma unroll
+                    for (int k = 2; k >= 0; --k)
+#pragma unroll
+                        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                            for (int g = 0; g < 2; ++g) S = mfma(TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane).p[0], fp[u][g].p[k], S);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) O[dt][i] = fmaf(O[dt][i], alpha, S[i]);
+                }
+            } else {       // a tile's sum from zero, then one rounding into the running one
+                Frag<NP> fp[SUB][2];
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) fp[u][g] = cut8<NP>(&p[u][8 * g]);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    Acc<NP> S;
+                    S.zero();
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) S.mma(TileY::cols(ldsV + buf * TileY::BYTES, 32 * u + 16 * g, dt, lane), fp[u][g]);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) O[dt][i] = fmaf(O[dt][i], alpha, S.get(i));
+                }
             }
-        }
         }
         if (more) {
             lk.finish(ldsK + (buf ^ 1) * TileY::BYTES);

@@ -329,6 +329,17 @@ def test_bias_of_far_distances(far):
     run("bf16", [900, 130], [1400, 130], 2, 1, 64, False, bias=32, far=far, both=True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_bias_whose_exponential_overflows(dtype):
+    """Softmax does not change with a constant: tables about 300 (and -300), with rows and keys behind the ends of tiles."""
+    lens = [33, 70]
+    x, vals = inputs(dtype, lens, lens, 2, 1, 32)
+    for shift in (300.0, -300.0):
+        table = torch.randn(2, 16, generator=torch.Generator().manual_seed(2)) + shift
+        a = Attention(*vals, lens, lens, 0.125, False, table.double(), 16, 50, True, DTYPES[dtype], dtype == "bf16")
+        check(call(x, 2, lengths(lens), lengths(lens), 0.125, False, table.cuda(), 50, True, dtype == "bf16"), a, DTYPES[dtype])
+
+
 def test_many_sequences():
     """More sequences than a wave looks through at once, some of them empty."""
     lens = [(7 * i) % 13 for i in range(150)]

@@ -38,7 +38,7 @@ def test_gradients_of_the_whole_sublayer():
     x64 = x.double().cpu().requires_grad_()
     ref = plain_loss(x64, target.double().cpu(), w, layer)
     ref.backward()
-    assert abs(float(loss) - float(ref)) < 1e-5 * float(ref)
+    assert abs(float(loss) - float(ref.detach())) < 1e-5 * float(ref.detach())
     for name, got in [*layer.grad.items(), ("x", dx)]:
         want = x64.grad if name == "x" else w[name].grad
         assert float((got.double().cpu() - want).abs().max()) < 1e-4 * float(want.abs().max()), name
