@@ -171,13 +171,13 @@ def _ptr(t):
 
 
 # the handle of torch.cuda.current_stream() without an object made for it, which takes 3 us a call
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) if hasattr(torch._C, "_cuda_getDevice") else None
 
 
 def _stream(s):
     if s is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(torch._C._cuda_getDevice())
         s = torch.cuda.current_stream()
     return s.cuda_stream
 
@@ -351,7 +351,8 @@ def cg_layernorm_workspace_bytes(d):
 
 
 def _norm_tensor(d, x, what):
-    if _type_of(x) != d.type or _shape_of_rows(x) != (d.rows, d.cols):
+    rows, cols = d.rows, d.cols
+    if _TYPES.get(x.dtype) != d.type or (x.shape != (rows, cols) and _shape_of_rows(x) != (rows, cols)):
         raise ValueError(f"{what}: not of the descriptor's type and shape")
 
 
@@ -391,54 +392,64 @@ def cg_dropout_add_layernorm_bwd(d, drop, dy, dsum, total, gamma, mean, rstd, dx
 
 def attn_desc(q, k, v, o, B, scale, causal=False, buckets=0, max_distance=0, both=False):
     """Descriptor of attention over B packed sequences: q, o [Tq][Hq][D], k, v [Tk][Hkv][D], of any token and head strides."""
-    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or q.shape != o.shape or q.shape[2] != k.shape[2]:
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or q.shape != o.shape:
         raise ValueError("expected q and o of one shape [tokens][heads][D], k and v of another with the same D")
-    if not (q.dtype == k.dtype == v.dtype == o.dtype):
-        raise TypeError("q, k, v and o have to be of one type")
-    if q.shape[2] > 1 and not (q.stride(2) == k.stride(2) == v.stride(2) == o.stride(2) == 1):
-        raise ValueError("the elements of a head have to lie next to each other")
     Tq, Hq, D = q.shape
-    Tk, Hkv, _ = k.shape
-    return cg_attn_desc(_type_of(q), B, Hq, Hkv, D, Tq, Tk, *q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *o.stride()[:2],
-                        scale, causal, buckets, max_distance, both)
+    Tk, Hkv, Dk = k.shape
+    (qt, qh, q1), (kt, kh, k1), (vt, vh, v1), (ot, oh, o1) = q.stride(), k.stride(), v.stride(), o.stride()
+    if D != Dk:
+        raise ValueError("expected q and o of one shape [tokens][heads][D], k and v of another with the same D")
+    dtype = q.dtype
+    if k.dtype is not dtype or v.dtype is not dtype or o.dtype is not dtype:
+        raise TypeError("q, k, v and o have to be of one type")
+    if not (q1 == k1 == v1 == o1 == 1) and D > 1:
+        raise ValueError("the elements of a head have to lie next to each other")
+    return cg_attn_desc(_type_of(q), B, Hq, Hkv, D, Tq, Tk, qt, qh, kt, kh, vt, vh, ot, oh, scale, causal, buckets, max_distance, both)
 
 
 def cg_attn_workspace_bytes(d, which):
     return int(lib().cg_attn_workspace_bytes(d, which))
 
 
-def _heads(t, d, T, H, tok, head, what):
-    """The pointer of a tensor [T][H][D] with the descriptor's type and strides."""
+_DTYPES = {code: dtype for dtype, code in _TYPES.items()}
+
+
+def _heads(dtype, shape, steps, t, what):
+    """The pointer of a tensor [T][H][D] with the descriptor's type, shape and strides."""
     if t is None:
         return None
-    if _TYPES.get(t.dtype) != d.type or not t.is_cuda:
+    if t.dtype is not dtype or not t.is_cuda:
         raise TypeError(f"{what}: expected a device tensor of the descriptor's type")
-    if t.shape != (T, H, d.D) or (t.stride() != (tok, head, 1) and t.numel() > 0 and any(
-            n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), (tok, head, 1)))):
+    if t.shape != shape or (t.stride() != steps and t.numel() > 0 and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), steps))):
         raise ValueError(f"{what}: not of the descriptor's shape and strides")
     return t.data_ptr()
 
 
 def _lengths(t, d, what):
-    if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != d.B + 1:
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype is not torch.int32 or not t.is_contiguous() or t.numel() != d.B + 1:
         raise TypeError(f"{what}: expected a contiguous device tensor of {d.B + 1} int32")
     return t.data_ptr()
 
 
 def cg_attn_fwd(d, q, k, v, cu_q, cu_k, bias, o, lse, o_rest=None, ws=None, stream=None):
-    Q, K, V, O = (d.Tq, d.Hq, d.q_tok, d.q_head), (d.Tk, d.Hkv, d.k_tok, d.k_head), (d.Tk, d.Hkv, d.v_tok, d.v_head), (d.Tq, d.Hq, d.o_tok, d.o_head)
-    _check(lib().cg_attn_fwd(d, _heads(q, d, *Q, "q"), _heads(k, d, *K, "k"), _heads(v, d, *V, "v"), _lengths(cu_q, d, "cu_q"),
-                             _lengths(cu_k, d, "cu_k"), _weights(bias, d.Hq * d.buckets, "bias"), _heads(o, d, *O, "o"),
-                             _weights(lse, d.Hq * d.Tq, "lse"), _heads(o_rest, d, *O, "o_rest"), *_ws_args(ws), _stream(stream)), "cg_attn_fwd")
+    t, of_q, of_k = _DTYPES.get(d.type), (d.Tq, d.Hq, d.D), (d.Tk, d.Hkv, d.D)
+    o_steps = (d.o_tok, d.o_head, 1)
+    _check(lib().cg_attn_fwd(d, _heads(t, of_q, (d.q_tok, d.q_head, 1), q, "q"), _heads(t, of_k, (d.k_tok, d.k_head, 1), k, "k"),
+                             _heads(t, of_k, (d.v_tok, d.v_head, 1), v, "v"), _lengths(cu_q, d, "cu_q"), _lengths(cu_k, d, "cu_k"),
+                             _weights(bias, d.Hq * d.buckets, "bias"), _heads(t, of_q, o_steps, o, "o"), _weights(lse, d.Hq * d.Tq, "lse"),
+                             _heads(t, of_q, o_steps, o_rest, "o_rest"), *_ws_args(ws), _stream(stream)), "cg_attn_fwd")
 
 
 def cg_attn_bwd(d, d_o, q, k, v, cu_q, cu_k, bias, o, o_rest, lse, dq, dk, dv, dbias, ws, stream=None):
-    Q, K, V, O = (d.Tq, d.Hq, d.q_tok, d.q_head), (d.Tk, d.Hkv, d.k_tok, d.k_head), (d.Tk, d.Hkv, d.v_tok, d.v_head), (d.Tq, d.Hq, d.o_tok, d.o_head)
-    _check(lib().cg_attn_bwd(d, _heads(d_o, d, *O, "d_o"), _heads(q, d, *Q, "q"), _heads(k, d, *K, "k"), _heads(v, d, *V, "v"),
-                             _lengths(cu_q, d, "cu_q"), _lengths(cu_k, d, "cu_k"), _weights(bias, d.Hq * d.buckets, "bias"),
-                             _heads(o, d, *O, "o"), _heads(o_rest, d, *O, "o_rest"), _weights(lse, d.Hq * d.Tq, "lse"),
-                             _heads(dq, d, *Q, "dq"), _heads(dk, d, *K, "dk"), _heads(dv, d, *V, "dv"),
-                             _weights(dbias, d.Hq * d.buckets, "dbias"), *_ws_args(ws), _stream(stream)), "cg_attn_bwd")
+    t, of_q, of_k, n = _DTYPES.get(d.type), (d.Tq, d.Hq, d.D), (d.Tk, d.Hkv, d.D), d.Hq * d.buckets
+    q_steps, k_steps, v_steps, o_steps = (d.q_tok, d.q_head, 1), (d.k_tok, d.k_head, 1), (d.v_tok, d.v_head, 1), (d.o_tok, d.o_head, 1)
+    _check(lib().cg_attn_bwd(d, _heads(t, of_q, o_steps, d_o, "d_o"), _heads(t, of_q, q_steps, q, "q"), _heads(t, of_k, k_steps, k, "k"),
+                             _heads(t, of_k, v_steps, v, "v"), _lengths(cu_q, d, "cu_q"), _lengths(cu_k, d, "cu_k"), _weights(bias, n, "bias"),
+                             _heads(t, of_q, o_steps, o, "o"), _heads(t, of_q, o_steps, o_rest, "o_rest"), _weights(lse, d.Hq * d.Tq, "lse"),
+                             _heads(t, of_q, q_steps, dq, "dq"), _heads(t, of_k, k_steps, dk, "dk"), _heads(t, of_k, v_steps, dv, "dv"),
+                             _weights(dbias, n, "dbias"), *_ws_args(ws), _stream(stream)), "cg_attn_bwd")
 
 
 def cg_debug_patch_min_tiles(tiles):
