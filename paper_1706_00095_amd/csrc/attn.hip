@@ -65,7 +65,7 @@ int check(const cg_attn_desc *d)
         if (n < 2 || (d->both && d->buckets % 2) || d->max_distance <= n / 2) return CG_EINVAL;
         if (d->buckets > kMaxBuckets || d->max_distance > kMaxDistance) return CG_EUNSUPPORTED;
     }
-    if (d->D > kAttnMaxD || d->Tq * d->Hq > INT32_MAX || d->Tk * d->Hkv > INT32_MAX || d->Tq > INT32_MAX || d->Tk > INT32_MAX) return CG_EUNSUPPORTED;
+    if (d->D > kAttnMaxD || d->Tq > INT32_MAX || d->Tk > INT32_MAX || d->Tq * d->Hq > INT32_MAX || d->Tk * d->Hkv > INT32_MAX) return CG_EUNSUPPORTED;
     if ((d->Tq * d->Hq / kAttnRows + d->B) * (int64_t)d->Hq > (1 << 30) || (d->Tk / kAttnRows + d->B) * (int64_t)d->Hkv > (1 << 30)) return CG_EUNSUPPORTED;
     return CG_OK;
 }
