@@ -44,8 +44,11 @@ __device__ __forceinline__ void add_runs(float v, int bucket, float *acc, int la
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
+// Waves a SIMD: two where registers and LDS (the squares of the bias's gradient take 36 KB) allow them.
+template <class T, int DP, bool BIAS> constexpr int kDqWaves = (Pieces<T>::N == 1 ? !BIAS || DP <= 64 : DP <= (BIAS ? 32 : 64)) ? 2 : 1;
+
 template <class T, int DP, bool BIAS, bool DMA>
-__global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void attn_dq_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(AttnArgs a)
 {
     constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
     using TileY = Tile<DP, YT, NP>;

@@ -264,19 +264,31 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dg[k][i] = db[k][i] = 0.f;
     }
-    int turn = 0;
-    for (int r0 = blockIdx.x * ROWS; r0 < a.rows; r0 += gridDim.x * ROWS, turn ^= 1) {
-        const int r = r0 + slot;
+    struct Row {
+        Raw8<T> x[CPT], d[CPT], s[CPT];
+        float mean, rstd;
+    };
+    auto load = [&](Row &v, int r) {
         const bool here = r < a.rows;
-        Raw8<T> vx[CPT], vd[CPT], vs[CPT];
 #pragma unroll
         for (int k = 0; k < CPT; ++k) {
             const int c = 8 * (k * LANES + t), n = here ? a.cols - c : 0;
-            vx[k] = load8(static_cast<const T *>(a.x) + (int64_t)r * a.x_ld + c, n);
-            vd[k] = load8(static_cast<const T *>(a.dy) + (int64_t)r * a.dy_ld + c, n);
-            if (ROOM && a.dsum) vs[k] = load8(static_cast<const T *>(a.dsum) + (int64_t)r * a.dsum_ld + c, n);
+            v.x[k] = load8(static_cast<const T *>(a.x) + (int64_t)r * a.x_ld + c, n);
+            v.d[k] = load8(static_cast<const T *>(a.dy) + (int64_t)r * a.dy_ld + c, n);
+            if (ROOM && a.dsum) v.s[k] = load8(static_cast<const T *>(a.dsum) + (int64_t)r * a.dsum_ld + c, n);
         }
-        const float mean = here ? a.mean[r] : 0.f, rstd = here ? a.rstd[r] : 0.f;
+        v.mean = here ? a.mean[r] : 0.f, v.rstd = here ? a.rstd[r] : 0.f;
+    };
+    int turn = 0;
+    Row row, next;
+    if (ROOM) load(row, blockIdx.x * ROWS + slot);
+    for (int r0 = blockIdx.x * ROWS; r0 < a.rows; r0 += gridDim.x * ROWS, turn ^= 1) {
+        const int r = r0 + slot, r1 = r + gridDim.x * ROWS;
+        const bool here = r < a.rows, more = r0 + (int)(gridDim.x * ROWS) < a.rows;
+        if (!ROOM) load(row, r);
+        else if (more) load(next, r1);       // on its way while this row is worked on
+        Raw8<T> (&vx)[CPT] = row.x, (&vd)[CPT] = row.d, (&vs)[CPT] = row.s;
+        const float mean = row.mean, rstd = row.rstd;
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < CPT; ++k) {
@@ -316,6 +328,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
                 store8(static_cast<T *>(a.dbranch) + (int64_t)r * a.dbranch_ld + c, to_raw<T>(f), n);
             }
         }
+        if (ROOM) row = next;
     }
     // the block's rows joined, then one row of sums a block
     float *const out[2] = {a.dgamma ? a.dgamma : a.part + (int64_t)blockIdx.x * 2 * a.cols,
@@ -539,17 +552,20 @@ int dropout_run(const cg_drop *drop, int type, int64_t rows, int64_t cols, const
 
 // Which kernel takes rows of `cols` columns.
 constexpr int SHORT_COLS = 512, MID_COLS = 4096, WIDE_COLS = 16384;
-// Blocks of the backward kernel: each writes a row of column sums, so no more of them than keep the memory busy.
+// Blocks of the backward kernel: each writes a row of column sums, so no more of them than the chip holds at once: two a compute unit of
+// the kernels with one chunk a thread, one of the others (8192 x 4096 joined, bf16: 69 us with 512 blocks and no row ahead, 65 so).
 // A single block takes ONE_BLOCK turns and writes the sums itself: a turn more costs 2 us at most, a second launch 7.
 constexpr int BWD_BLOCKS = 512, LONG_SLICES = 64, ONE_BLOCK = 4;
 
 int bwd_rows_at_once(int64_t cols) { return cols <= 2 * SHORT_COLS ? 8 : cols <= MID_COLS ? 2 : 1; }
+int bwd_blocks(int64_t cols) { return cols <= SHORT_COLS || (cols > 2 * SHORT_COLS && cols <= MID_COLS / 2) ? BWD_BLOCKS : BWD_BLOCKS / 2; }
 int bwd_parts(int64_t rows, int64_t cols)
 {
     if (cols > WIDE_COLS) return (int)(rows < LONG_SLICES ? rows : LONG_SLICES);
     const int64_t n = (rows + bwd_rows_at_once(cols) - 1) / bwd_rows_at_once(cols);
     if (n <= ONE_BLOCK) return n > 0;
-    return (int)(n < BWD_BLOCKS ? n : BWD_BLOCKS);
+    const int most = bwd_blocks(cols);
+    return (int)(n < most ? n : most);
 }
 
 template <class T, int JOIN> int norm_fwd_typed(const NormArgs &a, hipStream_t s)
