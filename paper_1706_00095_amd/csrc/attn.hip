@@ -241,6 +241,7 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
         a.dbias = dbias;
         a.dbias_part = reinterpret_cast<float *>(w + p.dbias);
         a.dbias_parts = any_q ? p.tiles_q * p.q.splits : 0;
+        a.dbias_splits = p.q.splits, a.dbias_chunk = p.q.chunk;
     }
     AttnArgs k_side = a;       // the dk/dv kernel's, which also adds up dbias
     if (any_q)

@@ -58,18 +58,14 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
     __shared__ __align__(16) float square[BIAS ? 4 : 1][BIAS ? 63 * kDiag : 4];
     extern __shared__ float by_wave[];          // [4][near_words(W)]
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
-    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, item = blockIdx.x / Hr, split = item % a.splits, tile = a.tiles - 1 - item / a.splits;
+    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr;
+    Place place;
+    if (!find_place<false>(a, blockIdx.x / Hr, place)) return;
+    const int t = place.t, split = place.split;
     const bool want_bias = BIAS && a.dbias_part;
     float *const mine = by_wave + wave * near_words(a.W);
-    int b, t;
-    const bool any = find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t);
-    float *const bias_out = want_bias ? a.dbias_part + (((int64_t)hr * a.tiles + tile) * a.splits + split) * a.buckets : nullptr;
-    auto no_bias = [&] {
-        if (want_bias)
-            for (int i = threadIdx.x; i < a.buckets; i += 256) bias_out[i] = 0.f;
-    };
-    if (!any) return no_bias();
-    const Seq s = seq_of(a, b);
+    float *const bias_out = want_bias ? a.dbias_part + ((int64_t)hr * a.dbias_parts + place.slot) * a.buckets : nullptr;
+    const Seq s = seq_of(a, place.b);
     const int row0 = t * kAttnRows, rows = s.n * a.Gp, off = s.m - s.n;
     const int h0 = hr * a.Gp, hkv = h0 / a.G;
     const int row = row0 + 32 * wave + (lane & 31);
@@ -81,7 +77,11 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
     const int wave_kend = row0 + 32 * wave >= rows ? 0 : keys_seen(a, s, row0 + 32 * wave + 32, rows);
     int kend = keys_seen(a, s, row0 + kAttnRows, rows), kbeg = 0;
     const int chunks = chunks_of(a, 0, kend);
-    if (split >= chunks) return no_bias();
+    if (split >= chunks) {
+        if (want_bias)
+            for (int i = threadIdx.x; i < a.buckets; i += 256) bias_out[i] = 0.f;
+        return;
+    }
     if (chunks > 1) {
         kbeg = split * a.chunk;
         kend = min(kend, kbeg + a.chunk);
@@ -264,19 +264,23 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
     }
     if (!here) return;
     if (chunks > 1)
-        store_row(a.part[0] + ((((int64_t)hr * a.tiles + tile) * a.splits + split) * kAttnRows + (row - row0)) * DP, dQ, a.scale, DP, h32);
+        store_row(a.part[0] + (((int64_t)hr * a.tiles * a.splits + place.slot) * kAttnRows + (row - row0)) * DP, dQ, a.scale, DP, h32);
     else store_row(static_cast<T *>(a.dq) + (int64_t)(s.q0 + tok) * a.q_tok + (int64_t)head * a.q_head, dQ, a.scale, a.D, h32);
 }
 
-// dbias[h][bucket]: the dq kernel's blocks' sums added in a fixed order, in 64 bits.  A block takes a head and 16 buckets, 16 threads a
+// dbias[h][bucket]: the dq kernel's items' sums added in a fixed order, in 64 bits.  A block takes a head and 16 buckets, 16 threads a
 // bucket.  It rides in the dk/dv launch, behind the blocks of that.
-__device__ __forceinline__ void sum_dbias(const AttnArgs &a, int item, double *lds)
+__device__ __forceinline__ void sum_dbias(AttnArgs a, int item, double *lds)
 {
+    a.splits = a.dbias_splits, a.chunk = a.dbias_chunk, a.gsplit = 1;
+    Place p;
+    find_place<false>(a, 0x7fffffff, p);
+    const int parts = min(p.slot, a.dbias_parts);       // the dq kernel's items
     const int groups = (a.buckets + 15) / 16, h = item / groups, x = threadIdx.x % 16, j = threadIdx.x / 16, i = item % groups * 16 + x;
     double s = 0;
     if (i < a.buckets)
 #pragma unroll 4
-        for (int t = j; t < a.dbias_parts; t += 16) s += a.dbias_part[((int64_t)h * a.dbias_parts + t) * a.buckets + i];
+        for (int t = j; t < parts; t += 16) s += a.dbias_part[((int64_t)h * a.dbias_parts + t) * a.buckets + i];
     lds[j * 17 + x] = s;
     __syncthreads();
     if (j == 0 && i < a.buckets) {
@@ -312,11 +316,11 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
             return;
         }
     }
-    const int hkv = blockIdx.x % a.Hkv, item = blockIdx.x / a.Hkv, slots = a.splits * a.gsplit, slot = item % slots, tile = item / slots;
-    const int split = slot / a.gsplit;
-    int b, t;
-    if (!find_tile(a.cu_k, a.Tk, a.B, kAttnRows, 1, tile, b, t)) return;
-    const Seq s = seq_of(a, b);
+    const int hkv = blockIdx.x % a.Hkv;
+    Place place;
+    if (!find_place<true>(a, blockIdx.x / a.Hkv, place)) return;
+    const int t = place.t, split = place.split / a.gsplit;
+    const Seq s = seq_of(a, place.b);
     const int key0 = t * kAttnRows, rows = s.n * a.Gp, off = s.m - s.n;
     const int key = key0 + 32 * wave + (lane & 31);
     // Row r of token r / Gp sees the key from first_seeing on.  Keys behind the last one need no mask: what is added up for them is
@@ -347,7 +351,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dK[dt] = v16f{}, dV[dt] = v16f{};
     const float c = a.scale * kLog2e;
-    const int heads = a.G / a.Gp, one_head = slot % a.gsplit;
+    const int heads = a.G / a.Gp, one_head = place.split % a.gsplit;
     for (int g = a.gsplit > 1 ? one_head : 0; g < (a.gsplit > 1 ? one_head + 1 : heads); ++g) {
         const int h0 = hkv * a.G + g * a.Gp;
         const Rows<T> Q{static_cast<const T *>(a.q) + (int64_t)s.q0 * a.q_tok + (int64_t)h0 * a.q_head, a.q_tok, a.q_head, rows, a.D, a.by_gp};
@@ -472,7 +476,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
     }
     if (key >= s.m) return;
     if (chunks * a.gsplit > 1) {
-        const int64_t at = ((((int64_t)hkv * a.tiles + tile) * slots + slot) * kAttnRows + (key - key0)) * DP;
+        const int64_t at = (((int64_t)hkv * a.tiles * a.splits * a.gsplit + place.slot) * kAttnRows + (key - key0)) * DP;
         store_row(a.part[0] + at, dK, a.scale, DP, h32);
         store_row(a.part[1] + at, dV, 1.f, DP, h32);
     } else {

@@ -34,15 +34,15 @@ struct AttnArgs {
     const float *btab;
     const uint8_t *bid;
     int W, buckets;
-    float *dbias_part, *dbias;             // [Hq][dbias_parts][buckets] of the dq kernel's blocks, tiles x splits; [Hq][buckets]
-    int dbias_parts;
+    float *dbias_part, *dbias;             // [Hq][dbias_parts][buckets] of the dq kernel's items; [Hq][buckets]
+    int dbias_parts, dbias_splits, dbias_chunk;      // items a head there is room for; how the dq kernel's axis is cut
     int tiles;                             // of X rows over all sequences, an upper bound
     // Y cut into at most `splits` chunks of `chunk` rows, a block each; a tile with several leaves partial results for attn_join_kernel
     int splits, chunk;
     int gsplit;                            // dk/dv kernel with a bias: chunks are of one head each (G), or of all (1)
     int yt;                                // rows of a Y tile in the dk/dv kernel (attn_dkdv_yt)
     int dma;                               // K and V (forward, dq), Q and dO (dk/dv) may travel without registers
-    float *part[2], *part_ml;              // [problem][tiles][splits gsplit][128][DP] (forward: o; dq; dk, dv), [..][2][128]
+    float *part[2], *part_ml;              // [problem][tiles splits gsplit][128][DP] by item (forward: o; dq; dk, dv), [..][2][128]
 };
 
 constexpr int kAttnRows = 128;             // X rows of a block: four waves of 32
@@ -199,30 +199,54 @@ __device__ __forceinline__ void bounds_of(const int32_t *cu, int T, int b, int &
     first = min(max(cu[b], 0), T);
     len = min(max(cu[b + 1], first), T) - first;
 }
-// The sequence that tile `tile` (of `rows` rows, `per` rows a token of cu) belongs to, and its number there.  64 sequences at a
-// time, one a lane.  false: there are fewer tiles.
-__device__ __forceinline__ bool find_tile(const int32_t *cu, int T, int B, int rows, int per, int tile, int &b, int &t)
+// Work items of a kernel: the X tiles of all sequences, each as often as its sequence has chunks of Y.  X_KEYS: X are keys and Y the
+// query rows, else the other way round.
+struct Place { int b, t, split, slot; };        // sequence, its tile, chunk, number of the item
+// Only the items that are there have numbers, so that the blocks for which a launch has room beside them end at once and last (32
+// sequences of 4096 keys, 4 queries each: 10 240 blocks for 128 items, 82 us; with a number for each tile and possible chunk, 199).  A
+// sequence's last row tiles come first: they see most keys under a causal mask.
+// Item number `index`, or (BY_TILE) the first item of tile number `index` of all sequences.  64 sequences at a time, one a lane.  false:
+// there are fewer.
+template <bool X_KEYS, bool BY_TILE = false> __device__ __forceinline__ bool find_place(const AttnArgs &a, int index, Place &p)
 {
     const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < B; b0 += 64) {
-        int first = 0, len = 0;
-        if (b0 + lane < B) bounds_of(cu, T, b0 + lane, first, len);
-        const int mine = (len * per + rows - 1) / rows;
-        int upto = mine;
+    int items_before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        int first = 0, len = 0, other = 0;
+        if (b0 + lane < a.B) {
+            if (X_KEYS) bounds_of(a.cu_k, a.Tk, b0 + lane, first, len);
+            else bounds_of(a.cu_q, a.Tq, b0 + lane, first, len);
+            if (a.splits > 1) {
+                if (X_KEYS) bounds_of(a.cu_q, a.Tq, b0 + lane, first, other);
+                else bounds_of(a.cu_k, a.Tk, b0 + lane, first, other);
+            }
+        }
+        const int tiles = ((X_KEYS ? len : len * a.Gp) + kAttnRows - 1) / kAttnRows;
+        const int chunks = (a.splits > 1 ? max(1, ((X_KEYS ? other * a.Gp : other) + a.chunk - 1) / a.chunk) : 1) * a.gsplit;
+        const int items = tiles * chunks, mine = BY_TILE ? tiles : items;
+        int upto = mine, items_upto = items;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int u = __shfl_up(upto, d);
-            if (lane >= d) upto += u;
+            const int u = __shfl_up(upto, d), w = BY_TILE ? __shfl_up(items_upto, d) : 0;
+            if (lane >= d) upto += u, items_upto += w;
         }
-        const uint64_t beyond = __ballot(upto > tile);
+        if (!BY_TILE) items_upto = upto;
+        const uint64_t beyond = __ballot(upto > index);
         if (beyond) {
             const int at = __builtin_ctzll(beyond);
-            b = b0 + at;
-            t = __builtin_amdgcn_readfirstlane(tile - (__shfl(upto, at) - __shfl(mine, at)));
-            return true;
+            const int within = __builtin_amdgcn_readfirstlane(index - __shfl(upto - mine, at)), n = __builtin_amdgcn_readfirstlane(__shfl(chunks, at));
+            p.b = b0 + at;
+            p.t = BY_TILE ? within : within / n;
+            p.split = BY_TILE ? 0 : within - p.t * n;
+            p.slot = items_before + __builtin_amdgcn_readfirstlane(__shfl(items_upto - items, at)) + p.t * n + p.split;
+            if (!X_KEYS) p.t = __builtin_amdgcn_readfirstlane(__shfl(tiles, at)) - 1 - p.t;
+            // sequences that overlap, against the rules, may have more items than there is room for
+            return !BY_TILE || p.slot + n <= a.tiles * a.splits * a.gsplit;
         }
-        tile -= __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+        index -= __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+        items_before += __builtin_amdgcn_readfirstlane(__shfl(items_upto, 63));
     }
+    p.slot = items_before;       // how many there are
     return false;
 }
 __device__ __forceinline__ Seq seq_of(const AttnArgs &a, int b)

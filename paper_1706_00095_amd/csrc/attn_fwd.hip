@@ -20,12 +20,11 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
     LdsByte *const ldsK = (LdsByte *)lds[0][0], *const ldsV = (LdsByte *)lds[1][0];
     __shared__ float window[2][BIAS ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
-    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr, item = blockIdx.x / Hr, split = item % a.splits;
-    // the last tiles of a sequence see most keys under a causal mask: they start first
-    const int tile = a.tiles - 1 - item / a.splits;
-    int b, t;
-    if (!find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t)) return;
-    const Seq s = seq_of(a, b);
+    const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr;
+    Place place;
+    if (!find_place<false>(a, blockIdx.x / Hr, place)) return;
+    const int t = place.t, split = place.split;
+    const Seq s = seq_of(a, place.b);
     const int row0 = t * kAttnRows, rows = s.n * a.Gp, off = s.m - s.n;
     const int h0 = hr * a.Gp, hkv = h0 / a.G;
     // what this lane's row sees: keys below `limit`
@@ -186,7 +185,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
     l = sum_halves(l);
     if (chunks > 1) {
         if (!here) return;
-        const int64_t at = ((int64_t)hr * a.tiles + tile) * a.splits + split;
+        const int64_t at = (int64_t)hr * a.tiles * a.splits + place.slot;
         float *ml = a.part_ml + at * 2 * kAttnRows;
         if (h32 == 0) {
             ml[row - row0] = BIAS ? m : m * a.scale;

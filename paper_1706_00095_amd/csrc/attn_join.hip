@@ -20,9 +20,11 @@ template <class T, int DP, int WHAT, bool ROWS> __device__ __forceinline__ void 
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int problems = WHAT == ATTN_JOIN_DKDV ? a.Hkv : a.Hq / a.Gp, pr = block % problems, item = block / problems;
     const int tile = item / (kAttnRows / J::PER_BLOCK), part = item % (kAttnRows / J::PER_BLOCK);
-    int b, t;
-    if (WHAT == ATTN_JOIN_DKDV ? !find_tile(a.cu_k, a.Tk, a.B, kAttnRows, 1, tile, b, t) : !find_tile(a.cu_q, a.Tq, a.B, kAttnRows, a.Gp, tile, b, t)) return;
-    const Seq s = seq_of(a, b);
+    constexpr bool X_KEYS = WHAT == ATTN_JOIN_DKDV;
+    Place place;
+    if (!find_place<X_KEYS, true>(a, tile, place)) return;
+    const Seq s = seq_of(a, place.b);
+    const int t = place.t;
     const int row0 = t * kAttnRows, yt = a.yt;
     int n, rows;
     if constexpr (WHAT == ATTN_JOIN_DKDV) {
@@ -33,7 +35,7 @@ template <class T, int DP, int WHAT, bool ROWS> __device__ __forceinline__ void 
         n = chunks_of(a, 0, keys_seen(a, s, row0 + kAttnRows, rows));
     }
     if (n == 1) return;
-    const int64_t at = ((int64_t)pr * a.tiles + tile) * a.splits * a.gsplit;
+    const int64_t at = (int64_t)pr * a.tiles * a.splits * a.gsplit + place.slot;
     const int group = lane / L, d = 4 * (lane % L);
     {
         const int row = row0 + part * J::PER_BLOCK + (ROWS ? wave * GROUPS + min(group, GROUPS - 1) : wave);

@@ -345,3 +345,23 @@ def test_many_sequences():
     lens = [(7 * i) % 13 for i in range(150)]
     run("bf16", lens, lens, 2, 1, 32, True)
     run("fp32", lens, [n + 3 for n in lens], 1, 1, 32, False, bias=8, far=9)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("bias", [0, 16])
+def test_long_axes_of_many_unequal_sequences(dtype, causal, bias):
+    """Sequences cut into different numbers of chunks, one or more tiles each, more of them than a wave looks through at once."""
+    lens_q, lens_k = [1, 0, 300, 2, 140], [700, 64, 1500, 0, 129]
+    run(dtype, lens_q, lens_k, 2, 1, 40, causal, bias=bias, far=64)
+    many = [(i % 3) for i in range(70)] + [260]
+    run(dtype, many, [n + 5 * (i % 2) for i, n in enumerate(many[:-1])] + [2000], 2, 1, 32, causal, bias=bias, far=64)
+
+
+def test_overlapping_lengths_of_cut_axes():
+    """More items than there is room for: the call returns, and writes nothing outside."""
+    x, _ = inputs("bf16", [300], [3000], 2, 1, 64)
+    cu_q, cu_k = (torch.tensor([0, n] * 40 + [0], device="cuda").int() for n in (300, 3000))
+    table = torch.zeros(2, 8, device="cuda")
+    for bias in (None, table):
+        call(x, 80, cu_q, cu_k, 0.125, False, bias, 9 if bias is not None else 0, True, True)
