@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
 // bucket.  It rides in the dk/dv launch, behind the blocks of that.
 __device__ __forceinline__ void sum_dbias(AttnArgs a, int item, double *lds)
 {
-    a.splits = a.dbias_splits, a.chunk = a.dbias_chunk, a.gsplit = 1;
+    a.splits = a.dbias_splits, a.chunk = a.dbias_chunk, a.gsplit = 1, a.fold = a.levels = 0;
     Place p;
     find_place<false>(a, 0x7fffffff, p);
     const int parts = min(p.slot, a.dbias_parts);       // the dq kernel's items
@@ -292,8 +292,10 @@ __device__ __forceinline__ void sum_dbias(AttnArgs a, int item, double *lds)
 
 // X: 128 keys of a key-value head; Y: the query rows that see them, of all Gp heads.  With a bias Gp = 1, and the G heads
 // are walked one after the other.
+template <class T, int DP> constexpr int kDkdvWaves = Pieces<T>::N == 1 || DP <= 32 ? 2 : 1;
+
 template <class T, int DP, bool BIAS, bool DMA>
-__global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void attn_dkdv_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, (kDkdvWaves<T, DP>)) void attn_dkdv_kernel(AttnArgs a)
 {
     constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = attn_dkdv_yt(NP == 1, DP), SUB = YT / 32;
     using TileY = Tile<DP, YT, NP>;
@@ -333,6 +335,7 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
         begin += split * a.chunk;
         end = min(end, begin + a.chunk);
     }
+    const int last = begin < end ? begin + (end - 1 - begin) / YT * YT : begin - YT;
 
     const FastDiv one = {1, 1, 0};
     const Rows<T> K{static_cast<const T *>(a.k) + (int64_t)s.k0 * a.k_tok + (int64_t)hkv * a.k_head, a.k_tok, 0, s.m, a.D, one};
@@ -385,20 +388,21 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
         int buf = 0;
         __syncthreads();      // the head before this one may still be read
         if (begin < end) {
-            lq.start(begin, ldsQ);
-            lo.start(begin, ldsO);
-            row_start(begin, 0);
+            lq.start(last, ldsQ);
+            lo.start(last, ldsO);
+            row_start(last, 0);
             lq.finish(ldsQ);
             lo.finish(ldsO);
             row_finish(0);
         }
-        for (int y0 = begin; y0 < end; y0 += YT, buf ^= 1) {
+        // backwards: all blocks of a sequence then ask for the same rows at about the same time
+        for (int y0 = last; y0 >= begin; y0 -= YT, buf ^= 1) {
             tile_sync();
-            const bool more = y0 + YT < end;
+            const bool more = y0 > begin;
             if (more) {
-                lq.start(y0 + YT, ldsQ + (buf ^ 1) * TileY::BYTES);
-                lo.start(y0 + YT, ldsO + (buf ^ 1) * TileY::BYTES);
-                row_start(y0 + YT, buf ^ 1);
+                lq.start(y0 - YT, ldsQ + (buf ^ 1) * TileY::BYTES);
+                lo.start(y0 - YT, ldsO + (buf ^ 1) * TileY::BYTES);
+                row_start(y0 - YT, buf ^ 1);
             }
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
@@ -485,8 +489,11 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 32 ? 2 : 1) void at
     }
 }
 
-template <class T, int DP, bool DMA> int dq_run(const AttnArgs &a, hipStream_t s)
+template <class T, int DP, bool DMA> int dq_run(AttnArgs a, hipStream_t s)
 {
+    const int problems = a.Hq / a.Gp, waves = a.btab ? kDqWaves<T, DP, true> : kDqWaves<T, DP, false>;
+    a.levels = levels_of(a, problems, waves == 2 && (a.btab || !DMA));
+    a.fold = fold_of(a, problems, waves);
     const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
     if (a.btab) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true, DMA>), grid, dim3(256), a.dbias_part ? 16 * near_words(a.W) : 0, s, a);
     else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
@@ -498,8 +505,10 @@ template <class T, int DP> int dq_dp(const AttnArgs &a, hipStream_t s)
     if (a.dma) return dq_run<T, DP, true>(a, s);
     return dq_run<T, DP, false>(a, s);
 }
-template <class T, int DP, bool DMA> int dkdv_run(const AttnArgs &a, hipStream_t s)
+template <class T, int DP, bool DMA> int dkdv_run(AttnArgs a, hipStream_t s)
 {
+    a.levels = levels_of(a, a.Hkv, kDkdvWaves<T, DP> == 2 && (a.btab || !DMA));
+    a.fold = fold_of(a, a.Hkv, kDkdvWaves<T, DP>);
     const dim3 grid((unsigned)a.Hkv * a.tiles * a.splits * a.gsplit + (a.dbias ? (unsigned)a.Hq * ((a.buckets + 15) / 16) : 0u));
     if (a.btab) hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, true, DMA>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_dkdv_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);

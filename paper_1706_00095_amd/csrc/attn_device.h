@@ -39,6 +39,8 @@ struct AttnArgs {
     int tiles;                             // of X rows over all sequences, an upper bound
     // Y cut into at most `splits` chunks of `chunk` rows, a block each; a tile with several leaves partial results for attn_join_kernel
     int splits, chunk;
+    int fold;                              // not 0: from which item of a problem on their order is turned round
+    int levels;                            // not 0: items by the length of what they see
     int gsplit;                            // dk/dv kernel with a bias: chunks are of one head each (G), or of all (1)
     int yt;                                // rows of a Y tile in the dk/dv kernel (attn_dkdv_yt)
     int dma;                               // K and V (forward, dq), Q and dO (dk/dv) may travel without registers
@@ -201,14 +203,63 @@ __device__ __forceinline__ void bounds_of(const int32_t *cu, int T, int b, int &
 }
 // Work items of a kernel: the X tiles of all sequences, each as often as its sequence has chunks of Y.  X_KEYS: X are keys and Y the
 // query rows, else the other way round.
+constexpr int kLevels = 4, kUnits = 256, kFoldMost = 640;      // compute units
 struct Place { int b, t, split, slot; };        // sequence, its tile, chunk, number of the item
 // Only the items that are there have numbers, so that the blocks for which a launch has room beside them end at once and last (32
 // sequences of 4096 keys, 4 queries each: 10 240 blocks for 128 items, 82 us; with a number for each tile and possible chunk, 199).  A
 // sequence's last row tiles come first: they see most keys under a causal mask.
+// Under a causal mask a launch of several rounds would end with the last sequence's longest tiles: its items then come by the length of
+// what they see, in kLevels steps of the longest, and by sequence within a step.
+__device__ __forceinline__ int wave_sum_upto(int v, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int u = __shfl_up(v, d);
+        if (lane >= d) v += u;
+    }
+    return v;
+}
+template <bool X_KEYS> __device__ __forceinline__ bool find_level(const AttnArgs &a, int index, Place &p)
+{
+    const int lane = threadIdx.x & 63;
+    int first, n = 0, m = 0;
+    if (lane < a.B) {
+        bounds_of(a.cu_q, a.Tq, lane, first, n);
+        bounds_of(a.cu_k, a.Tk, lane, first, m);
+    }
+    const int tiles = ((X_KEYS ? m : n * a.Gp) + kAttnRows - 1) / kAttnRows;
+    int top = X_KEYS ? n : m;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) top = max(top, __shfl_xor(top, d));
+    p.slot = index, p.split = 0;
+    int above = tiles;          // tiles of the sequence that are left: those that see no more than the step's upper end
+#pragma unroll 1
+    for (int l = kLevels - 1; l >= 0; --l) {
+        const int x = (int)((int64_t)top * l / kLevels);
+        int below = 0;          // that see no more than x
+        if (l > 0) {
+            if (X_KEYS) below = x >= n ? tiles : tiles - min(max((m - x + kAttnRows - 1) / kAttnRows, 0), tiles);
+            else below = min(min(max(x - (m - n), 0), n) * a.Gp / kAttnRows, tiles);
+        }
+        below = min(below, above);
+        const int mine = above - below, upto = wave_sum_upto(mine, lane);
+        const uint64_t beyond = __ballot(upto > index);
+        if (beyond) {
+            const int at = __builtin_ctzll(beyond), within = index - __shfl(upto - mine, at);
+            p.b = at;
+            p.t = __builtin_amdgcn_readfirstlane(X_KEYS ? __shfl(tiles - above, at) + within : __shfl(above, at) - 1 - within);
+            return true;
+        }
+        index -= __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+        above = below;
+    }
+    return false;
+}
 // Item number `index`, or (BY_TILE) the first item of tile number `index` of all sequences.  64 sequences at a time, one a lane.  false:
 // there are fewer.
 template <bool X_KEYS, bool BY_TILE = false> __device__ __forceinline__ bool find_place(const AttnArgs &a, int index, Place &p)
 {
+    if (!BY_TILE && a.levels) return find_level<X_KEYS>(a, index, p);
     const int lane = threadIdx.x & 63;
     int items_before = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
@@ -231,6 +282,11 @@ template <bool X_KEYS, bool BY_TILE = false> __device__ __forceinline__ bool fin
             if (lane >= d) upto += u, items_upto += w;
         }
         if (!BY_TILE) items_upto = upto;
+        if (!BY_TILE && a.fold && index >= a.fold) {
+            const int all = __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+            if (index >= all) return false;
+            index = all - 1 - (index - a.fold);
+        }
         const uint64_t beyond = __ballot(upto > index);
         if (beyond) {
             const int at = __builtin_ctzll(beyond);
@@ -538,6 +594,23 @@ __device__ __forceinline__ int first_seeing(const AttnArgs &a, const Seq &s, int
 __device__ __forceinline__ float window_load(const AttnArgs &a, int h, int first)
 {
     return a.btab[(int64_t)h * (2 * a.W + 1) + a.W + min(max(first + (int)threadIdx.x, -a.W), a.W)];
+}
+
+// Where the items come by length (`gains`).  What the rounds' end saves, the sequences lose that no longer follow one another in L2:
+// with two waves a SIMD it pays for kernels with a bias (4 x 2048, 16 heads of 64, both causal: forward 130 -> 109 us, dk/dv 124 -> 109) and
+// for those without loads into LDS (the same of 100: forward 305 -> 250), and for the forward kernel of narrow heads (4 x 4096, 16 of 64: 211
+// -> 193); the others, which the chip's power holds back, lose up to 4 %.
+inline int levels_of(const AttnArgs &a, int problems, bool gains)
+{
+    return gains && a.causal && a.splits == 1 && a.gsplit == 1 && a.B > 1 && a.B <= 64 && (int64_t)problems * a.tiles > kFoldMost;
+}
+// Where the order of a launch's items is turned round: if all blocks are resident at once, two a compute unit (block i and block i + 256,
+// as measured), the second ones would else meet first ones with as much work, a causal mask's long tiles twice in one place: dk/dv of
+// 4 x 2048, 32 heads on 8, 128 wide, 502 -> 446 us.
+inline int fold_of(const AttnArgs &a, int problems, int waves)
+{
+    const int64_t blocks = (int64_t)problems * a.tiles * a.gsplit;
+    return waves == 2 && a.splits == 1 && a.B <= 64 && blocks > kUnits && blocks <= kFoldMost ? (kUnits + problems - 1) / problems : 0;
 }
 
 }  // namespace

@@ -11,8 +11,10 @@ constexpr float kSlack = 8.f;
 // delta, a sum of o times do, from dP; where the differences are added up (the bias's gradient) or rows see a few keys only (sequences
 // of kFewKeys on average), dP is as near to delta as a rounded o is to o.
 constexpr int kFewKeys = 64;
+template <class T, int DP> constexpr int kFwdWaves = Pieces<T>::N == 1 || DP <= 64 ? 2 : 1;
+
 template <class T, int DP, bool BIAS, bool DMA, bool EXACT>
-__global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void attn_fwd_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, (kFwdWaves<T, DP>)) void attn_fwd_kernel(AttnArgs a)
 {
     constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 && !(EXACT && DP > 64) ? 64 : 32, SUB = YT / 32, AHEAD = 6;
     using TileY = Tile<DP, YT, NP>;
@@ -211,8 +213,10 @@ __global__ __launch_bounds__(256, Pieces<T>::N == 1 || DP <= 64 ? 2 : 1) void at
                 }
 }
 
-template <class T, int DP, bool DMA> int fwd_run(const AttnArgs &a, hipStream_t s)
+template <class T, int DP, bool DMA> int fwd_run(AttnArgs a, hipStream_t s)
 {
+    a.levels = levels_of(a, a.Hq / a.Gp, kFwdWaves<T, DP> == 2 && (a.btab || !DMA || DP <= 64));
+    a.fold = fold_of(a, a.Hq / a.Gp, kFwdWaves<T, DP>);
     const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
     constexpr bool can = sizeof(T) == 2;
     const bool exact = can && a.o_rest && (a.btab || a.Tk <= (int64_t)kFewKeys * a.B);

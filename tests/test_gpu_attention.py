@@ -365,3 +365,12 @@ def test_overlapping_lengths_of_cut_axes():
     table = torch.zeros(2, 8, device="cuda")
     for bias in (None, table):
         call(x, 80, cu_q, cu_k, 0.125, False, bias, 9 if bias is not None else 0, True, True)
+
+
+@pytest.mark.parametrize("dtype,D,bias", [("bf16", 33, 0), ("bf16", 64, 0), ("bf16", 64, 8), ("fp32", 32, 0), ("fp32", 32, 8)])
+@pytest.mark.parametrize("lens_k", [None, 40, -40])
+def test_many_tiles_under_a_causal_mask(dtype, D, bias, lens_k):
+    """More blocks than the chip holds at once, with sequences of unlike lengths, and as many as it holds."""
+    lens = [400, 1, 0, 130, 257, 700, 65]
+    for H in (48, 16):
+        run(dtype, lens, [max(n + (lens_k or 0), 0) for n in lens], H, H, D, True, bias=bias, far=30)
