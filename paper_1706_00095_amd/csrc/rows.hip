@@ -114,21 +114,23 @@ template <class T, bool DENSE, bool ADD> __global__ __launch_bounds__(256) void 
 }
 
 // ---- layer norm ---------------------------------------------------------------------------------------------------------
-// WPR waves share a row, a lane holds CPT chunks of eight columns: chunk k of lane t (of 64 WPR) covers the columns
-// 8 (k 64 WPR + t) ..  WPR = 1 needs no barrier (four or eight rows a block); wider rows join the waves' sums through LDS.
+// LANES lanes share a row, each holds CPT chunks of eight columns: chunk k of lane t covers the columns 8 (k LANES + t) ..  A quarter of a
+// wave (up to 128 columns), half of one and one need no barrier; wider rows join the waves' sums through LDS.  65536 x 256 bf16, half a
+// wave a row: forward 13 us (5.2 TB/s), backward 20 (5.1); with a whole one, half of whose lanes have nothing, 20 and 33.
 
-__device__ __forceinline__ float wave_sum(float x)
+template <int LANES = 64> __device__ __forceinline__ float wave_sum(float x)
 {
 #pragma unroll
-    for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
+    for (int m = (LANES < 64 ? LANES : 64) / 2; m; m >>= 1) x += __shfl_xor(x, m);
     return x;
 }
-// Sums of N numbers over the WPR waves of a row; every lane gets them.  `lds`: N * WPR floats of this row's, free for
+// Sums of N numbers over the LANES lanes of a row; every lane gets them.  `lds`: N floats for each of the row's waves, free for
 // use (the barrier behind the reads is the next call's or the caller's).
-template <int WPR, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float *lds)
+template <int LANES, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float *lds)
 {
+    constexpr int WPR = LANES / 64;
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = wave_sum<LANES>(v[i]);
     if constexpr (WPR > 1) {
         const int wave = (threadIdx.x >> 6) % WPR;
         if ((threadIdx.x & 63) == 0)
@@ -166,11 +168,11 @@ struct NormBwdArgs {
 };
 
 // JOIN: 0 = layer norm alone, 1 = joined, rows on the generator's blocks (cols a multiple of 8), 2 = joined, any cols
-template <class T, int WPR, int CPT, int JOIN, int BLOCK>
+template <class T, int LANES, int CPT, int JOIN, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a)
 {
-    constexpr int ROWS = BLOCK / (64 * WPR), LANES = 64 * WPR;
-    __shared__ float lds[ROWS][2][WPR];
+    constexpr int ROWS = BLOCK / LANES, WAVES = LANES < 64 ? 1 : LANES / 64;
+    __shared__ float lds[ROWS][2][WAVES];
     const int slot = threadIdx.x / LANES, t = threadIdx.x % LANES;
     const float inv = 1.f / (float)a.cols;
     float gam[CPT][8], bet[CPT][8];
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a)
                 s[0] += f[k][i];
             }
         }
-        row_sums<WPR, 1>(s, lds[slot][0]);
+        row_sums<LANES, 1>(s, lds[slot][0]);
         const float mean = s[0] * inv;
         float q[1] = {0.f};
 #pragma unroll
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a)
                 q[0] = fmaf(f[k][i], f[k][i], q[0]);
             }
         }
-        row_sums<WPR, 1>(q, lds[slot][1]);
+        row_sums<LANES, 1>(q, lds[slot][1]);
         const float rstd = 1.f / sqrtf(fmaf(q[0], inv, a.eps));
         if (here && t == 0 && a.mean) {
             a.mean[r] = mean;
@@ -241,11 +243,11 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a)
 // dx of a row needs two sums over it, <g> and <g xh> with g = dy gamma; dgamma and dbeta are sums over the rows, which each
 // thread keeps for its columns over all the rows that its block takes.  Blocks write their sums to `part`; sum_parts_kernel adds
 // them in order, so results do not depend on scheduling.
-template <class T, int WPR, int CPT, int JOIN, int BLOCK>
+template <class T, int LANES, int CPT, int JOIN, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
 {
-    constexpr int ROWS = BLOCK / (64 * WPR), LANES = 64 * WPR;
-    __shared__ float lds[2][ROWS][2][WPR];
+    constexpr int ROWS = BLOCK / LANES, WAVES = LANES < 64 ? 1 : LANES / 64;
+    __shared__ float lds[2][ROWS][2][WAVES];
     __shared__ float join[ROWS > 1 ? ROWS - 1 : 1][ROWS > 1 ? LANES * 8 : 1];
     const int slot = threadIdx.x / LANES, t = threadIdx.x % LANES;
     const float inv = 1.f / (float)a.cols;
@@ -303,7 +305,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
                 db[k][i] += dy;
             }
         }
-        row_sums<WPR, 2>(s, lds[turn][slot][0]);
+        row_sums<LANES, 2>(s, lds[turn][slot][0]);
         const float c1 = s[0] * inv, c2 = s[1] * inv;
 #pragma unroll
         for (int k = 0; k < CPT; ++k) {
@@ -379,7 +381,7 @@ template <class T, int JOIN> __global__ __launch_bounds__(LONG_BLOCK) void norm_
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[0] += elem(v, i);
         }
-        row_sums<W, 1>(s, lds[0]);
+        row_sums<LONG_BLOCK, 1>(s, lds[0]);
         const float mean = s[0] * inv;
         if constexpr (JOIN != 0) x = sum;
         for (int c = 8 * threadIdx.x; c < a.cols; c += 8 * LONG_BLOCK) {
@@ -390,7 +392,7 @@ template <class T, int JOIN> __global__ __launch_bounds__(LONG_BLOCK) void norm_
                 q[0] = fmaf(d, d, q[0]);
             }
         }
-        row_sums<W, 1>(q, lds[1]);
+        row_sums<LONG_BLOCK, 1>(q, lds[1]);
         const float rstd = 1.f / sqrtf(fmaf(q[0], inv, a.eps));
         if (threadIdx.x == 0 && a.mean) {
             a.mean[r] = mean;
@@ -426,7 +428,7 @@ template <class T, int JOIN> __global__ __launch_bounds__(LONG_BLOCK) void norm_
                 s[1] = fmaf(g, (elem(vx, i) - mean) * rstd, s[1]);
             }
         }
-        row_sums<W, 2>(s, lds[turn]);
+        row_sums<LONG_BLOCK, 2>(s, lds[turn]);
         const float c1 = s[0] * inv, c2 = s[1] * inv;
         for (int c = 8 * threadIdx.x; c < a.cols; c += 8 * LONG_BLOCK) {
             const Raw8<T> vx = load8(x + c, a.cols - c), vd = load8(dy + c, a.cols - c);
@@ -557,7 +559,7 @@ constexpr int SHORT_COLS = 512, MID_COLS = 4096, WIDE_COLS = 16384;
 // A single block takes ONE_BLOCK turns and writes the sums itself: a turn more costs 2 us at most, a second launch 7.
 constexpr int BWD_BLOCKS = 512, LONG_SLICES = 64, ONE_BLOCK = 4;
 
-int bwd_rows_at_once(int64_t cols) { return cols <= 2 * SHORT_COLS ? 8 : cols <= MID_COLS ? 2 : 1; }
+int bwd_rows_at_once(int64_t cols) { return cols <= SHORT_COLS / 4 ? 32 : cols <= SHORT_COLS / 2 ? 16 : cols <= 2 * SHORT_COLS ? 8 : cols <= MID_COLS ? 2 : 1; }
 int bwd_blocks(int64_t cols) { return cols <= SHORT_COLS || (cols > 2 * SHORT_COLS && cols <= MID_COLS / 2) ? BWD_BLOCKS : BWD_BLOCKS / 2; }
 int bwd_parts(int64_t rows, int64_t cols)
 {
@@ -575,12 +577,14 @@ template <class T, int JOIN> int norm_fwd_typed(const NormArgs &a, hipStream_t s
         const int64_t b = ((int64_t)a.rows + rows_at_once - 1) / rows_at_once;
         return dim3((unsigned)(b < most ? b : most));
     };
-    if (n <= SHORT_COLS) hipLaunchKernelGGL((norm_fwd_kernel<T, 1, 1, JOIN, 256>), grid(4, 2048), dim3(256), 0, s, a);
-    else if (n <= 2 * SHORT_COLS) hipLaunchKernelGGL((norm_fwd_kernel<T, 1, 2, JOIN, 256>), grid(4, 2048), dim3(256), 0, s, a);
-    else if (n <= MID_COLS / 2) hipLaunchKernelGGL((norm_fwd_kernel<T, 4, 1, JOIN, 256>), grid(1, 2048), dim3(256), 0, s, a);
-    else if (n <= MID_COLS) hipLaunchKernelGGL((norm_fwd_kernel<T, 4, 2, JOIN, 256>), grid(1, 2048), dim3(256), 0, s, a);
-    else if (n <= WIDE_COLS / 2) hipLaunchKernelGGL((norm_fwd_kernel<T, 8, 2, JOIN, 512>), grid(1, 1024), dim3(512), 0, s, a);
-    else if (n <= WIDE_COLS) hipLaunchKernelGGL((norm_fwd_kernel<T, 8, 4, JOIN, 512>), grid(1, 1024), dim3(512), 0, s, a);
+    if (n <= SHORT_COLS / 4) hipLaunchKernelGGL((norm_fwd_kernel<T, 16, 1, JOIN, 256>), grid(16, 2048), dim3(256), 0, s, a);
+    else if (n <= SHORT_COLS / 2) hipLaunchKernelGGL((norm_fwd_kernel<T, 32, 1, JOIN, 256>), grid(8, 2048), dim3(256), 0, s, a);
+    else if (n <= SHORT_COLS) hipLaunchKernelGGL((norm_fwd_kernel<T, 64, 1, JOIN, 256>), grid(4, 2048), dim3(256), 0, s, a);
+    else if (n <= 2 * SHORT_COLS) hipLaunchKernelGGL((norm_fwd_kernel<T, 64, 2, JOIN, 256>), grid(4, 2048), dim3(256), 0, s, a);
+    else if (n <= MID_COLS / 2) hipLaunchKernelGGL((norm_fwd_kernel<T, 256, 1, JOIN, 256>), grid(1, 2048), dim3(256), 0, s, a);
+    else if (n <= MID_COLS) hipLaunchKernelGGL((norm_fwd_kernel<T, 256, 2, JOIN, 256>), grid(1, 2048), dim3(256), 0, s, a);
+    else if (n <= WIDE_COLS / 2) hipLaunchKernelGGL((norm_fwd_kernel<T, 512, 2, JOIN, 512>), grid(1, 1024), dim3(512), 0, s, a);
+    else if (n <= WIDE_COLS) hipLaunchKernelGGL((norm_fwd_kernel<T, 512, 4, JOIN, 512>), grid(1, 1024), dim3(512), 0, s, a);
     else hipLaunchKernelGGL((norm_fwd_long_kernel<T, JOIN>), grid(1, 512), dim3(LONG_BLOCK), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
@@ -592,12 +596,14 @@ template <class T, int JOIN> int norm_bwd_typed(NormBwdArgs &a, float *dgamma, f
     if (whole) a.dgamma = dgamma, a.dbeta = dbeta;
     if (parts > 0) {
         const dim3 grid((unsigned)parts);
-        if (n <= SHORT_COLS) hipLaunchKernelGGL((norm_bwd_kernel<T, 1, 1, JOIN, 512>), grid, dim3(512), 0, s, a);
-        else if (n <= 2 * SHORT_COLS) hipLaunchKernelGGL((norm_bwd_kernel<T, 1, 2, JOIN, 512>), grid, dim3(512), 0, s, a);
-        else if (n <= MID_COLS / 2) hipLaunchKernelGGL((norm_bwd_kernel<T, 4, 1, JOIN, 512>), grid, dim3(512), 0, s, a);
-        else if (n <= MID_COLS) hipLaunchKernelGGL((norm_bwd_kernel<T, 4, 2, JOIN, 512>), grid, dim3(512), 0, s, a);
-        else if (n <= WIDE_COLS / 2) hipLaunchKernelGGL((norm_bwd_kernel<T, 8, 2, JOIN, 512>), grid, dim3(512), 0, s, a);
-        else if (n <= WIDE_COLS) hipLaunchKernelGGL((norm_bwd_kernel<T, 8, 4, JOIN, 512>), grid, dim3(512), 0, s, a);
+        if (n <= SHORT_COLS / 4) hipLaunchKernelGGL((norm_bwd_kernel<T, 16, 1, JOIN, 512>), grid, dim3(512), 0, s, a);
+        else if (n <= SHORT_COLS / 2) hipLaunchKernelGGL((norm_bwd_kernel<T, 32, 1, JOIN, 512>), grid, dim3(512), 0, s, a);
+        else if (n <= SHORT_COLS) hipLaunchKernelGGL((norm_bwd_kernel<T, 64, 1, JOIN, 512>), grid, dim3(512), 0, s, a);
+        else if (n <= 2 * SHORT_COLS) hipLaunchKernelGGL((norm_bwd_kernel<T, 64, 2, JOIN, 512>), grid, dim3(512), 0, s, a);
+        else if (n <= MID_COLS / 2) hipLaunchKernelGGL((norm_bwd_kernel<T, 256, 1, JOIN, 512>), grid, dim3(512), 0, s, a);
+        else if (n <= MID_COLS) hipLaunchKernelGGL((norm_bwd_kernel<T, 256, 2, JOIN, 512>), grid, dim3(512), 0, s, a);
+        else if (n <= WIDE_COLS / 2) hipLaunchKernelGGL((norm_bwd_kernel<T, 512, 2, JOIN, 512>), grid, dim3(512), 0, s, a);
+        else if (n <= WIDE_COLS) hipLaunchKernelGGL((norm_bwd_kernel<T, 512, 4, JOIN, 512>), grid, dim3(512), 0, s, a);
         else {
             hipLaunchKernelGGL((norm_bwd_long_kernel<T, JOIN>), dim3((unsigned)(a.rows < 512 ? a.rows : 512)), dim3(LONG_BLOCK), 0, s, a);
             hipLaunchKernelGGL((norm_columns_kernel<T>), dim3((unsigned)((n + 511) / 512), (unsigned)parts), dim3(64), 0, s, a);

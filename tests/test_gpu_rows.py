@@ -223,3 +223,18 @@ def test_layernorm_results_repeat_and_follow_the_stream():
         assert all(torch.equal(a, b) for a, b in zip(first, results()))
         step()
         assert all(torch.equal(a, b) for a, b in zip(first, results()))
+
+
+@pytest.mark.parametrize("cols", [120, 128, 129, 250, 256, 257])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("joined", [False, True])
+def test_layernorm_of_rows_that_share_a_wave(cols, dtype, joined):
+    """Widths around a quarter and half of a wave's; one row, a block's rows and one more, more than a single block's, many."""
+    dt = DTYPES[dtype]
+    g = torch.Generator().manual_seed(5)
+    gamma, beta = (torch.empty(cols).normal_(m, 0.2, generator=g).cuda() for m in (1.0, 0.0))
+    for rows in (1, 17, 32, 65, 129, 6001):
+        x, xr = rows_of((rows, cols), 3, dt, 1, 1.0, 0.25)
+        dy, dyr = rows_of((rows, cols), 3, dt, 2, 0.01)
+        br = rows_of((rows, cols), 3, dt, 4, 0.5) if joined else None
+        run_norm(x, xr, gamma, beta, dy, dyr, None, None, br, 3)
