@@ -338,7 +338,7 @@ int cg_dropout_bwd(const cg_drop *drop, int type, int64_t rows, int64_t cols, co
 
 /* Layer norm over the rows of x [rows][cols]:  y = (x - mean) * rstd * gamma + beta,
  * rstd = 1 / sqrt(mean((x - mean)^2) + eps).  cols >= 1; rows = 0 gives empty outputs
- * and zero gradients of the weights.  rows * cols < 2^31. */
+ * and zero gradients of the weights.  rows * cols <= 2^31 - 2^16. */
 typedef struct { int type; int64_t rows, cols; float eps; } cg_layernorm_desc;
 
 /* mean, rstd [rows]: kept for the backward pass; both NULL where there is none.
@@ -378,7 +378,7 @@ int cg_dropout_add_layernorm_bwd(const cg_layernorm_desc *d, const cg_drop *drop
  * (delta > 0) have the buckets n .. 2n - 1.  n >= 2, buckets <= 256, n / 2 < max_distance <= 65536.
  * *_tok, *_head: elements from a token and from a head to the next.  The strides of o are also those of o_rest and
  * do; those of q, k and v also those of dq, dk and dv.
- * 1 <= D <= 128; Tq * Hq, Tk * Hkv < 2^31; tensors may exceed 2^31 bytes.
+ * 1 <= D <= 128; Tq * Hq, Tk * Hkv <= 2^31 - 2^16; tensors may exceed 2^31 bytes.
  * Arithmetic: bf16 tensors are multiplied as they are, the probabilities and the gradients of the scores
  * rounded to bf16 for their products; fp32 tensors as three bf16 numbers in six products (CG_MATH_FP32 above).
  * Sequences that overlap or reach past Tq, Tk are cut there; rows of no sequence are neither read nor written.

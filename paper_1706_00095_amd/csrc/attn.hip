@@ -5,6 +5,7 @@
 namespace cg {
 namespace {
 
+constexpr int64_t kMaxRows = INT32_MAX - 65535;      // a tile's end behind the last row is still a number of 32 bits
 constexpr int kMaxBuckets = 256, kMaxDistance = 65536;
 
 // From which distance on the buckets E + 1 .. n - 1 apply: bucket(dist) = dist below E, else E + (how many are <= dist).
@@ -13,7 +14,7 @@ struct Thresholds {
     int from[kMaxBuckets / 2 + 1];
 };
 
-// Bias and bucket by distance, for the heads' tables [2 W + 1] in the workspace: a kernel of a few microseconds, so that the
+// Bias and bucket by distance, for the heads' tables [2 W + 1] in the workspace: a kernel of 4 to 9 microseconds, so that the
 // attention kernels look a distance up instead of taking its logarithm for every pair.
 __global__ __launch_bounds__(256) void bias_table_kernel(Thresholds th, const float *bias, int buckets, int W, float *tab, uint8_t *bid)
 {
@@ -65,7 +66,7 @@ int check(const cg_attn_desc *d)
         if (n < 2 || (d->both && d->buckets % 2) || d->max_distance <= n / 2) return CG_EINVAL;
         if (d->buckets > kMaxBuckets || d->max_distance > kMaxDistance) return CG_EUNSUPPORTED;
     }
-    if (d->D > kAttnMaxD || d->Tq > INT32_MAX || d->Tk > INT32_MAX || d->Tq * d->Hq > INT32_MAX || d->Tk * d->Hkv > INT32_MAX) return CG_EUNSUPPORTED;
+    if (d->D > kAttnMaxD || d->Tq > kMaxRows || d->Tk > kMaxRows || d->Tq * d->Hq > kMaxRows || d->Tk * d->Hkv > kMaxRows) return CG_EUNSUPPORTED;
     if ((d->Tq * d->Hq / kAttnRows + d->B) * (int64_t)d->Hq > (1 << 30) || (d->Tk / kAttnRows + d->B) * (int64_t)d->Hkv > (1 << 30)) return CG_EUNSUPPORTED;
     return CG_OK;
 }

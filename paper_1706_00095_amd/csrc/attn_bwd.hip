@@ -44,6 +44,9 @@ __device__ __forceinline__ void add_runs(float v, int bucket, float *acc, int la
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
+// dq, delta and the bias's gradient.  A block takes 128 query rows (X) and walks the keys (Y) they see, as the forward kernel does; the row's
+// statistics are known, so a tile is S, dP, dS and dS K: three products.  Bound as the forward kernel: 4 x 4096, 16 heads of 128, causal,
+// bf16 450 us, 915 TFLOP/s; 2862 packed tokens, 12 heads of 64, with a bias 43 us, of which the sums along diagonals are 8.
 // Waves a SIMD: two where registers and LDS (the squares of the bias's gradient take 36 KB) allow them.
 template <class T, int DP, bool BIAS> constexpr int kDqWaves = (Pieces<T>::N == 1 ? !BIAS || DP <= 64 : DP <= (BIAS ? 32 : 64)) ? 2 : 1;
 
@@ -291,7 +294,8 @@ __device__ __forceinline__ void sum_dbias(AttnArgs a, int item, double *lds)
 }
 
 // X: 128 keys of a key-value head; Y: the query rows that see them, of all Gp heads.  With a bias Gp = 1, and the G heads
-// are walked one after the other.
+// are walked one after the other.  Four products a tile: 4 x 4096, 16 heads of 128, causal, bf16 580 us, 945 TFLOP/s; 2 x 4096, 32 heads on 8,
+// 730, 750, because 64 blocks on a die read more rows at a time than its L2 holds.
 template <class T, int DP> constexpr int kDkdvWaves = Pieces<T>::N == 1 || DP <= 32 ? 2 : 1;
 
 template <class T, int DP, bool BIAS, bool DMA>

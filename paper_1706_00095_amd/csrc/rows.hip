@@ -59,7 +59,7 @@ __device__ __forceinline__ float dropped(float x, uint32_t keep, int i, const Dr
 // A thread takes the eight elements of one block of the generator, so each block is computed once whatever the width.
 // DENSE: rows follow each other without a gap in all tensors, and a block is eight neighbours.  Otherwise a block's
 // elements are neighbours unless a row ends among them.
-// MI355X, 16384 x 4096 bf16 with an addend: see the table in the design notes.
+// Bound by HBM: 16384 x 4096 bf16 with an addend 70 us, 5.8 TB/s (a large copy: 5.1); the generator's 1.7 G multiplications hide behind.
 struct DropoutArgs {
     const void *x, *add;
     void *y;
@@ -167,6 +167,7 @@ struct NormBwdArgs {
     DropArgs drop;
 };
 
+// Bound by HBM: 16384 x 2048 bf16 24 us (5.5 TB/s); joined, 8192 x 4096 bf16, 56 (4.8).
 // JOIN: 0 = layer norm alone, 1 = joined, rows on the generator's blocks (cols a multiple of 8), 2 = joined, any cols
 template <class T, int LANES, int CPT, int JOIN, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a)
@@ -243,6 +244,7 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a)
 // dx of a row needs two sums over it, <g> and <g xh> with g = dy gamma; dgamma and dbeta are sums over the rows, which each
 // thread keeps for its columns over all the rows that its block takes.  Blocks write their sums to `part`; sum_parts_kernel adds
 // them in order, so results do not depend on scheduling.
+// Bound by HBM: 16384 x 2048 bf16 40 us (5.0 TB/s); joined, 8192 x 4096 bf16, 62 (4.3); the sums of the blocks' sums 4 to 7.
 template <class T, int LANES, int CPT, int JOIN, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
 {
@@ -357,6 +359,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
 }
 
 // Rows longer than the registers of a block hold: a block walks the row three times, the second and third time out of L2.
+// 1024 x 32768 bf16: 47 us, 2.9 TB/s of what HBM has to move; backward 49, and 24 for the columns' sums.
 constexpr int LONG_BLOCK = 1024;
 template <class T, int JOIN> __global__ __launch_bounds__(LONG_BLOCK) void norm_fwd_long_kernel(NormArgs a)
 {
@@ -630,7 +633,8 @@ template <class A, class F> int for_type_and_join(int type, const A &a, bool joi
 int desc_check(const cg_layernorm_desc *d)
 {
     if (!d || !type_ok(d->type) || d->rows < 0 || d->cols < 1 || !(d->eps >= 0.f)) return CG_EINVAL;
-    if (!rows_fit(d->rows, d->cols)) return CG_EUNSUPPORTED;
+    // a launch's stride behind the last row or column is still a number of 32 bits
+    if (!rows_fit(d->rows, d->cols) || d->rows * d->cols > INT32_MAX - 65535) return CG_EUNSUPPORTED;
     return CG_OK;
 }
 

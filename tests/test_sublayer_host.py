@@ -182,3 +182,17 @@ def test_the_binding_refuses_what_does_not_fit():
     d = cg.attn_desc(q, q, q, q, 1, 1.0)
     with pytest.raises(TypeError):
         cg.cg_attn_fwd(d, q, q, q, None, None, None, q, None)
+
+
+def test_sizes_whose_loops_would_pass_32_bits_are_refused():
+    """A loop's step behind the last row has to fit as well: 2^16 below the largest number is the limit."""
+    L = cg.lib()
+    most = (1 << 31) - (1 << 16)
+    for rows, cols in ((most + 1, 1), (1, most + 1), ((1 << 31) - 1, 1)):
+        d = cg.cg_layernorm_desc(0, rows, cols, 1e-5)
+        assert L.cg_layernorm_fwd(d, 64, cols, 64, 64, 64, cols, None, None, None) == cg.CG_EUNSUPPORTED
+        assert cg.cg_layernorm_workspace_bytes(d) == 0
+    assert cg.cg_layernorm_workspace_bytes(cg.cg_layernorm_desc(0, most, 1, 1e-5)) > 0
+    for d in (attn(Tk=most + 1, Hkv=1, Hq=1, D=1), attn(Tq=most + 1, Hkv=1, Hq=1, D=1), attn(Tk=(1 << 31) - 1, Hkv=1, Hq=1, D=1)):
+        assert fwd(d) == cg.CG_EUNSUPPORTED and bwd(d) == cg.CG_EUNSUPPORTED
+    assert cg.cg_attn_workspace_bytes(attn(Tk=most, Hkv=1, Hq=1, D=1, B=1, Tq=1), cg.CG_PASS_FWD) > 0
