@@ -8,7 +8,7 @@ constexpr float kSlack = 8.f;
 
 // A block takes 128 query rows (X) of one problem and walks the keys (Y) they see in tiles of YT.
 // Prompts are bound by matrix and vector instructions at a clock that power holds to 1.6 .. 1.85 GHz: 8192 tokens, 32 heads on 8, 128 wide,
-// causal, bf16 536 .. 620 us, 890 .. 1025 TFLOP/s (a large library product: 1284).  Single tokens are bound by HBM: 64 sequences of 8192
+// causal, bf16 518 .. 620 us, 890 .. 1060 TFLOP/s (a large library product: 1284).  Single tokens are bound by HBM: 64 sequences of 8192
 // keys, the same heads, 361 us, 5.9 TB/s; fp32 1790, 2.4, since one of the four waves has rows and six products a term.
 // EXACT (bf16 in a training step): the probabilities that o is made of keep 24 bits, in three pieces.  The backward pass subtracts
 // delta, a sum of o times do, from dP; where the differences are added up (the bias's gradient) or rows see a few keys only (sequences
