@@ -6,7 +6,7 @@ namespace cg {
 namespace {
 
 constexpr int64_t kMaxRows = INT32_MAX - 65535;      // a tile's end behind the last row is still a number of 32 bits
-constexpr int kMaxBuckets = 256, kMaxDistance = 65536;
+constexpr int kMaxDistance = 65536;
 
 // From which distance on the buckets E + 1 .. n - 1 apply: bucket(dist) = dist below E, else E + (how many are <= dist).
 struct Thresholds {

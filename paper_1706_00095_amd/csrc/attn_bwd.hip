@@ -10,8 +10,15 @@ namespace {
 // r - c + 31 of a square in LDS, at place c; the places of a row that no (r, c) has stay zero, so a lane adds up one whole row
 // in eight wide reads.  Rows of kDiag words put eight lanes' reads on different banks.
 // Sums over a wave's parts are kept by distance (W <= kNear: a word a distance, which each lane has to itself), else by bucket.
-constexpr int kDiag = 36, kNear = 1024;
-__host__ __device__ inline int near_words(int W) { return W <= kNear ? 2 * W + 1 : 256; }
+constexpr int kDiag = 36, kLdsBytes = 160 << 10;
+// The dq kernel with a bias: LDS of its tiles, windows and squares; the words a wave that are left decide how far distances are kept one
+// by one: 1024, which all instances but the widest in fp32 have room for (849 there).
+template <class T, int DP> struct DqLds {
+    static constexpr int YT = Pieces<T>::N == 1 ? 64 : 32, FIXED = 4 * Tile<DP, YT, Pieces<T>::N>::BYTES + 2 * 256 * 4 + 4 * 63 * kDiag * 4;
+    static constexpr int LEFT = ((kLdsBytes - FIXED) / 16 - 1) / 2, NEAR = LEFT < 1024 ? LEFT : 1024;
+    static __host__ __device__ constexpr int words(int W) { return W <= NEAR ? 2 * W + 1 : kMaxBuckets; }
+    static_assert(NEAR > 0 && FIXED + 16 * (2 * NEAR + 1) <= kLdsBytes && FIXED + 16 * kMaxBuckets <= kLdsBytes, "more LDS than a compute unit has");
+};
 
 __device__ __forceinline__ float diagonal_sum(const float (&ds)[16], float *sq, int lane)
 {
@@ -53,20 +60,23 @@ template <class T, int DP, bool BIAS> constexpr int kDqWaves = (Pieces<T>::N == 
 template <class T, int DP, bool BIAS, bool DMA>
 __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(AttnArgs a)
 {
-    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = NP == 1 ? 64 : 32, SUB = YT / 32;
+    constexpr int NP = Pieces<T>::N, KS = DP / 16, DT = DP / 32, YT = DqLds<T, DP>::YT, SUB = YT / 32;
     using TileY = Tile<DP, YT, NP>;
     __shared__ __align__(16) char lds[2][2][TileY::BYTES];
     LdsByte *const ldsK = (LdsByte *)lds[0][0], *const ldsV = (LdsByte *)lds[1][0];
     __shared__ float window[2][BIAS ? 256 : 1];
     __shared__ __align__(16) float square[BIAS ? 4 : 1][BIAS ? 63 * kDiag : 4];
-    extern __shared__ float by_wave[];          // [4][near_words(W)]
+    extern __shared__ float by_wave[];          // [4][words(W)]
+    using Lds = DqLds<T, DP>;
+    static_assert(!BIAS || sizeof(lds) + sizeof(window) + sizeof(square) == Lds::FIXED, "what the launch's LDS is computed from");
+    constexpr int kNear = Lds::NEAR;
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
     const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr;
     Place place;
     if (!find_place<false>(a, blockIdx.x / Hr, place)) return;
     const int t = place.t, split = place.split;
     const bool want_bias = BIAS && a.dbias_part;
-    float *const mine = by_wave + wave * near_words(a.W);
+    float *const mine = by_wave + wave * Lds::words(a.W);
     float *const bias_out = want_bias ? a.dbias_part + ((int64_t)hr * a.dbias_parts + place.slot) * a.buckets : nullptr;
     const Seq s = seq_of(a, place.b);
     const int row0 = t * kAttnRows, rows = s.n * a.Gp, off = s.m - s.n;
@@ -91,7 +101,7 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
     }
     if (want_bias) {
         for (int i = threadIdx.x; i < 4 * 63 * kDiag; i += 256) square[0][i] = 0.f;
-        for (int i = threadIdx.x; i < 4 * near_words(a.W); i += 256) by_wave[i] = 0.f;
+        for (int i = threadIdx.x; i < 4 * Lds::words(a.W); i += 256) by_wave[i] = 0.f;
         __syncthreads();
     }
 
@@ -249,7 +259,7 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
 #pragma unroll
             for (int i = 0; i < 256; i += 64) sums[i + lane] = 0.f;
             __syncthreads();
-            const int words = near_words(a.W);
+            const int words = Lds::words(a.W);
             for (int i = 64 * wave; i < words; i += 256) {
                 const bool there = i + lane < words;
                 const float *w = by_wave + (there ? i + lane : 0);
@@ -262,7 +272,7 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
         }
         __syncthreads();
         const float *const all = a.W <= kNear ? square[0] : by_wave;
-        const int apart = a.W <= kNear ? 63 * kDiag : near_words(a.W);
+        const int apart = a.W <= kNear ? 63 * kDiag : Lds::words(a.W);
         for (int i = threadIdx.x; i < a.buckets; i += 256) bias_out[i] = (all[i] + all[apart + i]) + (all[2 * apart + i] + all[3 * apart + i]);
     }
     if (!here) return;
@@ -499,7 +509,8 @@ template <class T, int DP, bool DMA> int dq_run(AttnArgs a, hipStream_t s)
     a.levels = levels_of(a, problems, waves == 2 && (a.btab || !DMA));
     a.fold = fold_of(a, problems, waves);
     const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
-    if (a.btab) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true, DMA>), grid, dim3(256), a.dbias_part ? 16 * near_words(a.W) : 0, s, a);
+    const unsigned by_wave = a.dbias_part ? 4 * sizeof(float) * DqLds<T, DP>::words(a.W) : 0;
+    if (a.btab) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true, DMA>), grid, dim3(256), by_wave, s, a);
     else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false, DMA>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
