@@ -401,7 +401,10 @@ size_t cg_attn_workspace_bytes(const cg_attn_desc *d, int pass);
 int cg_attn_fwd(const cg_attn_desc *d, const void *q, const void *k, const void *v, const int32_t *cu_q,
                 const int32_t *cu_k, const float *bias, void *o, float *lse, void *o_rest, void *ws, size_t ws_bytes,
                 void *stream);
-/* dbias [Hq][buckets] fp32 (NULL: none wanted).  o_rest may be NULL. */
+/* dbias [Hq][buckets] fp32 (NULL: none wanted).  o_rest may be NULL.  Probabilities are taken again as e^(s - lse), and lse, one fp32
+ * number, is off by up to 2^-24 of itself.  With a bias, rows with |lse| >= 2^10 get maximum and sum anew from their scores (one more pass
+ * over the keys for them): all of a row's biases may be the type's lowest value.  Without one the products that make a lse large are
+ * off by as much themselves. */
 int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q, const void *k, const void *v, const int32_t *cu_q,
                 const int32_t *cu_k, const float *bias, const void *o, const void *o_rest, const float *lse, void *dq,
                 void *dk, void *dv, float *dbias, void *ws, size_t ws_bytes, void *stream);

@@ -99,7 +99,7 @@ struct Plan {
     int Gp, tiles_q, tiles_k, W, DP;
     int gsplit;
     Split q, k;                 // of the kernels whose X are queries (forward, dq) and keys (dk, dv)
-    size_t tab, bid, part_q, part_ml, part_k[2], delta, lse_b, dbias, bytes;
+    size_t tab, bid, part_q, part_ml, part_k[2], delta, lse_b, log_l, dbias, bytes;
 };
 
 Plan plan_of(const cg_attn_desc &d, int pass)
@@ -137,6 +137,7 @@ Plan plan_of(const cg_attn_desc &d, int pass)
         p.part_k[1] = take(k_rows * p.DP * 4);
         p.delta = take(d.Tq * d.Hq * 4);
         p.lse_b = take(d.Tq * d.Hq * 4);
+        p.log_l = take(d.buckets ? d.Tq * d.Hq * 4 : 0);
         p.dbias = take((int64_t)d.Hq * p.tiles_q * p.q.splits * d.buckets * 4);
     }
     p.bytes = (size_t)at;
@@ -237,6 +238,7 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
     a.dq = dq, a.dk = dk, a.dv = dv;
     a.delta = reinterpret_cast<float *>(w + p.delta);
     a.lse_b = reinterpret_cast<float *>(w + p.lse_b);
+    a.log_l = reinterpret_cast<float *>(w + p.log_l);
     const bool any_q = d->B > 0 && d->Tq > 0, any_k = d->B > 0 && d->Tk > 0;
     if (dbias) {
         a.dbias = dbias;

@@ -14,7 +14,7 @@ constexpr int kDiag = 36, kLdsBytes = 160 << 10;
 // The dq kernel with a bias: LDS of its tiles, windows and squares; the words a wave that are left decide how far distances are kept one
 // by one: 1024, which all instances but the widest in fp32 have room for (849 there).
 template <class T, int DP> struct DqLds {
-    static constexpr int YT = Pieces<T>::N == 1 ? 64 : 32, FIXED = 4 * Tile<DP, YT, Pieces<T>::N>::BYTES + 2 * 256 * 4 + 4 * 63 * kDiag * 4;
+    static constexpr int YT = Pieces<T>::N == 1 ? 64 : 32, FIXED = 4 * Tile<DP, YT, Pieces<T>::N>::BYTES + 2 * 256 * 4 + 4 * 63 * kDiag * 4 + 4 * 4;
     static constexpr int LEFT = ((kLdsBytes - FIXED) / 16 - 1) / 2, NEAR = LEFT < 1024 ? LEFT : 1024;
     static __host__ __device__ constexpr int words(int W) { return W <= NEAR ? 2 * W + 1 : kMaxBuckets; }
     static_assert(NEAR > 0 && FIXED + 16 * (2 * NEAR + 1) <= kLdsBytes && FIXED + 16 * kMaxBuckets <= kLdsBytes, "more LDS than a compute unit has");
@@ -51,6 +51,13 @@ __device__ __forceinline__ void add_runs(float v, int bucket, float *acc, int la
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
+// With a bias, rows whose lse is far from zero.  lse = m + log l is one number of 24 bits: beside a large m it keeps little of log l (nothing
+// where all that a row sees has the type's lowest value as its bias), and e^(s - lse) no longer sums to one.  Such a row gets its m and l
+// anew from the scores, and both kernels take e^(s - m - log l).  Below 2^10 a rounded lse costs a probability 2^-14 of itself, no more
+// than the score's own rounding does there.  The blocks that have such a row walk the keys once more for it, no others do.  Without a
+// bias scores are large only where products are, whose own rounding is as large as lse's.
+constexpr float kFar = 1024.f;
+
 // dq, delta and the bias's gradient.  A block takes 128 query rows (X) and walks the keys (Y) they see, as the forward kernel does; the row's
 // statistics are known, so a tile is S, dP, dS and dS K: three products.  Bound as the forward kernel: 4 x 4096, 16 heads of 128, causal,
 // bf16 450 us, 915 TFLOP/s; 2862 packed tokens, 12 heads of 64, with a bias 43 us, of which the sums along diagonals are 8.
@@ -66,9 +73,10 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
     LdsByte *const ldsK = (LdsByte *)lds[0][0], *const ldsV = (LdsByte *)lds[1][0];
     __shared__ float window[2][BIAS ? 256 : 1];
     __shared__ __align__(16) float square[BIAS ? 4 : 1][BIAS ? 63 * kDiag : 4];
+    __shared__ int far_rows[4];
     extern __shared__ float by_wave[];          // [4][words(W)]
     using Lds = DqLds<T, DP>;
-    static_assert(!BIAS || sizeof(lds) + sizeof(window) + sizeof(square) == Lds::FIXED, "what the launch's LDS is computed from");
+    static_assert(!BIAS || sizeof(lds) + sizeof(window) + sizeof(square) + sizeof(far_rows) == Lds::FIXED, "what the launch's LDS is computed from");
     constexpr int kNear = Lds::NEAR;
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
     const int Hr = a.Hq / a.Gp, hr = blockIdx.x % Hr;
@@ -142,14 +150,61 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
     const int64_t stat = (int64_t)head * a.Tq + s.q0 + tok;
     const float lse = here ? a.lse[stat] : -INFINITY;
     // the exponent takes lse in the scores' own units with a bias, else times log2 e; a row that sees nothing (or is none) has probabilities 0
-    const float c = a.scale * kLog2e, lse_b = lse == -INFINITY ? INFINITY : BIAS ? lse : lse * kLog2e;
-    if (here && h32 == 0 && split == 0) {
-        a.delta[stat] = delta;
-        a.lse_b[stat] = lse_b;
-    }
+    const float c = a.scale * kLog2e;
+    float lse_b = lse == -INFINITY ? INFINITY : BIAS ? lse : lse * kLog2e, log_l = 0.f;
 
     arrived(fq);
     arrived(fdo);
+
+    if constexpr (BIAS) {
+        const bool is_far = fabsf(lse) >= kFar && fabsf(lse) < INFINITY, any = __any(is_far);
+        if (lane == 0) far_rows[wave] = any;
+        __syncthreads();
+        if (__builtin_amdgcn_readfirstlane(far_rows[0] | far_rows[1] | far_rows[2] | far_rows[3])) {
+            tile_sync();       // the tiles asked for above have landed: K's buffer is free
+            const int all = keys_seen(a, s, row0 + kAttnRows, rows);       // whatever chunk of them is this block's
+            float m = -INFINITY, l = 0.f;
+            for (int k0 = 0; k0 < all; k0 += YT) {
+                lk.start(k0, ldsK);
+                lk.finish(ldsK);
+                window[0][threadIdx.x] = window_load(a, h0, k0 + window0);
+                tile_sync();
+                if (k0 < wave_kend)
+#pragma unroll 1
+                    for (int u = 0; u < SUB; ++u) {
+                        Acc<NP> S;
+                        S.zero();
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) S.mma(TileY::rows(ldsK, 32 * u, ks, lane), fq[ks]);
+                        float x[16], top = -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int y = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4;
+                            x[i] = fmaf(S.get(i), a.scale, window[0][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
+                            if (k0 + y >= limit) x[i] = -INFINITY;
+                            top = fmaxf(top, x[i]);
+                        }
+                        const float mn = fmaxf(m, max_halves(top)), ms = mn == -INFINITY ? 0.f : mn;
+                        l *= __builtin_amdgcn_exp2f((m - ms) * kLog2e);
+                        m = mn;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) l += __builtin_amdgcn_exp2f((x[i] - ms) * kLog2e);
+                    }
+                __syncthreads();       // the tile has been read
+            }
+            l = sum_halves(l);
+            if (is_far) lse_b = m == -INFINITY ? INFINITY : m, log_l = l == 0.f ? 0.f : __builtin_amdgcn_logf(l);
+            if (kbeg < kend) {
+                lk.start(kbeg, ldsK);
+                window[0][threadIdx.x] = window_load(a, h0, kbeg + window0);
+            }
+        }
+    }
+    if (here && h32 == 0 && split == 0) {
+        a.delta[stat] = delta;
+        a.lse_b[stat] = lse_b;
+        if constexpr (BIAS) a.log_l[stat] = log_l;
+    }
 
     v16f dQ[DT];
 #pragma unroll
@@ -188,7 +243,7 @@ __global__ __launch_bounds__(256, (kDqWaves<T, DP, BIAS>)) void attn_dq_kernel(A
                     float p;
                     if constexpr (BIAS) {
                         const float x = fmaf(S.get(i), a.scale, window[buf][y + kAttnRows - 1 - 32 * wave - (lane & 31)]);
-                        p = __builtin_amdgcn_exp2f((x - lse_b) * kLog2e);
+                        p = __builtin_amdgcn_exp2f(fmaf(x - lse_b, kLog2e, -log_l));
                     } else p = __builtin_amdgcn_exp2f(fmaf(S.get(i), c, -lse_b));
                     ds[i] = p * (P.get(i) - delta);
                 }
@@ -321,7 +376,8 @@ __global__ __launch_bounds__(256, (kDkdvWaves<T, DP>)) void attn_dkdv_kernel(Att
     LdsByte *const ldsV = (LdsByte *)lds_v;
     __shared__ __align__(16) char lds[2][2][TileY::BYTES];
     LdsByte *const ldsQ = (LdsByte *)lds[0][0], *const ldsO = (LdsByte *)lds[1][0];
-    __shared__ __align__(16) float stats[2][2][64];            // lse_b, delta of the tile's rows
+    constexpr int STATS = BIAS ? 3 : 2;
+    __shared__ __align__(16) float stats[2][STATS][64];        // lse_b, delta (and log_l) of the tile's rows
     __shared__ float window[2][BIAS ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h32 = lane >> 5;
     if constexpr (BIAS) {
@@ -376,12 +432,12 @@ __global__ __launch_bounds__(256, (kDkdvWaves<T, DP>)) void attn_dkdv_kernel(Att
         Loader<T, DP, YT, DMA> lq(Q), lo(dO);
         const int window0 = key0 - (YT - 1) - off;
         float bias_next = 0.f, stat_next = 0.f;
-        // What the tile's rows have apart from their elements: threads 0 .. 63 lse_b, 64 .. 127 delta, a row each.  Rows that are none get
-        // zeros: their elements are zeros as well, so that a probability of 1 adds nothing.
+        // What the tile's rows have apart from their elements: threads 0 .. 63 lse_b, 64 .. 127 delta, 128 .. 191 log_l, a row each.  Rows
+        // that are none get zeros: their elements are zeros as well, so that a probability of 1 adds nothing.
         auto row_start = [&](int y0, int to) {
-            if (wave < 2) {
+            if (wave < STATS) {
                 const int r = y0 + lane;
-                const float *from = (wave == 0 ? a.lse_b : a.delta) + (int64_t)h0 * a.Tq + s.q0;
+                const float *from = (wave == 0 ? a.lse_b : !BIAS || wave == 1 ? a.delta : a.log_l) + (int64_t)h0 * a.Tq + s.q0;
                 const bool here = lane < YT && r < rows;
                 if constexpr (DMA) {
                     const int tok = (int)fdiv((uint32_t)(here ? r : 0), a.by_gp);
@@ -396,7 +452,7 @@ __global__ __launch_bounds__(256, (kDkdvWaves<T, DP>)) void attn_dkdv_kernel(Att
         };
         auto row_finish = [&](int to) {
             if constexpr (!DMA)
-                if (wave < 2) stats[to][wave][lane] = stat_next;
+                if (wave < STATS) stats[to][wave][lane] = stat_next;
             if constexpr (BIAS) window[to][threadIdx.x] = bias_next;
         };
         int buf = 0;
@@ -436,13 +492,14 @@ __global__ __launch_bounds__(256, (kDkdvWaves<T, DP>)) void attn_dkdv_kernel(Att
                 for (int j = 0; j < 4; ++j) {
                     const int at = 32 * u + 8 * j + 4 * h32;
                     const float4 l4 = *reinterpret_cast<const float4 *>(stats[buf][0] + at), d4 = *reinterpret_cast<const float4 *>(stats[buf][1] + at);
-                    const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+                    const float4 g4 = BIAS ? *reinterpret_cast<const float4 *>(stats[buf][STATS - 1] + at) : float4{};
+                    const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w}, log_l[4] = {g4.x, g4.y, g4.z, g4.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         float x;
                         if constexpr (BIAS) {
                             x = fmaf(S.get(4 * j + i), a.scale, window[buf][32 * wave + (lane & 31) - (at + i) + YT - 1]);
-                            x = __builtin_amdgcn_exp2f((x - l[i]) * kLog2e);
+                            x = __builtin_amdgcn_exp2f(fmaf(x - l[i], kLog2e, -log_l[i]));
                         } else x = __builtin_amdgcn_exp2f(fmaf(S.get(4 * j + i), c, -l[i]));
                         p[4 * j + i] = x;
                         ds[4 * j + i] = x * (P.get(4 * j + i) - d[i]);

@@ -23,7 +23,9 @@ struct AttnArgs {
     const void *q, *k, *v, *d_o, *o_in, *o_rest_in;
     void *o, *o_rest, *dq, *dk, *dv;
     float *lse;                            // [Hq][Tq]
-    float *delta, *lse_b;                  // [Hq][Tq], written by the dq kernel: sums of do o, and lse as the exponent takes it
+    // [Hq][Tq], written by the dq kernel: sums of do o; lse as the exponent takes it; with a bias, what else it takes (log2, 0 but for rows
+    // whose lse is far from zero)
+    float *delta, *lse_b, *log_l;
     const int32_t *cu_q, *cu_k;
     int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
     int B, Tq, Tk, Hq, Hkv, G, Gp, D;      // G: query heads of a key-value head; Gp of them are packed (1 or G)
