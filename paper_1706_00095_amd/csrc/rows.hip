@@ -476,22 +476,28 @@ template <class T> __global__ __launch_bounds__(64) void norm_columns_kernel(Nor
 }
 
 // dgamma, dbeta: the blocks' sums, [parts][2][cols], added.  A block takes 16 of the 2 cols columns, 16 threads each: thread j
-// adds the parts j, j + 16, .. and the threads' sums are added in order.
+// adds the parts j, j + 16, .. and the threads' sums are added in order.  A launch has fewer than 2^32 threads, so blocks of rows
+// longer than 2^19 take 16 columns after the other.
+constexpr int SUM_BLOCKS = 1 << 16;
 __global__ __launch_bounds__(256) void sum_parts_kernel(const float *part, int parts, int cols, float *dgamma, float *dbeta)
 {
     __shared__ float lds[16][17];
     const int x = threadIdx.x % 16, j = threadIdx.x / 16;
-    const int64_t col = (int64_t)blockIdx.x * 16 + x;
-    float s = 0.f;
-    if (col < 2 * (int64_t)cols)
+    const int64_t n = 2 * (int64_t)cols;
+    for (int64_t c0 = (int64_t)blockIdx.x * 16; c0 < n; c0 += (int64_t)gridDim.x * 16) {
+        const int64_t col = c0 + x;
+        float s = 0.f;
+        if (col < n)
 #pragma unroll 4
-        for (int p = j; p < parts; p += 16) s += part[(int64_t)p * 2 * cols + col];
-    lds[j][x] = s;
-    __syncthreads();
-    if (j == 0 && col < 2 * (int64_t)cols) {
+            for (int p = j; p < parts; p += 16) s += part[p * n + col];
+        lds[j][x] = s;
+        __syncthreads();
+        if (j == 0 && col < n) {
 #pragma unroll
-        for (int i = 1; i < 16; ++i) s += lds[i][x];
-        (col < cols ? dgamma[col] : dbeta[col - cols]) = s;
+            for (int i = 1; i < 16; ++i) s += lds[i][x];
+            (col < cols ? dgamma[col] : dbeta[col - cols]) = s;
+        }
+        __syncthreads();
     }
 }
 
@@ -614,7 +620,8 @@ template <class T, int JOIN> int norm_bwd_typed(NormBwdArgs &a, float *dgamma, f
         CG_HIP_TRY(hipGetLastError());
         if (whole) return CG_OK;
     }
-    hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)((2 * (int64_t)n + 15) / 16)), dim3(256), 0, s, a.part, parts, n, dgamma, dbeta);
+    const int64_t sums = (2 * (int64_t)n + 15) / 16;
+    hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)(sums < SUM_BLOCKS ? sums : SUM_BLOCKS)), dim3(256), 0, s, a.part, parts, n, dgamma, dbeta);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
 }
