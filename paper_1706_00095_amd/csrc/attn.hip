@@ -7,6 +7,7 @@ namespace {
 
 constexpr int64_t kMaxRows = INT32_MAX - 65535;      // a tile's end behind the last row is still a number of 32 bits
 constexpr int kMaxDistance = 65536;
+constexpr int64_t kMaxBlocks = (1 << 24) - 1;        // of 256 threads: a launch has fewer than 2^32
 
 // From which distance on the buckets E + 1 .. n - 1 apply: bucket(dist) = dist below E, else E + (how many are <= dist).
 struct Thresholds {
@@ -55,7 +56,7 @@ Thresholds thresholds(const cg_attn_desc &d)
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-int check(const cg_attn_desc *d)
+int check(const cg_attn_desc *d, int pass)
 {
     if (!d || (d->type != CG_TYPE_FP32 && d->type != CG_TYPE_BF16)) return CG_EINVAL;
     if (d->B < 0 || d->Hq < 1 || d->Hkv < 1 || d->D < 1 || d->Hq % d->Hkv || d->Tq < 0 || d->Tk < 0) return CG_EINVAL;
@@ -67,7 +68,10 @@ int check(const cg_attn_desc *d)
         if (d->buckets > kMaxBuckets || d->max_distance > kMaxDistance) return CG_EUNSUPPORTED;
     }
     if (d->D > kAttnMaxD || d->Tq > kMaxRows || d->Tk > kMaxRows || d->Tq * d->Hq > kMaxRows || d->Tk * d->Hkv > kMaxRows) return CG_EUNSUPPORTED;
-    if ((d->Tq * d->Hq / kAttnRows + d->B) * (int64_t)d->Hq > (1 << 30) || (d->Tk / kAttnRows + d->B) * (int64_t)d->Hkv > (1 << 30)) return CG_EUNSUPPORTED;
+    // the blocks of the kernels whose X are queries, and keys (with the blocks that add up dbias); axes are cut only where these are few
+    const int64_t Gp = d->buckets ? 1 : d->Hq / d->Hkv;
+    if (d->Hq / Gp * (d->Tq * Gp / kAttnRows + d->B) > kMaxBlocks) return CG_EUNSUPPORTED;
+    if (pass != CG_PASS_FWD && d->Hkv * (d->Tk / kAttnRows + d->B) + (int64_t)d->Hq * ((d->buckets + 15) / 16) > kMaxBlocks) return CG_EUNSUPPORTED;
     return CG_OK;
 }
 
@@ -196,14 +200,14 @@ using namespace cg;
 
 extern "C" size_t cg_attn_workspace_bytes(const cg_attn_desc *d, int pass)
 {
-    if (check(d) != CG_OK || (pass != CG_PASS_FWD && pass != CG_PASS_BWD_DATA)) return 0;
+    if ((pass != CG_PASS_FWD && pass != CG_PASS_BWD_DATA) || check(d, pass) != CG_OK) return 0;
     return plan_of(*d, pass).bytes;
 }
 
 extern "C" int cg_attn_fwd(const cg_attn_desc *d, const void *q, const void *k, const void *v, const int32_t *cu_q, const int32_t *cu_k,
                            const float *bias, void *o, float *lse, void *o_rest, void *ws, size_t ws_bytes, void *stream)
 {
-    if (int rc = check(d)) return rc;
+    if (int rc = check(d, CG_PASS_FWD)) return rc;
     if (d->B == 0 || d->Tq == 0) return CG_OK;
     if (!tensor_ok(q, d->type, 1) || !tensor_ok(k, d->type, d->Tk) || !tensor_ok(v, d->type, d->Tk) || !tensor_ok(o, d->type, 1) || !words_ok(lse, 1) ||
         !words_ok(cu_q, 1) || !words_ok(cu_k, 1) || !words_ok(bias, d->buckets)) return CG_EINVAL;
@@ -223,7 +227,7 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
                            const int32_t *cu_k, const float *bias, const void *o, const void *o_rest, const float *lse, void *dq,
                            void *dk, void *dv, float *dbias, void *ws, size_t ws_bytes, void *stream)
 {
-    if (int rc = check(d)) return rc;
+    if (int rc = check(d, CG_PASS_BWD_DATA)) return rc;
     if (!tensor_ok(q, d->type, d->Tq) || !tensor_ok(k, d->type, d->Tk) || !tensor_ok(v, d->type, d->Tk) || !tensor_ok(o, d->type, d->Tq) ||
         !tensor_ok(d_o, d->type, d->Tq) || !tensor_ok(dq, d->type, d->Tq) || !tensor_ok(dk, d->type, d->Tk) || !tensor_ok(dv, d->type, d->Tk) ||
         !words_ok(lse, d->Tq) || !words_ok(cu_q, d->B) || !words_ok(cu_k, d->B) || !words_ok(bias, d->buckets)) return CG_EINVAL;
