@@ -377,7 +377,8 @@ int cg_dropout_add_layernorm_bwd(const cg_layernorm_desc *d, const cg_drop *drop
  * others have min(n - 1, E + floor(log(dist / E) / log(max_distance / E) * (n - E))); both: keys behind the query
  * (delta > 0) have the buckets n .. 2n - 1.  n >= 2, buckets <= 256, n / 2 < max_distance <= 65536.
  * *_tok, *_head: elements from a token and from a head to the next.  The strides of o are also those of o_rest and
- * do; those of q, k and v also those of dq, dk and dv.
+ * do; those of q, k and v also those of dq, dk and dv.  What is read may lie in one place several times (a stride of 0); what is written
+ * (o; backward, dq, dk and dv) may not.
  * 1 <= D <= 128; Tq * Hq, Tk * Hkv <= 2^31 - 2^16; tensors may exceed 2^31 bytes.  A launch has room for 2^24 - 1 blocks: enough where
  * Tq * Hq / 128 + B * Hq and, backward, Tk * Hkv / 128 + B * Hkv + Hq * (buckets / 16 + 1) are below 2^24.
  * Arithmetic: bf16 tensors are multiplied as they are, the probabilities and the gradients of the scores

@@ -1,5 +1,6 @@
 // Attention: descriptors, workspaces, the table of the bias by distance, and the order of the launches.
 #include <cmath>
+#include <utility>
 #include "attn_device.h"
 
 namespace cg {
@@ -152,6 +153,20 @@ bool tensor_ok(const void *p, int type, int64_t n)
 {
     return n == 0 || (p && (reinterpret_cast<uintptr_t>(p) & (type == CG_TYPE_FP32 ? 3 : 1)) == 0);
 }
+// May a tensor [T][H][D] of these strides be written: no two of its elements in one place?
+bool strides_ok(int64_t T, int64_t H, int64_t tok, int64_t head, int64_t D)
+{
+    if (T > H) std::swap(T, H), std::swap(tok, head);
+    if (T < 1) return true;
+    if ((T > 1 && tok < D) || (H > 1 && head < D)) return false;
+    if (T == 1 || (tok - D) / head >= H - 1 || (head - D) / tok >= T - 1) return true;      // one inside the other
+    for (int64_t i = 1; i < T; ++i) {       // T <= 2^15.5: i steps of tok, and the steps of head next to them
+        const __int128 at = (__int128)i * tok, n = at / head;
+        for (__int128 j = n; j <= n + 1 && j < H; ++j)
+            if (const __int128 gap = at - j * head; gap < D && -gap < D) return false;
+    }
+    return true;
+}
 bool words_ok(const void *p, int64_t n) { return n == 0 || (p && (reinterpret_cast<uintptr_t>(p) & 3) == 0); }
 
 AttnArgs args_of(const cg_attn_desc &d, const Plan &p, const void *q, const void *k, const void *v, const int32_t *cu_q, const int32_t *cu_k, char *ws)
@@ -212,6 +227,7 @@ extern "C" int cg_attn_fwd(const cg_attn_desc *d, const void *q, const void *k, 
     if (!tensor_ok(q, d->type, 1) || !tensor_ok(k, d->type, d->Tk) || !tensor_ok(v, d->type, d->Tk) || !tensor_ok(o, d->type, 1) || !words_ok(lse, 1) ||
         !words_ok(cu_q, 1) || !words_ok(cu_k, 1) || !words_ok(bias, d->buckets)) return CG_EINVAL;
     if (o_rest && (d->type != CG_TYPE_BF16 || !tensor_ok(o_rest, d->type, 1))) return CG_EINVAL;
+    if (!strides_ok(d->Tq, d->Hq, d->o_tok, d->o_head, d->D)) return CG_EINVAL;
     const Plan p = plan_of(*d, CG_PASS_FWD);
     if (int rc = ws_check(p, ws, ws_bytes)) return rc;
     char *w = static_cast<char *>(ws);
@@ -231,6 +247,8 @@ extern "C" int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q
     if (!tensor_ok(q, d->type, d->Tq) || !tensor_ok(k, d->type, d->Tk) || !tensor_ok(v, d->type, d->Tk) || !tensor_ok(o, d->type, d->Tq) ||
         !tensor_ok(d_o, d->type, d->Tq) || !tensor_ok(dq, d->type, d->Tq) || !tensor_ok(dk, d->type, d->Tk) || !tensor_ok(dv, d->type, d->Tk) ||
         !words_ok(lse, d->Tq) || !words_ok(cu_q, d->B) || !words_ok(cu_k, d->B) || !words_ok(bias, d->buckets)) return CG_EINVAL;
+    if (!strides_ok(d->Tq, d->Hq, d->q_tok, d->q_head, d->D) || !strides_ok(d->Tk, d->Hkv, d->k_tok, d->k_head, d->D) ||
+        !strides_ok(d->Tk, d->Hkv, d->v_tok, d->v_head, d->D)) return CG_EINVAL;
     if ((o_rest && (d->type != CG_TYPE_BF16 || !tensor_ok(o_rest, d->type, 1))) || (dbias && (!d->buckets || !words_ok(dbias, 1)))) return CG_EINVAL;
     const Plan p = plan_of(*d, CG_PASS_BWD_DATA);
     if (int rc = ws_check(p, ws, ws_bytes)) return rc;
