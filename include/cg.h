@@ -398,7 +398,7 @@ typedef struct {
 /* pass: CG_PASS_FWD or CG_PASS_BWD_DATA (0 for an invalid descriptor or pass). */
 size_t cg_attn_workspace_bytes(const cg_attn_desc *d, int pass);
 /* lse [Hq][Tq] fp32.  o_rest (bf16 tensors in a training step; else NULL): what o lost when it was rounded, 16 bits an element
- * in o's layout, for cg_attn_bwd alone (not a bf16 number).  With it, and with a bias or for sequences of 64 keys or fewer on average, the
+ * in o's layout, for cg_attn_bwd alone (not a bf16 number).  With it, and with a bias or for sequences of 64 keys or fewer, the
  * probabilities keep 24 bits in the product with v: the gradient of the bias is a sum of differences that a rounded o would spoil. */
 int cg_attn_fwd(const cg_attn_desc *d, const void *q, const void *k, const void *v, const int32_t *cu_q,
                 const int32_t *cu_k, const float *bias, void *o, float *lse, void *o_rest, void *ws, size_t ws_bytes,

@@ -10,9 +10,12 @@ constexpr float kSlack = 8.f;
 // Prompts are bound by matrix and vector instructions at a clock that power holds to 1.6 .. 1.85 GHz: 8192 tokens, 32 heads on 8, 128 wide,
 // causal, bf16 518 .. 620 us, 890 .. 1060 TFLOP/s (a large library product: 1284).  Single tokens are bound by HBM: 64 sequences of 8192
 // keys, the same heads, 361 us, 5.9 TB/s; fp32 1790, 2.4, since one of the four waves has rows and six products a term.
-// EXACT (bf16 in a training step): the probabilities that o is made of keep 24 bits, in three pieces.  The backward pass subtracts
-// delta, a sum of o times do, from dP; where the differences are added up (the bias's gradient) or rows see a few keys only (sequences
-// of kFewKeys on average), dP is as near to delta as a rounded o is to o.
+// bf16 tensors: probabilities are rounded to 8 bits for the product with V, as they are for P^T do: half a step of the result's type on
+// a term (o is 1.3 to 1.45 times as far from 64 bits as with unrounded ones; a second piece would take half as many products again).
+// The backward pass subtracts delta, a sum of o times do, from dP.  Where the differences are added up (the bias's gradient) or rows see
+// a few keys only, dP is as near to delta as a rounded o is to o: the probabilities that o is made of then keep 24 bits, in three
+// pieces.  With a bias that is a kernel of its own (EXACT); without, the two other pieces' products follow the only tile of a sequence
+// of kFewKeys keys or fewer, so that what a sequence gets does not depend on the others.
 constexpr int kFewKeys = 64;
 template <class T, int DP> constexpr int kFwdWaves = Pieces<T>::N == 1 || DP <= 64 ? 2 : 1;
 
@@ -187,6 +190,34 @@ __global__ __launch_bounds__(256, (kFwdWaves<T, DP>)) void attn_fwd_kernel(AttnA
             if constexpr (BIAS) window[buf ^ 1][threadIdx.x] = bias_next;
         }
     }
+    if constexpr (NP == 1 && !BIAS)
+        if (__builtin_expect(s.m <= kFewKeys && kend > 0 && a.o_rest, 0)) {       // the tile is in the first buffer still; not expected, so that the end of short kernels stays next to their loop
+            static_assert(kFewKeys <= YT, "one tile");
+            const float ms = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                Acc<NP> S;
+                S.zero();
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) S.mma(TileY::rows(ldsK, 32 * u, ks, lane), fq[ks]);
+                float p[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    p[i] = 32 * u + 8 * (i / 4) + 4 * h32 + i % 4 >= limit ? 0.f : __builtin_amdgcn_exp2f(fmaf(S.get(i), c, -ms * c));
+                    p[i] -= to_f32(from_f32<bf16raw>(p[i]));       // what the loop above took
+                }
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const Frag<2> fp = cut8<2>(&p[8 * g]);
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const u32x4 v = TileY::cols(ldsV, 32 * u + 16 * g, dt, lane).p[0];
+                        O[dt] = mfma(v, fp.p[0], O[dt]);
+                        O[dt] = mfma(v, fp.p[1], O[dt]);
+                    }
+                }
+            }
+        }
     l = sum_halves(l);
     if (chunks > 1) {
         if (!here) return;
@@ -222,10 +253,8 @@ template <class T, int DP, bool DMA> int fwd_run(AttnArgs a, hipStream_t s)
     a.fold = fold_of(a, a.Hq / a.Gp, kFwdWaves<T, DP>);
     const dim3 grid((unsigned)(a.Hq / a.Gp) * a.tiles * a.splits);
     constexpr bool can = sizeof(T) == 2;
-    const bool exact = can && a.o_rest && (a.btab || a.Tk <= (int64_t)kFewKeys * a.B);
-    if (exact && a.btab) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, true, DMA, can>), grid, dim3(256), 0, s, a);
-    else if (exact) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, false, DMA, can>), grid, dim3(256), 0, s, a);
-    else if (!a.btab) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, false, DMA, false>), grid, dim3(256), 0, s, a);
+    if (!a.btab) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, false, DMA, false>), grid, dim3(256), 0, s, a);
+    else if (can && a.o_rest) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, true, DMA, can>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_fwd_kernel<T, DP, true, DMA, false>), grid, dim3(256), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
