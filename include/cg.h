@@ -381,8 +381,10 @@ int cg_dropout_add_layernorm_bwd(const cg_layernorm_desc *d, const cg_drop *drop
  * (o; backward, dq, dk and dv) may not.
  * 1 <= D <= 128; Tq * Hq, Tk * Hkv <= 2^31 - 2^16; tensors may exceed 2^31 bytes.  A launch has room for 2^24 - 1 blocks: enough where
  * Tq * Hq / 128 + B * Hq and, backward, Tk * Hkv / 128 + B * Hkv + Hq * (buckets / 16 + 1) are below 2^24.
- * Arithmetic: bf16 tensors are multiplied as they are, the probabilities and the gradients of the scores
- * rounded to bf16 for their products; fp32 tensors as three bf16 numbers in six products (CG_MATH_FP32 above).
+ * Arithmetic: bf16 tensors are multiplied as they are, the probabilities and the gradients of the scores rounded to bf16 for
+ * their products; in two bf16 numbers where the terms are few: dq of a sequence of 64 keys or fewer, dk and dv of one of 32 query rows
+ * or fewer (tokens times the heads that share keys, without a bias; tokens with one).  fp32 tensors are multiplied as three bf16 numbers
+ * in six products (CG_MATH_FP32 above).
  * Sequences that overlap or reach past Tq, Tk are cut there; rows of no sequence are neither read nor written.
  * A q, k or v that is not finite makes what sees it not finite; within its own sequence it may do so to rows that a causal mask
  * or a bias of -inf keeps from it as well (0 times it), never in another sequence. */

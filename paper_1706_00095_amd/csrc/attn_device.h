@@ -52,6 +52,7 @@ struct AttnArgs {
 constexpr int kAttnRows = 128;             // X rows of a block: four waves of 32
 constexpr int kAttnMaxD = 128;
 constexpr int kMaxBuckets = 256;
+constexpr int kFewKeys = 64, kFewRows = 32;       // keys, and query rows, of a sequence whose products keep more bits (attn_fwd.hip, attn_bwd.hip)
 constexpr int attn_dkdv_yt(bool bf16, int DP) { return bf16 && DP < 128 ? 64 : 32; }
 
 // May the loaders that go by buffers take rows of these strides (elements)?  `per`: heads packed as rows (a tile of 32 begins with

@@ -16,7 +16,6 @@ constexpr float kSlack = 8.f;
 // a few keys only, dP is as near to delta as a rounded o is to o: the probabilities that o is made of then keep 24 bits, in three
 // pieces.  With a bias that is a kernel of its own (EXACT); without, the two other pieces' products follow the only tile of a sequence
 // of kFewKeys keys or fewer, so that what a sequence gets does not depend on the others.
-constexpr int kFewKeys = 64;
 template <class T, int DP> constexpr int kFwdWaves = Pieces<T>::N == 1 || DP <= 64 ? 2 : 1;
 
 template <class T, int DP, bool BIAS, bool DMA, bool EXACT>

@@ -34,8 +34,15 @@ def pieces(x, n):
     return got
 
 
-def dq_with(vals, lens, scale, causal, p_pieces):
-    """dq (before its own rounding) where the probabilities of the forward product have `p_pieces` bf16 numbers; the rest in 64 bits."""
+def unrounded_bounds(vals, lens_q, lens_k, scale, causal, bias=None, far=0):
+    """The plain form with the tolerances of probabilities and dS that keep 16 bits or more in all products (2^-18 of themselves, the 64
+    roundings of 2^-24 that sublayer_util.Attention allows a product's sum in fp32), where only results are rounded to bf16."""
+    n = bias.shape[1] if bias is not None else 0
+    return Attention(*vals, lens_q, lens_k, scale, causal, bias, n, far, not causal, torch.float32, False)
+
+
+def dq_with(vals, lens, scale, causal, p_pieces, ds_pieces=9):
+    """dq (before its own rounding) where the probabilities of the forward product, and dS, have so many bf16 numbers; the rest in 64 bits."""
     q, k, v, do = vals
     dq, at = torch.zeros_like(q), 0
     for n in lens:
@@ -46,7 +53,7 @@ def dq_with(vals, lens, scale, causal, p_pieces):
             p = torch.exp(S - S.amax(1, keepdim=True))
             l = p.sum(1, keepdim=True)
             delta = (do[s, h] * (pieces(p, p_pieces) @ v[s, h] / l)).sum(1, keepdim=True)
-            dq[s, h] = (p / l * (do[s, h] @ v[s, h].T - delta)) @ k[s, h] * scale
+            dq[s, h] = pieces(p / l * (do[s, h] @ v[s, h].T - delta), ds_pieces) @ k[s, h] * scale
         at += n
     return dq
 

@@ -3,7 +3,7 @@ probabilities, or whose o, have fewer bits."""
 import pytest
 import torch
 
-from precision_util import BF, RMS, dq_with, few_keys_bounds, few_keys_values, outer_differences, pieces, three_tokens
+from precision_util import BF, RMS, dq_with, few_keys_bounds, few_keys_values, outer_differences, pieces, three_tokens, unrounded_bounds
 from sublayer_util import half_step
 
 
@@ -18,6 +18,20 @@ def test_few_keys_need_more_than_8_bits(causal):
     assert not any(bool(x.any()) for n in (2, 3) for x in outside(dq_with(vals, lens, 0.125, causal, n)))
     for n, x in zip(lens, outside(dq_with(vals, lens, 0.125, causal, 1))):
         assert n < 5 or bool(x.any()), n
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_few_keys_need_more_than_8_bits_of_the_scores_gradients(causal):
+    lens = [5, 64, 33, 2, 40]
+    g = torch.Generator().manual_seed(1)
+    vals = [torch.empty(sum(lens), 2, 64, dtype=torch.float64).normal_(0, 1, generator=g).to(BF).double() for _ in range(4)]
+    a = unrounded_bounds(vals, lens, lens, 0.125, causal)
+
+    def outside(n):
+        dq = dq_with(vals, lens, 0.125, causal, 3, n)
+        return ((dq - a.dq).abs() > half_step(BF) * (a.dq.abs() + a.tol_dq) + a.tol_dq).any(2).any(1).split(lens)
+    assert not any(bool(x.any()) for x in outside(2))
+    assert all(bool(x.any()) for n, x in zip(lens, outside(1)) if n >= 5)
 
 
 @pytest.mark.parametrize("D", [8, 64])
