@@ -5,8 +5,8 @@
 // bf16 tensors: dS is rounded to 8 bits for dS K and dS^T Q, P for P^T do, half a step of the results' type on a term, which many terms
 // average (results are 1.4 times as far from 64 bits as if only they were rounded; second pieces would take three products
 // for two).  A few terms do not average: where a sequence has kFewKeys keys or fewer (dq), or kFewRows query rows or fewer (dk, dv), what
-// rounding left is multiplied too, behind the loop, from the tile that is in LDS still.  512 texts of 32, 12 heads of 64: dq 96 -> 101 us,
-// dk/dv 117 -> 130; calls without such sequences are as fast as before.  Lanes' numbers are made anew there, lest the loop keep
+// rounding left is multiplied too, behind the loop, from the tile that is in LDS still.  512 texts of 32, 12 heads of 64: dq 96 -> 102 us,
+// dk/dv 117 -> 126; calls without such sequences are as fast as without it.  Lanes' numbers are made anew there, lest the loop keep
 // addresses for it in registers.
 #include "attn_device.h"
 
@@ -593,50 +593,64 @@ __global__ __launch_bounds__(256, (kDkdvWaves<T, DP>)) void attn_dkdv_kernel(Att
             }
         }
         if constexpr (NP == 1)
-            if (__builtin_expect(rows <= kFewRows && key0 + 32 * wave < s.m, 0)) {       // the tiles are in their buffers
+            if (__builtin_expect(rows <= kFewRows && begin < end && key0 + 32 * wave < s.m, 0)) {       // the rows are in the first buffers
                 int ln = lane;
                 asm("" : "+v"(ln));
+                int y = begin;
                 const int hf = ln >> 5;
-                static_assert(kFewRows <= 2 * YT, "two buffers");
 #pragma unroll 1
-                for (int y = max(begin, wave_first / 32 * 32); y < rows; y += 32) {
-                    const int of = (last - y + YT - 1) / YT & 1, u32 = y & (YT - 32);
-                    LdsByte *const q = ldsQ + of * TileY::BYTES, *const o = ldsO + of * TileY::BYTES;
+                do {
                     Acc<NP> S, P;
                     S.zero();
                     P.zero();
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) {
-                        S.mma(TileY::rows(q, u32, ks, ln), fk[ks]);
-                        if constexpr (V_IN_LDS) P.mma(TileY::rows(o, u32, ks, ln), TileX::rows(ldsV, 32 * wave, ks, ln));
-                        else P.mma(TileY::rows(o, u32, ks, ln), fv[ks]);
+                        S.mma(TileY::rows(ldsQ, 0, ks, ln), fk[ks]);
+                        if constexpr (V_IN_LDS) P.mma(TileY::rows(ldsO, 0, ks, ln), TileX::rows(ldsV, 32 * wave, ks, ln));
+                        else P.mma(TileY::rows(ldsO, 0, ks, ln), fv[ks]);
                     }
+                    reads_ahead<2 * KS, 6, V_IN_LDS ? 2 : 1>();
                     float p[16], ds[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int at = 8 * (i / 4) + 4 * hf + i % 4;
-                        float x;
-                        if constexpr (BIAS) {
-                            x = fmaf(S.get(i), a.scale, window[of][32 * wave + (ln & 31) - (u32 + at) + YT - 1]);
-                            x = __builtin_amdgcn_exp2f(fmaf(x - stats[of][0][u32 + at], kLog2e, -stats[of][STATS - 1][u32 + at]));
-                        } else x = __builtin_amdgcn_exp2f(fmaf(S.get(i), c, -stats[of][0][u32 + at]));
-                        if (y + at < first_row || y + at >= rows) x = 0.f;
-                        p[i] = x;
-                        ds[i] = x * (P.get(i) - stats[of][1][u32 + at]);
-                        p[i] -= to_f32(from_f32<bf16raw>(p[i]));
-                        ds[i] -= to_f32(from_f32<bf16raw>(ds[i]));
+                    for (int j = 0; j < 4; ++j) {
+                        const int at = 8 * j + 4 * hf;
+                        const float4 l4 = *reinterpret_cast<const float4 *>(stats[0][0] + at), d4 = *reinterpret_cast<const float4 *>(stats[0][1] + at);
+                        const float4 g4 = BIAS ? *reinterpret_cast<const float4 *>(stats[0][STATS - 1] + at) : float4{};
+                        const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w}, log_l[4] = {g4.x, g4.y, g4.z, g4.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float x;
+                            if constexpr (BIAS) {
+                                x = fmaf(S.get(4 * j + i), a.scale, window[0][32 * wave + (ln & 31) - (at + i) + YT - 1]);
+                                x = __builtin_amdgcn_exp2f(fmaf(x - l[i], kLog2e, -log_l[i]));
+                            } else x = __builtin_amdgcn_exp2f(fmaf(S.get(4 * j + i), c, -l[i]));
+                            p[4 * j + i] = x;
+                            ds[4 * j + i] = x * (P.get(4 * j + i) - d[i]);
+                        }
                     }
+                    if (wave_all > 0 || BIAS)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int r = 8 * (i / 4) + i % 4;
+                            if (r < first_row - 4 * hf || (BIAS && r >= rows - 4 * hf)) p[i] = 0.f, ds[i] = 0.f;
+                        }
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int i = 8 * e; i < 8 * e + 8; ++i) {
+                            p[i] -= to_f32(from_f32<bf16raw>(p[i]));
+                            ds[i] -= to_f32(from_f32<bf16raw>(ds[i]));
+                        }
                         const Frag<NP> fp = cut8<NP>(&p[8 * e]), fds = cut8<NP>(&ds[8 * e]);
 #pragma unroll
                         for (int dt = 0; dt < DT; ++dt) {
-                            dV[dt] = mfma(TileY::cols(o, u32 + 16 * e, dt, ln).p[0], fp.p[0], dV[dt]);
-                            dK[dt] = mfma(TileY::cols(q, u32 + 16 * e, dt, ln).p[0], fds.p[0], dK[dt]);
+                            dV[dt] = mfma(TileY::cols(ldsO, 16 * e, dt, ln).p[0], fp.p[0], dV[dt]);
+                            dK[dt] = mfma(TileY::cols(ldsQ, 16 * e, dt, ln).p[0], fds.p[0], dK[dt]);
                         }
                     }
-                }
+                } while (!BIAS && (y += 32) < rows);       // one turn; told so, the compiler spills in the loop above at 128 wide (600 -> 680 us)
             }
+        if constexpr (!BIAS && NP == 1) break;       // all heads that share the keys are one problem
     }
     if (key >= s.m) return;
     if (chunks * a.gsplit > 1) {

@@ -190,11 +190,12 @@ __global__ __launch_bounds__(256, (kFwdWaves<T, DP>)) void attn_fwd_kernel(AttnA
         }
     }
     if constexpr (NP == 1 && !BIAS)
-        if (__builtin_expect(s.m <= kFewKeys && kend > 0 && a.o_rest, 0)) {       // the tile is in the first buffer still; not expected, so that the end of short kernels stays next to their loop
+        if (__builtin_expect(s.m <= kFewKeys && wave_kend > 0 && a.o_rest, 0)) {       // the tile is in the first buffer still; not expected, so that the end of short kernels stays next to their loop
             static_assert(kFewKeys <= YT, "one tile");
             const float ms = m == -INFINITY ? 0.f : m;
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
+                if (32 * u >= wave_kend) break;
                 Acc<NP> S;
                 S.zero();
 #pragma unroll
