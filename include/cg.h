@@ -385,7 +385,8 @@ int cg_dropout_add_layernorm_bwd(const cg_layernorm_desc *d, const cg_drop *drop
  * their products; in two bf16 numbers where the terms are few: dq of a sequence of 64 keys or fewer, dk and dv of one of 32 query rows
  * or fewer (tokens times the heads that share keys, without a bias; tokens with one).  fp32 tensors are multiplied as three bf16 numbers
  * in six products (CG_MATH_FP32 above).
- * Sequences that overlap or reach past Tq, Tk are cut there; rows of no sequence are neither read nor written.
+ * Sequences that reach past Tq, Tk are cut there; rows of no sequence are neither read nor written.  With numbers that do not
+ * ascend nothing outside the tensors is read or written either, but what the outputs hold is not defined.
  * A q, k or v that is not finite makes what sees it not finite; within its own sequence it may do so to rows that a causal mask
  * or a bias of -inf keeps from it as well (0 times it), never in another sequence. */
 typedef struct {

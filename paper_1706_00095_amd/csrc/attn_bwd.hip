@@ -67,7 +67,7 @@ constexpr float kFar = 1024.f;
 
 // dq, delta and the bias's gradient.  A block takes 128 query rows (X) and walks the keys (Y) they see, as the forward kernel does; the row's
 // statistics are known, so a tile is S, dP, dS and dS K: three products.  Bound as the forward kernel: 4 x 4096, 16 heads of 128, causal,
-// bf16 450 us, 915 TFLOP/s; 2862 packed tokens, 12 heads of 64, with a bias 43 us, of which the sums along diagonals are 8.
+// bf16 450 us, 915 TFLOP/s; 2862 packed tokens, 12 heads of 64, with a bias 45 us, of which the sums along diagonals are 8.
 // Waves a SIMD: two where registers and LDS (the squares of the bias's gradient take 36 KB) allow them.
 template <class T, int DP, bool BIAS> constexpr int kDqWaves = (Pieces<T>::N == 1 ? !BIAS || DP <= 64 : DP <= (BIAS ? 32 : 64)) ? 2 : 1;
 

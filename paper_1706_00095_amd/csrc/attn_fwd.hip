@@ -7,11 +7,11 @@ namespace {
 constexpr float kSlack = 8.f;
 
 // A block takes 128 query rows (X) of one problem and walks the keys (Y) they see in tiles of YT.
-// Prompts are bound by matrix and vector instructions at a clock that power holds to 1.6 .. 1.85 GHz: 8192 tokens, 32 heads on 8, 128 wide,
-// causal, bf16 518 .. 620 us, 890 .. 1060 TFLOP/s (a large library product: 1284).  Single tokens are bound by HBM: 64 sequences of 8192
+// Prompts are bound by matrix and vector instructions at a clock that power holds to 1.7 .. 1.8 GHz (the matrix pipeline 56 % busy): 8192
+// tokens, 32 heads on 8, 128 wide, causal, bf16 525 .. 600 us, 920 .. 1050 TFLOP/s (a large library product: 1284).  Single tokens are bound by HBM: 64 sequences of 8192
 // keys, the same heads, 361 us, 5.9 TB/s; fp32 1790, 2.4, since one of the four waves has rows and six products a term.
 // bf16 tensors: probabilities are rounded to 8 bits for the product with V, as they are for P^T do: half a step of the result's type on
-// a term (o is 1.3 to 1.45 times as far from 64 bits as with unrounded ones; a second piece would take half as many products again).
+// a term (o is 1.2 to 1.4 times as far from 64 bits as with unrounded ones; a second piece would take half as many products again).
 // The backward pass subtracts delta, a sum of o times do, from dP.  Where the differences are added up (the bias's gradient) or rows see
 // a few keys only, dP is as near to delta as a rounded o is to o: the probabilities that o is made of then keep 24 bits, in three
 // pieces.  With a bias that is a kernel of its own (EXACT); without, the two other pieces' products follow the only tile of a sequence

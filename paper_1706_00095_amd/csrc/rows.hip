@@ -244,7 +244,8 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(NormArgs a)
 // dx of a row needs two sums over it, <g> and <g xh> with g = dy gamma; dgamma and dbeta are sums over the rows, which each
 // thread keeps for its columns over all the rows that its block takes.  Blocks write their sums to `part`; sum_parts_kernel adds
 // them in order, so results do not depend on scheduling.
-// Bound by HBM: 16384 x 2048 bf16 40 us (5.0 TB/s); joined, 8192 x 4096 bf16, 62 (4.3); the sums of the blocks' sums 4 to 7.
+// Bound by HBM: 16384 x 2048 bf16 40 us (5.0 TB/s); joined, 8192 x 4096 bf16, 62 (4.3); the sums of the blocks' sums 4 to 7.  With four
+// chunks a thread in fp32 (8193 to 16384 columns) 13 to 15 registers are spilled.
 template <class T, int LANES, int CPT, int JOIN, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(NormBwdArgs a)
 {
