@@ -414,6 +414,62 @@ int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q, const voi
                 const int32_t *cu_k, const float *bias, const void *o, const void *o_rest, const float *lse, void *dq,
                 void *dk, void *dv, float *dbias, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- the operators of a block over tokens ---------------------------------
+ *
+ * The way in (embedding), linear layers with what follows the product in its epilogue, and activations
+ * kept for the backward pass in 8 bits.  Types, strides and order of sums are those of the operators above:
+ * fp32 or bf16 tensors of rows that may lie in wider ones, biases and gradients of weights in dense fp32. */
+
+/* y[t] = scale * table[tokens[t]], table [vocab][cols] of `table_type`, y [tokens][cols] of `type`; a token outside
+ * 0 .. vocab - 1 is none: its row of y is zero and it has no gradient.  tokens: device array.  vocab, cols >= 1; tokens = 0: fwd is a no-op.
+ * tokens <= 2^28, tokens * ceil(cols / 8) < 2^30. */
+typedef struct { int table_type, type; int64_t vocab, cols, tokens; float scale; } cg_embedding_desc;
+int cg_embedding_fwd(const cg_embedding_desc *d, const int32_t *tokens, const void *table, int64_t table_ld, void *y, int64_t y_ld,
+                     void *stream);
+size_t cg_embedding_workspace_bytes(const cg_embedding_desc *d);      /* of the backward pass; 0 for an invalid descriptor */
+/* dtable[v] = scale * sum over t with tokens[t] = v, in order of t, of dy[t]; [vocab][cols] fp32, every row written (zeros where
+ * there is none).  ws: 16-byte aligned. */
+int cg_embedding_bwd(const cg_embedding_desc *d, const int32_t *tokens, const void *dy, int64_t dy_ld, float *dtable, void *ws,
+                     size_t ws_bytes, void *stream);
+
+/* A tensor [rows][cols] in 8 bits: 32 neighbours of a row (the last block of a row may be shorter) share a power of two,
+ *     x[r][c] ~ codes[r][c] * 2^(scales[r][c / 32] - 133),   codes rounded to the nearest (halves to even), -127 .. 127,
+ * with the smallest power, 2^-133 or above, that the block's largest magnitude allows: it is off by 1/127 of that magnitude at
+ * most, by 1/254 where it is least.  What is not finite has the code -128 and comes back as NaN; the others of its block are as if it were 0.
+ * Every value is a bf16 number.  *_ld: elements from a row to the next; no alignment is asked for.
+ * rows * ceil(cols / 32) <= 2^29 - 2^16. */
+typedef struct { int8_t *codes; int64_t codes_ld; uint8_t *scales; int64_t scales_ld; } cg_packed8;
+int cg_pack8(int type, int64_t rows, int64_t cols, const void *x, int64_t x_ld, const cg_packed8 *p, void *stream);
+int cg_unpack8(int type, int64_t rows, int64_t cols, const cg_packed8 *p, void *y, int64_t y_ld, void *stream);
+
+/* A linear layer over M tokens: x [M][K], w [N][K], y [M][N].
+ *     z = x w^T + bias,   y = act(z) + residual;
+ *     dx = (dz w) * act_in'(z_in) + add,   dw = dz^T x,   dbias = sum over tokens of dz.
+ * act: NONE, RELU, GELU (z Phi(z)) or SILU (z / (1 + e^-z)).  act_in is the activation that made x out of z_in: with it the backward pass
+ * leaves the gradient of z_in, which is the dz of the layer that z_in came from; NONE: of x itself.  RELU'(0) = 0.
+ * M >= 0, N, K >= 1, each at most 2^31 - 2^16; of the products of two of them, tiles of 128 x 128, 2^22 at most; tensors may exceed 2^31 bytes.
+ * Arithmetic: bf16 tensors are multiplied as they are and summed in fp32.  fp32 tensors are multiplied as three bf16 numbers in six products
+ * (CG_MATH_FP32 above), up to 32 tokens forward in fp32 multiply-adds; what meets an operand that is not finite is not finite, as NaN where
+ * multiply-adds may give an infinity. */
+enum { CG_ACT_NONE = 0, CG_ACT_RELU = 1, CG_ACT_GELU = 2, CG_ACT_SILU = 3 };
+typedef struct { int type; int64_t M, N, K; int act, act_in; } cg_linear_desc;
+/* pass: CG_PASS_FWD, CG_PASS_BWD_DATA or CG_PASS_BWD_WEIGHT; 0 for an invalid descriptor or pass.  Workspaces are 16-byte aligned. */
+size_t cg_linear_workspace_bytes(const cg_linear_desc *d, int pass);
+/* bias, residual, z: NULL: none (z: the pre-activation, rounded to `type`, kept for the backward pass). */
+int cg_linear_fwd(const cg_linear_desc *d, const void *x, int64_t x_ld, const void *w, int64_t w_ld, const float *bias, const void *residual,
+                  int64_t residual_ld, void *y, int64_t y_ld, void *z, int64_t z_ld, void *ws, size_t ws_bytes, void *stream);
+/* With an act_in, z_in [M][K] as a tensor or in 8 bits (the other NULL); without, both are ignored.  add: a gradient that reaches the
+ * same place past this layer (NULL: none). */
+int cg_linear_bwd_data(const cg_linear_desc *d, const void *dz, int64_t dz_ld, const void *w, int64_t w_ld, const void *z_in, int64_t z_in_ld,
+                       const cg_packed8 *z_in8, const void *add, int64_t add_ld, void *dx, int64_t dx_ld, void *ws, size_t ws_bytes, void *stream);
+/* x as a tensor or in 8 bits (the other NULL).  dw [N][K], dbias [N] (NULL: not wanted).  M = 0 gives zeros. */
+int cg_linear_bwd_weight(const cg_linear_desc *d, const void *dz, int64_t dz_ld, const void *x, int64_t x_ld, const cg_packed8 *x8, float *dw,
+                         float *dbias, void *ws, size_t ws_bytes, void *stream);
+/* dz = dy * act'(z), z as a tensor or in 8 bits (the other NULL): the gradient through an activation whose output goes elsewhere than into
+ * a linear layer.  rows * ceil(cols / 8) < 2^30. */
+int cg_act_bwd(int act, int type, int64_t rows, int64_t cols, const void *dy, int64_t dy_ld, const void *z, int64_t z_ld, const cg_packed8 *z8,
+               void *dz, int64_t dz_ld, void *stream);
+
 const char *cg_strerror(int code);
 const char *cg_version(void);
 int cg_last_hip_error(void);   /* hipError_t of the most recent CG_EHIP on this thread */

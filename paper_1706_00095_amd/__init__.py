@@ -18,6 +18,8 @@ CG_PASS_FWD, CG_PASS_BWD_DATA, CG_PASS_BWD_WEIGHT = 0, 1, 2
 CG_STEP_OVERLAP, CG_STEP_SERIAL, CG_STEP_JOIN, CG_STEP_TREE_SUM, CG_STEP_BF16, CG_STEP_BF16X3 = 0, 1, 2, 4, 8, 16
 CG_MATH_FP32, CG_MATH_BF16, CG_MATH_BF16X3 = 0, 1, 2
 CG_TYPE_FP32, CG_TYPE_BF16 = 0, 1
+CG_ACT_NONE, CG_ACT_RELU, CG_ACT_GELU, CG_ACT_SILU = 0, 1, 2, 3
+ACTS = {"none": CG_ACT_NONE, "relu": CG_ACT_RELU, "gelu": CG_ACT_GELU, "silu": CG_ACT_SILU}
 CG_MAX_PEERS = 64
 CG_NOALLOC_SCRATCH_BYTES = 64 << 20
 LAYER_KINDS = {"conv": 0, "relu": 1, "lrn": 2, "maxpool": 3, "avgpool": 4, "fc": 5, "dropout": 6,
@@ -32,6 +34,8 @@ EXPORTS = [
     "cg_dropout_fwd", "cg_dropout_bwd", "cg_layernorm_fwd", "cg_layernorm_workspace_bytes", "cg_layernorm_bwd",
     "cg_dropout_add_layernorm_fwd", "cg_dropout_add_layernorm_bwd",
     "cg_attn_workspace_bytes", "cg_attn_fwd", "cg_attn_bwd",
+    "cg_embedding_fwd", "cg_embedding_workspace_bytes", "cg_embedding_bwd", "cg_pack8", "cg_unpack8",
+    "cg_linear_workspace_bytes", "cg_linear_fwd", "cg_linear_bwd_data", "cg_linear_bwd_weight", "cg_act_bwd",
 ]
 
 
@@ -71,6 +75,19 @@ class cg_attn_desc(C.Structure):
                 ("q_tok", C.c_int64), ("q_head", C.c_int64), ("k_tok", C.c_int64), ("k_head", C.c_int64),
                 ("v_tok", C.c_int64), ("v_head", C.c_int64), ("o_tok", C.c_int64), ("o_head", C.c_int64),
                 ("scale", C.c_float), ("causal", C.c_int), ("buckets", C.c_int), ("max_distance", C.c_int), ("both", C.c_int)]
+
+
+class cg_embedding_desc(C.Structure):
+    _fields_ = [("table_type", C.c_int), ("type", C.c_int), ("vocab", C.c_int64), ("cols", C.c_int64), ("tokens", C.c_int64),
+                ("scale", C.c_float)]
+
+
+class cg_packed8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("codes_ld", C.c_int64), ("scales", C.c_void_p), ("scales_ld", C.c_int64)]
+
+
+class cg_linear_desc(C.Structure):
+    _fields_ = [("type", C.c_int), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("act", C.c_int), ("act_in", C.c_int)]
 
 
 class cg_profile_record(C.Structure):
@@ -141,6 +158,19 @@ def lib():
         L.cg_attn_workspace_bytes.restype = sz
         L.cg_attn_fwd.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.cg_attn_bwd.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        ep, pp, lp = C.POINTER(cg_embedding_desc), C.POINTER(cg_packed8), C.POINTER(cg_linear_desc)
+        L.cg_embedding_fwd.argtypes = [ep, vp, vp, i64, vp, i64, vp]
+        L.cg_embedding_workspace_bytes.argtypes = [ep]
+        L.cg_embedding_workspace_bytes.restype = sz
+        L.cg_embedding_bwd.argtypes = [ep, vp, vp, i64, vp, vp, sz, vp]
+        L.cg_pack8.argtypes = [C.c_int, i64, i64, vp, i64, pp, vp]
+        L.cg_unpack8.argtypes = [C.c_int, i64, i64, pp, vp, i64, vp]
+        L.cg_linear_workspace_bytes.argtypes = [lp, C.c_int]
+        L.cg_linear_workspace_bytes.restype = sz
+        L.cg_linear_fwd.argtypes = [lp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, sz, vp]
+        L.cg_linear_bwd_data.argtypes = [lp, vp, i64, vp, i64, vp, i64, pp, vp, i64, vp, i64, vp, sz, vp]
+        L.cg_linear_bwd_weight.argtypes = [lp, vp, i64, vp, i64, pp, vp, vp, vp, sz, vp]
+        L.cg_act_bwd.argtypes = [C.c_int, C.c_int, i64, i64, vp, i64, vp, i64, pp, vp, i64, vp]
         L.cg_strerror.argtypes = [C.c_int]
         L.cg_strerror.restype = C.c_char_p
         L.cg_version.restype = C.c_char_p
@@ -450,6 +480,136 @@ def cg_attn_bwd(d, d_o, q, k, v, cu_q, cu_k, bias, o, o_rest, lse, dq, dk, dv, d
                              _heads(t, of_q, o_steps, o, "o"), _heads(t, of_q, o_steps, o_rest, "o_rest"), _weights(lse, d.Hq * d.Tq, "lse"),
                              _heads(t, of_q, q_steps, dq, "dq"), _heads(t, of_k, k_steps, dk, "dk"), _heads(t, of_k, v_steps, dv, "dv"),
                              _weights(dbias, n, "dbias"), *_ws_args(ws), _stream(stream)), "cg_attn_bwd")
+
+
+# ---- the operators of a block over tokens ----
+
+def embedding_desc(table, y, scale=1.0):
+    """Descriptor for a table [vocab][cols] and rows y [tokens][cols]; each in fp32 or bf16."""
+    if table.dim() != 2 or y.dim() != 2 or table.shape[1] != y.shape[1]:
+        raise ValueError("expected a table [vocab][cols] and y [tokens][cols]")
+    return cg_embedding_desc(_type_of(table), _type_of(y), table.shape[0], table.shape[1], y.shape[0], scale)
+
+
+def _tokens(t, n):
+    if not t.is_cuda or t.dtype is not torch.int32 or not t.is_contiguous() or t.numel() != n:
+        raise TypeError(f"tokens: expected a contiguous device tensor of {n} int32")
+    return t.data_ptr()
+
+
+def _matrix(t, type_, shape, what):
+    """(pointer, elements from a row to the next) of a tensor [rows][cols] of a descriptor's type; its rows may lie in wider ones."""
+    if t is None:
+        return None, 0
+    if t.dtype is not _DTYPES.get(type_) or not t.is_cuda:
+        raise TypeError(f"{what}: expected a device tensor of the descriptor's type")
+    if t.shape != shape:
+        raise ValueError(f"{what}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        raise ValueError(f"{what}: the elements of a row have to lie next to each other")
+    return t.data_ptr(), (ld if shape[0] > 1 else shape[1])
+
+
+def cg_embedding_fwd(d, tokens, table, y, stream=None):
+    _check(lib().cg_embedding_fwd(d, _tokens(tokens, d.tokens), *_matrix(table, d.table_type, (d.vocab, d.cols), "table"),
+                                  *_matrix(y, d.type, (d.tokens, d.cols), "y"), _stream(stream)), "cg_embedding_fwd")
+
+
+def cg_embedding_workspace_bytes(d):
+    return int(lib().cg_embedding_workspace_bytes(d))
+
+
+def cg_embedding_bwd(d, tokens, dy, dtable, ws, stream=None):
+    _check(lib().cg_embedding_bwd(d, _tokens(tokens, d.tokens), *_matrix(dy, d.type, (d.tokens, d.cols), "dy"),
+                                  _weights(dtable, d.vocab * d.cols, "dtable"), *_ws_args(ws), _stream(stream)), "cg_embedding_bwd")
+
+
+class Packed8:
+    """A tensor [rows][cols] in 8 bits: codes [rows][cols] int8 and scales [rows][ceil(cols / 32)] uint8, whose rows may lie in wider ones."""
+
+    def __init__(self, codes, scales):
+        rows, cols = codes.shape
+        if codes.dtype is not torch.int8 or scales.dtype is not torch.uint8 or not codes.is_cuda or not scales.is_cuda:
+            raise TypeError("expected device tensors: codes of int8, scales of uint8")
+        if scales.shape != (rows, (cols + 31) // 32):
+            raise ValueError(f"scales: expected the shape {(rows, (cols + 31) // 32)}, got {tuple(scales.shape)}")
+        if (codes.stride(1) != 1 and cols > 1) or (scales.stride(1) != 1 and cols > 32):
+            raise ValueError("the elements of a row have to lie next to each other")
+        self.codes, self.scales, self.shape = codes, scales, codes.shape
+        self.arg = cg_packed8(codes.data_ptr(), codes.stride(0) if rows > 1 else cols, scales.data_ptr(), scales.stride(0) if rows > 1 else (cols + 31) // 32)
+
+
+def packed8_like(x):
+    """Room for x [rows][cols] in 8 bits, on its device."""
+    rows, cols = x.shape
+    return Packed8(torch.empty(rows, cols, dtype=torch.int8, device=x.device), torch.empty(rows, (cols + 31) // 32, dtype=torch.uint8, device=x.device))
+
+
+def _packed(p, shape, what):
+    if p.shape != shape:
+        raise ValueError(f"{what}: expected the shape {tuple(shape)}, got {tuple(p.shape)}")
+    return p.arg
+
+
+def cg_pack8(x, p, stream=None):
+    code = _type_of(x)
+    _check(lib().cg_pack8(code, *p.shape, *_matrix(x, code, p.shape, "x"), p.arg, _stream(stream)), "cg_pack8")
+
+
+def cg_unpack8(p, y, stream=None):
+    code = _type_of(y)
+    _check(lib().cg_unpack8(code, *p.shape, p.arg, *_matrix(y, code, p.shape, "y"), _stream(stream)), "cg_unpack8")
+
+
+def linear_desc(x, w, act="none", act_in="none"):
+    """Descriptor of a linear layer on x [M][K] with the weights w [N][K]; act, act_in: "none", "relu", "gelu" or "silu"."""
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
+        raise ValueError("expected x [tokens][inputs] and w [outputs][inputs]")
+    if x.dtype is not w.dtype:
+        raise TypeError("x and w have to be of one type")
+    return cg_linear_desc(_type_of(x), x.shape[0], w.shape[0], x.shape[1], ACTS[act], ACTS[act_in])
+
+
+def cg_linear_workspace_bytes(d, which):
+    return int(lib().cg_linear_workspace_bytes(d, which))
+
+
+def cg_linear_fwd(d, x, w, bias, residual, y, z=None, ws=None, stream=None):
+    """y = act(x w^T + bias) + residual; z (None: not kept): x w^T + bias."""
+    t, of_y = d.type, (d.M, d.N)
+    _check(lib().cg_linear_fwd(d, *_matrix(x, t, (d.M, d.K), "x"), *_matrix(w, t, (d.N, d.K), "w"), _weights(bias, d.N, "bias"),
+                               *_matrix(residual, t, of_y, "residual"), *_matrix(y, t, of_y, "y"), *_matrix(z, t, of_y, "z"), *_ws_args(ws),
+                               _stream(stream)), "cg_linear_fwd")
+
+
+def _either(t, type_, shape, what):
+    """(pointer, stride, packed) of what is a tensor or a Packed8."""
+    if isinstance(t, Packed8):
+        return None, 0, _packed(t, shape, what)
+    return *_matrix(t, type_, shape, what), None
+
+
+def cg_linear_bwd_data(d, dz, w, z_in, add, dx, ws=None, stream=None):
+    """dx = (dz w) * act_in'(z_in) + add; z_in: a tensor, a Packed8 or (act_in "none") None."""
+    t, of_x = d.type, (d.M, d.K)
+    _check(lib().cg_linear_bwd_data(d, *_matrix(dz, t, (d.M, d.N), "dz"), *_matrix(w, t, (d.N, d.K), "w"), *_either(z_in, t, of_x, "z_in"),
+                                    *_matrix(add, t, of_x, "add"), *_matrix(dx, t, of_x, "dx"), *_ws_args(ws), _stream(stream)),
+           "cg_linear_bwd_data")
+
+
+def cg_linear_bwd_weight(d, dz, x, dw, dbias, ws=None, stream=None):
+    """dw = dz^T x, dbias (None: not wanted) = sum of dz; x: a tensor or a Packed8."""
+    t = d.type
+    _check(lib().cg_linear_bwd_weight(d, *_matrix(dz, t, (d.M, d.N), "dz"), *_either(x, t, (d.M, d.K), "x"), _weights(dw, d.N * d.K, "dw"),
+                                      _weights(dbias, d.N, "dbias"), *_ws_args(ws), _stream(stream)), "cg_linear_bwd_weight")
+
+
+def cg_act_bwd(act, dy, z, dz, stream=None):
+    """dz = dy * act'(z); z: a tensor or a Packed8."""
+    t, shape = _type_of(dy), dy.shape
+    _check(lib().cg_act_bwd(ACTS[act], t, *shape, *_matrix(dy, t, shape, "dy"), *_either(z, t, shape, "z"), *_matrix(dz, t, shape, "dz"),
+                            _stream(stream)), "cg_act_bwd")
 
 
 def cg_debug_patch_min_tiles(tiles):

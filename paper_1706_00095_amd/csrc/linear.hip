@@ -1,0 +1,387 @@
+// Linear layers: what the entry points check and plan, and the kernels beside the tiles of linear_gemm.hip: few tokens, the join of a
+// cut k, sums of columns, the gradient through an activation alone.
+#include "linear_device.h"
+#include "row_checks.h"
+
+namespace cg {
+namespace {
+
+// ---- few tokens -------------------------------------------------------------------------------------------------------------
+// Forward for up to 16 MT tokens: the weights are read once and that is all there is to do.  A block takes 16 rows of w, its eight waves every
+// eighth step along k; a step is a lane's 16 bytes of one row (4 lanes a row), AHEAD of them in flight.  w is the matrix instruction's first operand, the
+// tokens are the second; bf16: 16x16x32, fp32: 16x16x4 on the values as they are.  The waves' sums meet in LDS.
+constexpr int kFewWaves = 8, kFewRows = 16;
+typedef float v4f __attribute__((ext_vector_type(4)));
+struct FewArgs {
+    const void *x, *w;
+    int64_t x_ld, w_ld;
+    int M, N, K;
+    EpiArgs epi;
+};
+
+template <class T> struct FewStep;
+template <> struct FewStep<bf16raw> {
+    static constexpr int PER = 8;         // values of a lane
+    static __device__ __forceinline__ u32x4 load(const bf16raw *p, int n)
+    {
+        const Raw8<bf16raw> r = load8(p, n);
+        return u32x4{r.w[0], r.w[1], r.w[2], r.w[3]};
+    }
+    static __device__ __forceinline__ v4f mma(u32x4 w, u32x4 x, v4f c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
+    }
+};
+template <> struct FewStep<float> {
+    static constexpr int PER = 4;
+    static __device__ __forceinline__ u32x4 load(const float *p, int n)
+    {
+        if (n >= 4) {
+            const Loose16<float> q = *reinterpret_cast<const Loose16<float> *>(p);
+            return u32x4{q.w[0], q.w[1], q.w[2], q.w[3]};
+        }
+        u32x4 r = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) r[i] = __float_as_uint(p[i]);
+        return r;
+    }
+    static __device__ __forceinline__ v4f mma(u32x4 w, u32x4 x, v4f c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i]), __uint_as_float(x[i]), c, 0, 0, 0);
+        return c;
+    }
+};
+
+template <class T, int MT> __global__ __launch_bounds__(64 * kFewWaves) void few_tokens_kernel(FewArgs a)
+{
+    using S = FewStep<T>;
+    constexpr int STEP = 4 * S::PER, AHEAD = MT == 1 ? 8 : 4;
+    __shared__ __align__(16) float sums[kFewWaves][MT * 16][kFewRows + 4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = lane & 15, k0 = (lane >> 4) * S::PER;
+    const int n0 = blockIdx.x * kFewRows, row = n0 + at;
+    const T *w = static_cast<const T *>(a.w) + (row < a.N ? row * a.w_ld : 0);
+    const T *x[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) x[t] = static_cast<const T *>(a.x) + (16 * t + at < a.M ? (16 * t + at) * a.x_ld : 0);
+    v4f acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = v4f{};
+    // rows and tokens that are none read the first one's values, and their sums go nowhere
+    for (int s0 = wave * AHEAD * STEP; s0 < a.K; s0 += kFewWaves * AHEAD * STEP) {
+        u32x4 vw[AHEAD], vx[MT][AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int k = s0 + u * STEP + k0;
+            vw[u] = S::load(w + k, a.K - k);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) vx[t][u] = S::load(x[t] + k, a.K - k);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) acc[t] = S::mma(vw[u], vx[t][u], acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) *reinterpret_cast<v4f *>(&sums[wave][16 * t + at][4 * (lane >> 4)]) = acc[t];
+    __syncthreads();
+    if (threadIdx.x < MT * 32) {
+        const int m = threadIdx.x / 2, c = 8 * (threadIdx.x & 1);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = 0.f;
+#pragma unroll
+            for (int u = 0; u < kFewWaves; ++u) v[i] += sums[u][m][c + i];
+        }
+        if (m < a.M && n0 + c < a.N) finish8<T>(a.epi, v, m, n0 + c, a.N - n0 - c);
+    }
+}
+
+// ---- the join of a cut k --------------------------------------------------------------------------------------------------
+template <class T> __global__ __launch_bounds__(256) void gemm_join_kernel(const float *part, int splits, int R, int C, FastDiv by_chunks, uint32_t count, EpiArgs e)
+{
+    const int64_t plane = (int64_t)R * C;
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < count; i += gridDim.x * 256) {
+        const int r = (int)fdiv(i, by_chunks), c = 8 * (int)(i - r * by_chunks.d), n = C - c;
+        const float *p = part + (int64_t)r * C + c;
+        float v[8] = {};
+        for (int s = 0; s < splits; ++s, p += plane) {
+            const Raw8<float> x = load8(p, n);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += elem(x, j);
+        }
+        finish8<T>(e, v, r, c, n);
+    }
+}
+
+// ---- sums of columns: the gradient of a bias ----------------------------------------------------------------------------------
+// A block sums a slice of the rows for 256 columns, eight neighbours a thread, eight threads a column; slices are added in order.
+constexpr int kColumns = 256;
+template <class T> __global__ __launch_bounds__(256) void column_sums_kernel(const T *x, int64_t ld, int rows, int cols, int slice, float *out)
+{
+    __shared__ __align__(16) float lds[8][kColumns];
+    const int c = blockIdx.x * kColumns + 8 * (threadIdx.x & 31), ty = threadIdx.x >> 5, n = cols - c;
+    const int64_t r0 = (int64_t)blockIdx.y * slice;
+    const int r1 = (int)min((int64_t)rows, r0 + slice);
+    float v[8] = {};
+    for (int64_t r = r0 + ty; r < r1; r += 32) {
+        Raw8<T> q[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) q[u] = load8(x + (r + 8 * u < r1 && n > 0 ? (r + 8 * u) * ld + c : 0), r + 8 * u < r1 ? n : 0);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += elem(q[u], i);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lds[ty][8 * (threadIdx.x & 31) + i] = v[i];
+    __syncthreads();
+    const int mine = blockIdx.x * kColumns + threadIdx.x;
+    if (mine < cols) {
+        float s = 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += lds[u][threadIdx.x];
+        out[(int64_t)blockIdx.y * cols + mine] = s;
+    }
+}
+__global__ __launch_bounds__(256) void column_join_kernel(const float *part, int slices, int cols, float *out)
+{
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= cols) return;
+    float s = 0.f;
+    for (int i = 0; i < slices; ++i) s += part[(int64_t)i * cols + c];
+    out[c] = s;
+}
+
+// ---- the gradient through an activation alone -----------------------------------------------------------------------------------
+template <class T> __global__ __launch_bounds__(256) void act_bwd_kernel(const T *dy, int64_t dy_ld, int cols, FastDiv by_chunks, uint32_t count, EpiArgs e)
+{
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < count; i += gridDim.x * 256) {
+        const int64_t r = fdiv(i, by_chunks);
+        const int c = 8 * (int)(i - (uint32_t)r * by_chunks.d), n = cols - c;
+        const Raw8<T> g = load8(dy + r * dy_ld + c, n);
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = elem(g, j);
+        finish8<T>(e, v, r, c, n);
+    }
+}
+
+// ---- plans ------------------------------------------------------------------------------------------------------------------------
+constexpr int64_t kMostBlocks = 1 << 22;       // of 512 threads a launch has room for less than 2^32
+constexpr int kFewTokens = 32;
+constexpr int kMostSplits = 32, kLeastChunk = 4 * kGemmStep;
+
+bool act_ok(int act) { return act >= CG_ACT_NONE && act <= CG_ACT_SILU; }
+int desc_check(const cg_linear_desc *d)
+{
+    if (!d || !type_ok(d->type) || d->M < 0 || d->N < 1 || d->K < 1 || !act_ok(d->act) || !act_ok(d->act_in)) return CG_EINVAL;
+    const int64_t most = INT32_MAX - 65535;
+    if (d->M > most || d->N > most || d->K > most) return CG_EUNSUPPORTED;
+    auto tiles = [](int64_t n) { return (n + 127) / 128; };
+    if (tiles(d->M) * tiles(d->N) > kMostBlocks || tiles(d->M) * tiles(d->K) > kMostBlocks || tiles(d->N) * tiles(d->K) > kMostBlocks) return CG_EUNSUPPORTED;
+    return CG_OK;
+}
+struct Plan {
+    int R, C, K;              // of the product
+    bool few;
+    int splits, chunk;        // of tiles of 128
+    bool large;               // where rows allow it: tiles of 256, k uncut
+};
+Plan plan_of(const cg_linear_desc *d, int pass)
+{
+    Plan p{};
+    const int M = (int)d->M, N = (int)d->N, K = (int)d->K;
+    p.R = pass == CG_PASS_BWD_WEIGHT ? N : M;
+    p.C = pass == CG_PASS_FWD ? N : K;
+    p.K = pass == CG_PASS_FWD ? K : pass == CG_PASS_BWD_DATA ? N : M;
+    p.few = pass == CG_PASS_FWD && M <= kFewTokens;
+    p.splits = 1, p.chunk = p.K;
+    if (p.few) return p;
+    auto tiles = [&](int64_t t) { return ((p.R + t - 1) / t) * ((p.C + t - 1) / t); };
+    p.large = d->type == CG_TYPE_BF16 && tiles(256) >= 128;
+    const int64_t n = tiles(128);
+    int64_t s = n >= 512 ? 1 : 512 / n;
+    const int64_t most = (p.K + kLeastChunk - 1) / kLeastChunk;
+    if (s > most) s = most;
+    if (s > kMostSplits) s = kMostSplits;
+    if (s > 1) {
+        const int64_t per = ((p.K + s - 1) / s + kGemmStep - 1) / kGemmStep * kGemmStep;
+        p.chunk = (int)per;
+        p.splits = (int)((p.K + per - 1) / per);
+    }
+    return p;
+}
+size_t part_bytes(const Plan &p) { return p.splits > 1 ? (size_t)p.splits * (size_t)p.R * (size_t)p.C * sizeof(float) : 0; }
+int column_slices(int64_t M, int64_t N)
+{
+    const int64_t blocks = (N + kColumns - 1) / kColumns, most = 1024 / blocks, want = (M + 63) / 64;
+    int64_t s = want < most ? want : most;
+    return (int)(s < 1 ? 1 : s > 256 ? 256 : s);
+}
+size_t slice_bytes(const cg_linear_desc *d)
+{
+    const int s = column_slices(d->M, d->N);
+    return s > 1 ? (size_t)s * (size_t)d->N * sizeof(float) : 0;
+}
+
+bool dma_ok(const void *p, int64_t ld, int64_t cols) { return aligned16(p) && ld % 8 == 0 && cols % 8 == 0 && ld <= 1 << 21; }
+int ws_check(void *ws, size_t ws_bytes, size_t need)
+{
+    if (need && (!ws || !aligned16(ws))) return CG_EINVAL;
+    return ws_bytes < need ? CG_ENOSPC : CG_OK;
+}
+unsigned blocks_for(uint64_t n, unsigned most) { const uint64_t b = (n + 255) / 256; return (unsigned)(b < most ? b : most); }
+
+int product(const cg_linear_desc *d, int pass, const Plan &p, GemmArgs &a, bool packed, bool dma, void *ws, hipStream_t s)
+{
+    const bool large = p.large && dma;
+    const int tile = gemm_tile(large);
+    a.R = p.R, a.C = p.C, a.K = p.K;
+    a.tiles_r = (p.R + tile - 1) / tile, a.tiles_c = (p.C + tile - 1) / tile;
+    a.splits = large ? 1 : p.splits, a.chunk = large ? p.K : p.chunk;
+    a.part = static_cast<float *>(ws);
+    if (int rc = gemm_launch({d->type, pass, packed, large, dma}, a, s)) return rc;
+    if (a.splits == 1) return CG_OK;
+    const uint32_t chunks = (uint32_t)((p.C + 7) / 8), count = chunks * (uint32_t)p.R;
+    const dim3 grid(blocks_for(count, 4096));
+    const FastDiv by = make_fastdiv(chunks);
+    if (pass == CG_PASS_BWD_WEIGHT || d->type == CG_TYPE_FP32)
+        hipLaunchKernelGGL((gemm_join_kernel<float>), grid, dim3(256), 0, s, a.part, a.splits, p.R, p.C, by, count, a.epi);
+    else hipLaunchKernelGGL((gemm_join_kernel<bf16raw>), grid, dim3(256), 0, s, a.part, a.splits, p.R, p.C, by, count, a.epi);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
+template <class T> int few_tokens(const FewArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.N + kFewRows - 1) / kFewRows)), block(64 * kFewWaves);
+    if (a.M <= 16) hipLaunchKernelGGL((few_tokens_kernel<T, 1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((few_tokens_kernel<T, 2>), grid, block, 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
+bool packed_ok(const cg_packed8 *p, int64_t cols)
+{
+    return p->codes && p->scales && p->codes_ld >= cols && p->scales_ld >= (cols + kPackBlock - 1) / kPackBlock;
+}
+// where an activation's slope is wanted: its inputs in one form or the other
+bool slope_ok(int act, const void *z, int64_t z_ld, const cg_packed8 *z8, int64_t cols, int type)
+{
+    if (act == CG_ACT_NONE) return true;
+    if (z8) return !z && packed_ok(z8, cols);
+    return tensor_ok(z, z_ld, cols, type);
+}
+void slope_args(EpiArgs &e, int act, const void *z, int64_t z_ld, const cg_packed8 *z8)
+{
+    e.slope = act;
+    if (act == CG_ACT_NONE) return;
+    if (z8) e.z_in8 = {z8->codes, z8->scales, z8->codes_ld, z8->scales_ld};
+    else e.z_in = z, e.z_in_ld = z_ld;
+}
+
+}  // namespace
+}  // namespace cg
+
+using namespace cg;
+
+extern "C" size_t cg_linear_workspace_bytes(const cg_linear_desc *d, int pass)
+{
+    if (desc_check(d) != CG_OK || d->M == 0 || (pass != CG_PASS_FWD && pass != CG_PASS_BWD_DATA && pass != CG_PASS_BWD_WEIGHT)) return 0;
+    const size_t part = part_bytes(plan_of(d, pass));
+    if (pass != CG_PASS_BWD_WEIGHT) return part;
+    return part > slice_bytes(d) ? part : slice_bytes(d);
+}
+
+extern "C" int cg_linear_fwd(const cg_linear_desc *d, const void *x, int64_t x_ld, const void *w, int64_t w_ld, const float *bias,
+                             const void *residual, int64_t residual_ld, void *y, int64_t y_ld, void *z, int64_t z_ld, void *ws,
+                             size_t ws_bytes, void *stream)
+{
+    if (int rc = desc_check(d)) return rc;
+    if (d->M == 0) return CG_OK;
+    if (!tensor_ok(x, x_ld, d->K, d->type) || !tensor_ok(w, w_ld, d->K, d->type) || (bias && !floats_ok(bias)) ||
+        !optional_ok(residual, residual_ld, d->N, d->type) || !tensor_ok(y, y_ld, d->N, d->type) || !optional_ok(z, z_ld, d->N, d->type)) return CG_EINVAL;
+    const Plan p = plan_of(d, CG_PASS_FWD);
+    if (int rc = ws_check(ws, ws_bytes, part_bytes(p))) return rc;
+    EpiArgs e{};
+    e.bias = bias, e.add = residual, e.add_ld = residual_ld, e.out = y, e.out_ld = y_ld, e.z = z, e.z_ld = z_ld, e.act = d->act;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (p.few) {
+        const FewArgs a = {x, w, x_ld, w_ld, (int)d->M, (int)d->N, (int)d->K, e};
+        return d->type == CG_TYPE_FP32 ? few_tokens<float>(a, s) : few_tokens<bf16raw>(a, s);
+    }
+    GemmArgs a{};
+    a.A = x, a.a_ld = x_ld, a.B = w, a.b_ld = w_ld, a.epi = e;
+    return product(d, CG_PASS_FWD, p, a, false, d->type == CG_TYPE_BF16 && dma_ok(x, x_ld, d->K) && dma_ok(w, w_ld, d->K), ws, s);
+}
+
+extern "C" int cg_linear_bwd_data(const cg_linear_desc *d, const void *dz, int64_t dz_ld, const void *w, int64_t w_ld, const void *z_in,
+                                  int64_t z_in_ld, const cg_packed8 *z_in8, const void *add, int64_t add_ld, void *dx, int64_t dx_ld,
+                                  void *ws, size_t ws_bytes, void *stream)
+{
+    if (int rc = desc_check(d)) return rc;
+    if (d->M == 0) return CG_OK;
+    if (!tensor_ok(dz, dz_ld, d->N, d->type) || !tensor_ok(w, w_ld, d->K, d->type) || !tensor_ok(dx, dx_ld, d->K, d->type) ||
+        !optional_ok(add, add_ld, d->K, d->type) || !slope_ok(d->act_in, z_in, z_in_ld, z_in8, d->K, d->type)) return CG_EINVAL;
+    const Plan p = plan_of(d, CG_PASS_BWD_DATA);
+    if (int rc = ws_check(ws, ws_bytes, part_bytes(p))) return rc;
+    GemmArgs a{};
+    a.A = dz, a.a_ld = dz_ld, a.B = w, a.b_ld = w_ld;
+    a.epi.add = add, a.epi.add_ld = add_ld, a.epi.out = dx, a.epi.out_ld = dx_ld;
+    slope_args(a.epi, d->act_in, z_in, z_in_ld, z_in8);
+    return product(d, CG_PASS_BWD_DATA, p, a, false, d->type == CG_TYPE_BF16 && dma_ok(dz, dz_ld, d->N) && dma_ok(w, w_ld, d->K), ws,
+                   static_cast<hipStream_t>(stream));
+}
+
+extern "C" int cg_linear_bwd_weight(const cg_linear_desc *d, const void *dz, int64_t dz_ld, const void *x, int64_t x_ld, const cg_packed8 *x8,
+                                    float *dw, float *dbias, void *ws, size_t ws_bytes, void *stream)
+{
+    if (int rc = desc_check(d)) return rc;
+    if (!floats_ok(dw) || (dbias && !floats_ok(dbias)) || (x && x8)) return CG_EINVAL;
+    if (d->M > 0 && (!tensor_ok(dz, dz_ld, d->N, d->type) || (x8 ? !packed_ok(x8, d->K) : !tensor_ok(x, x_ld, d->K, d->type)))) return CG_EINVAL;
+    if (int rc = ws_check(ws, ws_bytes, cg_linear_workspace_bytes(d, CG_PASS_BWD_WEIGHT))) return rc;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const int M = (int)d->M, N = (int)d->N;
+    if (dbias) {       // before the product, whose sums take the workspace afterwards
+        const int slices = column_slices(M, N), slice = (M + slices - 1) / slices;
+        float *const to = slices > 1 ? static_cast<float *>(ws) : dbias;
+        const dim3 grid((unsigned)((N + kColumns - 1) / kColumns), (unsigned)slices);
+        if (d->type == CG_TYPE_FP32) hipLaunchKernelGGL((column_sums_kernel<float>), grid, dim3(256), 0, s, static_cast<const float *>(dz), dz_ld, M, N, slice, to);
+        else hipLaunchKernelGGL((column_sums_kernel<bf16raw>), grid, dim3(256), 0, s, static_cast<const bf16raw *>(dz), dz_ld, M, N, slice, to);
+        CG_HIP_TRY(hipGetLastError());
+        if (slices > 1) {
+            hipLaunchKernelGGL(column_join_kernel, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, s, to, slices, N, dbias);
+            CG_HIP_TRY(hipGetLastError());
+        }
+    }
+    GemmArgs a{};
+    a.A = dz, a.a_ld = dz_ld, a.epi.out = dw, a.epi.out_ld = d->K;
+    if (x8) a.B8 = {x8->codes, x8->scales, x8->codes_ld, x8->scales_ld};
+    else a.B = x, a.b_ld = x_ld;
+    const bool dma = d->type == CG_TYPE_BF16 && dma_ok(dz, dz_ld, d->N) && (x8 || dma_ok(x, x_ld, d->K));
+    return product(d, CG_PASS_BWD_WEIGHT, plan_of(d, CG_PASS_BWD_WEIGHT), a, x8 != nullptr, dma, ws, s);
+}
+
+extern "C" int cg_act_bwd(int act, int type, int64_t rows, int64_t cols, const void *dy, int64_t dy_ld, const void *z, int64_t z_ld,
+                          const cg_packed8 *z8, void *dz, int64_t dz_ld, void *stream)
+{
+    if (!act_ok(act) || act == CG_ACT_NONE || !type_ok(type) || rows < 0 || cols < 0) return CG_EINVAL;
+    if (rows == 0 || cols == 0) return CG_OK;
+    if (!tensor_ok(dy, dy_ld, cols, type) || !tensor_ok(dz, dz_ld, cols, type) || !slope_ok(act, z, z_ld, z8, cols, type)) return CG_EINVAL;
+    const int64_t chunks = (cols + 7) / 8;
+    if (!rows_fit(rows, cols) || rows * chunks > INT32_MAX / 2) return CG_EUNSUPPORTED;
+    EpiArgs e{};
+    e.out = dz, e.out_ld = dz_ld;
+    slope_args(e, act, z, z_ld, z8);
+    const uint32_t count = (uint32_t)(rows * chunks);
+    const dim3 grid(blocks_for(count, 16384));
+    const FastDiv by = make_fastdiv((uint32_t)chunks);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (type == CG_TYPE_FP32) hipLaunchKernelGGL((act_bwd_kernel<float>), grid, dim3(256), 0, s, static_cast<const float *>(dy), dy_ld, (int)cols, by, count, e);
+    else hipLaunchKernelGGL((act_bwd_kernel<bf16raw>), grid, dim3(256), 0, s, static_cast<const bf16raw *>(dy), dy_ld, (int)cols, by, count, e);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}

@@ -1,0 +1,120 @@
+// Device code shared by the kernels of the linear layers (linear.hip, linear_gemm.hip) and what their host side passes to them.
+//
+// All three passes are one product, C[r][c] = sum_k A(r, k) B(c, k), of operands that lie with their rows along k (forward: x and w) or
+// across it (backward-data: w; backward-weight: dz and x), and one epilogue on rows of fp32 sums.
+#pragma once
+#include "cg_internal.h"
+#include "packed_device.h"
+#include "tile_device.h"
+
+namespace cg {
+
+// What becomes of eight neighbouring sums of a row: forward  out = act(sum + bias) + add, z = sum + bias;  backward-data  out = sum *
+// slope of act at z_in + add;  backward-weight and sums of a part of k: out = sum.
+struct EpiArgs {
+    const float *bias;
+    const void *add, *z_in;
+    Packed z_in8;                     // codes NULL: none
+    void *out, *z;
+    int64_t add_ld, z_in_ld, out_ld, z_ld;
+    int act, slope;                   // CG_ACT_*
+};
+
+struct GemmArgs {
+    const void *A, *B;
+    Packed B8;                        // instead of B
+    int64_t a_ld, b_ld;
+    int R, C, K;
+    int tiles_r, tiles_c, splits, chunk;      // k is cut into `splits` chunks (a multiple of a step each)
+    float *part;                      // [splits][R][C] where there are several
+    EpiArgs epi;
+};
+
+// linear_gemm.hip.  Which of its kernels: PASS_*; large: tiles of 256 x 256, else 128 x 128; dma: both operands travel to LDS without registers.
+struct GemmKind { int type, pass, packed, large, dma; };
+int gemm_launch(const GemmKind &kind, const GemmArgs &a, hipStream_t s);
+constexpr int kGemmStep = 64;         // chunks of k are multiples of it
+constexpr int gemm_tile(bool large) { return large ? 256 : 128; }
+
+namespace {
+
+// ---- activations ----------------------------------------------------------------------------------------------------------
+// gelu(z) = z Phi(z).  Phi(-|z|) = e^(-z^2/2) t P(t), t = 1 / (1 + 0.36 |z|), with a P of degree 8 fitted to the scaled complementary
+// error function by iterated least squares on 0 <= |z| <= 40: off by 9e-8 relative at most, and by roundings.  No branch, where the
+// library's erff has two sides that both run in a wave: 9 multiply-adds, an exponential, a reciprocal.
+__device__ __forceinline__ float tail_of_normal(float z, float &e)
+{
+    const float a = fabsf(z);
+    e = __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.36f, a, 1.f));
+    float p = -0.030240084f;
+    p = fmaf(p, t, 0.13951595f);
+    p = fmaf(p, t, -0.22361257f);
+    p = fmaf(p, t, 0.10738120f);
+    p = fmaf(p, t, -0.00039283623f);
+    p = fmaf(p, t, 0.096039394f);
+    p = fmaf(p, t, 0.12400939f);
+    p = fmaf(p, t, 0.14368191f);
+    p = fmaf(p, t, 0.14361766f);
+    return p * t * e;
+}
+__device__ __forceinline__ float act_of(float z, int act)
+{
+    if (act == CG_ACT_RELU) return z < 0.f ? 0.f : z;
+    if (act == CG_ACT_GELU) {
+        float e;
+        const float q = tail_of_normal(z, e);
+        return z * (z > 0.f ? 1.f - q : q);
+    }
+    if (act == CG_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+    return z;
+}
+// g times the slope of the activation at z
+__device__ __forceinline__ float slope_times(float g, float z, int act)
+{
+    if (act == CG_ACT_RELU) return z > 0.f ? g : z == z ? 0.f : z;
+    if (act == CG_ACT_GELU) {
+        float e;
+        const float q = tail_of_normal(z, e);
+        return g * fmaf(z * 0.3989422804f, e, z > 0.f ? 1.f - q : q);
+    }
+    if (act == CG_ACT_SILU) {
+        const float p = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+        return g * (p * fmaf(z, 1.f - p, 1.f));
+    }
+    return g;
+}
+
+template <class T> __device__ __forceinline__ void finish8(const EpiArgs &e, float (&v)[8], int64_t row, int c, int n)
+{
+    if (e.bias) {
+        const Raw8<float> b = load8(e.bias + c, n);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += elem(b, i);
+    }
+    if (e.z) store8(static_cast<T *>(e.z) + row * e.z_ld + c, to_raw<T>(v), n);
+    if (e.act != CG_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = act_of(v[i], e.act);
+    }
+    if (e.slope != CG_ACT_NONE) {
+        if (e.z_in8.codes) {
+            const Raw8Packed z = load8(e.z_in8, row, c, n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(z, i), e.slope);
+        } else {
+            const Raw8<T> z = load8(static_cast<const T *>(e.z_in) + row * e.z_in_ld + c, n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(z, i), e.slope);
+        }
+    }
+    if (e.add) {
+        const Raw8<T> a = load8(static_cast<const T *>(e.add) + row * e.add_ld + c, n);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += elem(a, i);
+    }
+    store8(static_cast<T *>(e.out) + row * e.out_ld + c, to_raw<T>(v), n);
+}
+
+}  // namespace
+}  // namespace cg

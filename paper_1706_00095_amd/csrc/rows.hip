@@ -5,6 +5,7 @@
 // mean would lose the variance of rows whose mean is large).
 #include <cmath>
 #include "cg_internal.h"
+#include "row_checks.h"
 #include "typed_device.h"
 
 namespace cg {
@@ -517,17 +518,6 @@ DropArgs drop_args(const cg_drop &d)
     return a;
 }
 bool drop_ok(const cg_drop *d) { return d && d->p >= 0.0 && d->p < 1.0; }
-bool type_ok(int type) { return type == CG_TYPE_FP32 || type == CG_TYPE_BF16; }
-size_t type_size(int type) { return type == CG_TYPE_FP32 ? 4 : 2; }
-bool rows_fit(int64_t rows, int64_t cols) { return rows <= INT32_MAX && cols <= INT32_MAX && rows * cols <= INT32_MAX; }
-// a tensor of `rows` rows: there, on an element's boundary, rows that do not overlap
-bool tensor_ok(const void *p, int64_t ld, int64_t cols, int type)
-{
-    return p && (reinterpret_cast<uintptr_t>(p) & (type_size(type) - 1)) == 0 && ld >= cols;
-}
-bool optional_ok(const void *p, int64_t ld, int64_t cols, int type) { return !p || tensor_ok(p, ld, cols, type); }
-bool floats_ok(const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
-
 template <class T> void dropout_launch_typed(const DropoutArgs &a, bool dense, unsigned grid, hipStream_t s)
 {
     if (dense) {

@@ -1,0 +1,167 @@
+"""Embedding lookup and its gradient by sorted tokens against their 64-bit form."""
+import pytest
+import torch
+
+import block_util as bu
+
+pytestmark = pytest.mark.gpu
+
+
+def _cg():
+    import paper_1706_00095_amd as cg
+    return cg
+
+
+def _ws(d):
+    return torch.full((_cg().cg_embedding_workspace_bytes(d),), 0xFF, dtype=torch.uint8, device="cuda")
+
+
+def _tokens(n, vocab, kind, seed):
+    g = torch.Generator().manual_seed(seed)
+    if kind == "same":
+        t = torch.full((n,), vocab // 2)
+    elif kind == "skewed":
+        t = (vocab ** torch.rand(n, generator=g, dtype=torch.float64) - 1).long().clamp(0, vocab - 1)
+    elif kind == "falling":
+        t = (vocab - 1 - torch.arange(n) % vocab)
+    else:
+        t = torch.randint(0, vocab, (n,), generator=g)
+    if kind == "gaps":
+        t[torch.rand(n, generator=g) < 0.4] = -1
+        t[:: 7] = vocab
+        t[1:: 11] = torch.iinfo(torch.int32).min
+    return t.int()
+
+
+@pytest.mark.parametrize("table_type", ["fp32", "bf16"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,vocab,cols,pad", [(1, 1, 1, 0), (3, 5, 7, 2), (8, 100, 256, 0), (1000, 37, 33, 5), (65, 70000, 130, 8)])
+def test_lookup(table_type, dtype, n, vocab, cols, pad):
+    cg, tt, dt = _cg(), bu.DTYPES[table_type], bu.DTYPES[dtype]
+    table = bu.normal((vocab, cols), tt, 1)
+    tokens = _tokens(n, vocab, "gaps", 2)
+    td = bu.wide(table, pad, tt)[0]
+    y, whole = bu.wide(torch.full((n, cols), 7.0), pad, dt, fill=5.0)
+    scale = cols ** 0.5
+    cg.cg_embedding_fwd(cg.embedding_desc(td, y, scale), tokens.cuda(), td, y)
+    there = ((tokens >= 0) & (tokens < vocab))[:, None]
+    want = torch.where(there, table[tokens.long().clamp(0, vocab - 1)] * scale, 0.0)
+    bu.near(y, want, (bu.half_step(dt) + 3 * bu.U) * want.abs(), "y")      # the scale in fp32, the product, the type
+    assert bool((whole[:, cols:] == 5.0).all())
+
+
+GRADS = [  # places, vocab, columns, pad, kind
+    (0, 10, 12, 0, "any"), (1, 1, 1, 0, "any"), (1, 3000, 40, 0, "any"), (2, 255, 8, 0, "same"), (31, 256, 7, 3, "any"), (32, 257, 33, 0, "same"), (33, 2, 130, 0, "skewed"),
+    (64, 64, 64, 0, "falling"), (65, 1000, 513, 1, "gaps"), (1000, 50, 24, 0, "skewed"), (1024, 70000, 16, 0, "any"), (1025, 300, 600, 8, "gaps"), (5000, 1, 40, 0, "same"),
+    (16384, 1000, 40, 0, "skewed"), (16384, 20000, 9, 0, "falling"), (16385, 4000, 33, 0, "skewed"), (20000, 3, 8, 0, "gaps"), (40000, 100000, 12, 0, "any"), (70000, 500, 20, 0, "skewed"),
+    (300000, 17000000, 1, 0, "skewed"),
+]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,vocab,cols,pad,kind", GRADS)
+def test_gradient(dtype, n, vocab, cols, pad, kind):
+    """Random values within the roundings of a sum, and whole numbers bit for bit; the same bits again."""
+    cg, dt = _cg(), bu.DTYPES[dtype]
+    tokens = _tokens(n, vocab, kind, n + vocab)
+    table = torch.empty(vocab, cols, device="cuda")
+    y = torch.empty(n, cols, dtype=dt, device="cuda")
+    for scale, dy in ((0.37, bu.normal((n, cols), dt, 3)), (2.0, bu.whole((n, cols), 3, 4))):
+        d = cg.embedding_desc(table, y, scale)
+        ws = _ws(d)
+        g = bu.wide(dy, pad, dt)[0]
+        got, again = (torch.full((vocab, cols), 7.0, device="cuda") for _ in range(2))
+        cg.cg_embedding_bwd(d, tokens.cuda(), g, got, ws)
+        cg.cg_embedding_bwd(d, tokens.cuda(), g, again, ws)
+        want, tol = bu.embedding_grad(tokens, dy, vocab, scale)
+        if scale == 2.0:
+            assert torch.equal(got.cpu(), want.float())
+        else:
+            bu.near(got, want, tol + 2 * bu.U * want.abs(), "dtable")
+        assert torch.equal(got, again)
+
+
+def test_far_rows():
+    """A table of more than 2^31 elements, forward and its gradient."""
+    cg, cols, vocab, n = _cg(), 1024, (1 << 21) + 5, 700
+    table = torch.zeros(vocab, cols, dtype=torch.bfloat16, device="cuda")
+    tokens = torch.tensor([vocab - 1, 0, vocab - 2, 1 << 20] * (n // 4), dtype=torch.int32)
+    rows = bu.whole((4, cols), 3, 1)
+    for i in range(4):
+        table[int(tokens[i])] = rows[i].bfloat16().cuda()
+    y = torch.empty(n, cols, dtype=torch.bfloat16, device="cuda")
+    d = cg.embedding_desc(table, y, 1.0)
+    cg.cg_embedding_fwd(d, tokens.cuda(), table, y)
+    assert torch.equal(y.double().cpu(), rows.repeat(n // 4, 1))
+    del table
+    dtable = torch.full((vocab, cols), 7.0, device="cuda")
+    dy = bu.whole((n, cols), 3, 2)
+    cg.cg_embedding_bwd(d, tokens.cuda(), dy.bfloat16().cuda(), dtable, _ws(d))
+    for i in range(4):
+        assert torch.equal(dtable[int(tokens[i])].double().cpu(), dy[i::4].sum(0))
+    assert not dtable[1:1 << 20].any() and not dtable[(1 << 20) + 1:vocab - 2].any()
+
+
+def test_gradient_by_differences():
+    cg, n, vocab, cols = _cg(), 50, 9, 6
+    tokens = _tokens(n, vocab, "skewed", 1).cuda()
+    table = bu.normal((vocab, cols), torch.float32, 1).float().cuda()
+    dy = bu.normal((n, cols), torch.float32, 2)
+    y = torch.empty(n, cols, device="cuda")
+    d = cg.embedding_desc(table, y, 1.5)
+    dtable = torch.empty_like(table)
+    cg.cg_embedding_bwd(d, tokens, dy.float().cuda(), dtable, _ws(d))
+
+    def total():
+        cg.cg_embedding_fwd(d, tokens, table, y)
+        return float((y.double().cpu() * dy).sum())
+
+    for at in ((0, 0), (3, 5), (8, 2)):
+        old = float(table[at])
+        table[at] = old + 0.5
+        up = total()
+        table[at] = old - 0.5
+        down = total()
+        table[at] = old
+        # linear: y is off by a rounding on either side, and so are the places
+        tol = 4 * bu.U * float((y.double().cpu().abs() + 2).mul(dy.abs()).sum()) + n * bu.U * float(dy.abs().sum())
+        assert abs(up - down - float(dtable[at])) <= tol
+
+
+@pytest.mark.parametrize("n", [700, 20000])
+def test_graph_and_stream(n):
+    """Captured and replayed between eager calls with other tokens, and on another stream: the same bits."""
+    cg, vocab, cols = _cg(), 400, 40
+    tokens = [_tokens(n, vocab, "skewed", i).cuda() for i in range(2)]
+    dy = bu.normal((n, cols), torch.bfloat16, 2).bfloat16().cuda()
+    table = bu.normal((vocab, cols), torch.float32, 1).float().cuda()
+    y = torch.empty(n, cols, dtype=torch.bfloat16, device="cuda")
+    d = cg.embedding_desc(table, y, 1.5)
+    ws, held, dtable = _ws(d), tokens[0].clone(), torch.empty_like(table)
+
+    def both():
+        cg.cg_embedding_fwd(d, held, table, y)
+        cg.cg_embedding_bwd(d, held, dy, dtable, ws)
+
+    want = []
+    for t in tokens:
+        held.copy_(t)
+        both()
+        want.append((y.clone(), dtable.clone()))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        both()
+    torch.cuda.synchronize()
+    assert torch.equal(dtable, want[1][1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+    for i in (0, 1, 0, 1):
+        held.copy_(tokens[i])
+        dtable.fill_(3.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[i][0]) and torch.equal(dtable, want[i][1])
+        held.copy_(tokens[1 - i])
+        both()
