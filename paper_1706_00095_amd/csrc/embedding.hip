@@ -2,8 +2,9 @@
 //
 // The gradient is dense (the update takes whole buckets): row v is the sum of dy over the places that hold v, zero where there are none.
 // Places are sorted by token, stably, so that each row's sum is taken in the order of the places and results are the same bits run to
-// run.  A token that is frequent has thousands of places: the sorted places are cut into chunks, chunks of one token alone are summed by
-// blocks of their own, and the row adds what they leave.  Every row of the gradient is then written once.
+// run.  A token that is frequent has thousands of places: the sorted places are cut into chunks, a wave each, and what runs that cross a
+// border leave in their chunks is added by a second kernel.  The table's gradient is filled with zeros by blocks beside those that sort,
+// and the rows of tokens that occur are written over.
 #include <algorithm>
 #include "cg_internal.h"
 #include "row_checks.h"
@@ -23,30 +24,44 @@ struct LookupArgs {
     FastDiv by_chunks;
     float scale;
 };
-// A thread takes eight neighbours of a row.  Bound by HBM.
-template <class TT, class T> __global__ __launch_bounds__(256) void lookup_kernel(LookupArgs a)
+// A thread takes eight neighbours of a row, AHEAD of them at a time: their tokens are asked for together, then their rows.
+template <class TT, class T, int AHEAD> __global__ __launch_bounds__(256) void lookup_kernel(LookupArgs a)
 {
-    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < a.count; i += gridDim.x * 256) {
-        const int64_t t = fdiv(i, a.by_chunks);
-        const int c = 8 * (int)(i - (uint32_t)t * a.by_chunks.d), n = a.cols - c;
-        const int v = a.tokens[t];
-        float f[8] = {};
-        if ((uint32_t)v < (uint32_t)a.vocab) {
-            const Raw8<TT> x = load8(static_cast<const TT *>(a.table) + v * a.table_ld + c, n);
+    const uint32_t step = gridDim.x * 256;
+    for (uint32_t i0 = blockIdx.x * 256 + threadIdx.x; i0 < a.count; i0 += AHEAD * step) {
+        int t[AHEAD], c[AHEAD], v[AHEAD];
+        Raw8<TT> x[AHEAD];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = elem(x, j) * a.scale;
+        for (int u = 0; u < AHEAD; ++u) {
+            const uint32_t i = min(i0 + u * step, a.count - 1);       // the last one several times, the same
+            t[u] = (int)fdiv(i, a.by_chunks);
+            c[u] = 8 * (int)(i - (uint32_t)t[u] * a.by_chunks.d);
+            v[u] = a.tokens[t[u]];
         }
-        store8(static_cast<T *>(a.y) + t * a.y_ld + c, to_raw<T>(f), n);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const bool some = (uint32_t)v[u] < (uint32_t)a.vocab;
+            x[u] = load8(static_cast<const TT *>(a.table) + (some ? v[u] : 0) * a.table_ld + c[u], a.cols - c[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const float scale = a.scale;
+            const bool some = (uint32_t)v[u] < (uint32_t)a.vocab;
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = some ? elem(x[u], j) * scale : 0.f;
+            store8(static_cast<T *>(a.y) + (int64_t)t[u] * a.y_ld + c[u], to_raw<T>(f), a.cols - c[u]);
+        }
     }
 }
 
 // ---- places sorted by token --------------------------------------------------------------------------------------------------------
 // Least significant digit first, stably.  A wave numbers 64 places at a time: those with its digit among the lanes before it, and
 // those the wave has had before (counted in LDS).  Places without a token have the key `vocab` and come last.
-constexpr int kItems = 16;                  // of a lane
 constexpr int kDigits = 256;
-constexpr int kOneBlock = 1024, kTileBlock = 256, kTile = kTileBlock * kItems;       // threads; places of a block where there are several
-constexpr int kMostOne = kOneBlock * kItems;
+constexpr int kOneBlock = 1024, kOneItems = 4, kMostOne = kOneBlock * kOneItems;      // threads, places of a lane, of the block
+constexpr int kMostPass = 1 << 16;          // places up to which a pass is one launch
+constexpr int kTileBlock = 256, kItems = 16, kTile = kTileBlock * kItems;             // beyond: threads, places of a lane, of a block
 
 __device__ __forceinline__ uint32_t key_of(const int32_t *tokens, int i, int n, int vocab)
 {
@@ -55,12 +70,12 @@ __device__ __forceinline__ uint32_t key_of(const int32_t *tokens, int i, int n, 
     return v < (uint32_t)vocab ? v : (uint32_t)vocab;
 }
 // Numbers this wave's items by digit: rank[j] among the wave's of the same digit; counts[] (of the wave, zeroed) ends with their numbers.
-__device__ __forceinline__ void number_items(const uint32_t (&key)[kItems], int items, int shift, int bits, uint32_t *counts, uint32_t (&rank)[kItems])
+template <int ITEMS> __device__ __forceinline__ void number_items(const uint32_t (&key)[ITEMS], int items, int shift, int bits, uint32_t *counts, uint32_t (&rank)[ITEMS])
 {
     const int lane = threadIdx.x & 63;
     const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
-    for (int j = 0; j < kItems; ++j) {
+    for (int j = 0; j < ITEMS; ++j) {
         if (j < items) {
             const uint32_t d = key[j] >> shift & ((1u << bits) - 1);
             uint64_t same = ~(uint64_t)0;
@@ -94,70 +109,137 @@ template <int THREADS> __device__ __forceinline__ uint32_t block_before(uint32_t
     return before + upto - x;
 }
 
+// Zeros for `count` floats, by the blocks from `first` on: beside those of a launch that leaves the chip empty, so that sorting costs little.
+struct Fill {
+    float *to;
+    int64_t count;
+    int first;
+};
+__device__ __forceinline__ bool fills(const Fill &f)
+{
+    if ((int)blockIdx.x < f.first) return false;
+    const int64_t step = (int64_t)(gridDim.x - f.first) * blockDim.x * 4;
+    for (int64_t i = ((int64_t)(blockIdx.x - f.first) * blockDim.x + threadIdx.x) * 4; i < f.count; i += step) {
+        if (i + 4 <= f.count) *reinterpret_cast<Loose16<float> *>(f.to + i) = Loose16<float>{{0, 0, 0, 0}};
+        else
+            for (int64_t j = i; j < f.count; ++j) f.to[j] = 0.f;
+    }
+    return true;
+}
+__global__ __launch_bounds__(1024) void fill_kernel(Fill f) { fills(f); }
+
 struct SortArgs {
     const int32_t *tokens;                   // NULL: keys and places as they lie in key_in, place_in
     const uint32_t *key_in, *place_in;
     uint32_t *key, *place;
     uint32_t *counts;                        // [kDigits][tiles]
     int n, vocab, shift, bits, tiles;
+    Fill fill;
 };
 
-// All of up to kMostOne places by one block, the items going through LDS between passes.
-__global__ __launch_bounds__(kOneBlock) void sort_one_kernel(const int32_t *tokens, int n, int vocab, int passes, int bits, uint32_t *keys, uint32_t *places)
+// All of up to kMostOne places by one block, the items going through LDS between passes.  16384 places in one block (16 a lane) took 35 us.
+__global__ __launch_bounds__(kOneBlock) void sort_one_kernel(SortArgs a, int passes)
 {
+    if (fills(a.fill)) return;
     constexpr int W = kOneBlock / 64;
-    extern __shared__ __align__(16) uint32_t smem[];
-    uint32_t *const counts = smem, *const sums = counts + W * kDigits, *const ex_key = sums + W;      // counts [W][kDigits]
-    uint16_t *const ex_place = reinterpret_cast<uint16_t *>(ex_key + kMostOne);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, items = (n + kOneBlock - 1) / kOneBlock, at = wave * items * 64 + lane;
-    uint32_t key[kItems], place[kItems], rank[kItems];
+    __shared__ uint32_t counts[W][kDigits], sums[W], ex_key[kMostOne];
+    __shared__ uint16_t ex_place[kMostOne];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, items = (a.n + kOneBlock - 1) / kOneBlock, at = wave * items * 64 + lane;
+    const uint32_t mask = (1u << a.bits) - 1;
+    uint32_t key[kOneItems], place[kOneItems], rank[kOneItems];
 #pragma unroll
-    for (int j = 0; j < kItems; ++j) {
+    for (int j = 0; j < kOneItems; ++j)
         if (j < items) {
             place[j] = (uint32_t)(at + 64 * j);
-            key[j] = key_of(tokens, at + 64 * j, n, vocab);
+            key[j] = key_of(a.tokens, at + 64 * j, a.n, a.vocab);
         }
-    }
     for (int p = 0; p < passes; ++p) {
-        for (int i = threadIdx.x; i < W * kDigits; i += kOneBlock) counts[i] = 0;
+        const int shift = p * a.bits;
+        for (int i = threadIdx.x; i < W * kDigits; i += kOneBlock) counts[0][i] = 0;
         __syncthreads();
-        number_items(key, items, p * bits, bits, counts + wave * kDigits, rank);
+        number_items(key, items, shift, a.bits, counts[wave], rank);
         __syncthreads();
         // in the order of digits, then waves: thread t has digit t / 4 of four waves
         const int d = threadIdx.x >> 2, w0 = 4 * (threadIdx.x & 3);
         uint32_t c[4], sum = 0;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) c[u] = counts[(w0 + u) * kDigits + d], sum += c[u];
+        for (int u = 0; u < 4; ++u) c[u] = counts[w0 + u][d], sum += c[u];
         uint32_t before = block_before<kOneBlock>(sum, sums);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            counts[(w0 + u) * kDigits + d] = before;
+            counts[w0 + u][d] = before;
             before += c[u];
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kItems; ++j) {
+        for (int j = 0; j < kOneItems; ++j)
             if (j < items) {
-                const uint32_t to = counts[wave * kDigits + (key[j] >> (p * bits) & ((1u << bits) - 1))] + rank[j];
+                const uint32_t to = counts[wave][key[j] >> shift & mask] + rank[j];
                 ex_key[to] = key[j];
                 ex_place[to] = (uint16_t)place[j];
             }
-        }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kItems; ++j) {
+        for (int j = 0; j < kOneItems; ++j)
             if (j < items) {
                 key[j] = ex_key[at + 64 * j];
                 place[j] = ex_place[at + 64 * j];
             }
-        }
     }
 #pragma unroll
-    for (int j = 0; j < kItems; ++j) {
-        if (j < items && at + 64 * j < n) keys[at + 64 * j] = key[j], places[at + 64 * j] = place[j];
-    }
+    for (int j = 0; j < kOneItems; ++j)
+        if (j < items && at + 64 * j < a.n) a.key[at + 64 * j] = key[j], a.place[at + 64 * j] = place[j];
 }
-constexpr int kOneLds = (kOneBlock / 64 * kDigits + kOneBlock / 64 + kMostOne) * 4 + kMostOne * 2;
+
+// A pass over up to kMostPass places in one launch, a place a thread: every block counts the digits of all places, before its own and from
+// there on, so that no other launch has to.
+__global__ __launch_bounds__(kOneBlock) void sort_pass_kernel(SortArgs a)
+{
+    if (fills(a.fill)) return;
+    constexpr int W = kOneBlock / 64;
+    __shared__ uint32_t counts[W][kDigits], ahead[kDigits], rest[kDigits], sums[W];
+    const int wave = threadIdx.x >> 6, own = blockIdx.x * kOneBlock, i = own + threadIdx.x;
+    const uint32_t mask = (1u << a.bits) - 1;
+    auto key_at = [&](int j) { return a.tokens ? key_of(a.tokens, j, a.n, a.vocab) : j < a.n ? a.key_in[j] : 0xffffffffu; };
+    for (int j = threadIdx.x; j < W * kDigits; j += kOneBlock) counts[0][j] = 0;
+    if (threadIdx.x < kDigits) ahead[threadIdx.x] = rest[threadIdx.x] = 0;
+    uint32_t key[1] = {key_at(i)}, rank[1];
+    const uint32_t place = a.tokens || i >= a.n ? (uint32_t)i : a.place_in[i];
+    __syncthreads();
+    for (int j0 = threadIdx.x; j0 < a.tiles * kOneBlock; j0 += 16 * kOneBlock) {
+        uint32_t k[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) k[u] = key_at(j0 + u * kOneBlock);
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            const int j = j0 + u * kOneBlock;
+            if (j < a.tiles * kOneBlock) atomicAdd(&(j < own ? ahead : rest)[k[u] >> a.shift & mask], 1u);       // whole numbers: in any order
+        }
+    }
+    number_items(key, 1, a.shift, a.bits, counts[wave], rank);
+    __syncthreads();
+    const uint32_t before = block_before<kOneBlock>(threadIdx.x < kDigits ? ahead[threadIdx.x] + rest[threadIdx.x] : 0, sums);
+    if (threadIdx.x < kDigits) rest[threadIdx.x] = before + ahead[threadIdx.x];
+    __syncthreads();
+    const int d = threadIdx.x >> 2, w0 = 4 * (threadIdx.x & 3);
+    uint32_t c[4], sum = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) c[u] = counts[w0 + u][d], sum += c[u];
+    uint32_t at = rest[d];
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+        const uint32_t other = (uint32_t)__shfl((int)sum, (int)((threadIdx.x & 60) + u));
+        at += u < (int)(threadIdx.x & 3) ? other : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        counts[w0 + u][d] = at;
+        at += c[u];
+    }
+    __syncthreads();
+    const uint32_t to = counts[wave][key[0] >> a.shift & mask] + rank[0];
+    if (i < a.n) a.key[to] = key[0], a.place[to] = place;       // what lies behind the last place comes last
+}
 
 // Several blocks, a pass in three launches: how often each digit occurs in each tile, sums before in the order of digits, then tiles, and
 // the items to their places.
@@ -173,6 +255,7 @@ __device__ __forceinline__ void load_items(const SortArgs &a, uint32_t (&key)[kI
 }
 __global__ __launch_bounds__(kTileBlock) void sort_count_kernel(SortArgs a)
 {
+    if (fills(a.fill)) return;
     __shared__ uint32_t counts[kDigits];
     counts[threadIdx.x] = 0;
     __syncthreads();
@@ -239,83 +322,134 @@ __global__ __launch_bounds__(kTileBlock) void sort_move_kernel(SortArgs a)
 struct GradArgs {
     const uint32_t *key, *place;
     const void *dy;
-    float *part;                             // [chunks][cols]
-    uint32_t *first;                         // [vocab + 1]: where each token's places begin
+    // [chunks][cols]: sums of the run that a chunk begins with, where it began earlier, and of the one that it ends with, where it goes on and
+    // began here
+    float *head, *tail;
     float *dtable;
     int64_t dy_ld;
-    int n, vocab, cols, chunk, chunk_shift;
+    int n, vocab, cols, chunk_shift;
     float scale;
 };
-constexpr int kGradThreads = 64;
 
-template <class T> __device__ __forceinline__ void add_places(const GradArgs &a, int from, int to, int c, float (&v)[8])
+// The columns of a lane: eight, the last ones of a row where it would reach past them (two lanes then make the same numbers), so that loads
+// need no bounds and many are on their way at a time; fewer only where a row has fewer.
+struct Columns {
+    int c, n;
+    __device__ __forceinline__ Columns(int at, int cols) : c(cols >= 8 ? min(at, cols - 8) : 0), n(cols >= 8 ? 8 : cols) {}
+};
+// WIDE: rows of eight columns and more
+template <bool WIDE, class T> __device__ __forceinline__ Raw8<T> load_row(const GradArgs &a, uint32_t place, Columns at)
 {
-    constexpr int AHEAD = 8;
-    const int n = a.cols - c;
-    for (int i = from; i < to; i += AHEAD) {
-        Raw8<T> x[AHEAD];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            x[u] = load8(static_cast<const T *>(a.dy) + (int64_t)a.place[min(i + u, to - 1)] * a.dy_ld + c, i + u < to ? n : 0);
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += elem(x[u], j);
-    }
+    return load8(static_cast<const T *>(a.dy) + (int64_t)place * a.dy_ld + at.c, WIDE ? 8 : at.n);
 }
-// Blocks 0 .. bounds - 1: where each token's places begin, by halving, a thread a token.  The others: chunks of one token alone.
-template <class T> __global__ __launch_bounds__(kGradThreads) void chunk_sums_kernel(GradArgs a, int bounds, int per_chunk)
-{
-    if ((int)blockIdx.x < bounds) {
-        for (int v = blockIdx.x * kGradThreads + threadIdx.x; v <= a.vocab; v += bounds * kGradThreads) {
-            int lo = 0, hi = a.n;
-            while (lo < hi) {
-                const int m = lo + (hi - lo) / 2;
-                if (a.key[m] < (uint32_t)v) lo = m + 1;
-                else hi = m;
-            }
-            a.first[v] = (uint32_t)lo;
-        }
-        return;
+// What the lanes of a group, LANES of them with eight columns each, have to do: a chunk, and as many groups as its columns take.
+template <int LANES> struct Group {
+    int chunk, lane, c, from, to;
+    bool some;
+    __device__ __forceinline__ Group(const GradArgs &a, int per_chunk, int64_t groups)
+    {
+        const int64_t g = (int64_t)blockIdx.x * (256 / LANES) + (LANES == 64 ? (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : (int)threadIdx.x / LANES);
+        some = g < groups;
+        chunk = (int)(g / per_chunk), lane = threadIdx.x % LANES;
+        c = (int)(g - (int64_t)chunk * per_chunk) * 8 * LANES + 8 * lane;
+        from = chunk << a.chunk_shift, to = min(from + (1 << a.chunk_shift), a.n);
     }
-    const int b = (int)blockIdx.x - bounds, chunk = b / per_chunk, c = (b - chunk * per_chunk) * kGradThreads * 8 + 8 * threadIdx.x;
-    const int from = chunk << a.chunk_shift, to = from + a.chunk;       // whole chunks only
-    if (c >= a.cols || a.key[from] != a.key[to - 1] || a.key[from] >= (uint32_t)a.vocab) return;
+};
+// Sums of the runs of equal tokens in a chunk.  Bound by latency: a chunk's places, then their rows, a few at a time.
+template <class T, int LANES, bool WIDE> __global__ __launch_bounds__(256) void runs_kernel(GradArgs a, int per_chunk, int64_t groups)
+{
+    constexpr int MOST = 32 / (int)sizeof(T), STEP = LANES < MOST ? LANES : MOST;
+    const Group<LANES> g(a, per_chunk, groups);
+    if (!g.some) return;
+    const Columns at(g.c, a.cols);
+    const bool here = g.c < a.cols;            // lanes behind the last column go along
+    const int from = g.from, to = g.to;
+    const uint32_t none = (uint32_t)a.vocab, before = from > 0 ? a.key[from - 1] : none, behind = to < a.n ? a.key[to] : none;
+    // of lane i of the group; the same number in all lanes of a wave may live in a scalar register
+    auto lanes = [](uint32_t x, int i) { return LANES == 64 ? (uint32_t)__builtin_amdgcn_readlane((int)x, i) : (uint32_t)__shfl((int)x, i, LANES); };
     float v[8] = {};
-    add_places<T>(a, from, to, c, v);
-    store8(a.part + (int64_t)chunk * a.cols + c, to_raw<float>(v), a.cols - c);
-}
-// LANES lanes a row, eight columns each at a time.  Bound by writing the table's gradient.
-template <class T, int LANES> __global__ __launch_bounds__(256) void rows_kernel(GradArgs a)
-{
-    constexpr int ROWS = 256 / LANES;
-    const int lane = threadIdx.x % LANES;
-    for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; r < a.vocab; r += (int64_t)gridDim.x * ROWS) {
-        const int from = (int)a.first[r], to = (int)a.first[r + 1];
-        // whole chunks among the row's places
-        const int c0 = (int)(((uint32_t)from + a.chunk - 1) >> a.chunk_shift), c1 = to >> a.chunk_shift;
-        for (int c = 8 * lane; c < a.cols; c += 8 * LANES) {
-            float v[8] = {};
-            if (c0 >= c1) add_places<T>(a, from, to, c, v);
-            else {
-                add_places<T>(a, from, c0 << a.chunk_shift, c, v);
-                const float *p = a.part + (int64_t)c0 * a.cols + c;
-                for (int k = c0; k < c1; k += 4, p += 4 * (int64_t)a.cols) {
-                    Raw8<float> x[4];
+    uint32_t now = none;                       // the run that is being summed
+    auto store = [&](bool goes_on) {
+        const bool whole = now != before && !goes_on;
+        float *const p = (whole ? a.dtable + (int64_t)now * a.cols : (now == before ? a.head : a.tail) + (int64_t)g.chunk * a.cols) + at.c;
+        const float scale = whole ? a.scale : 1.f;
+        float f[8];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) x[u] = load8(k + u < c1 ? p + u * (int64_t)a.cols : p, k + u < c1 ? a.cols - c : 0);
+        for (int j = 0; j < 8; ++j) f[j] = v[j] * scale, v[j] = 0.f;
+        if (here) store8(p, to_raw<float>(f), at.n);
+    };
+    // The next places' rows are asked for before these are added: a row that is stored in between would have to be there first.
+    uint32_t key = 0, place = 0, k[2][STEP];
+    Raw8<T> x[2][STEP];
+    auto ask = [&](int i, auto half) {
+        const int b = (i - from) % LANES;
+        if (b == 0) {        // a lane has a place of its own at hand, all of them take it from there
+            const int own = min(i + g.lane, to - 1);
+            key = a.key[own], place = a.place[own];
+        }
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < STEP; ++u) {
+            k[half.value][u] = lanes(key, b + u);
+            x[half.value][u] = load_row<WIDE, T>(a, lanes(place, b + u), at);
+        }
+    };
+    auto take = [&](int i, auto half) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] += elem(x[u], j);
-                }
-                add_places<T>(a, c1 << a.chunk_shift, to, c, v);
+        for (int u = 0; u < STEP; ++u) {
+            const uint32_t q = k[half.value][u];
+            if (i + u >= to) continue;
+            if (q != now) {
+                if (now != none) store(false);
+                now = q;
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= a.scale;
-            store8(a.dtable + r * a.cols + c, to_raw<float>(v), a.cols - c);
+            for (int j = 0; j < 8; ++j) v[j] += now != none ? elem(x[half.value][u], j) : 0.f;
         }
+    };
+    const std::integral_constant<int, 0> _0;
+    const std::integral_constant<int, 1> _1;
+    ask(from, _0);
+    for (int i = from; i < to; i += 2 * STEP) {
+        if (i + STEP < to) ask(i + STEP, _1);
+        take(i, _0);
+        if (i + 2 * STEP < to) ask(i + 2 * STEP, _0);
+        if (i + STEP < to) take(i + STEP, _1);
     }
+    if (now != none) store(behind == now);
+}
+// The runs that end in another chunk than they began in: what they left, added in order.
+template <int LANES, bool WIDE> __global__ __launch_bounds__(256) void join_runs_kernel(GradArgs a, int per_chunk, int64_t groups)
+{
+    constexpr int AHEAD = 16;
+    const Group<LANES> g(a, per_chunk, groups);
+    if (!g.some || g.to >= a.n || g.c >= a.cols) return;
+    const uint32_t now = a.key[g.to - 1];
+    if (a.key[g.to] != now || now >= (uint32_t)a.vocab || (g.from > 0 && a.key[g.from - 1] == now)) return;
+    const Columns at(g.c, a.cols);
+    const int chunks = (int)(((int64_t)a.n + (1 << a.chunk_shift) - 1) >> a.chunk_shift);
+    float v[8];
+    const Raw8<float> first = load8(a.tail + (int64_t)g.chunk * a.cols + at.c, WIDE ? 8 : at.n);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = elem(first, j);
+    bool more = true;
+    for (int q = g.chunk + 1; more; q += AHEAD) {
+        bool mine[AHEAD];
+        Raw8<float> x[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int r = min(q + u, chunks - 1);
+            mine[u] = q + u < chunks && a.key[r << a.chunk_shift] == now;      // keys ascend: it is the run that the chunk begins with
+            x[u] = load8(a.head + (int64_t)r * a.cols + at.c, WIDE ? 8 : at.n);      // of other chunks: anything
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += mine[u] ? elem(x[u], j) : 0.f;
+        more = mine[AHEAD - 1];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= a.scale;
+    store8(a.dtable + (int64_t)now * a.cols + at.c, to_raw<float>(v), at.n);
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------------------
@@ -326,11 +460,14 @@ int desc_check(const cg_embedding_desc *d)
     if (d->vocab > most || d->cols > most || d->tokens > (1 << 28) || d->tokens * chunks > INT32_MAX / 2) return CG_EUNSUPPORTED;
     return CG_OK;
 }
-int chunk_shift_of(int64_t tokens) { return tokens <= 1 << 16 ? 5 : tokens <= 1 << 20 ? 7 : 9; }
+// More chunks, more waves; fewer, fewer parts of a frequent token to add one after the other: 3001 places of 769 columns 36 us with chunks of 32,
+// 32 with chunks of 16; 16384 of 1024 95 and 101 (lookup and gradient).
+int chunk_shift_of(int64_t tokens) { return tokens <= 4096 ? 4 : tokens <= kMostPass ? 5 : tokens <= 1 << 20 ? 7 : 9; }
 size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
 struct Layout {
-    size_t key[2], place[2], counts, first, part, total;
-    int tiles;                // 0: one block
+    size_t key[2], place[2], counts, head, tail, total;
+    int tiles;                // of the sort; 1: one block
+    bool passes;              // a pass is one launch
 };
 Layout layout_of(const cg_embedding_desc *d)
 {
@@ -338,39 +475,49 @@ Layout layout_of(const cg_embedding_desc *d)
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t p = at; at += round16(bytes); return p; };
     const size_t n = (size_t)d->tokens;
-    l.tiles = n <= (size_t)kMostOne ? 0 : (int)((n + kTile - 1) / kTile);
-    for (int i = 0; i < (l.tiles ? 2 : 1); ++i) l.key[i] = take(4 * n), l.place[i] = take(4 * n);
-    l.counts = take(l.tiles ? sizeof(uint32_t) * kDigits * (size_t)l.tiles : 0);
-    l.first = take(4 * ((size_t)d->vocab + 1));
-    l.part = take(4 * (n >> chunk_shift_of(d->tokens)) * (size_t)d->cols);
+    l.passes = n <= (size_t)kMostPass;
+    l.tiles = n <= (size_t)kMostOne ? 1 : (int)(l.passes ? (n + kOneBlock - 1) / kOneBlock : (n + kTile - 1) / kTile);
+    for (int i = 0; i < (l.tiles > 1 ? 2 : 1); ++i) l.key[i] = take(4 * n), l.place[i] = take(4 * n);
+    l.counts = take(l.passes ? 0 : sizeof(uint32_t) * kDigits * (size_t)l.tiles);
+    const size_t chunks = (n + ((size_t)1 << chunk_shift_of(d->tokens)) - 1) >> chunk_shift_of(d->tokens);
+    if (chunks > 1) l.head = take(4 * chunks * (size_t)d->cols), l.tail = take(4 * chunks * (size_t)d->cols);
     l.total = at;
     return l;
 }
 
-template <class TT> int lookup_typed(const LookupArgs &a, int type, dim3 grid, hipStream_t s)
+// One at a time where that does not fill the chip.
+template <class TT, class T> void lookup_launch(const LookupArgs &a, hipStream_t s)
 {
-    if (type == CG_TYPE_FP32) hipLaunchKernelGGL((lookup_kernel<TT, float>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((lookup_kernel<TT, bf16raw>), grid, dim3(256), 0, s, a);
+    const uint32_t b = (a.count + 255) / 256;
+    if (b <= 2048) hipLaunchKernelGGL((lookup_kernel<TT, T, 1>), dim3(b), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((lookup_kernel<TT, T, 4>), dim3(b < 4 * 8192 ? (b + 3) / 4 : 8192), dim3(256), 0, s, a);
+}
+template <class TT> int lookup_typed(const LookupArgs &a, int type, hipStream_t s)
+{
+    if (type == CG_TYPE_FP32) lookup_launch<TT, float>(a, s);
+    else lookup_launch<TT, bf16raw>(a, s);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
 }
-template <class T, int LANES> void rows_launch(const GradArgs &a, hipStream_t s)
+template <class T, int LANES, bool WIDE> void runs_launch(const GradArgs &a, hipStream_t s)
 {
-    const int64_t b = ((int64_t)a.vocab + 256 / LANES - 1) / (256 / LANES);
-    hipLaunchKernelGGL((rows_kernel<T, LANES>), dim3((unsigned)(b < 65536 ? b : 65536)), dim3(256), 0, s, a);
+    const int per = (a.cols + 8 * LANES - 1) / (8 * LANES);
+    const int64_t chunks = ((int64_t)a.n + (1 << a.chunk_shift) - 1) >> a.chunk_shift, groups = chunks * per;
+    const dim3 grid((unsigned)((groups + 256 / LANES - 1) / (256 / LANES)));
+    hipLaunchKernelGGL((runs_kernel<T, LANES, WIDE>), grid, dim3(256), 0, s, a, per, groups);
+    if (chunks > 1) hipLaunchKernelGGL((join_runs_kernel<LANES, WIDE>), grid, dim3(256), 0, s, a, per, groups);
 }
 template <class T> int grad_typed(const GradArgs &a, hipStream_t s)
 {
-    const int per = (a.cols + kGradThreads * 8 - 1) / (kGradThreads * 8), bounds = (int)std::min<int64_t>(((int64_t)a.vocab + kGradThreads) / kGradThreads, 4096);
-    hipLaunchKernelGGL((chunk_sums_kernel<T>), dim3((unsigned)(bounds + (a.n >> a.chunk_shift) * per)), dim3(kGradThreads), 0, s, a, bounds, per);
-    CG_HIP_TRY(hipGetLastError());
-    if (a.cols <= 32) rows_launch<T, 4>(a, s);
-    else if (a.cols <= 128) rows_launch<T, 16>(a, s);
-    else if (a.cols <= 512) rows_launch<T, 64>(a, s);
-    else rows_launch<T, 128>(a, s);
+    if (a.cols < 8) runs_launch<T, 4, false>(a, s);
+    else if (a.cols <= 32) runs_launch<T, 4, true>(a, s);
+    else if (a.cols <= 128) runs_launch<T, 16, true>(a, s);
+    else runs_launch<T, 64, true>(a, s);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
 }
+// Blocks of 1024 threads that fill `count` floats, 16 a thread at least.
+unsigned fillers(int64_t count) { return (unsigned)std::min<int64_t>((count + 16383) / 16384, 1024); }
 
 }  // namespace
 }  // namespace cg
@@ -388,10 +535,8 @@ extern "C" int cg_embedding_fwd(const cg_embedding_desc *d, const int32_t *token
     const uint32_t chunks = (uint32_t)((d->cols + 7) / 8);
     a.count = (uint32_t)d->tokens * chunks;
     a.by_chunks = make_fastdiv(chunks);
-    const uint32_t b = (a.count + 255) / 256;
-    const dim3 grid(b < 8192 ? b : 8192);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return d->table_type == CG_TYPE_FP32 ? lookup_typed<float>(a, d->type, grid, s) : lookup_typed<bf16raw>(a, d->type, grid, s);
+    return d->table_type == CG_TYPE_FP32 ? lookup_typed<float>(a, d->type, s) : lookup_typed<bf16raw>(a, d->type, s);
 }
 
 extern "C" size_t cg_embedding_workspace_bytes(const cg_embedding_desc *d) { return desc_check(d) == CG_OK ? layout_of(d).total : 0; }
@@ -401,7 +546,7 @@ extern "C" int cg_embedding_bwd(const cg_embedding_desc *d, const int32_t *token
     if (int rc = desc_check(d)) return rc;
     if (!floats_ok(dtable) || (d->tokens > 0 && (!floats_ok(tokens) || !tensor_ok(dy, dy_ld, d->cols, d->type)))) return CG_EINVAL;
     const Layout l = layout_of(d);
-    if (!ws || !aligned16(ws)) return CG_EINVAL;
+    if (l.total && (!ws || !aligned16(ws))) return CG_EINVAL;
     if (ws_bytes < l.total) return CG_ENOSPC;
     char *const base = static_cast<char *>(ws);
     auto words = [&](size_t at) { return reinterpret_cast<uint32_t *>(base + at); };
@@ -409,27 +554,50 @@ extern "C" int cg_embedding_bwd(const cg_embedding_desc *d, const int32_t *token
     int bits = 1;
     while (d->vocab >> bits) ++bits;           // keys are at most vocab
     const int passes = (bits + 7) / 8, per = (bits + passes - 1) / passes, n = (int)d->tokens;
-    int last = 0;
-    if (n > 0 && l.tiles == 0) {
-        CG_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&sort_one_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kOneLds));
-        hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(kOneBlock), kOneLds, s, tokens, n, (int)d->vocab, passes, per, words(l.key[0]), words(l.place[0]));
+    const int64_t count = d->vocab * d->cols;
+    if (n == 0) {
+        hipLaunchKernelGGL(fill_kernel, dim3(fillers(count)), dim3(1024), 0, s, Fill{dtable, count, 0});
         CG_HIP_TRY(hipGetLastError());
-    } else if (n > 0) {
+        return CG_OK;
+    }
+    int last = 0;
+    SortArgs a{};
+    a.tokens = tokens, a.counts = words(l.counts), a.n = n, a.vocab = (int)d->vocab, a.bits = per, a.tiles = l.tiles;
+    // a part beside each launch of the sort that goes over the places once
+    const int shares = l.tiles > 1 && l.passes ? passes : 1;
+    const int64_t share = (count + shares - 1) / shares;
+    int64_t filled = 0;
+    auto fill = [&](int first) {
+        const Fill f{dtable + filled, std::min(share, count - filled), first};
+        filled += f.count;
+        return f;
+    };
+    if (l.tiles == 1) {
+        a.key = words(l.key[0]), a.place = words(l.place[0]);
+        a.fill = fill(1);
+        hipLaunchKernelGGL(sort_one_kernel, dim3(1 + fillers(a.fill.count)), dim3(kOneBlock), 0, s, a, passes);
+        CG_HIP_TRY(hipGetLastError());
+    } else {
         for (int p = 0; p < passes; ++p) {
             last = p & 1;
-            SortArgs a{};
-            a.tokens = p == 0 ? tokens : nullptr;
             a.key_in = words(l.key[1 - last]), a.place_in = words(l.place[1 - last]), a.key = words(l.key[last]), a.place = words(l.place[last]);
-            a.counts = words(l.counts), a.n = n, a.vocab = (int)d->vocab, a.shift = p * per, a.bits = per, a.tiles = l.tiles;
-            hipLaunchKernelGGL(sort_count_kernel, dim3((unsigned)l.tiles), dim3(kTileBlock), 0, s, a);
-            hipLaunchKernelGGL(sort_sums_kernel, dim3(1), dim3(1024), 0, s, a.counts, kDigits * l.tiles);
-            hipLaunchKernelGGL(sort_move_kernel, dim3((unsigned)l.tiles), dim3(kTileBlock), 0, s, a);
+            a.shift = p * per;
+            a.fill = fill(l.tiles);
+            const unsigned beside = fillers(a.fill.count);
+            if (l.passes) hipLaunchKernelGGL(sort_pass_kernel, dim3((unsigned)l.tiles + beside), dim3(kOneBlock), 0, s, a);
+            else {
+                hipLaunchKernelGGL(sort_count_kernel, dim3((unsigned)l.tiles + 4 * beside), dim3(kTileBlock), 0, s, a);
+                hipLaunchKernelGGL(sort_sums_kernel, dim3(1), dim3(1024), 0, s, a.counts, kDigits * l.tiles);
+                hipLaunchKernelGGL(sort_move_kernel, dim3((unsigned)l.tiles), dim3(kTileBlock), 0, s, a);
+            }
             CG_HIP_TRY(hipGetLastError());
+            a.tokens = nullptr;
         }
     }
     GradArgs g{};
-    g.key = words(l.key[last]), g.place = words(l.place[last]), g.dy = dy, g.dy_ld = dy_ld, g.part = reinterpret_cast<float *>(base + l.part);
-    g.first = words(l.first), g.dtable = dtable, g.n = n, g.vocab = (int)d->vocab, g.cols = (int)d->cols, g.scale = d->scale;
-    g.chunk_shift = chunk_shift_of(d->tokens), g.chunk = 1 << g.chunk_shift;
+    g.key = words(l.key[last]), g.place = words(l.place[last]), g.dy = dy, g.dy_ld = dy_ld;
+    g.head = reinterpret_cast<float *>(base + l.head), g.tail = reinterpret_cast<float *>(base + l.tail);
+    g.dtable = dtable, g.n = n, g.vocab = (int)d->vocab, g.cols = (int)d->cols, g.scale = d->scale;
+    g.chunk_shift = chunk_shift_of(d->tokens);
     return d->type == CG_TYPE_FP32 ? grad_typed<float>(g, s) : grad_typed<bf16raw>(g, s);
 }

@@ -146,13 +146,27 @@ template <class T> __global__ __launch_bounds__(256) void column_sums_kernel(con
         out[(int64_t)blockIdx.y * cols + mine] = s;
     }
 }
+// The slices of 32 columns a block: eight threads a column take every eighth, four of them asked for at a time.
 __global__ __launch_bounds__(256) void column_join_kernel(const float *part, int slices, int cols, float *out)
 {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= cols) return;
+    __shared__ float lds[8][32];
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
     float s = 0.f;
-    for (int i = 0; i < slices; ++i) s += part[(int64_t)i * cols + c];
-    out[c] = s;
+    if (c < cols)
+        for (int i = ty; i < slices; i += 32) {
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = i + 8 * u < slices ? part[(int64_t)(i + 8 * u) * cols + c] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s += v[u];
+        }
+    lds[ty][tx] = s;
+    __syncthreads();
+    if (ty == 0 && c < cols) {
+#pragma unroll
+        for (int u = 1; u < 8; ++u) s += lds[u][tx];
+        out[c] = s;
+    }
 }
 
 // ---- the gradient through an activation alone -----------------------------------------------------------------------------------
@@ -221,6 +235,10 @@ int column_slices(int64_t M, int64_t N)
     int64_t s = want < most ? want : most;
     return (int)(s < 1 ? 1 : s > 256 ? 256 : s);
 }
+// Backward-weight in large tiles multiplies bf16 numbers: x in 8 bits is unpacked first.  Eight rows of tiles would each turn it into bf16 on
+// its way into LDS otherwise (8192 tokens, 8192 x 2048 weights: 521 us in tiles of 256 through registers, 812 in tiles of 128; 36 and 208 so).
+bool unpacks(const cg_linear_desc *d, const Plan &p) { return p.large && d->K % 8 == 0 && d->M * ((d->K + kPackBlock - 1) / kPackBlock) <= (INT32_MAX >> 2) - 65535; }
+size_t unpacked_bytes(const cg_linear_desc *d) { return (size_t)d->M * (size_t)d->K * 2; }
 size_t slice_bytes(const cg_linear_desc *d)
 {
     const int s = column_slices(d->M, d->N);
@@ -237,7 +255,7 @@ unsigned blocks_for(uint64_t n, unsigned most) { const uint64_t b = (n + 255) / 
 
 int product(const cg_linear_desc *d, int pass, const Plan &p, GemmArgs &a, bool packed, bool dma, void *ws, hipStream_t s)
 {
-    const bool large = p.large && dma;
+    const bool large = p.large && dma && !packed;
     const int tile = gemm_tile(large);
     a.R = p.R, a.C = p.C, a.K = p.K;
     a.tiles_r = (p.R + tile - 1) / tile, a.tiles_c = (p.C + tile - 1) / tile;
@@ -291,9 +309,12 @@ using namespace cg;
 extern "C" size_t cg_linear_workspace_bytes(const cg_linear_desc *d, int pass)
 {
     if (desc_check(d) != CG_OK || d->M == 0 || (pass != CG_PASS_FWD && pass != CG_PASS_BWD_DATA && pass != CG_PASS_BWD_WEIGHT)) return 0;
-    const size_t part = part_bytes(plan_of(d, pass));
-    if (pass != CG_PASS_BWD_WEIGHT) return part;
-    return part > slice_bytes(d) ? part : slice_bytes(d);
+    const Plan p = plan_of(d, pass);
+    size_t need = part_bytes(p);
+    if (pass != CG_PASS_BWD_WEIGHT) return need;
+    if (slice_bytes(d) > need) need = slice_bytes(d);
+    if (unpacks(d, p) && unpacked_bytes(d) > need) need = unpacked_bytes(d);
+    return need;
 }
 
 extern "C" int cg_linear_fwd(const cg_linear_desc *d, const void *x, int64_t x_ld, const void *w, int64_t w_ld, const float *bias,
@@ -353,16 +374,21 @@ extern "C" int cg_linear_bwd_weight(const cg_linear_desc *d, const void *dz, int
         else hipLaunchKernelGGL((column_sums_kernel<bf16raw>), grid, dim3(256), 0, s, static_cast<const bf16raw *>(dz), dz_ld, M, N, slice, to);
         CG_HIP_TRY(hipGetLastError());
         if (slices > 1) {
-            hipLaunchKernelGGL(column_join_kernel, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, s, to, slices, N, dbias);
+            hipLaunchKernelGGL(column_join_kernel, dim3((unsigned)((N + 31) / 32)), dim3(256), 0, s, to, slices, N, dbias);
             CG_HIP_TRY(hipGetLastError());
         }
     }
     GemmArgs a{};
     a.A = dz, a.a_ld = dz_ld, a.epi.out = dw, a.epi.out_ld = d->K;
+    const Plan p = plan_of(d, CG_PASS_BWD_WEIGHT);
+    const bool dz_dma = d->type == CG_TYPE_BF16 && dma_ok(dz, dz_ld, d->N);
+    if (x8 && dz_dma && unpacks(d, p)) {
+        if (int rc = cg_unpack8(d->type, d->M, d->K, x8, ws, d->K, stream)) return rc;
+        x = ws, x_ld = d->K, x8 = nullptr;
+    }
     if (x8) a.B8 = {x8->codes, x8->scales, x8->codes_ld, x8->scales_ld};
     else a.B = x, a.b_ld = x_ld;
-    const bool dma = d->type == CG_TYPE_BF16 && dma_ok(dz, dz_ld, d->N) && (x8 || dma_ok(x, x_ld, d->K));
-    return product(d, CG_PASS_BWD_WEIGHT, plan_of(d, CG_PASS_BWD_WEIGHT), a, x8 != nullptr, dma, ws, s);
+    return product(d, CG_PASS_BWD_WEIGHT, p, a, x8 != nullptr, dz_dma && (x8 || dma_ok(x, x_ld, d->K)), ws, s);
 }
 
 extern "C" int cg_act_bwd(int act, int type, int64_t rows, int64_t cols, const void *dy, int64_t dy_ld, const void *z, int64_t z_ld,

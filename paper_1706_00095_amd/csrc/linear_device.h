@@ -85,12 +85,26 @@ __device__ __forceinline__ float slope_times(float g, float z, int act)
     return g;
 }
 
-template <class T> __device__ __forceinline__ void finish8(const EpiArgs &e, float (&v)[8], int64_t row, int c, int n)
+// What the epilogue reads for eight sums of a row, apart from the bias: asked for ahead of its use.
+template <class T> struct EpiIn {
+    Raw8<T> add, z;
+    Raw8Packed z8;
+};
+template <class T> __device__ __forceinline__ EpiIn<T> epi_load(const EpiArgs &e, int64_t row, int c, int n)
+{
+    EpiIn<T> in = {};
+    if (e.add) in.add = load8(static_cast<const T *>(e.add) + (n > 0 ? row * e.add_ld + c : 0), n);
+    if (e.slope != CG_ACT_NONE) {
+        if (e.z_in8.codes) in.z8 = load8(e.z_in8, row, c, n);
+        else in.z = load8(static_cast<const T *>(e.z_in) + (n > 0 ? row * e.z_in_ld + c : 0), n);
+    }
+    return in;
+}
+template <class T> __device__ __forceinline__ void epi_finish(const EpiArgs &e, float (&v)[8], const Raw8<float> &bias, const EpiIn<T> &in, int64_t row, int c, int n)
 {
     if (e.bias) {
-        const Raw8<float> b = load8(e.bias + c, n);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += elem(b, i);
+        for (int i = 0; i < 8; ++i) v[i] += elem(bias, i);
     }
     if (e.z) store8(static_cast<T *>(e.z) + row * e.z_ld + c, to_raw<T>(v), n);
     if (e.act != CG_ACT_NONE) {
@@ -99,21 +113,25 @@ template <class T> __device__ __forceinline__ void finish8(const EpiArgs &e, flo
     }
     if (e.slope != CG_ACT_NONE) {
         if (e.z_in8.codes) {
-            const Raw8Packed z = load8(e.z_in8, row, c, n);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(z, i), e.slope);
+            for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(in.z8, i), e.slope);
         } else {
-            const Raw8<T> z = load8(static_cast<const T *>(e.z_in) + row * e.z_in_ld + c, n);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(z, i), e.slope);
+            for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(in.z, i), e.slope);
         }
     }
     if (e.add) {
-        const Raw8<T> a = load8(static_cast<const T *>(e.add) + row * e.add_ld + c, n);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += elem(a, i);
+        for (int i = 0; i < 8; ++i) v[i] += elem(in.add, i);
     }
     store8(static_cast<T *>(e.out) + row * e.out_ld + c, to_raw<T>(v), n);
+}
+template <class T> __device__ __forceinline__ void finish8(const EpiArgs &e, float (&v)[8], int64_t row, int c, int n)
+{
+    Raw8<float> bias = {};
+    if (e.bias) bias = load8(e.bias + c, n);
+    const EpiIn<T> in = epi_load<T>(e, row, c, n);
+    epi_finish(e, v, bias, in, row, c, n);
 }
 
 }  // namespace

@@ -96,6 +96,56 @@ template <bool ACROSS, int XT, int STEP, int NT> struct TileLoader<bf16raw, ACRO
     __device__ __forceinline__ void finish(LdsByte *) const {}
 };
 
+// The same for one half (128 rows or columns of C) of a large tile, step after step; 512 threads, two loads each.  The buffer is the half's
+// rows (of a step, where they lie across k), so that its size is a number of 32 bits.
+template <bool ACROSS> struct HalfLoader {
+    static constexpr int STEP = 64, ROWS = ACROSS ? STEP : 128, COLS = ACROSS ? 128 : STEP;
+    using Lds = LdsTile<ACROSS, ROWS, COLS, 1>;
+    uint64_t at, advance;             // address of the next step's tile, bytes from a step to the next
+    uint32_t bytes, row;              // from `at` on; from a row to the next (across k)
+    int k_left;
+    uint32_t voff[2];
+    __device__ __forceinline__ HalfLoader(const void *p, int64_t ld, int x0, int count, int kbeg, int kend)
+    {
+        const int row0 = ACROSS ? kbeg : x0, col0 = ACROSS ? x0 : kbeg, rows = min((ACROSS ? kend : count) - row0, ROWS), cols = (ACROSS ? count : kend) - col0;
+        at = (uint64_t)reinterpret_cast<uintptr_t>(p) + (uint64_t)((row0 * ld + col0) * 2);
+        row = (uint32_t)ld * 2;
+        bytes = rows > 0 && cols > 0 ? (uint32_t)(rows - 1) * row + (uint32_t)min(cols, ACROSS ? 128 : INT32_MAX) * 2 : 0;       // none: zeros
+        advance = ACROSS ? (uint64_t)row * STEP : 2 * STEP;
+        k_left = kend - kbeg;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) voff[j] = ACROSS && 8 * chunk_of(j) >= cols ? OOB_ROW : (uint32_t)row_of(j) * row + (uint32_t)chunk_of(j) * 16;
+    }
+    static __device__ __forceinline__ int place(int j) { return (j * 8 + (int)(threadIdx.x >> 6)) * 1024 + (int)(threadIdx.x & 63) * 16; }
+    static __device__ __forceinline__ int row_of(int j) { return place(j) / (COLS * 2); }
+    static __device__ __forceinline__ int chunk_of(int j) { return place(j) % (COLS * 2) / 16 ^ Lds::swizzle(row_of(j)); }
+    // One of the step's two loads; behind the second the loader stands at the next step.  WHOLE: not the last step.
+    template <bool WHOLE, int J> __device__ __forceinline__ void load(LdsByte *lds, int wave)
+    {
+        BufferRsrc r;
+        r.x = __builtin_amdgcn_readfirstlane((uint32_t)at);
+        r.y = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu);
+        uint32_t size = bytes, off = voff[J];
+        if constexpr (!WHOLE) {
+            if (ACROSS) size -= k_left < STEP && bytes ? (uint32_t)(STEP - max(k_left, 1)) * row : 0;
+            else off = 8 * chunk_of(J) < k_left ? off : OOB_ROW;
+        }
+        r.z = __builtin_amdgcn_readfirstlane(size);
+        r.w = 0x00020000u;
+        dma16(r, lds + (J * 8 + wave) * 1024, off);
+        if (J == 1) {
+            at += advance;
+            if (!ACROSS) bytes -= bytes ? 2 * STEP : 0;
+            k_left -= STEP;
+        }
+    }
+    __device__ __forceinline__ void next(LdsByte *lds, int wave)
+    {
+        load<false, 0>(lds, wave);
+        load<false, 1>(lds, wave);
+    }
+};
+
 // Otherwise through registers, at any alignment; fp32 is cut on the way.
 template <class T, bool ACROSS, int XT, int STEP, int NT> struct TileLoader<T, ACROSS, XT, STEP, NT, false> {
     static constexpr int NP = Pieces<T>::N, ROWS = ACROSS ? STEP : XT, COLS = ACROSS ? XT : STEP, CH = COLS / 8, N = ROWS * CH / NT;
@@ -174,6 +224,13 @@ template <int NA, int NB> struct Sums {
     }
     __device__ __forceinline__ float get(int i) const { return CUT ? big[i] + small[i] : big[i]; }
 };
+
+// This wave's loads into LDS but the latest LOADS have landed, its reads of LDS but the latest READS are done, and everyone's.  The compiler's
+// barrier would wait for all of them.
+template <int LOADS, int READS> __device__ __forceinline__ void end_phase()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)\n\ts_barrier" ::"n"(LOADS), "n"(READS) : "memory");
+}
 
 // Consecutive blocks run on different XCDs, each with an L2 of its own: every XCD gets a stretch of neighbouring tiles, in groups of
 // 8 rows of tiles, so that the 32 blocks it runs at a time read 8 strips of A and 4 of B.
@@ -312,6 +369,162 @@ __global__ __launch_bounds__((XT == 256 ? 512 : 256), 2) void gemm_kernel(GemmAr
     }
 }
 
+// Tiles of 256 x 256 of bf16 tensors, eight waves.  Operands pass through LDS in halves of 128 rows or columns, A0 A1 B0 B1, 64 values of k at
+// a time, two steps in LDS.  A wave makes 64 x 32 of each quarter of the tile, a quarter a phase, and reads in each phase the half that it
+// needs next, so that its operands are in registers when a phase begins (what a phase uses for the last time is overwritten as it goes):
+//     even steps   A0 B0 (reads B1)   A0 B1 (A1)   A1 B1 (B1 of the next step)   A1 B0 (A0 of the next step)
+//     odd steps    A0 B1 (reads B0)   A0 B0 (A1)   A1 B0 (B0 of the next step)   A1 B1 (A0 of the next step)
+// Two phases after a half was read its place is filled with what is read there eight phases after, so loads have five phases to arrive.  The
+// barrier at a phase's end: everyone's reads of the phase before are done, and everyone's part of the next half has landed.
+constexpr int kHalf = 128 * 64 * 2, kLargeRow = (32 + 4) * 4;
+template <bool AX, bool BX, class TO> __global__ __launch_bounds__(512, 2) void gemm_large_kernel(GemmArgs a)
+{
+    using LA = HalfLoader<AX>;
+    using LB = HalfLoader<BX>;
+    extern __shared__ __align__(16) char smem[];
+    LdsByte *const lds = (LdsByte *)smem;
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave >> 2, wc = wave & 3;
+    int tr, tc, split;
+    place_of(a, tr, tc, split);
+    const int r0 = tr * 256, c0 = tc * 256, kbeg = split * a.chunk, kend = min(a.K, kbeg + a.chunk), n = (kend - kbeg + 63) / 64;
+
+    LA la[2] = {LA(a.A, a.a_ld, r0, a.R, kbeg, kend), LA(a.A, a.a_ld, r0 + 128, a.R, kbeg, kend)};
+    LB lb[2] = {LB(a.B, a.b_ld, c0, a.C, kbeg, kend), LB(a.B, a.b_ld, c0 + 128, a.C, kbeg, kend)};
+    // a lane's places of either operand lie within what an instruction's offset reaches
+    auto at_a = [&](int h, int s) { return lds + ((s & 1) * 2 + h) * kHalf; };
+    auto at_b = [&](int h, int s) { return lds + (4 + (s & 1) * 2 + h) * kHalf; };
+    Frag<1> fa[4][2], fb[2][4];
+    v16f acc[2][2][2];               // half of A, half of B, 32 rows
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i >> 2][i >> 1 & 1][i & 1] = v16f{};
+
+    auto read_a = [&](int h, int s, int ks) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) fa[ks][i] = LA::Lds::read(at_a(h, s), 64 * wr + 32 * i, ks, lane);
+    };
+    auto read_b = [&](auto h, int s, int ks) { fb[h.value][ks] = LB::Lds::read(at_b(h.value, s), 32 * wc, ks, lane); };
+    auto multiply = [&](auto ha, auto hb, int ks) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) acc[ha.value][hb.value][i] = mfma(fb[hb.value][ks].p[0], fa[ks][i].p[0], acc[ha.value][hb.value][i]);
+    };
+    const std::integral_constant<int, 0> _0;
+    const std::integral_constant<int, 1> _1;
+    // A phase: two products, what they leave to be read, and in the middle the loads (at its beginning all waves would wait for each other's).
+    auto phase = [&](auto ha, auto hb, auto full, bool fill, auto &loader, LdsByte *to, auto read) {
+        constexpr bool FULL = decltype(full)::value;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            multiply(ha, hb, ks);
+            read(ks);
+            if (ks == 0 && (FULL || fill)) loader.template load<FULL, 0>(to, wave);
+            if (ks == 2 && (FULL || fill)) loader.template load<FULL, 1>(to, wave);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // first: the half of B that the step begins with.  full: all that the step loads and reads ahead is there, and no load the last one
+    auto step = [&](int s, auto first, auto full) {
+        constexpr bool FULL = decltype(full)::value;
+        const std::integral_constant<int, 1 - decltype(first)::value> second;
+        constexpr int READS_A = AX ? 15 : 8, READS_B = BX ? 8 : 4, LOADS = FULL ? 10 : 0;
+        const bool fill = s + 2 < n, more = FULL || s + 1 < n;
+        phase(_0, first, full, fill, lb[first.value], at_b(first.value, s), [&](int ks) { read_b(second, s, ks); });
+        end_phase<LOADS, READS_B>();
+        phase(_0, second, full, fill, la[0], at_a(0, s), [&](int ks) { read_a(1, s, ks); });
+        end_phase<LOADS, READS_A>();
+        phase(_1, second, full, fill, lb[second.value], at_b(second.value, s), [&](int ks) { if (more) read_b(second, s + 1, ks); });
+        end_phase<LOADS, READS_B>();
+        phase(_1, first, full, fill, la[1], at_a(1, s), [&](int ks) { if (more) read_a(0, s + 1, ks); });
+        end_phase<LOADS, READS_A>();
+    };
+    if (n > 0) {
+        lb[0].next(at_b(0, 0), wave);
+        la[0].next(at_a(0, 0), wave);
+        lb[1].next(at_b(1, 0), wave);
+        la[1].next(at_a(1, 0), wave);
+        if (n > 1) {
+            lb[1].next(at_b(1, 1), wave);
+            la[0].next(at_a(0, 1), wave);
+            lb[0].next(at_b(0, 1), wave);
+            la[1].next(at_a(1, 1), wave);
+        }
+        if (n > 1) end_phase<12, 0>();
+        else end_phase<0, 0>();
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            read_b(_0, 0, ks);
+            read_a(0, 0, ks);
+        }
+        if (n > 1) end_phase<10, 0>();
+        else end_phase<0, 0>();
+        int s = 0;
+        for (; s + 4 < n; s += 2) {
+            step(s, _0, std::true_type());
+            step(s + 1, _1, std::true_type());
+        }
+        for (; s < n; s += 2) {
+            step(s, _0, std::false_type());
+            if (s + 1 < n) step(s + 1, _1, std::false_type());
+        }
+    }
+
+    // What a half of the rows needs is asked for at once: a wave has nothing else to do while it waits.
+    LdsByte *const mine = lds + wave * 32 * kLargeRow;
+    const EpiArgs e = a.epi;
+    constexpr bool PLAIN = AX;          // backward-weight: sums are the result
+    const int c_of = c0 + 32 * wc + 8 * (lane & 3), r_of = r0 + 64 * wr + lane / 4;
+    Raw8<float> bias[2] = {};
+    if (!PLAIN && e.bias)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) bias[h] = load8(e.bias + (c_of + 128 * h < a.C ? c_of + 128 * h : 0), a.C - c_of - 128 * h);
+#pragma unroll
+    for (int ha = 0; ha < 2; ++ha) {
+        EpiIn<TO> in[2][2][2];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int r = r_of + 128 * ha + 32 * (q >> 1 & 1) + 16 * (q & 1), c = c_of + 128 * (q >> 2);
+            if constexpr (!PLAIN) in[q >> 2][q >> 1 & 1][q & 1] = epi_load<TO>(e, r, c, r < a.R ? a.C - c : 0);
+        }
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    u32x4 v;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) v[x] = __float_as_uint(acc[ha][hb][i][4 * u + x]);
+                    CG_LDS(u32x4, mine + (lane & 31) * kLargeRow + (8 * u + 4 * (lane >> 5)) * 4) = v;
+                }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int c = c_of + 128 * hb, r = r_of + 128 * ha + 32 * i + 16 * t;
+                    float v[8];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const u32x4 x = CG_LDS(u32x4, mine + (16 * t + lane / 4) * kLargeRow + (8 * (lane & 3) + 4 * h) * 4);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) v[4 * h + y] = __uint_as_float(x[y]);
+                    }
+                    if (r < a.R && c < a.C) {
+                        if constexpr (PLAIN) store8(static_cast<TO *>(e.out) + r * e.out_ld + c, to_raw<TO>(v), a.C - c);
+                        else epi_finish<TO>(e, v, bias[hb], in[hb][i][t], r, c, a.C - c);
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+    }
+}
+template <bool AX, bool BX, class TO> int launch_large(const GemmArgs &a, hipStream_t s)
+{
+    constexpr int LDS = 8 * kHalf;
+    auto *const kernel = gemm_large_kernel<AX, BX, TO>;
+    CG_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles_r * a.tiles_c)), dim3(512), LDS, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
 template <class T, class TB, bool AX, bool BX, int XT, bool DMA, class TO> int launch(const GemmArgs &a, hipStream_t s)
 {
     using Cfg = Config<T, TB, AX, BX, XT, DMA>;
@@ -324,7 +537,8 @@ template <class T, class TB, bool AX, bool BX, int XT, bool DMA, class TO> int l
 }
 template <class T, class TB, bool AX, bool BX, class TO> int launch_bf16(const GemmKind &k, const GemmArgs &a, hipStream_t s)
 {
-    if (k.large) return launch<T, TB, AX, BX, 256, true, TO>(a, s);
+    if constexpr (sizeof(TB) == 2)
+        if (k.large) return launch_large<AX, BX, TO>(a, s);
     if (k.dma) return launch<T, TB, AX, BX, 128, true, TO>(a, s);
     return launch<T, TB, AX, BX, 128, false, TO>(a, s);
 }
