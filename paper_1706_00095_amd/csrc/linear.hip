@@ -186,7 +186,7 @@ template <class T> __global__ __launch_bounds__(256) void act_bwd_kernel(const T
 // ---- plans ------------------------------------------------------------------------------------------------------------------------
 constexpr int64_t kMostBlocks = 1 << 22;       // of 512 threads a launch has room for less than 2^32
 constexpr int kFewTokens = 32;
-constexpr int kMostSplits = 32, kLeastChunk = 4 * kGemmStep;
+constexpr int kMostSplits = 32, kLeastChunk = 4 * kGemmStep, kLeastChunkFp32 = 2 * kGemmStep;
 
 bool act_ok(int act) { return act >= CG_ACT_NONE && act <= CG_ACT_SILU; }
 int desc_check(const cg_linear_desc *d)
@@ -201,8 +201,8 @@ int desc_check(const cg_linear_desc *d)
 struct Plan {
     int R, C, K;              // of the product
     bool few;
-    int splits, chunk;        // of tiles of 128
-    bool large;               // where rows allow it: tiles of 256, k uncut
+    bool large;               // tiles of 256 x 256, k uncut, where rows allow it (bf16)
+    int splits, chunk;        // of tiles of 128 x 128
 };
 Plan plan_of(const cg_linear_desc *d, int pass)
 {
@@ -216,9 +216,10 @@ Plan plan_of(const cg_linear_desc *d, int pass)
     if (p.few) return p;
     auto tiles = [&](int64_t t) { return ((p.R + t - 1) / t) * ((p.C + t - 1) / t); };
     p.large = d->type == CG_TYPE_BF16 && tiles(256) >= 128;
+    // two blocks a compute unit
     const int64_t n = tiles(128);
     int64_t s = n >= 512 ? 1 : 512 / n;
-    const int64_t most = (p.K + kLeastChunk - 1) / kLeastChunk;
+    const int64_t least = d->type == CG_TYPE_FP32 ? kLeastChunkFp32 : kLeastChunk, most = (p.K + least - 1) / least;
     if (s > most) s = most;
     if (s > kMostSplits) s = kMostSplits;
     if (s > 1) {
@@ -256,7 +257,7 @@ unsigned blocks_for(uint64_t n, unsigned most) { const uint64_t b = (n + 255) / 
 int product(const cg_linear_desc *d, int pass, const Plan &p, GemmArgs &a, bool packed, bool dma, void *ws, hipStream_t s)
 {
     const bool large = p.large && dma && !packed;
-    const int tile = gemm_tile(large);
+    const int tile = large ? 256 : 128;
     a.R = p.R, a.C = p.C, a.K = p.K;
     a.tiles_r = (p.R + tile - 1) / tile, a.tiles_c = (p.C + tile - 1) / tile;
     a.splits = large ? 1 : p.splits, a.chunk = large ? p.K : p.chunk;

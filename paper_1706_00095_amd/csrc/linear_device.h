@@ -30,11 +30,11 @@ struct GemmArgs {
     EpiArgs epi;
 };
 
-// linear_gemm.hip.  Which of its kernels: PASS_*; large: tiles of 256 x 256, else 128 x 128; dma: both operands travel to LDS without registers.
+// linear_gemm.hip.  Which of its kernels: PASS_*; large: tiles of 256 x 256, else 128 x 128; dma: bf16 operands travel to LDS
+// without registers.
 struct GemmKind { int type, pass, packed, large, dma; };
 int gemm_launch(const GemmKind &kind, const GemmArgs &a, hipStream_t s);
 constexpr int kGemmStep = 64;         // chunks of k are multiples of it
-constexpr int gemm_tile(bool large) { return large ? 256 : 128; }
 
 namespace {
 

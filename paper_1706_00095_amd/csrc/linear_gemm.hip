@@ -32,21 +32,19 @@ template <bool ACROSS, int ROWS, int COLS, int NP> struct LdsTile {
         for (int k = 0; k < NP; ++k) CG_LDS(u32x4, t + k * PLANE + at(row, chunk)) = f.p[k];
     }
     // operand of 32 rows or columns of C from x0 on, the values 16 ks .. 16 ks + 15 of the step; lane l has those from 8 (l / 32) on
+    static __device__ __forceinline__ u32x4 read_plane(LdsByte *t, int x0, int ks, int lane, int plane)
+    {
+        if constexpr (!ACROSS) return CG_LDS(u32x4, t + plane * PLANE + at(x0 + (lane & 31), 2 * ks + (lane >> 5)));
+        const int row = 16 * ks + 8 * (lane >> 5) + (lane >> 2 & 3), chunk = (x0 >> 3) + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        LdsByte *base = t + plane * PLANE + at(row, chunk) + 8 * (lane & 1);
+        const uint2 a = __builtin_bit_cast(uint2, read_tr(base)), b = __builtin_bit_cast(uint2, read_tr(base + 4 * COLS * 2));
+        return u32x4{a.x, a.y, b.x, b.y};
+    }
     static __device__ __forceinline__ Frag<NP> read(LdsByte *t, int x0, int ks, int lane)
     {
         Frag<NP> f;
-        if constexpr (!ACROSS) {
 #pragma unroll
-            for (int k = 0; k < NP; ++k) f.p[k] = CG_LDS(u32x4, t + k * PLANE + at(x0 + (lane & 31), 2 * ks + (lane >> 5)));
-        } else {
-            const int row = 16 * ks + 8 * (lane >> 5) + (lane >> 2 & 3), chunk = (x0 >> 3) + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-#pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                LdsByte *base = t + k * PLANE + at(row, chunk) + 8 * (lane & 1);
-                const uint2 a = __builtin_bit_cast(uint2, read_tr(base)), b = __builtin_bit_cast(uint2, read_tr(base + 4 * COLS * 2));
-                f.p[k] = u32x4{a.x, a.y, b.x, b.y};
-            }
-        }
+        for (int k = 0; k < NP; ++k) f.p[k] = read_plane(t, x0, ks, lane, k);
         return f;
     }
 };
@@ -67,7 +65,7 @@ template <bool ACROSS, int XT, int STEP, int NT> struct TileLoader<bf16raw, ACRO
     int64_t ld;
     int count, kend, x0;
     uint32_t voff[N];
-    __device__ __forceinline__ TileLoader(const void *p, const Packed &, int64_t ld_, int x0_, int count_, int kend_)
+    __device__ __forceinline__ TileLoader(const void *p, const Packed &, int64_t ld_, int x0_, int count_, int, int kend_, int)
         : base(static_cast<const bf16raw *>(p)), ld(ld_), count(count_), kend(kend_), x0(x0_)
     {
 #pragma unroll
@@ -79,7 +77,8 @@ template <bool ACROSS, int XT, int STEP, int NT> struct TileLoader<bf16raw, ACRO
     static __device__ __forceinline__ int at(int j) { return (j * WAVES + (int)(threadIdx.x >> 6)) * 1024 + (int)(threadIdx.x & 63) * 16; }
     static __device__ __forceinline__ int row_of(int j) { return at(j) / (COLS * 2); }
     static __device__ __forceinline__ int chunk_of(int j) { return at(j) % (COLS * 2) / 16 ^ Lds::swizzle(row_of(j)); }
-    __device__ __forceinline__ void start(int k, LdsByte *lds) const
+    __device__ __forceinline__ bool inside(int) const { return true; }
+    template <bool> __device__ __forceinline__ void start(int k, LdsByte *lds) const
     {
         const int row0 = ACROSS ? k : x0, col0 = ACROSS ? x0 : k, rows = (ACROSS ? kend : count) - row0, cols = (ACROSS ? count : kend) - col0;
         const BufferRsrc r = raw_buffer((uint64_t)reinterpret_cast<uintptr_t>(base) + (uint64_t)((row0 * ld + col0) * 2),
@@ -146,83 +145,129 @@ template <bool ACROSS> struct HalfLoader {
     }
 };
 
-// Otherwise through registers, at any alignment; fp32 is cut on the way.
-template <class T, bool ACROSS, int XT, int STEP, int NT> struct TileLoader<T, ACROSS, XT, STEP, NT, false> {
-    static constexpr int NP = Pieces<T>::N, ROWS = ACROSS ? STEP : XT, COLS = ACROSS ? XT : STEP, CH = COLS / 8, N = ROWS * CH / NT;
-    static_assert(ROWS * CH % NT == 0, "every thread loads as much");
-    using Lds = LdsTile<ACROSS, ROWS, COLS, NP>;
+// Otherwise through registers, at any alignment; fp32 is cut, and 8-bit numbers become bf16, on the way.
+// inside(k): the step that begins at k may be loaded without bounds.  All of its values of k are there, and where rows lie across k another row
+// behind them, into which the last chunk of a row may reach; rows and chunks behind the last one are others again: what they give is not stored.
+template <class T> struct Source;
+template <class T> struct Source {
     const T *base;
     int64_t ld;
-    int count, kend, x0;
-    Raw8<T> r[N];
-    __device__ __forceinline__ TileLoader(const void *p, const Packed &, int64_t ld_, int x0_, int count_, int kend_)
-        : base(static_cast<const T *>(p)), ld(ld_), count(count_), kend(kend_), x0(x0_) {}
-    __device__ __forceinline__ void start(int k, LdsByte *)
-    {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int i = threadIdx.x + j * NT, row = (ACROSS ? k : x0) + i / CH, c = (ACROSS ? x0 : k) + 8 * (i % CH);
-            const int n = row < (ACROSS ? kend : count) ? (ACROSS ? count : kend) - c : 0;
-            r[j] = load8(base + (n > 0 ? row * ld + c : 0), n);
+    using Raw = Raw8<T>;
+    __device__ __forceinline__ Source(const void *p, const Packed &, int64_t ld_) : base(static_cast<const T *>(p)), ld(ld_) {}
+    __device__ __forceinline__ Raw load(int64_t row, int c, int n) const { return load8(base + (n > 0 ? row * ld + c : 0), n); }
+    struct At {
+        const T *p;
+        __device__ __forceinline__ Raw take(const Source &s, int rows, int cols)
+        {
+            const Raw r = load8(p, 8);
+            p += rows * s.ld + cols;
+            return r;
         }
-    }
-    __device__ __forceinline__ void finish(LdsByte *t) const
-    {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int i = threadIdx.x + j * NT;
-            Lds::put(t, i / CH, i % CH, frag_of(r[j]));
-        }
-    }
+    };
+    __device__ __forceinline__ At at(int64_t row, int c) const { return {base + row * ld + c}; }
 };
-
-// 8-bit tensors
-template <bool ACROSS, int XT, int STEP, int NT> struct TileLoader<int8_t, ACROSS, XT, STEP, NT, false> {
-    static constexpr int NP = 1, ROWS = ACROSS ? STEP : XT, COLS = ACROSS ? XT : STEP, CH = COLS / 8, N = ROWS * CH / NT;
-    static_assert(ROWS * CH % NT == 0, "every thread loads as much");
-    using Lds = LdsTile<ACROSS, ROWS, COLS, 1>;
+template <> struct Source<int8_t> {
     Packed p;
-    int count, kend, x0;
-    Raw8Packed r[N];
-    __device__ __forceinline__ TileLoader(const void *, const Packed &p_, int64_t, int x0_, int count_, int kend_) : p(p_), count(count_), kend(kend_), x0(x0_) {}
-    __device__ __forceinline__ void start(int k, LdsByte *)
+    using Raw = Raw8Packed;
+    __device__ __forceinline__ Source(const void *, const Packed &p_, int64_t) : p(p_) {}
+    __device__ __forceinline__ Raw load(int64_t row, int c, int n) const { return load8(p, row, c, n); }
+    struct At {
+        const int8_t *q;
+        const uint8_t *e;
+        __device__ __forceinline__ Raw take(const Source &s, int rows, int)        // rows lie across k: columns stay
+        {
+            const Loose8 v = *reinterpret_cast<const Loose8 *>(q);
+            const Raw r = {{v.w[0], v.w[1]}, (int)*e - kPackBias};
+            q += rows * s.p.codes_ld, e += rows * s.p.scales_ld;
+            return r;
+        }
+    };
+    __device__ __forceinline__ At at(int64_t row, int c) const { return {p.codes + row * p.codes_ld + c, p.scales + row * p.scales_ld + c / kPackBlock}; }
+};
+__device__ __forceinline__ Frag<1> frag_of(const Raw8Packed &r)
+{
+    Frag<1> f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f.p[0][q] = pack_bf16(elem(r, 2 * q), elem(r, 2 * q + 1));
+    return f;
+}
+template <class T, bool ACROSS, int XT, int STEP, int NT> struct TileLoader<T, ACROSS, XT, STEP, NT, false> {
+    static constexpr int NP = sizeof(T) == 4 ? 3 : 1, ROWS = ACROSS ? STEP : XT, COLS = ACROSS ? XT : STEP, CH = COLS / 8, N = ROWS * CH / NT;
+    static_assert(ROWS * CH % NT == 0, "every thread loads as much");
+    using Lds = LdsTile<ACROSS, ROWS, COLS, NP>;
+    Source<T> src;
+    int count, kend, x0, last;          // last: where the tensor ends along k
+    typename Source<T>::At at[N];
+    typename Source<T>::Raw r[N];
+    __device__ __forceinline__ TileLoader(const void *p, const Packed &p8, int64_t ld, int x0_, int count_, int kbeg, int kend_, int last_)
+        : src(p, p8, ld), count(count_), kend(kend_), x0(x0_), last(last_)
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int i = threadIdx.x + j * NT, x = x0 + (ACROSS ? 8 * (i % CH) : i / CH), k = kbeg + (ACROSS ? i / CH : 8 * (i % CH));
+            const int xc = ACROSS ? min(x, (count - 1) / 8 * 8) : min(x, count - 1);
+            at[j] = ACROSS ? src.at(k, xc) : src.at(xc, k);
+        }
+    }
+    __device__ __forceinline__ bool inside(int k) const { return k + STEP <= kend && (!ACROSS || (count >= 8 && (count % 8 == 0 || k + STEP < last))); }
+    // steps in order, those inside first
+    template <bool INSIDE> __device__ __forceinline__ void start(int k, LdsByte *)
     {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const int i = threadIdx.x + j * NT, row = (ACROSS ? k : x0) + i / CH, c = (ACROSS ? x0 : k) + 8 * (i % CH);
-            r[j] = load8(p, row, c, row < (ACROSS ? kend : count) ? (ACROSS ? count : kend) - c : 0);
+            if constexpr (INSIDE) r[j] = at[j].take(src, ACROSS ? STEP : 0, ACROSS ? 0 : STEP);
+            else r[j] = src.load(row, c, row < (ACROSS ? kend : count) ? (ACROSS ? count : kend) - c : 0);
         }
+    }
+    __device__ __forceinline__ void finish_one(LdsByte *t, int j) const
+    {
+        const int i = threadIdx.x + j * NT;
+        Lds::put(t, i / CH, i % CH, frag_of(r[j]));
     }
     __device__ __forceinline__ void finish(LdsByte *t) const
     {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int i = threadIdx.x + j * NT;
-            Frag<1> f;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) f.p[0][q] = pack_bf16(elem(r[j], 2 * q), elem(r[j], 2 * q + 1));
-            Lds::put(t, i / CH, i % CH, f);
-        }
+        for (int j = 0; j < N; ++j) finish_one(t, j);
     }
 };
 
 // ---- sums ------------------------------------------------------------------------------------------------------------------------
 // Pieces: the products below the first are added up on their own, because an instruction drops what lies below the last place of the
 // sum it adds to; products of pieces i and j with i + j > 2 are below 2^-24 of the whole and left out.
-template <int NA, int NB> struct Sums {
+template <int NA, int NB, int MR, int MC> struct Sums {
     static constexpr bool CUT = NA * NB > 1;
-    v16f big, small;
-    __device__ __forceinline__ void zero() { big = v16f{}, small = v16f{}; }
-    __device__ __forceinline__ void mma(const Frag<NA> &a, const Frag<NB> &b)
+    v16f big[MR][MC], small[CUT ? MR : 1][CUT ? MC : 1];
+    __device__ __forceinline__ void zero()
     {
 #pragma unroll
-        for (int d = 2; d > 0; --d)
+        for (int i = 0; i < MR; ++i)
 #pragma unroll
-            for (int i = 0; i < NA; ++i)
-                if (d - i >= 0 && d - i < NB) small = mfma(b.p[d - i], a.p[i], small);
-        big = mfma(b.p[0], a.p[0], big);
+            for (int j = 0; j < MC; ++j) {
+                big[i][j] = v16f{};
+                if constexpr (CUT) small[i][j] = v16f{};
+            }
     }
-    __device__ __forceinline__ float get(int i) const { return CUT ? big[i] + small[i] : big[i]; }
+    // the product of one piece of each: the first two add to the big sums
+    __device__ __forceinline__ void mma(const u32x4 (&a)[MR], const u32x4 (&b)[MC], bool first)
+    {
+#pragma unroll
+        for (int i = 0; i < MR; ++i)
+#pragma unroll
+            for (int j = 0; j < MC; ++j) {
+                if constexpr (CUT)
+                    if (!first) {
+                        small[i][j] = mfma(b[j], a[i], small[i][j]);
+                        continue;
+                    }
+                big[i][j] = mfma(b[j], a[i], big[i][j]);
+            }
+    }
+    __device__ __forceinline__ float get(int i, int j, int u) const
+    {
+        if constexpr (CUT) return big[i][j][u] + small[i][j][u];
+        else return big[i][j][u];
+    }
 };
 
 // This wave's loads into LDS but the latest LOADS have landed, its reads of LDS but the latest READS are done, and everyone's.  The compiler's
@@ -246,127 +291,182 @@ __device__ __forceinline__ void place_of(const GemmArgs &a, int &tr, int &tc, in
     tc = within / high;
 }
 
-template <class T, class TB, bool AX, bool BX, int XT_, bool DMA> struct Config {
-    using TA = T;
-    static constexpr bool kDmaA = DMA, kDmaB = DMA && sizeof(TB) == 2;
-    static constexpr int XT = XT_, NT = XT == 256 ? 512 : 256, WR = 2, WC = NT / 64 / WR;      // waves along the rows and the columns
-    static constexpr int NA = Pieces<T>::N, NB = sizeof(TB) == 4 ? 3 : 1;
-    // three pieces leave room for one buffer and two blocks a compute unit
-    static constexpr int STEP = NA == 3 ? 32 : 64, STAGES = NA == 3 ? 1 : 2;
-    using LA = TileLoader<T, AX, XT, STEP, NT, kDmaA>;
-    using LB = TileLoader<TB, BX, XT, STEP, NT, kDmaB>;
-    static constexpr int MR = XT / WR / 32, MC = XT / WC / 32;       // 32 x 32 tiles of a wave
-    static constexpr int STAGE = LA::Lds::BYTES + LB::Lds::BYTES;
-    static constexpr int EPI_ROW = (MC * 32 + 4) * 4, EPI = NT / 64 * 32 * EPI_ROW;
-    static constexpr int LDS = STAGES * STAGE > EPI ? STAGES * STAGE : EPI;
-};
-
-template <class T, class TB, bool AX, bool BX, int XT, bool DMA, class TO>
-__global__ __launch_bounds__((XT == 256 ? 512 : 256), 2) void gemm_kernel(GemmArgs a)
+// A wave's tile of sums, MR x MC of 32 x 32 from (r0, c0) on, through `mine` (32 rows of kEpiRow<MC> bytes, the wave's own): rows whose
+// lanes have eight neighbours each.  What 32 rows need is asked for at once.
+template <int MC> constexpr int kEpiRow = (MC * 32 + 4) * 4;
+template <class TO, int MR, int MC, class S> __device__ __forceinline__ void store_wave(const GemmArgs &a, int split, LdsByte *mine, int r0, int c0, int lane, const S &acc)
 {
-    using Cfg = Config<T, TB, AX, BX, XT, DMA>;
-    using LA = typename Cfg::LA;
-    using LB = typename Cfg::LB;
-    constexpr int STEP = Cfg::STEP, MR = Cfg::MR, MC = Cfg::MC;
-    extern __shared__ __align__(16) char smem[];
-    LdsByte *const lds = (LdsByte *)smem;
-    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wr = wave / Cfg::WC * (MR * 32), wc = wave % Cfg::WC * (MC * 32);
-    int tr, tc, split;
-    place_of(a, tr, tc, split);
-    const int r0 = tr * XT, c0 = tc * XT, kbeg = split * a.chunk, kend = min(a.K, kbeg + a.chunk);
-
-    LA la(a.A, Packed{}, a.a_ld, r0, a.R, kend);
-    LB lb(a.B, a.B8, a.b_ld, c0, a.C, kend);
-    Sums<Cfg::NA, Cfg::NB> acc[MR][MC];
-#pragma unroll
-    for (int i = 0; i < MR; ++i)
-#pragma unroll
-        for (int j = 0; j < MC; ++j) acc[i][j].zero();
-
-    auto multiply = [&](LdsByte *at) {
-#pragma unroll
-        for (int ks = 0; ks < STEP / 16; ++ks) {
-            Frag<Cfg::NA> fa[MR];
-            Frag<Cfg::NB> fb[MC];
-#pragma unroll
-            for (int j = 0; j < MC; ++j) fb[j] = LB::Lds::read(at + LA::Lds::BYTES, wc + 32 * j, ks, lane);
-#pragma unroll
-            for (int i = 0; i < MR; ++i) fa[i] = LA::Lds::read(at, wr + 32 * i, ks, lane);
-#pragma unroll
-            for (int i = 0; i < MR; ++i)
-#pragma unroll
-                for (int j = 0; j < MC; ++j) acc[i][j].mma(fa[i], fb[j]);
-        }
-    };
-    auto start = [&](int k, LdsByte *at) {
-        la.start(k, at);
-        lb.start(k, at + LA::Lds::BYTES);
-    };
-    auto finish = [&](LdsByte *at) {
-        la.finish(at);
-        lb.finish(at + LA::Lds::BYTES);
-    };
-    if (kbeg < kend) {
-        start(kbeg, lds);
-        finish(lds);
-    }
-    if constexpr (Cfg::STAGES == 2) {
-        // behind the barrier a step's tiles are there and everyone is done with the ones before, whose buffer is filled while these are multiplied
-        int buf = 0;
-        for (int k = kbeg; k < kend; k += STEP, buf ^= 1) {
-            tile_sync();
-            const bool more = k + STEP < kend;
-            if (more) start(k + STEP, lds + (buf ^ 1) * Cfg::STAGE);
-            multiply(lds + buf * Cfg::STAGE);
-            if (more) finish(lds + (buf ^ 1) * Cfg::STAGE);
-        }
-    } else {
-        for (int k = kbeg; k < kend; k += STEP) {
-            __syncthreads();
-            const bool more = k + STEP < kend;
-            if (more) start(k + STEP, lds);
-            multiply(lds);
-            __syncthreads();
-            if (more) finish(lds);
-        }
-    }
-    __syncthreads();
-
-    EpiArgs e = a.epi;
+    constexpr int PER = 4 * MC, ROWS = 64 / PER, N = 32 / ROWS;       // lanes of a row, rows at a time
+    const EpiArgs e = a.epi;
     const bool whole = a.splits == 1;
-    LdsByte *const mine = lds + wave * 32 * Cfg::EPI_ROW;
-    constexpr int PER = 4 * MC;                     // lanes of a row
+    const int c = c0 + 8 * (lane % PER);
+    Raw8<float> bias = {};
+    if (whole && e.bias && c < a.C) bias = load8(e.bias + c, a.C - c);
 #pragma unroll
     for (int i = 0; i < MR; ++i) {
+        const int r = r0 + 32 * i + lane / PER;
+        auto load = [&](int t) { return epi_load<TO>(e, r + t * ROWS, c, r + t * ROWS < a.R ? a.C - c : 0); };
+        constexpr bool AHEAD = sizeof(TO) == 2;        // fp32: registers
+        EpiIn<TO> in[N];
+        if (AHEAD && whole)
+#pragma unroll
+            for (int t = 0; t < N; ++t) in[t] = load(t);
 #pragma unroll
         for (int j = 0; j < MC; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 u32x4 v;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = __float_as_uint(acc[i][j].get(4 * q + u));
-                CG_LDS(u32x4, mine + (lane & 31) * Cfg::EPI_ROW + (32 * j + 8 * q + 4 * (lane >> 5)) * 4) = v;
+                for (int u = 0; u < 4; ++u) v[u] = __float_as_uint(acc.get(i, j, 4 * q + u));
+                CG_LDS(u32x4, mine + (lane & 31) * kEpiRow<MC> + (32 * j + 8 * q + 4 * (lane >> 5)) * 4) = v;
             }
         __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int t = 0; t < 32 * PER / 64; ++t) {
-            const int row = t * (64 / PER) + lane / PER, c = c0 + wc + 8 * (lane % PER);
-            const int r = r0 + wr + 32 * i + row;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
             float v[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const u32x4 x = CG_LDS(u32x4, mine + row * Cfg::EPI_ROW + (8 * (lane % PER) + 4 * h) * 4);
+                const u32x4 x = CG_LDS(u32x4, mine + (t * ROWS + lane / PER) * kEpiRow<MC> + (8 * (lane % PER) + 4 * h) * 4);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) v[4 * h + u] = __uint_as_float(x[u]);
             }
-            if (r < a.R && c < a.C) {
-                if (whole) finish8<TO>(e, v, r, c, a.C - c);
-                else store8(a.part + ((int64_t)split * a.R + r) * a.C + c, to_raw<float>(v), a.C - c);
+            if (r + t * ROWS < a.R && c < a.C) {
+                if (whole) epi_finish<TO>(e, v, bias, AHEAD ? in[t] : load(t), r + t * ROWS, c, a.C - c);
+                else store8(a.part + ((int64_t)split * a.R + r + t * ROWS) * a.C + c, to_raw<float>(v), a.C - c);
             }
         }
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+// Tiles of 128 x 128 of bf16 (and 8-bit) tensors, four waves, two steps in LDS; two blocks a compute unit.
+template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bounds__(256, 2) void gemm_kernel(GemmArgs a)
+{
+    constexpr int STEP = 64, XT = 128;
+    using LA = TileLoader<bf16raw, AX, XT, STEP, 256, DMA>;
+    using LB = TileLoader<TB, BX, XT, STEP, 256, DMA && sizeof(TB) == 2>;
+    constexpr int STAGE = LA::Lds::BYTES + LB::Lds::BYTES;
+    __shared__ __align__(16) char smem[2 * STAGE];
+    static_assert(4 * 32 * kEpiRow<2> <= 2 * STAGE, "room for the epilogue");
+    LdsByte *const lds = (LdsByte *)smem;
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / 2 * 64, wc = wave % 2 * 64;
+    int tr, tc, split;
+    place_of(a, tr, tc, split);
+    const int r0 = tr * XT, c0 = tc * XT, kbeg = split * a.chunk, kend = min(a.K, kbeg + a.chunk);
+
+    LA la(a.A, Packed{}, a.a_ld, r0, a.R, kbeg, kend, a.K);
+    LB lb(a.B, a.B8, a.b_ld, c0, a.C, kbeg, kend, a.K);
+    Sums<1, 1, 2, 2> acc;
+    acc.zero();
+    auto start = [&](int k, LdsByte *at, auto inside) {
+        la.template start<decltype(inside)::value>(k, at);
+        lb.template start<decltype(inside)::value>(k, at + LA::Lds::BYTES);
+    };
+    auto finish = [&](LdsByte *at) {
+        la.finish(at);
+        lb.finish(at + LA::Lds::BYTES);
+    };
+    // behind the barrier a step's tiles are there and everyone is done with the ones before, whose buffer is filled while these are multiplied
+    auto step = [&](int k, int buf, auto inside) {
+        tile_sync();
+        const bool more = decltype(inside)::value || k + STEP < kend;
+        if (more) start(k + STEP, lds + (buf ^ 1) * STAGE, inside);
+        LdsByte *const at = lds + buf * STAGE;
+#pragma unroll
+        for (int ks = 0; ks < STEP / 16; ++ks) {
+            u32x4 fa[2], fb[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) fb[j] = LB::Lds::read_plane(at + LA::Lds::BYTES, wc + 32 * j, ks, lane, 0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) fa[i] = LA::Lds::read_plane(at, wr + 32 * i, ks, lane, 0);
+            acc.mma(fa, fb, true);
+        }
+        if (more) finish(lds + (buf ^ 1) * STAGE);
+    };
+    auto is_inside = [&](int k) { return k < kend && la.inside(k) && lb.inside(k); };
+    if (kbeg < kend) {
+        const bool in = is_inside(kbeg);
+        if (in) start(kbeg, lds, std::true_type());
+        else start(kbeg, lds, std::false_type());
+        finish(lds);
+        int buf = 0, k = kbeg;
+        if (in)
+            for (; is_inside(k + STEP); k += STEP, buf ^= 1) step(k, buf, std::true_type());
+        for (; k < kend; k += STEP, buf ^= 1) step(k, buf, std::false_type());
+    }
+    __syncthreads();
+    store_wave<TO, 2, 2>(a, split, lds + wave * 32 * kEpiRow<2>, r0 + wr, c0 + wc, lane, acc);
+}
+template <class TB, bool AX, bool BX, bool DMA, class TO> int launch(const GemmArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((gemm_kernel<TB, AX, BX, DMA, TO>), dim3((unsigned)(a.tiles_r * a.tiles_c * a.splits)), dim3(256), 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
+// fp32 tensors: tiles of 128 x 128, eight waves, one step in LDS; two blocks a compute unit, one of which multiplies while the other cuts.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }       // lets loads go on
+template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void gemm_cut_kernel(GemmArgs a)
+{
+    constexpr int STEP = 32, XT = 128;
+    using LA = TileLoader<float, AX, XT, STEP, 512, false>;
+    using LB = TileLoader<TB, BX, XT, STEP, 512, false>;
+    constexpr int NB = LB::NP, TILES = LA::Lds::BYTES + LB::Lds::BYTES, EPI = 8 * 32 * kEpiRow<2>;
+    __shared__ __align__(16) char smem[TILES > EPI ? TILES : EPI];
+    LdsByte *const lds = (LdsByte *)smem;
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / 2 * 32, wc = wave % 2 * 64;
+    int tr, tc, split;
+    place_of(a, tr, tc, split);
+    const int r0 = tr * XT, c0 = tc * XT, kbeg = split * a.chunk, kend = min(a.K, kbeg + a.chunk);
+
+    LA la(a.A, Packed{}, a.a_ld, r0, a.R, kbeg, kend, a.K);
+    LB lb(a.B, a.B8, a.b_ld, c0, a.C, kbeg, kend, a.K);
+    Sums<3, NB, 1, 2> acc;
+    acc.zero();
+    auto start = [&](int k, auto inside) {
+        la.template start<decltype(inside)::value>(k, lds);
+        lb.template start<decltype(inside)::value>(k, lds);
+    };
+    auto step = [&](int k, auto inside) {
+        la.finish(lds);
+        lb.finish(lds + LA::Lds::BYTES);
+        lds_barrier();
+        if (decltype(inside)::value || k + STEP < kend) start(k + STEP, inside);
+#pragma unroll
+        for (int ks = 0; ks < STEP / 16; ++ks) {
+            u32x4 fa[3][1], fb[NB][2];
+#pragma unroll
+            for (int p = 2; p >= 0; --p) {
+                fa[p][0] = LA::Lds::read_plane(lds, wr, ks, lane, p);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (p < NB) fb[p < NB ? p : 0][j] = LB::Lds::read_plane(lds + LA::Lds::BYTES, wc + 32 * j, ks, lane, p);
+            }
+#pragma unroll
+            for (int d = 2; d >= 0; --d)
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+                    if (d - p >= 0 && d - p < NB) acc.mma(fa[p], fb[d - p < NB && d - p >= 0 ? d - p : 0], d == 0);
+        }
+        lds_barrier();
+    };
+    auto is_inside = [&](int k) { return k < kend && la.inside(k) && lb.inside(k); };
+    if (kbeg < kend) {
+        const bool in = is_inside(kbeg);
+        if (in) start(kbeg, std::true_type());
+        else start(kbeg, std::false_type());
+        int k = kbeg;
+        if (in)
+            for (; is_inside(k + STEP); k += STEP) step(k, std::true_type());
+        for (; k < kend; k += STEP) step(k, std::false_type());
+    }
+    store_wave<float, 1, 2>(a, split, lds + wave * 32 * kEpiRow<2>, r0 + wr, c0 + wc, lane, acc);
+}
+template <class TB, bool AX, bool BX> int launch_cut(const GemmArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((gemm_cut_kernel<TB, AX, BX>), dim3((unsigned)(a.tiles_r * a.tiles_c * a.splits)), dim3(512), 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
 }
 
 // Tiles of 256 x 256 of bf16 tensors, eight waves.  Operands pass through LDS in halves of 128 rows or columns, A0 A1 B0 B1, 64 values of k at
@@ -525,22 +625,11 @@ template <bool AX, bool BX, class TO> int launch_large(const GemmArgs &a, hipStr
     return CG_OK;
 }
 
-template <class T, class TB, bool AX, bool BX, int XT, bool DMA, class TO> int launch(const GemmArgs &a, hipStream_t s)
-{
-    using Cfg = Config<T, TB, AX, BX, XT, DMA>;
-    auto *const kernel = gemm_kernel<T, TB, AX, BX, XT, DMA, TO>;
-    if constexpr (Cfg::LDS > 64 * 1024)       // asked for at every call: it holds for the current device alone
-        CG_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::LDS));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles_r * a.tiles_c * a.splits)), dim3(Cfg::NT), Cfg::LDS, s, a);
-    CG_HIP_TRY(hipGetLastError());
-    return CG_OK;
-}
-template <class T, class TB, bool AX, bool BX, class TO> int launch_bf16(const GemmKind &k, const GemmArgs &a, hipStream_t s)
+template <class TB, bool AX, bool BX, class TO> int launch_bf16(const GemmKind &k, const GemmArgs &a, hipStream_t s)
 {
     if constexpr (sizeof(TB) == 2)
         if (k.large) return launch_large<AX, BX, TO>(a, s);
-    if (k.dma) return launch<T, TB, AX, BX, 128, true, TO>(a, s);
-    return launch<T, TB, AX, BX, 128, false, TO>(a, s);
+    return k.dma ? launch<TB, AX, BX, true, TO>(a, s) : launch<TB, AX, BX, false, TO>(a, s);
 }
 
 }  // namespace
@@ -548,15 +637,13 @@ template <class T, class TB, bool AX, bool BX, class TO> int launch_bf16(const G
 int gemm_launch(const GemmKind &k, const GemmArgs &a, hipStream_t s)
 {
     if (k.type == CG_TYPE_FP32) {
-        if (k.pass == CG_PASS_FWD) return launch<float, float, false, false, 128, false, float>(a, s);
-        if (k.pass == CG_PASS_BWD_DATA) return launch<float, float, false, true, 128, false, float>(a, s);
-        if (k.packed) return launch<float, int8_t, true, true, 128, false, float>(a, s);
-        return launch<float, float, true, true, 128, false, float>(a, s);
+        if (k.pass == CG_PASS_FWD) return launch_cut<float, false, false>(a, s);
+        if (k.pass == CG_PASS_BWD_DATA) return launch_cut<float, false, true>(a, s);
+        return k.packed ? launch_cut<int8_t, true, true>(a, s) : launch_cut<float, true, true>(a, s);
     }
-    if (k.pass == CG_PASS_FWD) return launch_bf16<bf16raw, bf16raw, false, false, bf16raw>(k, a, s);
-    if (k.pass == CG_PASS_BWD_DATA) return launch_bf16<bf16raw, bf16raw, false, true, bf16raw>(k, a, s);
-    if (k.packed) return launch_bf16<bf16raw, int8_t, true, true, float>(k, a, s);
-    return launch_bf16<bf16raw, bf16raw, true, true, float>(k, a, s);
+    if (k.pass == CG_PASS_FWD) return launch_bf16<bf16raw, false, false, bf16raw>(k, a, s);
+    if (k.pass == CG_PASS_BWD_DATA) return launch_bf16<bf16raw, false, true, bf16raw>(k, a, s);
+    return k.packed ? launch_bf16<int8_t, true, true, float>(k, a, s) : launch_bf16<bf16raw, true, true, float>(k, a, s);
 }
 
 }  // namespace cg
