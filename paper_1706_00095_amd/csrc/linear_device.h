@@ -85,39 +85,53 @@ __device__ __forceinline__ float slope_times(float g, float z, int act)
     return g;
 }
 
-// What the epilogue reads for eight sums of a row, apart from the bias: asked for ahead of its use.
+// What the epilogue reads for eight sums of a row, apart from the bias: asked for ahead of its use.  z: the input of the activation, as a
+// tensor's values or in 8 bits.
 template <class T> struct EpiIn {
     Raw8<T> add, z;
-    Raw8Packed z8;
 };
-template <class T> __device__ __forceinline__ EpiIn<T> epi_load(const EpiArgs &e, int64_t row, int c, int n)
+enum EpiSide { EPI_EITHER, EPI_FWD, EPI_BWD };       // what a kernel knows of its pass: forward has no slope, backward nothing but it and an addition
+template <EpiSide SIDE, class T> __device__ __forceinline__ Raw8<T> epi_load_z(const EpiArgs &e, int64_t row, int c, int n)
 {
-    EpiIn<T> in = {};
-    if (e.add) in.add = load8(static_cast<const T *>(e.add) + (n > 0 ? row * e.add_ld + c : 0), n);
-    if (e.slope != CG_ACT_NONE) {
-        if (e.z_in8.codes) in.z8 = load8(e.z_in8, row, c, n);
-        else in.z = load8(static_cast<const T *>(e.z_in) + (n > 0 ? row * e.z_in_ld + c : 0), n);
-    }
-    return in;
-}
-template <class T> __device__ __forceinline__ void epi_finish(const EpiArgs &e, float (&v)[8], const Raw8<float> &bias, const EpiIn<T> &in, int64_t row, int c, int n)
-{
-    if (e.bias) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += elem(bias, i);
-    }
-    if (e.z) store8(static_cast<T *>(e.z) + row * e.z_ld + c, to_raw<T>(v), n);
-    if (e.act != CG_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = act_of(v[i], e.act);
-    }
-    if (e.slope != CG_ACT_NONE) {
+    Raw8<T> z = {};
+    if (SIDE != EPI_FWD && e.slope != CG_ACT_NONE) {
         if (e.z_in8.codes) {
+            const Raw8Packed q = load8(e.z_in8, row, c, n);
+            z.w[0] = q.w[0], z.w[1] = q.w[1], z.w[2] = (uint32_t)q.e;
+        } else z = load8(static_cast<const T *>(e.z_in) + (n > 0 ? row * e.z_in_ld + c : 0), n);
+    }
+    return z;
+}
+template <class T> __device__ __forceinline__ Raw8<T> epi_load_add(const EpiArgs &e, int64_t row, int c, int n)
+{
+    Raw8<T> add = {};
+    if (e.add) add = load8(static_cast<const T *>(e.add) + (n > 0 ? row * e.add_ld + c : 0), n);
+    return add;
+}
+template <EpiSide SIDE, class T>
+__device__ __forceinline__ void epi_finish(const EpiArgs &e, float (&v)[8], const Raw8<float> &bias, const EpiIn<T> &in, int64_t row, int c, int n)
+{
+    if constexpr (SIDE != EPI_BWD) {
+        if (e.bias) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(in.z8, i), e.slope);
-        } else {
+            for (int i = 0; i < 8; ++i) v[i] += elem(bias, i);
+        }
+        if (e.z) store8(static_cast<T *>(e.z) + row * e.z_ld + c, to_raw<T>(v), n);
+        if (e.act != CG_ACT_NONE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(in.z, i), e.slope);
+            for (int i = 0; i < 8; ++i) v[i] = act_of(v[i], e.act);
+        }
+    }
+    if constexpr (SIDE != EPI_FWD) {
+        if (e.slope != CG_ACT_NONE) {
+            if (e.z_in8.codes) {
+                const Raw8Packed q = {{in.z.w[0], in.z.w[1]}, (int)in.z.w[2]};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(q, i), e.slope);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = slope_times(v[i], elem(in.z, i), e.slope);
+            }
         }
     }
     if (e.add) {
@@ -130,8 +144,8 @@ template <class T> __device__ __forceinline__ void finish8(const EpiArgs &e, flo
 {
     Raw8<float> bias = {};
     if (e.bias) bias = load8(e.bias + c, n);
-    const EpiIn<T> in = epi_load<T>(e, row, c, n);
-    epi_finish(e, v, bias, in, row, c, n);
+    const EpiIn<T> in = {epi_load_add<T>(e, row, c, n), epi_load_z<EPI_EITHER, T>(e, row, c, n)};
+    epi_finish<EPI_EITHER, T>(e, v, bias, in, row, c, n);
 }
 
 }  // namespace

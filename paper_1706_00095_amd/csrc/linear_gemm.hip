@@ -305,7 +305,10 @@ template <class TO, int MR, int MC, class S> __device__ __forceinline__ void sto
 #pragma unroll
     for (int i = 0; i < MR; ++i) {
         const int r = r0 + 32 * i + lane / PER;
-        auto load = [&](int t) { return epi_load<TO>(e, r + t * ROWS, c, r + t * ROWS < a.R ? a.C - c : 0); };
+        auto load = [&](int t) {
+            const int n = r + t * ROWS < a.R ? a.C - c : 0;
+            return EpiIn<TO>{epi_load_add<TO>(e, r + t * ROWS, c, n), epi_load_z<EPI_EITHER, TO>(e, r + t * ROWS, c, n)};
+        };
         constexpr bool AHEAD = sizeof(TO) == 2;        // fp32: registers
         EpiIn<TO> in[N];
         if (AHEAD && whole)
@@ -331,7 +334,7 @@ template <class TO, int MR, int MC, class S> __device__ __forceinline__ void sto
                 for (int u = 0; u < 4; ++u) v[4 * h + u] = __uint_as_float(x[u]);
             }
             if (r + t * ROWS < a.R && c < a.C) {
-                if (whole) epi_finish<TO>(e, v, bias, AHEAD ? in[t] : load(t), r + t * ROWS, c, a.C - c);
+                if (whole) epi_finish<EPI_EITHER, TO>(e, v, bias, AHEAD ? in[t] : load(t), r + t * ROWS, c, a.C - c);
                 else store8(a.part + ((int64_t)split * a.R + r + t * ROWS) * a.C + c, to_raw<float>(v), a.C - c);
             }
         }
@@ -516,25 +519,33 @@ template <bool AX, bool BX, class TO> __global__ __launch_bounds__(512, 2) void 
         for (int ks = 0; ks < 4; ++ks) {
             multiply(ha, hb, ks);
             read(ks);
-            if (ks == 0 && (FULL || fill)) loader.template load<FULL, 0>(to, wave);
-            if (ks == 2 && (FULL || fill)) loader.template load<FULL, 1>(to, wave);
+            if (ks == 1 && (FULL || fill)) loader.template load<FULL, 0>(to, wave);
+            if (ks == 3 && (FULL || fill)) loader.template load<FULL, 1>(to, wave);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // first: the half of B that the step begins with.  full: all that the step loads and reads ahead is there, and no load the last one
+    // first: the half of B that the step begins with.  full: a step behind the one after the next is there too
     auto step = [&](int s, auto first, auto full) {
         constexpr bool FULL = decltype(full)::value;
         const std::integral_constant<int, 1 - decltype(first)::value> second;
-        constexpr int READS_A = AX ? 15 : 8, READS_B = BX ? 8 : 4, LOADS = FULL ? 10 : 0;
         const bool fill = s + 2 < n, more = FULL || s + 1 < n;
+        // loads that may still be on their way at a phase's end: five halves' while they go on, one fewer from phase to phase in the last but
+        // one step, none in the last
+        auto end = [&](auto reads, auto i) {
+            if (FULL || fill) end_phase<10, decltype(reads)::value>();
+            else if (more) end_phase<8 - 2 * decltype(i)::value, decltype(reads)::value>();
+            else end_phase<0, decltype(reads)::value>();
+        };
+        const std::integral_constant<int, AX ? 15 : 8> reads_a;
+        const std::integral_constant<int, BX ? 8 : 4> reads_b;
         phase(_0, first, full, fill, lb[first.value], at_b(first.value, s), [&](int ks) { read_b(second, s, ks); });
-        end_phase<LOADS, READS_B>();
+        end(reads_b, _0);
         phase(_0, second, full, fill, la[0], at_a(0, s), [&](int ks) { read_a(1, s, ks); });
-        end_phase<LOADS, READS_A>();
+        end(reads_a, _1);
         phase(_1, second, full, fill, lb[second.value], at_b(second.value, s), [&](int ks) { if (more) read_b(second, s + 1, ks); });
-        end_phase<LOADS, READS_B>();
+        end(reads_b, std::integral_constant<int, 2>());
         phase(_1, first, full, fill, la[1], at_a(1, s), [&](int ks) { if (more) read_a(0, s + 1, ks); });
-        end_phase<LOADS, READS_A>();
+        end(reads_a, std::integral_constant<int, 3>());
     };
     if (n > 0) {
         lb[0].next(at_b(0, 0), wave);
@@ -567,52 +578,58 @@ template <bool AX, bool BX, class TO> __global__ __launch_bounds__(512, 2) void 
         }
     }
 
-    // What a half of the rows needs is asked for at once: a wave has nothing else to do while it waits.
+    // What the epilogue reads is asked for at once, the registers of the operands are free: forward the residual, backward what the slope is
+    // taken of.  (A gradient that is added there comes as it is needed.)
     LdsByte *const mine = lds + wave * 32 * kLargeRow;
     const EpiArgs e = a.epi;
     constexpr bool PLAIN = AX;          // backward-weight: sums are the result
     const int c_of = c0 + 32 * wc + 8 * (lane & 3), r_of = r0 + 64 * wr + lane / 4;
+    auto row_of = [&](int q) { return r_of + 128 * (q >> 3) + 32 * (q >> 1 & 1) + 16 * (q & 1); };       // q: half of A, half of B, 32 rows, 16 rows
+    auto col_of = [&](int q) { return c_of + 128 * (q >> 2 & 1); };
     Raw8<float> bias[2] = {};
     if (!PLAIN && e.bias)
 #pragma unroll
         for (int h = 0; h < 2; ++h) bias[h] = load8(e.bias + (c_of + 128 * h < a.C ? c_of + 128 * h : 0), a.C - c_of - 128 * h);
+    Raw8<TO> in[16];
+    if constexpr (!PLAIN) {
 #pragma unroll
-    for (int ha = 0; ha < 2; ++ha) {
-        EpiIn<TO> in[2][2][2];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const int r = r_of + 128 * ha + 32 * (q >> 1 & 1) + 16 * (q & 1), c = c_of + 128 * (q >> 2);
-            if constexpr (!PLAIN) in[q >> 2][q >> 1 & 1][q & 1] = epi_load<TO>(e, r, c, r < a.R ? a.C - c : 0);
+        for (int q = 0; q < 16; ++q) {
+            const int n = row_of(q) < a.R ? a.C - col_of(q) : 0;
+            in[q] = BX ? epi_load_z<EPI_BWD, TO>(e, row_of(q), col_of(q), n) : epi_load_add<TO>(e, row_of(q), col_of(q), n);
         }
+    }
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb)
+    for (int p = 0; p < 8; ++p) {
+        const int ha = p >> 2, hb = p >> 1 & 1, i = p & 1;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+        for (int u = 0; u < 4; ++u) {
+            u32x4 v;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    u32x4 v;
+            for (int x = 0; x < 4; ++x) v[x] = __float_as_uint(acc[ha][hb][i][4 * u + x]);
+            CG_LDS(u32x4, mine + (lane & 31) * kLargeRow + (8 * u + 4 * (lane >> 5)) * 4) = v;
+        }
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) v[x] = __float_as_uint(acc[ha][hb][i][4 * u + x]);
-                    CG_LDS(u32x4, mine + (lane & 31) * kLargeRow + (8 * u + 4 * (lane >> 5)) * 4) = v;
-                }
-                __builtin_amdgcn_wave_barrier();
+        for (int t = 0; t < 2; ++t) {
+            const int q = 2 * p + t, r = row_of(q), c = col_of(q);
+            float v[8];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int c = c_of + 128 * hb, r = r_of + 128 * ha + 32 * i + 16 * t;
-                    float v[8];
+            for (int h = 0; h < 2; ++h) {
+                const u32x4 x = CG_LDS(u32x4, mine + (16 * t + lane / 4) * kLargeRow + (8 * (lane & 3) + 4 * h) * 4);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const u32x4 x = CG_LDS(u32x4, mine + (16 * t + lane / 4) * kLargeRow + (8 * (lane & 3) + 4 * h) * 4);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) v[4 * h + y] = __uint_as_float(x[y]);
-                    }
-                    if (r < a.R && c < a.C) {
-                        if constexpr (PLAIN) store8(static_cast<TO *>(e.out) + r * e.out_ld + c, to_raw<TO>(v), a.C - c);
-                        else epi_finish<TO>(e, v, bias[hb], in[hb][i][t], r, c, a.C - c);
-                    }
-                }
-                __builtin_amdgcn_wave_barrier();
+                for (int y = 0; y < 4; ++y) v[4 * h + y] = __uint_as_float(x[y]);
             }
+            if (r < a.R && c < a.C) {
+                if constexpr (PLAIN) store8(static_cast<TO *>(e.out) + r * e.out_ld + c, to_raw<TO>(v), a.C - c);
+                else {
+                    EpiIn<TO> of;
+                    of.z = of.add = in[q];
+                    if (BX) of.add = epi_load_add<TO>(e, r, c, a.C - c);
+                    epi_finish<BX ? EPI_BWD : EPI_FWD, TO>(e, v, bias[hb], of, r, c, a.C - c);
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 template <bool AX, bool BX, class TO> int launch_large(const GemmArgs &a, hipStream_t s)
