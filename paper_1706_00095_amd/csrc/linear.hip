@@ -186,7 +186,7 @@ template <class T> __global__ __launch_bounds__(256) void act_bwd_kernel(const T
 // ---- plans ------------------------------------------------------------------------------------------------------------------------
 constexpr int64_t kMostBlocks = 1 << 22;       // of 512 threads a launch has room for less than 2^32
 constexpr int kFewTokens = 32;
-constexpr int kMostSplits = 32, kLeastChunk = 4 * kGemmStep, kLeastChunkFp32 = 2 * kGemmStep;
+constexpr int kMostSplits = 32;
 
 bool act_ok(int act) { return act >= CG_ACT_NONE && act <= CG_ACT_SILU; }
 int desc_check(const cg_linear_desc *d)
@@ -198,6 +198,17 @@ int desc_check(const cg_linear_desc *d)
     if (tiles(d->M) * tiles(d->N) > kMostBlocks || tiles(d->M) * tiles(d->K) > kMostBlocks || tiles(d->N) * tiles(d->K) > kMostBlocks) return CG_EUNSUPPORTED;
     return CG_OK;
 }
+// Microseconds that `blocks` tiles of 128 x 128 take for `steps` steps of 64 values of k each, and that the join of a cut k takes: what was measured
+// on products of 64 to 9216 rows, columns and values of k.  A compute unit's second block costs less than its first, others as much
+// again.  bf16, 1024^3: 14 us uncut, 17 in two parts, 20 in four; 64 x 4096 x 4096: 15 in eight parts, 19 in sixteen, 17 in four.  fp32, 256 x
+// 9216 x 4096: 120 us in three parts, 186 uncut; 1500 x 771 x 515: 26 in four, 27 in seven, 38 uncut.
+double cost(int type, int64_t blocks, int64_t steps)
+{
+    const int64_t each = (blocks + 255) / 256;
+    const double of = type == CG_TYPE_FP32 ? each == 1 ? 2.8 : 2.4 * (double)each : each == 1 ? 0.55 : 0.4 * (double)each;
+    return 4.0 + of * (double)steps;
+}
+double join_cost(int64_t splits, int64_t R, int64_t C) { return 3.5 + (double)splits * (double)R * (double)C * 2e-6; }
 struct Plan {
     int R, C, K;              // of the product
     bool few;
@@ -215,18 +226,16 @@ Plan plan_of(const cg_linear_desc *d, int pass)
     p.splits = 1, p.chunk = p.K;
     if (p.few) return p;
     auto tiles = [&](int64_t t) { return ((p.R + t - 1) / t) * ((p.C + t - 1) / t); };
-    p.large = d->type == CG_TYPE_BF16 && tiles(256) >= 128;
-    // two blocks a compute unit
-    const int64_t n = tiles(128);
-    int64_t s = n >= 512 ? 1 : 512 / n;
-    const int64_t least = d->type == CG_TYPE_FP32 ? kLeastChunkFp32 : kLeastChunk, most = (p.K + least - 1) / least;
-    if (s > most) s = most;
-    if (s > kMostSplits) s = kMostSplits;
-    if (s > 1) {
-        const int64_t per = ((p.K + s - 1) / s + kGemmStep - 1) / kGemmStep * kGemmStep;
-        p.chunk = (int)per;
-        p.splits = (int)((p.K + per - 1) / per);
+    const int64_t n = tiles(128), pieces = (p.K + kGemmStep - 1) / kGemmStep;
+    double best = 0;
+    for (int64_t s = 1; s <= kMostSplits && s <= pieces; ++s) {
+        const int64_t per = (pieces + s - 1) / s, have = (pieces + per - 1) / per;
+        if (have != s || n * s > kMostBlocks) continue;
+        const double t = cost(d->type, n * s, per) + (s > 1 ? join_cost(s, p.R, p.C) : 0);
+        if (s == 1 || t < best) best = t, p.splits = (int)s, p.chunk = (int)(s > 1 ? per * kGemmStep : p.K);
     }
+    // a block a compute unit: microseconds a step, and before and after the steps
+    p.large = d->type == CG_TYPE_BF16 && (double)((tiles(256) + 255) / 256) * (9.0 + 1.0 * (double)pieces) < best + 4.0;
     return p;
 }
 size_t part_bytes(const Plan &p) { return p.splits > 1 ? (size_t)p.splits * (size_t)p.R * (size_t)p.C * sizeof(float) : 0; }
