@@ -100,9 +100,15 @@ template <class T, int MT> __global__ __launch_bounds__(64 * kFewWaves) void few
 }
 
 // ---- the join of a cut k --------------------------------------------------------------------------------------------------
-template <class T> __global__ __launch_bounds__(256) void gemm_join_kernel(const float *part, int splits, int R, int C, FastDiv by_chunks, uint32_t count, EpiArgs e)
+template <class T> __global__ __launch_bounds__(256) void gemm_join_kernel(const float *part, int splits, int R, int C, FastDiv by_chunks, uint32_t count, EpiArgs e, float *dbias)
 {
     const int64_t plane = (int64_t)R * C;
+    if (dbias)
+        for (uint32_t r = blockIdx.x * 256 + threadIdx.x; r < (uint32_t)R; r += gridDim.x * 256) {
+            float s = 0.f;
+            for (int i = 0; i < splits; ++i) s += part[splits * plane + (int64_t)i * R + r];
+            dbias[r] = s;
+        }
     for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < count; i += gridDim.x * 256) {
         const int r = (int)fdiv(i, by_chunks), c = 8 * (int)(i - r * by_chunks.d), n = C - c;
         const float *p = part + (int64_t)r * C + c;
@@ -238,7 +244,7 @@ Plan plan_of(const cg_linear_desc *d, int pass)
     p.large = d->type == CG_TYPE_BF16 && (double)((tiles(256) + 255) / 256) * (9.0 + 1.0 * (double)pieces) < best + 4.0;
     return p;
 }
-size_t part_bytes(const Plan &p) { return p.splits > 1 ? (size_t)p.splits * (size_t)p.R * (size_t)p.C * sizeof(float) : 0; }
+size_t part_bytes(const Plan &p) { return p.splits > 1 ? (size_t)p.splits * (size_t)p.R * ((size_t)p.C + 1) * sizeof(float) : 0; }
 int column_slices(int64_t M, int64_t N)
 {
     const int64_t blocks = (N + kColumns - 1) / kColumns, most = 1024 / blocks, want = (M + 63) / 64;
@@ -277,9 +283,24 @@ int product(const cg_linear_desc *d, int pass, const Plan &p, GemmArgs &a, bool 
     const dim3 grid(blocks_for(count, 4096));
     const FastDiv by = make_fastdiv(chunks);
     if (pass == CG_PASS_BWD_WEIGHT || d->type == CG_TYPE_FP32)
-        hipLaunchKernelGGL((gemm_join_kernel<float>), grid, dim3(256), 0, s, a.part, a.splits, p.R, p.C, by, count, a.epi);
-    else hipLaunchKernelGGL((gemm_join_kernel<bf16raw>), grid, dim3(256), 0, s, a.part, a.splits, p.R, p.C, by, count, a.epi);
+        hipLaunchKernelGGL((gemm_join_kernel<float>), grid, dim3(256), 0, s, a.part, a.splits, p.R, p.C, by, count, a.epi, a.dbias);
+    else hipLaunchKernelGGL((gemm_join_kernel<bf16raw>), grid, dim3(256), 0, s, a.part, a.splits, p.R, p.C, by, count, a.epi, a.dbias);
     CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
+// dbias by a pass of its own; its slices' sums lie in the workspace until it is done.
+int bias_pass(const cg_linear_desc *d, const void *dz, int64_t dz_ld, float *dbias, void *ws, hipStream_t s)
+{
+    const int M = (int)d->M, N = (int)d->N, slices = column_slices(M, N), slice = (M + slices - 1) / slices;
+    float *const to = slices > 1 ? static_cast<float *>(ws) : dbias;
+    const dim3 grid((unsigned)((N + kColumns - 1) / kColumns), (unsigned)slices);
+    hipLaunchKernelGGL((column_sums_kernel<bf16raw>), grid, dim3(256), 0, s, static_cast<const bf16raw *>(dz), dz_ld, M, N, slice, to);
+    CG_HIP_TRY(hipGetLastError());
+    if (slices > 1) {
+        hipLaunchKernelGGL(column_join_kernel, dim3((unsigned)((N + 31) / 32)), dim3(256), 0, s, to, slices, N, dbias);
+        CG_HIP_TRY(hipGetLastError());
+    }
     return CG_OK;
 }
 
@@ -322,7 +343,7 @@ extern "C" size_t cg_linear_workspace_bytes(const cg_linear_desc *d, int pass)
     const Plan p = plan_of(d, pass);
     size_t need = part_bytes(p);
     if (pass != CG_PASS_BWD_WEIGHT) return need;
-    if (slice_bytes(d) > need) need = slice_bytes(d);
+    if (p.large && slice_bytes(d) > need) need = slice_bytes(d);
     if (unpacks(d, p) && unpacked_bytes(d) > need) need = unpacked_bytes(d);
     return need;
 }
@@ -375,30 +396,23 @@ extern "C" int cg_linear_bwd_weight(const cg_linear_desc *d, const void *dz, int
     if (d->M > 0 && (!tensor_ok(dz, dz_ld, d->N, d->type) || (x8 ? !packed_ok(x8, d->K) : !tensor_ok(x, x_ld, d->K, d->type)))) return CG_EINVAL;
     if (int rc = ws_check(ws, ws_bytes, cg_linear_workspace_bytes(d, CG_PASS_BWD_WEIGHT))) return rc;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const int M = (int)d->M, N = (int)d->N;
-    if (dbias) {       // before the product, whose sums take the workspace afterwards
-        const int slices = column_slices(M, N), slice = (M + slices - 1) / slices;
-        float *const to = slices > 1 ? static_cast<float *>(ws) : dbias;
-        const dim3 grid((unsigned)((N + kColumns - 1) / kColumns), (unsigned)slices);
-        if (d->type == CG_TYPE_FP32) hipLaunchKernelGGL((column_sums_kernel<float>), grid, dim3(256), 0, s, static_cast<const float *>(dz), dz_ld, M, N, slice, to);
-        else hipLaunchKernelGGL((column_sums_kernel<bf16raw>), grid, dim3(256), 0, s, static_cast<const bf16raw *>(dz), dz_ld, M, N, slice, to);
-        CG_HIP_TRY(hipGetLastError());
-        if (slices > 1) {
-            hipLaunchKernelGGL(column_join_kernel, dim3((unsigned)((N + 31) / 32)), dim3(256), 0, s, to, slices, N, dbias);
-            CG_HIP_TRY(hipGetLastError());
-        }
-    }
+    const Plan p = plan_of(d, CG_PASS_BWD_WEIGHT);
+    const bool dz_dma = d->type == CG_TYPE_BF16 && dma_ok(dz, dz_ld, d->N), unpack = x8 && dz_dma && unpacks(d, p);
     GemmArgs a{};
     a.A = dz, a.a_ld = dz_ld, a.epi.out = dw, a.epi.out_ld = d->K;
-    const Plan p = plan_of(d, CG_PASS_BWD_WEIGHT);
-    const bool dz_dma = d->type == CG_TYPE_BF16 && dma_ok(dz, dz_ld, d->N);
-    if (x8 && dz_dma && unpacks(d, p)) {
+    const bool dma = dz_dma && (x8 || dma_ok(x, x_ld, d->K));
+    // large tiles leave no room for the bias's sums: they come first, and the workspace is the product's afterwards
+    if (p.large && dma && (!x8 || unpack)) {
+        if (dbias)
+            if (int rc = bias_pass(d, dz, dz_ld, dbias, ws, s)) return rc;
+    } else a.dbias = dbias;
+    if (unpack) {
         if (int rc = cg_unpack8(d->type, d->M, d->K, x8, ws, d->K, stream)) return rc;
         x = ws, x_ld = d->K, x8 = nullptr;
     }
     if (x8) a.B8 = {x8->codes, x8->scales, x8->codes_ld, x8->scales_ld};
     else a.B = x, a.b_ld = x_ld;
-    return product(d, CG_PASS_BWD_WEIGHT, p, a, x8 != nullptr, dz_dma && (x8 || dma_ok(x, x_ld, d->K)), ws, s);
+    return product(d, CG_PASS_BWD_WEIGHT, p, a, x8 != nullptr, dma, ws, s);
 }
 
 extern "C" int cg_act_bwd(int act, int type, int64_t rows, int64_t cols, const void *dy, int64_t dy_ld, const void *z, int64_t z_ld,

@@ -26,7 +26,8 @@ struct GemmArgs {
     int64_t a_ld, b_ld;
     int R, C, K;
     int tiles_r, tiles_c, splits, chunk;      // k is cut into `splits` chunks (a multiple of a step each)
-    float *part;                      // [splits][R][C] where there are several
+    float *part;                      // [splits][R][C] where there are several, then [splits][R] for the bias
+    float *dbias;                     // backward-weight, tiles of 128: sums of A over k as well; NULL: not wanted
     EpiArgs epi;
 };
 

@@ -342,6 +342,27 @@ template <class TO, int MR, int MC, class S> __device__ __forceinline__ void sto
     }
 }
 
+// The gradient of a bias beside that of the weights: the blocks of the first columns' tiles add up what they read of A.  A lane sees eight values
+// of k of its row, in NP pieces, at a time; the lane 32 further the next eight.
+template <int NP> __device__ __forceinline__ float sum_of(const u32x4 (&f)[NP])
+{
+    float s = 0.f;
+#pragma unroll
+    for (int p = NP - 1; p >= 0; --p) {
+        float v[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) v[t] = __uint_as_float(f[p][t] << 16) + __uint_as_float(f[p][t] & 0xffff0000u);
+        s += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    return s;
+}
+__device__ __forceinline__ void store_bias(const GemmArgs &a, int split, int row, int lane, float s)
+{
+    s += __shfl_xor(s, 32);
+    float *const to = a.splits == 1 ? a.dbias : a.part + (int64_t)a.splits * a.R * a.C + (int64_t)split * a.R;
+    if (lane < 32 && row + lane < a.R) to[row + lane] = s;
+}
+
 // Tiles of 128 x 128 of bf16 (and 8-bit) tensors, four waves, two steps in LDS; two blocks a compute unit.
 template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bounds__(256, 2) void gemm_kernel(GemmArgs a)
 {
@@ -361,6 +382,8 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bo
     LB lb(a.B, a.B8, a.b_ld, c0, a.C, kbeg, kend, a.K);
     Sums<1, 1, 2, 2> acc;
     acc.zero();
+    const bool with_bias = AX && a.dbias && tc == 0 && wc == 0;
+    float bias[2] = {0.f, 0.f};
     auto start = [&](int k, LdsByte *at, auto inside) {
         la.template start<decltype(inside)::value>(k, at);
         lb.template start<decltype(inside)::value>(k, at + LA::Lds::BYTES);
@@ -383,6 +406,12 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bo
 #pragma unroll
             for (int i = 0; i < 2; ++i) fa[i] = LA::Lds::read_plane(at, wr + 32 * i, ks, lane, 0);
             acc.mma(fa, fb, true);
+            if (with_bias)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x4 f[1] = {fa[i]};
+                    bias[i] += sum_of<1>(f);
+                }
         }
         if (more) finish(lds + (buf ^ 1) * STAGE);
     };
@@ -397,6 +426,9 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bo
             for (; is_inside(k + STEP); k += STEP, buf ^= 1) step(k, buf, std::true_type());
         for (; k < kend; k += STEP, buf ^= 1) step(k, buf, std::false_type());
     }
+    if (with_bias)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) store_bias(a, split, r0 + wr + 32 * i, lane, bias[i]);
     __syncthreads();
     store_wave<TO, 2, 2>(a, split, lds + wave * 32 * kEpiRow<2>, r0 + wr, c0 + wc, lane, acc);
 }
@@ -426,6 +458,8 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
     LB lb(a.B, a.B8, a.b_ld, c0, a.C, kbeg, kend, a.K);
     Sums<3, NB, 1, 2> acc;
     acc.zero();
+    const bool with_bias = AX && a.dbias && tc == 0 && wc == 0;
+    float bias = 0.f;
     auto start = [&](int k, auto inside) {
         la.template start<decltype(inside)::value>(k, lds);
         lb.template start<decltype(inside)::value>(k, lds);
@@ -450,6 +484,10 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
 #pragma unroll
                 for (int p = 0; p < 3; ++p)
                     if (d - p >= 0 && d - p < NB) acc.mma(fa[p], fb[d - p < NB && d - p >= 0 ? d - p : 0], d == 0);
+            if (with_bias) {
+                const u32x4 f[3] = {fa[0][0], fa[1][0], fa[2][0]};
+                bias += sum_of<3>(f);
+            }
         }
         lds_barrier();
     };
@@ -463,6 +501,7 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
             for (; is_inside(k + STEP); k += STEP) step(k, std::true_type());
         for (; k < kend; k += STEP) step(k, std::false_type());
     }
+    if (with_bias) store_bias(a, split, r0 + wr, lane, bias);
     store_wave<float, 1, 2>(a, split, lds + wave * 32 * kEpiRow<2>, r0 + wr, c0 + wc, lane, acc);
 }
 template <class TB, bool AX, bool BX> int launch_cut(const GemmArgs &a, hipStream_t s)
