@@ -447,7 +447,7 @@ int cg_unpack8(int type, int64_t rows, int64_t cols, const cg_packed8 *p, void *
  *     dx = (dz w) * act_in'(z_in) + add,   dw = dz^T x,   dbias = sum over tokens of dz.
  * act: NONE, RELU, GELU (z Phi(z)) or SILU (z / (1 + e^-z)).  act_in is the activation that made x out of z_in: with it the backward pass
  * leaves the gradient of z_in, which is the dz of the layer that z_in came from; NONE: of x itself.  RELU'(0) = 0.
- * M >= 0, N, K >= 1, each at most 2^31 - 2^16; of the products of two of them, tiles of 128 x 128, 2^22 at most; tensors may exceed 2^31 bytes.
+ * M >= 0, N, K >= 1, each at most 2^26; of the products of two of them, tiles of 128 x 128, 2^22 at most; tensors may exceed 2^31 bytes.
  * Arithmetic: bf16 tensors are multiplied as they are and summed in fp32.  fp32 tensors are multiplied as three bf16 numbers in six products
  * (CG_MATH_FP32 above), up to 32 tokens forward in fp32 multiply-adds; what meets an operand that is not finite is not finite, as NaN where
  * multiply-adds may give an infinity. */

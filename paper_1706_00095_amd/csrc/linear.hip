@@ -198,7 +198,7 @@ bool act_ok(int act) { return act >= CG_ACT_NONE && act <= CG_ACT_SILU; }
 int desc_check(const cg_linear_desc *d)
 {
     if (!d || !type_ok(d->type) || d->M < 0 || d->N < 1 || d->K < 1 || !act_ok(d->act) || !act_ok(d->act_in)) return CG_EINVAL;
-    const int64_t most = INT32_MAX - 65535;
+    const int64_t most = 1 << 26;
     if (d->M > most || d->N > most || d->K > most) return CG_EUNSUPPORTED;
     auto tiles = [](int64_t n) { return (n + 127) / 128; };
     if (tiles(d->M) * tiles(d->N) > kMostBlocks || tiles(d->M) * tiles(d->K) > kMostBlocks || tiles(d->N) * tiles(d->K) > kMostBlocks) return CG_EUNSUPPORTED;

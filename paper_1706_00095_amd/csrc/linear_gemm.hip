@@ -106,7 +106,7 @@ template <bool ACROSS> struct HalfLoader {
     uint32_t voff[2];
     __device__ __forceinline__ HalfLoader(const void *p, int64_t ld, int x0, int count, int kbeg, int kend)
     {
-        const int row0 = ACROSS ? kbeg : x0, col0 = ACROSS ? x0 : kbeg, rows = min((ACROSS ? kend : count) - row0, ROWS), cols = (ACROSS ? count : kend) - col0;
+        const int row0 = ACROSS ? kbeg : x0, col0 = ACROSS ? x0 : kbeg, rows = ACROSS ? STEP : min(count - row0, ROWS), cols = (ACROSS ? count : kend) - col0;
         at = (uint64_t)reinterpret_cast<uintptr_t>(p) + (uint64_t)((row0 * ld + col0) * 2);
         row = (uint32_t)ld * 2;
         bytes = rows > 0 && cols > 0 ? (uint32_t)(rows - 1) * row + (uint32_t)min(cols, ACROSS ? 128 : INT32_MAX) * 2 : 0;       // none: zeros
@@ -126,7 +126,7 @@ template <bool ACROSS> struct HalfLoader {
         r.y = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu);
         uint32_t size = bytes, off = voff[J];
         if constexpr (!WHOLE) {
-            if (ACROSS) size -= k_left < STEP && bytes ? (uint32_t)(STEP - max(k_left, 1)) * row : 0;
+            if (ACROSS) size -= k_left < STEP && bytes ? (uint32_t)(STEP - k_left) * row : 0;       // fewer rows
             else off = 8 * chunk_of(J) < k_left ? off : OOB_ROW;
         }
         r.z = __builtin_amdgcn_readfirstlane(size);

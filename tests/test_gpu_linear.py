@@ -120,6 +120,50 @@ def test_large_tiles_whole_numbers(M, K, N, pack):
     assert torch.equal(dw.cpu(), h["dz"].T @ h["x"]) and torch.equal(db.cpu(), h["dz"].sum(0))
 
 
+@pytest.mark.parametrize("M,K,N", [(4096, 136, 4096), (4104, 200, 4088), (4096, 72, 4096), (4096, 4096, 136), (136, 4096, 4096), (72, 4096, 4096), (8, 4096, 4096)])
+def test_large_tiles_of_few_steps(M, K, N):
+    """Tiles of 256 whose k ends within their first steps."""
+    L = Layer("bf16", M, K, N, bias=True, residual=False, values=lambda s, i: bu.whole(s, 3, 60 + i))
+    h = {k: None if v is None else v.float() for k, v in L.h.items()}
+    y, _ = L.fwd()
+    assert torch.equal(y.cpu(), (h["x"] @ h["w"].T + h["bias"]).bfloat16())
+    assert torch.equal(L.dx().cpu(), (h["dz"] @ h["w"]).bfloat16())
+    dw, db = L.dw()
+    assert torch.equal(dw.cpu(), h["dz"].T @ h["x"]) and torch.equal(db.cpu(), h["dz"].sum(0))
+
+
+@pytest.mark.parametrize("act,act_in,packed", [("gelu", "silu", False), ("silu", "gelu", True), ("relu", "relu", False)])
+def test_large_tiles_with_epilogues(act, act_in, packed):
+    """Tiles of 256 with all that an epilogue has, rows of wider tensors and tiles that reach past the last row and column."""
+    L = Layer("bf16", 2056, 1064, 4104, act, act_in, True, True, 8, seed=12)
+    check(L, pack=packed)
+
+
+def test_large_tiles_in_a_graph():
+    """Captured, and replayed between eager calls: the same bits."""
+    L = Layer("bf16", 2048, 2048, 4096, "gelu", "none", seed=2)
+    cg, d = _cg(), L.d
+    y, dw, db = torch.empty(L.M, L.N, dtype=L.dt, device="cuda"), torch.empty(L.N, L.K, device="cuda"), torch.empty(L.N, device="cuda")
+    x8, ws = L.packed("x"), _ws(cg.cg_linear_workspace_bytes(L.desc, cg.CG_PASS_BWD_WEIGHT))
+
+    def into():
+        cg.cg_linear_fwd(L.desc, d["x"], d["w"], d["bias"], None, y)
+        cg.cg_linear_bwd_weight(L.desc, d["dz"], x8, dw, db, ws)
+
+    into()
+    first = [t.clone() for t in (y, dw, db)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        into()
+    for _ in range(3):
+        for t in (y, dw, db):
+            t.fill_(3.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, (y, dw, db)))
+        into()
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("M,K,N,pad", [(1, 4096, 48, 0), (16, 1000, 100, 8), (31, 77, 130, 1), (200, 520, 136, 0), (333, 129, 65, 2), (128, 4096, 128, 0)])
 def test_whole_numbers(dtype, M, K, N, pad):
