@@ -497,11 +497,11 @@ def _tokens(t, n):
     return t.data_ptr()
 
 
-def _matrix(t, type_, shape, what):
+def _matrix(t, dtype, shape, what):
     """(pointer, elements from a row to the next) of a tensor [rows][cols] of a descriptor's type; its rows may lie in wider ones."""
     if t is None:
         return None, 0
-    if t.dtype is not _DTYPES.get(type_) or not t.is_cuda:
+    if t.dtype is not dtype or not t.is_cuda:
         raise TypeError(f"{what}: expected a device tensor of the descriptor's type")
     if t.shape != shape:
         raise ValueError(f"{what}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
@@ -512,8 +512,8 @@ def _matrix(t, type_, shape, what):
 
 
 def cg_embedding_fwd(d, tokens, table, y, stream=None):
-    _check(lib().cg_embedding_fwd(d, _tokens(tokens, d.tokens), *_matrix(table, d.table_type, (d.vocab, d.cols), "table"),
-                                  *_matrix(y, d.type, (d.tokens, d.cols), "y"), _stream(stream)), "cg_embedding_fwd")
+    _check(lib().cg_embedding_fwd(d, _tokens(tokens, d.tokens), *_matrix(table, _DTYPES[d.table_type], (d.vocab, d.cols), "table"),
+                                  *_matrix(y, _DTYPES[d.type], (d.tokens, d.cols), "y"), _stream(stream)), "cg_embedding_fwd")
 
 
 def cg_embedding_workspace_bytes(d):
@@ -521,7 +521,7 @@ def cg_embedding_workspace_bytes(d):
 
 
 def cg_embedding_bwd(d, tokens, dy, dtable, ws, stream=None):
-    _check(lib().cg_embedding_bwd(d, _tokens(tokens, d.tokens), *_matrix(dy, d.type, (d.tokens, d.cols), "dy"),
+    _check(lib().cg_embedding_bwd(d, _tokens(tokens, d.tokens), *_matrix(dy, _DTYPES[d.type], (d.tokens, d.cols), "dy"),
                                   _weights(dtable, d.vocab * d.cols, "dtable"), *_ws_args(ws), _stream(stream)), "cg_embedding_bwd")
 
 
@@ -542,8 +542,14 @@ class Packed8:
 
 def packed8_like(x):
     """Room for x [rows][cols] in 8 bits, on its device."""
+    if not x.is_cuda:
+        raise TypeError("expected a device tensor")
     rows, cols = x.shape
-    return Packed8(torch.empty(rows, cols, dtype=torch.int8, device=x.device), torch.empty(rows, (cols + 31) // 32, dtype=torch.uint8, device=x.device))
+    blocks, device = (cols + 31) // 32, x.device
+    p = Packed8.__new__(Packed8)          # nothing to check
+    p.codes, p.scales, p.shape = torch.empty(rows, cols, dtype=torch.int8, device=device), torch.empty(rows, blocks, dtype=torch.uint8, device=device), x.shape
+    p.arg = cg_packed8(p.codes.data_ptr(), cols, p.scales.data_ptr(), blocks)
+    return p
 
 
 def _packed(p, shape, what):
@@ -554,12 +560,12 @@ def _packed(p, shape, what):
 
 def cg_pack8(x, p, stream=None):
     code = _type_of(x)
-    _check(lib().cg_pack8(code, *p.shape, *_matrix(x, code, p.shape, "x"), p.arg, _stream(stream)), "cg_pack8")
+    _check(lib().cg_pack8(code, *p.shape, *_matrix(x, x.dtype, p.shape, "x"), p.arg, _stream(stream)), "cg_pack8")
 
 
 def cg_unpack8(p, y, stream=None):
     code = _type_of(y)
-    _check(lib().cg_unpack8(code, *p.shape, p.arg, *_matrix(y, code, p.shape, "y"), _stream(stream)), "cg_unpack8")
+    _check(lib().cg_unpack8(code, *p.shape, p.arg, *_matrix(y, y.dtype, p.shape, "y"), _stream(stream)), "cg_unpack8")
 
 
 def linear_desc(x, w, act="none", act_in="none"):
@@ -577,22 +583,22 @@ def cg_linear_workspace_bytes(d, which):
 
 def cg_linear_fwd(d, x, w, bias, residual, y, z=None, ws=None, stream=None):
     """y = act(x w^T + bias) + residual; z (None: not kept): x w^T + bias."""
-    t, of_y = d.type, (d.M, d.N)
+    t, of_y = _DTYPES[d.type], (d.M, d.N)
     _check(lib().cg_linear_fwd(d, *_matrix(x, t, (d.M, d.K), "x"), *_matrix(w, t, (d.N, d.K), "w"), _weights(bias, d.N, "bias"),
                                *_matrix(residual, t, of_y, "residual"), *_matrix(y, t, of_y, "y"), *_matrix(z, t, of_y, "z"), *_ws_args(ws),
                                _stream(stream)), "cg_linear_fwd")
 
 
-def _either(t, type_, shape, what):
+def _either(t, dtype, shape, what):
     """(pointer, stride, packed) of what is a tensor or a Packed8."""
     if isinstance(t, Packed8):
         return None, 0, _packed(t, shape, what)
-    return *_matrix(t, type_, shape, what), None
+    return *_matrix(t, dtype, shape, what), None
 
 
 def cg_linear_bwd_data(d, dz, w, z_in, add, dx, ws=None, stream=None):
     """dx = (dz w) * act_in'(z_in) + add; z_in: a tensor, a Packed8 or (act_in "none") None."""
-    t, of_x = d.type, (d.M, d.K)
+    t, of_x = _DTYPES[d.type], (d.M, d.K)
     _check(lib().cg_linear_bwd_data(d, *_matrix(dz, t, (d.M, d.N), "dz"), *_matrix(w, t, (d.N, d.K), "w"), *_either(z_in, t, of_x, "z_in"),
                                     *_matrix(add, t, of_x, "add"), *_matrix(dx, t, of_x, "dx"), *_ws_args(ws), _stream(stream)),
            "cg_linear_bwd_data")
@@ -600,15 +606,15 @@ def cg_linear_bwd_data(d, dz, w, z_in, add, dx, ws=None, stream=None):
 
 def cg_linear_bwd_weight(d, dz, x, dw, dbias, ws=None, stream=None):
     """dw = dz^T x, dbias (None: not wanted) = sum of dz; x: a tensor or a Packed8."""
-    t = d.type
+    t = _DTYPES[d.type]
     _check(lib().cg_linear_bwd_weight(d, *_matrix(dz, t, (d.M, d.N), "dz"), *_either(x, t, (d.M, d.K), "x"), _weights(dw, d.N * d.K, "dw"),
                                       _weights(dbias, d.N, "dbias"), *_ws_args(ws), _stream(stream)), "cg_linear_bwd_weight")
 
 
 def cg_act_bwd(act, dy, z, dz, stream=None):
     """dz = dy * act'(z); z: a tensor or a Packed8."""
-    t, shape = _type_of(dy), dy.shape
-    _check(lib().cg_act_bwd(ACTS[act], t, *shape, *_matrix(dy, t, shape, "dy"), *_either(z, t, shape, "z"), *_matrix(dz, t, shape, "dz"),
+    t, shape = dy.dtype, dy.shape
+    _check(lib().cg_act_bwd(ACTS[act], _type_of(dy), *shape, *_matrix(dy, t, shape, "dy"), *_either(z, t, shape, "z"), *_matrix(dz, t, shape, "dz"),
                             _stream(stream)), "cg_act_bwd")
 
 

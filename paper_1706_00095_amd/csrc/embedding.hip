@@ -58,7 +58,9 @@ template <class TT, class T, int AHEAD> __global__ __launch_bounds__(256) void l
 // ---- places sorted by token --------------------------------------------------------------------------------------------------------
 // Least significant digit first, stably.  A wave numbers 64 places at a time: those with its digit among the lanes before it, and
 // those the wave has had before (counted in LDS).  Places without a token have the key `vocab` and come last.
-constexpr int kDigits = 256;
+// A digit has up to 10 bits where a pass is one launch (a table of a million rows takes two passes), up to 8 beyond.  Six at least, so that a block's
+// threads share out the waves' counts of all digits in whole lines.
+constexpr int kDigits = 256, kMostDigits = 1024, kLeastBits = 6;
 constexpr int kOneBlock = 1024, kOneItems = 4, kMostOne = kOneBlock * kOneItems;      // threads, places of a lane, of the block
 constexpr int kMostPass = 1 << 16;          // places up to which a pass is one launch
 constexpr int kTileBlock = 256, kItems = 16, kTile = kTileBlock * kItems;             // beyond: threads, places of a lane, of a block
@@ -137,15 +139,40 @@ struct SortArgs {
     Fill fill;
 };
 
+// What a block of kOneBlock threads counts: counts[wave][digit].  They become where each wave's places of a digit begin: in the order of digits, then
+// waves, from `base`[digit] (NULL: from 0 on, all digits one after the other).  Thread t has digit t / E of some waves, E threads a digit.
+constexpr int kOneWaves = kOneBlock / 64;
+__device__ __forceinline__ void places_of_waves(uint32_t *counts, int bits, const uint32_t *base, uint32_t *sums)
+{
+    const int digits = 1 << bits, shift = bits < 10 ? 10 - bits : 0, each = kOneWaves >> shift;
+    const int d = threadIdx.x >> shift, w0 = (threadIdx.x & ((1 << shift) - 1)) * each;
+    uint32_t c[kOneWaves], sum = 0;
+#pragma unroll
+    for (int u = 0; u < kOneWaves; ++u) {
+        c[u] = u < each ? counts[(w0 + u) * digits + d] : 0;
+        sum += c[u];
+    }
+    uint32_t at = block_before<kOneBlock>(sum, sums);
+    if (base) {          // what the threads of the same digit before this one have
+        const uint32_t first = (uint32_t)__shfl((int)at, (int)((threadIdx.x & 63) >> shift << shift));
+        at = at - first + base[d];
+    }
+#pragma unroll
+    for (int u = 0; u < kOneWaves; ++u) {
+        if (u < each) counts[(w0 + u) * digits + d] = at;
+        at += c[u];
+    }
+}
+
 // All of up to kMostOne places by one block, the items going through LDS between passes.  16384 places in one block (16 a lane) took 35 us.
 __global__ __launch_bounds__(kOneBlock) void sort_one_kernel(SortArgs a, int passes)
 {
     if (fills(a.fill)) return;
-    constexpr int W = kOneBlock / 64;
-    __shared__ uint32_t counts[W][kDigits], sums[W], ex_key[kMostOne];
+    __shared__ uint32_t counts[kOneWaves * kMostDigits], sums[kOneWaves], ex_key[kMostOne];
     __shared__ uint16_t ex_place[kMostOne];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, items = (a.n + kOneBlock - 1) / kOneBlock, at = wave * items * 64 + lane;
-    const uint32_t mask = (1u << a.bits) - 1;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, items = (a.n + kOneBlock - 1) / kOneBlock, at = wave * items * 64 + lane, digits = 1 << a.bits;
+    const uint32_t mask = (uint32_t)digits - 1;
+    uint32_t *const mine = counts + wave * digits;
     uint32_t key[kOneItems], place[kOneItems], rank[kOneItems];
 #pragma unroll
     for (int j = 0; j < kOneItems; ++j)
@@ -155,26 +182,16 @@ __global__ __launch_bounds__(kOneBlock) void sort_one_kernel(SortArgs a, int pas
         }
     for (int p = 0; p < passes; ++p) {
         const int shift = p * a.bits;
-        for (int i = threadIdx.x; i < W * kDigits; i += kOneBlock) counts[0][i] = 0;
+        for (int i = threadIdx.x; i < kOneWaves * digits; i += kOneBlock) counts[i] = 0;
         __syncthreads();
-        number_items(key, items, shift, a.bits, counts[wave], rank);
+        number_items(key, items, shift, a.bits, mine, rank);
         __syncthreads();
-        // in the order of digits, then waves: thread t has digit t / 4 of four waves
-        const int d = threadIdx.x >> 2, w0 = 4 * (threadIdx.x & 3);
-        uint32_t c[4], sum = 0;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) c[u] = counts[w0 + u][d], sum += c[u];
-        uint32_t before = block_before<kOneBlock>(sum, sums);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            counts[w0 + u][d] = before;
-            before += c[u];
-        }
+        places_of_waves(counts, a.bits, nullptr, sums);
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kOneItems; ++j)
             if (j < items) {
-                const uint32_t to = counts[wave][key[j] >> shift & mask] + rank[j];
+                const uint32_t to = mine[key[j] >> shift & mask] + rank[j];
                 ex_key[to] = key[j];
                 ex_place[to] = (uint16_t)place[j];
             }
@@ -196,48 +213,34 @@ __global__ __launch_bounds__(kOneBlock) void sort_one_kernel(SortArgs a, int pas
 __global__ __launch_bounds__(kOneBlock) void sort_pass_kernel(SortArgs a)
 {
     if (fills(a.fill)) return;
-    constexpr int W = kOneBlock / 64;
-    __shared__ uint32_t counts[W][kDigits], ahead[kDigits], rest[kDigits], sums[W];
-    const int wave = threadIdx.x >> 6, own = blockIdx.x * kOneBlock, i = own + threadIdx.x;
-    const uint32_t mask = (1u << a.bits) - 1;
+    __shared__ uint32_t counts[kOneWaves * kMostDigits], ahead[kMostDigits], rest[kMostDigits], sums[kOneWaves];
+    const int wave = threadIdx.x >> 6, own = blockIdx.x * kOneBlock, i = own + threadIdx.x, digits = 1 << a.bits, all = a.tiles * kOneBlock;
+    const uint32_t mask = (uint32_t)digits - 1;
+    uint32_t *const mine = counts + wave * digits;
     auto key_at = [&](int j) { return a.tokens ? key_of(a.tokens, j, a.n, a.vocab) : j < a.n ? a.key_in[j] : 0xffffffffu; };
-    for (int j = threadIdx.x; j < W * kDigits; j += kOneBlock) counts[0][j] = 0;
-    if (threadIdx.x < kDigits) ahead[threadIdx.x] = rest[threadIdx.x] = 0;
+    for (int j = threadIdx.x; j < kOneWaves * digits; j += kOneBlock) counts[j] = 0;
+    ahead[threadIdx.x] = rest[threadIdx.x] = 0;
     uint32_t key[1] = {key_at(i)}, rank[1];
     const uint32_t place = a.tokens || i >= a.n ? (uint32_t)i : a.place_in[i];
     __syncthreads();
-    for (int j0 = threadIdx.x; j0 < a.tiles * kOneBlock; j0 += 16 * kOneBlock) {
+    for (int j0 = threadIdx.x; j0 < all; j0 += 16 * kOneBlock) {
         uint32_t k[16];
 #pragma unroll
         for (int u = 0; u < 16; ++u) k[u] = key_at(j0 + u * kOneBlock);
 #pragma unroll
         for (int u = 0; u < 16; ++u) {
             const int j = j0 + u * kOneBlock;
-            if (j < a.tiles * kOneBlock) atomicAdd(&(j < own ? ahead : rest)[k[u] >> a.shift & mask], 1u);       // whole numbers: in any order
+            if (j < all) atomicAdd(&(j < own ? ahead : rest)[k[u] >> a.shift & mask], 1u);       // whole numbers: in any order
         }
     }
-    number_items(key, 1, a.shift, a.bits, counts[wave], rank);
+    number_items(key, 1, a.shift, a.bits, mine, rank);
     __syncthreads();
-    const uint32_t before = block_before<kOneBlock>(threadIdx.x < kDigits ? ahead[threadIdx.x] + rest[threadIdx.x] : 0, sums);
-    if (threadIdx.x < kDigits) rest[threadIdx.x] = before + ahead[threadIdx.x];
+    const uint32_t before = block_before<kOneBlock>(ahead[threadIdx.x] + rest[threadIdx.x], sums);
+    rest[threadIdx.x] = before + ahead[threadIdx.x];
     __syncthreads();
-    const int d = threadIdx.x >> 2, w0 = 4 * (threadIdx.x & 3);
-    uint32_t c[4], sum = 0;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) c[u] = counts[w0 + u][d], sum += c[u];
-    uint32_t at = rest[d];
-#pragma unroll
-    for (int u = 0; u < 3; ++u) {
-        const uint32_t other = (uint32_t)__shfl((int)sum, (int)((threadIdx.x & 60) + u));
-        at += u < (int)(threadIdx.x & 3) ? other : 0;
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        counts[w0 + u][d] = at;
-        at += c[u];
-    }
+    places_of_waves(counts, a.bits, rest, sums);
     __syncthreads();
-    const uint32_t to = counts[wave][key[0] >> a.shift & mask] + rank[0];
+    const uint32_t to = mine[key[0] >> a.shift & mask] + rank[0];
     if (i < a.n) a.key[to] = key[0], a.place[to] = place;       // what lies behind the last place comes last
 }
 
@@ -553,7 +556,8 @@ extern "C" int cg_embedding_bwd(const cg_embedding_desc *d, const int32_t *token
     const hipStream_t s = static_cast<hipStream_t>(stream);
     int bits = 1;
     while (d->vocab >> bits) ++bits;           // keys are at most vocab
-    const int passes = (bits + 7) / 8, per = (bits + passes - 1) / passes, n = (int)d->tokens;
+    const int most = l.passes ? 10 : 8, passes = (bits + most - 1) / most, n = (int)d->tokens;
+    const int per = std::max((bits + passes - 1) / passes, kLeastBits);
     const int64_t count = d->vocab * d->cols;
     if (n == 0) {
         hipLaunchKernelGGL(fill_kernel, dim3(fillers(count)), dim3(1024), 0, s, Fill{dtable, count, 0});

@@ -54,7 +54,8 @@ GRADS = [  # places, vocab, columns, pad, kind
     (0, 10, 12, 0, "any"), (1, 1, 1, 0, "any"), (1, 3000, 40, 0, "any"), (2, 255, 8, 0, "same"), (31, 256, 7, 3, "any"), (32, 257, 33, 0, "same"), (33, 2, 130, 0, "skewed"),
     (64, 64, 64, 0, "falling"), (65, 1000, 513, 1, "gaps"), (1000, 50, 24, 0, "skewed"), (1024, 70000, 16, 0, "any"), (1025, 300, 600, 8, "gaps"), (5000, 1, 40, 0, "same"),
     (16384, 1000, 40, 0, "skewed"), (16384, 20000, 9, 0, "falling"), (16385, 4000, 33, 0, "skewed"), (20000, 3, 8, 0, "gaps"), (40000, 100000, 12, 0, "any"), (70000, 500, 20, 0, "skewed"),
-    (300000, 17000000, 1, 0, "skewed"),
+    (300000, 17000000, 1, 0, "skewed"), (5000, 2000000, 3, 0, "skewed"), (3000, 1100000, 2, 0, "gaps"), (6000, 600, 20, 0, "gaps"), (4096, 30, 10, 0, "any"), (4097, 1023, 8, 0, "skewed"),
+    (65536, 1025, 16, 0, "skewed"), (65537, 1025, 16, 0, "skewed"), (9000, 300000, 300, 0, "skewed"),
 ]
 
 
