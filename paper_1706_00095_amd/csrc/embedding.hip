@@ -465,7 +465,7 @@ int desc_check(const cg_embedding_desc *d)
 }
 // More chunks, more waves; fewer, fewer parts of a frequent token to add one after the other: 3001 places of 769 columns 36 us with chunks of 32,
 // 32 with chunks of 16; 16384 of 1024 95 and 101 (lookup and gradient).
-int chunk_shift_of(int64_t tokens) { return tokens <= 4096 ? 4 : tokens <= kMostPass ? 5 : tokens <= 1 << 20 ? 7 : 9; }
+int chunk_shift_of(int64_t tokens, int64_t cols) { return tokens <= (cols <= 128 ? kMostPass : 4096) ? 4 : tokens <= kMostPass ? 5 : tokens <= 1 << 20 ? 7 : 9; }
 size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
 struct Layout {
     size_t key[2], place[2], counts, head, tail, total;
@@ -482,7 +482,7 @@ Layout layout_of(const cg_embedding_desc *d)
     l.tiles = n <= (size_t)kMostOne ? 1 : (int)(l.passes ? (n + kOneBlock - 1) / kOneBlock : (n + kTile - 1) / kTile);
     for (int i = 0; i < (l.tiles > 1 ? 2 : 1); ++i) l.key[i] = take(4 * n), l.place[i] = take(4 * n);
     l.counts = take(l.passes ? 0 : sizeof(uint32_t) * kDigits * (size_t)l.tiles);
-    const size_t chunks = (n + ((size_t)1 << chunk_shift_of(d->tokens)) - 1) >> chunk_shift_of(d->tokens);
+    const size_t chunks = (n + ((size_t)1 << chunk_shift_of(d->tokens, d->cols)) - 1) >> chunk_shift_of(d->tokens, d->cols);
     if (chunks > 1) l.head = take(4 * chunks * (size_t)d->cols), l.tail = take(4 * chunks * (size_t)d->cols);
     l.total = at;
     return l;
@@ -602,6 +602,6 @@ extern "C" int cg_embedding_bwd(const cg_embedding_desc *d, const int32_t *token
     g.key = words(l.key[last]), g.place = words(l.place[last]), g.dy = dy, g.dy_ld = dy_ld;
     g.head = reinterpret_cast<float *>(base + l.head), g.tail = reinterpret_cast<float *>(base + l.tail);
     g.dtable = dtable, g.n = n, g.vocab = (int)d->vocab, g.cols = (int)d->cols, g.scale = d->scale;
-    g.chunk_shift = chunk_shift_of(d->tokens);
+    g.chunk_shift = chunk_shift_of(d->tokens, d->cols);
     return d->type == CG_TYPE_FP32 ? grad_typed<float>(g, s) : grad_typed<bf16raw>(g, s);
 }

@@ -234,7 +234,8 @@ Plan plan_of(const cg_linear_desc *d, int pass)
     auto tiles = [&](int64_t t) { return ((p.R + t - 1) / t) * ((p.C + t - 1) / t); };
     const int64_t n = tiles(128), pieces = (p.K + kGemmStep - 1) / kGemmStep;
     double best = 0;
-    for (int64_t s = 1; s <= kMostSplits && s <= pieces; ++s) {
+    const int64_t splits = (int64_t)p.R * p.C <= 1 << 28 ? kMostSplits : 1;       // of large outputs there are tiles enough
+    for (int64_t s = 1; s <= splits && s <= pieces; ++s) {
         const int64_t per = (pieces + s - 1) / s, have = (pieces + per - 1) / per;
         if (have != s || n * s > kMostBlocks) continue;
         const double t = cost(d->type, n * s, per) + (s > 1 ? join_cost(s, p.R, p.C) : 0);

@@ -278,8 +278,8 @@ template <int LOADS, int READS> __device__ __forceinline__ void end_phase()
 }
 
 // Consecutive blocks run on different XCDs, each with an L2 of its own: every XCD gets a stretch of neighbouring tiles, in groups of
-// 8 rows of tiles, so that the 32 blocks it runs at a time read 8 strips of A and 4 of B.
-constexpr int kXcds = 8, kGroup = 8;
+// 4 rows of tiles, so that the 32 blocks it runs at a time read 4 strips of A and 8 of B.
+constexpr int kXcds = 8, kGroup = 4;
 __device__ __forceinline__ void place_of(const GemmArgs &a, int &tr, int &tc, int &split)
 {
     const int n = a.tiles_r * a.tiles_c, all = n * a.splits, id = (int)blockIdx.x;
