@@ -12,6 +12,8 @@
 namespace cg {
 namespace {
 
+typedef float v4f __attribute__((ext_vector_type(4)));
+
 // ---- tiles in LDS -----------------------------------------------------------------------------------------------------------
 // ROWS x COLS bf16 as in memory, NP planes.  ACROSS: rows are values of k.  16-byte chunks of a row are exchanged by a function of the row so that
 // neither 16 rows' same chunk (reads in rows take 16 lanes at a time) nor four rows' same 64 bytes (transposing reads) fall on the
@@ -21,7 +23,7 @@ template <bool ACROSS, int ROWS, int COLS, int NP> struct LdsTile {
     static_assert(ACROSS ? COLS >= 128 : COLS == 64 || COLS == 32, "the exchange of chunks");
     static __device__ __forceinline__ int swizzle(int row)
     {
-        if constexpr (ACROSS) return (row & 3) << 2;
+        if constexpr (ACROSS) return (row & 3) << 2 | (row >> 3 & 1) << 1;
         else if constexpr (COLS == 64) return row >> 1 & 7;
         else return row >> 2 & 3;
     }
@@ -37,6 +39,15 @@ template <bool ACROSS, int ROWS, int COLS, int NP> struct LdsTile {
         if constexpr (!ACROSS) return CG_LDS(u32x4, t + plane * PLANE + at(x0 + (lane & 31), 2 * ks + (lane >> 5)));
         const int row = 16 * ks + 8 * (lane >> 5) + (lane >> 2 & 3), chunk = (x0 >> 3) + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
         LdsByte *base = t + plane * PLANE + at(row, chunk) + 8 * (lane & 1);
+        const uint2 a = __builtin_bit_cast(uint2, read_tr(base)), b = __builtin_bit_cast(uint2, read_tr(base + 4 * COLS * 2));
+        return u32x4{a.x, a.y, b.x, b.y};
+    }
+    // the same of 16 rows or columns, the values 32 ks .. 32 ks + 31; lane l has those from 8 (l / 16) on
+    static __device__ __forceinline__ u32x4 read16(LdsByte *t, int x0, int ks, int lane)
+    {
+        if constexpr (!ACROSS) return CG_LDS(u32x4, t + at(x0 + (lane & 15), 4 * ks + (lane >> 4)));
+        const int row = 32 * ks + 8 * (lane >> 4) + (lane >> 2 & 3), chunk = (x0 >> 3) + (lane >> 1 & 1);
+        LdsByte *base = t + at(row, chunk) + 8 * (lane & 1);
         const uint2 a = __builtin_bit_cast(uint2, read_tr(base)), b = __builtin_bit_cast(uint2, read_tr(base + 4 * COLS * 2));
         return u32x4{a.x, a.y, b.x, b.y};
     }
@@ -535,19 +546,18 @@ template <bool AX, bool BX, class TO> __global__ __launch_bounds__(512, 2) void 
     // a lane's places of either operand lie within what an instruction's offset reaches
     auto at_a = [&](int h, int s) { return lds + ((s & 1) * 2 + h) * kHalf; };
     auto at_b = [&](int h, int s) { return lds + (4 + (s & 1) * 2 + h) * kHalf; };
-    Frag<1> fa[4][2], fb[2][4];
-    v16f acc[2][2][2];               // half of A, half of B, 32 rows
+    u32x4 fa[2][4], fb[2][2][2];     // [values of k, 32 at a time][16 rows]; half of B
+    v4f acc[2][2][4][2];             // half of A, half of B, 16 rows, 16 columns
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i >> 2][i >> 1 & 1][i & 1] = v16f{};
+    for (int i = 0; i < 32; ++i) acc[i >> 4][i >> 3 & 1][i >> 1 & 3][i & 1] = v4f{};
 
-    auto read_a = [&](int h, int s, int ks) {
+    auto read_a = [&](int h, int s, int ks, int i) { fa[ks][i] = LA::Lds::read16(at_a(h, s), 64 * wr + 16 * i, ks, lane); };
+    auto read_b = [&](auto h, int s, int ks, int j) { fb[h.value][ks][j] = LB::Lds::read16(at_b(h.value, s), 32 * wc + 16 * j, ks, lane); };
+    auto multiply = [&](auto ha, auto hb, int ks, int i) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) fa[ks][i] = LA::Lds::read(at_a(h, s), 64 * wr + 32 * i, ks, lane);
-    };
-    auto read_b = [&](auto h, int s, int ks) { fb[h.value][ks] = LB::Lds::read(at_b(h.value, s), 32 * wc, ks, lane); };
-    auto multiply = [&](auto ha, auto hb, int ks) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) acc[ha.value][hb.value][i] = mfma(fb[hb.value][ks].p[0], fa[ks][i].p[0], acc[ha.value][hb.value][i]);
+        for (int j = 0; j < 2; ++j)
+            acc[ha.value][hb.value][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[hb.value][ks][j]), __builtin_bit_cast(bf16x8, fa[ks][i]),
+                                                                                    acc[ha.value][hb.value][i][j], 0, 0, 0);
     };
     const std::integral_constant<int, 0> _0;
     const std::integral_constant<int, 1> _1;
@@ -555,11 +565,12 @@ template <bool AX, bool BX, class TO> __global__ __launch_bounds__(512, 2) void 
     auto phase = [&](auto ha, auto hb, auto full, bool fill, auto &loader, LdsByte *to, auto read) {
         constexpr bool FULL = decltype(full)::value;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            multiply(ha, hb, ks);
-            read(ks);
-            if (ks == 1 && (FULL || fill)) loader.template load<FULL, 0>(to, wave);
-            if (ks == 3 && (FULL || fill)) loader.template load<FULL, 1>(to, wave);
+        for (int t = 0; t < 4; ++t) {         // half a 32 of k: two of four 16 rows
+            multiply(ha, hb, t >> 1, 2 * (t & 1));
+            multiply(ha, hb, t >> 1, 2 * (t & 1) + 1);
+            read(t);
+            if (t == 1 && (FULL || fill)) loader.template load<FULL, 0>(to, wave);
+            if (t == 3 && (FULL || fill)) loader.template load<FULL, 1>(to, wave);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -577,13 +588,16 @@ template <bool AX, bool BX, class TO> __global__ __launch_bounds__(512, 2) void 
         };
         const std::integral_constant<int, AX ? 15 : 8> reads_a;
         const std::integral_constant<int, BX ? 8 : 4> reads_b;
-        phase(_0, first, full, fill, lb[first.value], at_b(first.value, s), [&](int ks) { read_b(second, s, ks); });
+        phase(_0, first, full, fill, lb[first.value], at_b(first.value, s), [&](int t) { read_b(second, s, t >> 1, t & 1); });
         end(reads_b, _0);
-        phase(_0, second, full, fill, la[0], at_a(0, s), [&](int ks) { read_a(1, s, ks); });
+        phase(_0, second, full, fill, la[0], at_a(0, s), [&](int t) { read_a(1, s, t >> 1, 2 * (t & 1)), read_a(1, s, t >> 1, 2 * (t & 1) + 1); });
         end(reads_a, _1);
-        phase(_1, second, full, fill, lb[second.value], at_b(second.value, s), [&](int ks) { if (more) read_b(second, s + 1, ks); });
+        phase(_1, second, full, fill, lb[second.value], at_b(second.value, s), [&](int t) {
+            // columns' operands serve all rows of their 32 of k: read behind the last of them
+            if (more && (t & 1)) read_b(second, s + 1, t >> 1, 0), read_b(second, s + 1, t >> 1, 1);
+        });
         end(reads_b, std::integral_constant<int, 2>());
-        phase(_1, first, full, fill, la[1], at_a(1, s), [&](int ks) { if (more) read_a(0, s + 1, ks); });
+        phase(_1, first, full, fill, la[1], at_a(1, s), [&](int t) { if (more) read_a(0, s + 1, t >> 1, 2 * (t & 1)), read_a(0, s + 1, t >> 1, 2 * (t & 1) + 1); });
         end(reads_a, std::integral_constant<int, 3>());
     };
     if (n > 0) {
@@ -600,9 +614,9 @@ template <bool AX, bool BX, class TO> __global__ __launch_bounds__(512, 2) void 
         if (n > 1) end_phase<12, 0>();
         else end_phase<0, 0>();
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            read_b(_0, 0, ks);
-            read_a(0, 0, ks);
+        for (int t = 0; t < 8; ++t) {
+            if (t < 4) read_b(_0, 0, t >> 1, t & 1);
+            read_a(0, 0, t >> 2, t & 3);
         }
         if (n > 1) end_phase<10, 0>();
         else end_phase<0, 0>();
@@ -641,12 +655,8 @@ template <bool AX, bool BX, class TO> __global__ __launch_bounds__(512, 2) void 
     for (int p = 0; p < 8; ++p) {
         const int ha = p >> 2, hb = p >> 1 & 1, i = p & 1;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            u32x4 v;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = __float_as_uint(acc[ha][hb][i][4 * u + x]);
-            CG_LDS(u32x4, mine + (lane & 31) * kLargeRow + (8 * u + 4 * (lane >> 5)) * 4) = v;
-        }
+        for (int u = 0; u < 4; ++u)       // 16 rows, 16 columns
+            CG_LDS(u32x4, mine + (16 * (u >> 1) + (lane & 15)) * kLargeRow + (16 * (u & 1) + 4 * (lane >> 4)) * 4) = __builtin_bit_cast(u32x4, acc[ha][hb][2 * i + (u >> 1)][u & 1]);
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
