@@ -1,11 +1,12 @@
-// The linear layers' products on the matrix cores: C[r][c] = sum_k A(r, k) B(c, k), v_mfma_f32_32x32x16_bf16.
+// The linear layers' products on the matrix cores: C[r][c] = sum_k A(r, k) B(c, k), on v_mfma_f32_16x16x32_bf16 (v_mfma_f32_32x32x16_bf16 is as
+// fast by itself, but power bounds these kernels, and it takes more: 8192^3 1401 TFLOP/s, and 1522 so; on zeros 1914 and 1903).
 //
 // A block makes a tile of C, its waves a rectangle of it each.  Per step, STEP values of k of both operands pass through LDS in the
 // order they have in memory: a tile of rows along k is read in rows, a tile of rows across k by transposing reads, so no operand is
 // ever laid out anew.  bf16 tensors are multiplied as they are; fp32 tensors are cut in three bf16 pieces on their way into LDS, six
 // products; 8-bit tensors become bf16 numbers, exactly, on theirs.
 //
-// The first operand of the instruction is B, so that a lane holds sums of one row r and 4 x 4 neighbouring columns; for the epilogue
+// The first operand of the instruction is B, so that a lane holds sums of one row r and four neighbouring columns; for the epilogue
 // the sums are exchanged through LDS, 32 rows of a wave at a time, and every lane takes eight neighbours of a row.
 #include "linear_device.h"
 
@@ -33,30 +34,14 @@ template <bool ACROSS, int ROWS, int COLS, int NP> struct LdsTile {
 #pragma unroll
         for (int k = 0; k < NP; ++k) CG_LDS(u32x4, t + k * PLANE + at(row, chunk)) = f.p[k];
     }
-    // operand of 32 rows or columns of C from x0 on, the values 16 ks .. 16 ks + 15 of the step; lane l has those from 8 (l / 32) on
-    static __device__ __forceinline__ u32x4 read_plane(LdsByte *t, int x0, int ks, int lane, int plane)
+    // operand of 16 rows or columns of C from x0 on, the values 32 ks .. 32 ks + 31 of the step; lane l has those from 8 (l / 16) on
+    static __device__ __forceinline__ u32x4 read(LdsByte *t, int x0, int ks, int lane, int plane = 0)
     {
-        if constexpr (!ACROSS) return CG_LDS(u32x4, t + plane * PLANE + at(x0 + (lane & 31), 2 * ks + (lane >> 5)));
-        const int row = 16 * ks + 8 * (lane >> 5) + (lane >> 2 & 3), chunk = (x0 >> 3) + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        if constexpr (!ACROSS) return CG_LDS(u32x4, t + plane * PLANE + at(x0 + (lane & 15), 4 * ks + (lane >> 4)));
+        const int row = 32 * ks + 8 * (lane >> 4) + (lane >> 2 & 3), chunk = (x0 >> 3) + (lane >> 1 & 1);
         LdsByte *base = t + plane * PLANE + at(row, chunk) + 8 * (lane & 1);
         const uint2 a = __builtin_bit_cast(uint2, read_tr(base)), b = __builtin_bit_cast(uint2, read_tr(base + 4 * COLS * 2));
         return u32x4{a.x, a.y, b.x, b.y};
-    }
-    // the same of 16 rows or columns, the values 32 ks .. 32 ks + 31; lane l has those from 8 (l / 16) on
-    static __device__ __forceinline__ u32x4 read16(LdsByte *t, int x0, int ks, int lane)
-    {
-        if constexpr (!ACROSS) return CG_LDS(u32x4, t + at(x0 + (lane & 15), 4 * ks + (lane >> 4)));
-        const int row = 32 * ks + 8 * (lane >> 4) + (lane >> 2 & 3), chunk = (x0 >> 3) + (lane >> 1 & 1);
-        LdsByte *base = t + at(row, chunk) + 8 * (lane & 1);
-        const uint2 a = __builtin_bit_cast(uint2, read_tr(base)), b = __builtin_bit_cast(uint2, read_tr(base + 4 * COLS * 2));
-        return u32x4{a.x, a.y, b.x, b.y};
-    }
-    static __device__ __forceinline__ Frag<NP> read(LdsByte *t, int x0, int ks, int lane)
-    {
-        Frag<NP> f;
-#pragma unroll
-        for (int k = 0; k < NP; ++k) f.p[k] = read_plane(t, x0, ks, lane, k);
-        return f;
     }
 };
 
@@ -246,38 +231,40 @@ template <class T, bool ACROSS, int XT, int STEP, int NT> struct TileLoader<T, A
 // ---- sums ------------------------------------------------------------------------------------------------------------------------
 // Pieces: the products below the first are added up on their own, because an instruction drops what lies below the last place of the
 // sum it adds to; products of pieces i and j with i + j > 2 are below 2^-24 of the whole and left out.
-template <int NA, int NB, int MR, int MC> struct Sums {
-    static constexpr bool CUT = NA * NB > 1;
-    v16f big[MR][MC], small[CUT ? MR : 1][CUT ? MC : 1];
+__device__ __forceinline__ v4f mfma16(u32x4 a, u32x4 b, v4f c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// MR x MC tiles of 16 x 16.  A lane has row lane % 16, columns 4 (lane / 16) .. of each.
+template <bool CUT, int MR, int MC> struct Sums {
+    v4f big[MR][MC], small[CUT ? MR : 1][CUT ? MC : 1];
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
         for (int i = 0; i < MR; ++i)
 #pragma unroll
             for (int j = 0; j < MC; ++j) {
-                big[i][j] = v16f{};
-                if constexpr (CUT) small[i][j] = v16f{};
+                big[i][j] = v4f{};
+                if constexpr (CUT) small[i][j] = v4f{};
             }
     }
-    // the product of one piece of each: the first two add to the big sums
-    __device__ __forceinline__ void mma(const u32x4 (&a)[MR], const u32x4 (&b)[MC], bool first)
+    // the product of a piece of A's and one of B's column j; first: of the leading ones
+    __device__ __forceinline__ void mma(const u32x4 (&a)[MR], u32x4 b, int j, bool first)
     {
 #pragma unroll
-        for (int i = 0; i < MR; ++i)
-#pragma unroll
-            for (int j = 0; j < MC; ++j) {
-                if constexpr (CUT)
-                    if (!first) {
-                        small[i][j] = mfma(b[j], a[i], small[i][j]);
-                        continue;
-                    }
-                big[i][j] = mfma(b[j], a[i], big[i][j]);
-            }
+        for (int i = 0; i < MR; ++i) {
+            if constexpr (CUT)
+                if (!first) {
+                    small[i][j] = mfma16(b, a[i], small[i][j]);
+                    continue;
+                }
+            big[i][j] = mfma16(b, a[i], big[i][j]);
+        }
     }
-    __device__ __forceinline__ float get(int i, int j, int u) const
+    __device__ __forceinline__ u32x4 get(int i, int j) const
     {
-        if constexpr (CUT) return big[i][j][u] + small[i][j][u];
-        else return big[i][j][u];
+        if constexpr (CUT) return __builtin_bit_cast(u32x4, big[i][j] + small[i][j]);
+        else return __builtin_bit_cast(u32x4, big[i][j]);
     }
 };
 
@@ -302,7 +289,7 @@ __device__ __forceinline__ void place_of(const GemmArgs &a, int &tr, int &tc, in
     tc = within / high;
 }
 
-// A wave's tile of sums, MR x MC of 32 x 32 from (r0, c0) on, through `mine` (32 rows of kEpiRow<MC> bytes, the wave's own): rows whose
+// A wave's tile of sums, 2 MR x 2 MC of 16 x 16 from (r0, c0) on, through `mine` (32 rows of kEpiRow<MC> bytes, the wave's own): rows whose
 // lanes have eight neighbours each.  What 32 rows need is asked for at once.
 template <int MC> constexpr int kEpiRow = (MC * 32 + 4) * 4;
 template <class TO, int MR, int MC, class S> __device__ __forceinline__ void store_wave(const GemmArgs &a, int split, LdsByte *mine, int r0, int c0, int lane, const S &acc)
@@ -326,14 +313,10 @@ template <class TO, int MR, int MC, class S> __device__ __forceinline__ void sto
 #pragma unroll
             for (int t = 0; t < N; ++t) in[t] = load(t);
 #pragma unroll
-        for (int j = 0; j < MC; ++j)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                u32x4 v;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = __float_as_uint(acc.get(i, j, 4 * q + u));
-                CG_LDS(u32x4, mine + (lane & 31) * kEpiRow<MC> + (32 * j + 8 * q + 4 * (lane >> 5)) * 4) = v;
-            }
+            for (int j = 0; j < 2 * MC; ++j)
+                CG_LDS(u32x4, mine + (16 * h + (lane & 15)) * kEpiRow<MC> + (16 * j + 4 * (lane >> 4)) * 4) = acc.get(2 * i + h, j);
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int t = 0; t < N; ++t) {
@@ -354,7 +337,7 @@ template <class TO, int MR, int MC, class S> __device__ __forceinline__ void sto
 }
 
 // The gradient of a bias beside that of the weights: the blocks of the first columns' tiles add up what they read of A.  A lane sees eight values
-// of k of its row, in NP pieces, at a time; the lane 32 further the next eight.
+// of k of its row, in NP pieces, at a time; the lane 16 further the next eight.
 template <int NP> __device__ __forceinline__ float sum_of(const u32x4 (&f)[NP])
 {
     float s = 0.f;
@@ -369,9 +352,10 @@ template <int NP> __device__ __forceinline__ float sum_of(const u32x4 (&f)[NP])
 }
 __device__ __forceinline__ void store_bias(const GemmArgs &a, int split, int row, int lane, float s)
 {
+    s += __shfl_xor(s, 16);
     s += __shfl_xor(s, 32);
     float *const to = a.splits == 1 ? a.dbias : a.part + (int64_t)a.splits * a.R * a.C + (int64_t)split * a.R;
-    if (lane < 32 && row + lane < a.R) to[row + lane] = s;
+    if (lane < 16 && row + lane < a.R) to[row + lane] = s;
 }
 
 // Tiles of 128 x 128 of bf16 (and 8-bit) tensors, four waves, two steps in LDS; two blocks a compute unit.
@@ -391,10 +375,10 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bo
 
     LA la(a.A, Packed{}, a.a_ld, r0, a.R, kbeg, kend, a.K);
     LB lb(a.B, a.B8, a.b_ld, c0, a.C, kbeg, kend, a.K);
-    Sums<1, 1, 2, 2> acc;
+    Sums<false, 4, 4> acc;
     acc.zero();
     const bool with_bias = AX && a.dbias && tc == 0 && wc == 0;
-    float bias[2] = {0.f, 0.f};
+    float bias[4] = {};
     auto start = [&](int k, LdsByte *at, auto inside) {
         la.template start<decltype(inside)::value>(k, at);
         lb.template start<decltype(inside)::value>(k, at + LA::Lds::BYTES);
@@ -410,16 +394,17 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bo
         if (more) start(k + STEP, lds + (buf ^ 1) * STAGE, inside);
         LdsByte *const at = lds + buf * STAGE;
 #pragma unroll
-        for (int ks = 0; ks < STEP / 16; ++ks) {
-            u32x4 fa[2], fb[2];
+        for (int ks = 0; ks < STEP / 32; ++ks) {
+            u32x4 fa[4], fb[4];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) fb[j] = LB::Lds::read_plane(at + LA::Lds::BYTES, wc + 32 * j, ks, lane, 0);
+            for (int i = 0; i < 4; ++i) fb[i] = LB::Lds::read(at + LA::Lds::BYTES, wc + 16 * i, ks, lane);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) fa[i] = LA::Lds::read_plane(at, wr + 32 * i, ks, lane, 0);
-            acc.mma(fa, fb, true);
+            for (int i = 0; i < 4; ++i) fa[i] = LA::Lds::read(at, wr + 16 * i, ks, lane);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc.mma(fa, fb[j], j, true);
             if (with_bias)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < 4; ++i) {
                     const u32x4 f[1] = {fa[i]};
                     bias[i] += sum_of<1>(f);
                 }
@@ -439,7 +424,7 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bo
     }
     if (with_bias)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) store_bias(a, split, r0 + wr + 32 * i, lane, bias[i]);
+        for (int i = 0; i < 4; ++i) store_bias(a, split, r0 + wr + 16 * i, lane, bias[i]);
     __syncthreads();
     store_wave<TO, 2, 2>(a, split, lds + wave * 32 * kEpiRow<2>, r0 + wr, c0 + wc, lane, acc);
 }
@@ -467,10 +452,10 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
 
     LA la(a.A, Packed{}, a.a_ld, r0, a.R, kbeg, kend, a.K);
     LB lb(a.B, a.B8, a.b_ld, c0, a.C, kbeg, kend, a.K);
-    Sums<3, NB, 1, 2> acc;
+    Sums<true, 2, 4> acc;
     acc.zero();
     const bool with_bias = AX && a.dbias && tc == 0 && wc == 0;
-    float bias = 0.f;
+    float bias[2] = {};
     auto start = [&](int k, auto inside) {
         la.template start<decltype(inside)::value>(k, lds);
         lb.template start<decltype(inside)::value>(k, lds);
@@ -480,26 +465,28 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
         lb.finish(lds + LA::Lds::BYTES);
         lds_barrier();
         if (decltype(inside)::value || k + STEP < kend) start(k + STEP, inside);
+        u32x4 fa[3][2];
 #pragma unroll
-        for (int ks = 0; ks < STEP / 16; ++ks) {
-            u32x4 fa[3][1], fb[NB][2];
+        for (int p = 2; p >= 0; --p)
 #pragma unroll
-            for (int p = 2; p >= 0; --p) {
-                fa[p][0] = LA::Lds::read_plane(lds, wr, ks, lane, p);
+            for (int i = 0; i < 2; ++i) fa[p][i] = LA::Lds::read(lds, wr + 16 * i, 0, lane, p);
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (p < NB) fb[p < NB ? p : 0][j] = LB::Lds::read_plane(lds + LA::Lds::BYTES, wc + 32 * j, ks, lane, p);
-            }
+        for (int j = 0; j < 4; ++j) {
+            u32x4 fb[NB];
+#pragma unroll
+            for (int p = NB - 1; p >= 0; --p) fb[p] = LB::Lds::read(lds + LA::Lds::BYTES, wc + 16 * j, 0, lane, p);
 #pragma unroll
             for (int d = 2; d >= 0; --d)
 #pragma unroll
                 for (int p = 0; p < 3; ++p)
-                    if (d - p >= 0 && d - p < NB) acc.mma(fa[p], fb[d - p < NB && d - p >= 0 ? d - p : 0], d == 0);
-            if (with_bias) {
-                const u32x4 f[3] = {fa[0][0], fa[1][0], fa[2][0]};
-                bias += sum_of<3>(f);
-            }
+                    if (d - p >= 0 && d - p < NB) acc.mma(fa[p], fb[d - p < NB && d - p >= 0 ? d - p : 0], j, d == 0);
         }
+        if (with_bias)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const u32x4 f[3] = {fa[0][i], fa[1][i], fa[2][i]};
+                bias[i] += sum_of<3>(f);
+            }
         lds_barrier();
     };
     auto is_inside = [&](int k) { return k < kend && la.inside(k) && lb.inside(k); };
@@ -512,7 +499,9 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
             for (; is_inside(k + STEP); k += STEP) step(k, std::true_type());
         for (; k < kend; k += STEP) step(k, std::false_type());
     }
-    if (with_bias) store_bias(a, split, r0 + wr, lane, bias);
+    if (with_bias)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) store_bias(a, split, r0 + wr + 16 * i, lane, bias[i]);
     store_wave<float, 1, 2>(a, split, lds + wave * 32 * kEpiRow<2>, r0 + wr, c0 + wc, lane, acc);
 }
 template <class TB, bool AX, bool BX> int launch_cut(const GemmArgs &a, hipStream_t s)
@@ -551,13 +540,12 @@ template <bool AX, bool BX, class TO> __global__ __launch_bounds__(512, 2) void 
 #pragma unroll
     for (int i = 0; i < 32; ++i) acc[i >> 4][i >> 3 & 1][i >> 1 & 3][i & 1] = v4f{};
 
-    auto read_a = [&](int h, int s, int ks, int i) { fa[ks][i] = LA::Lds::read16(at_a(h, s), 64 * wr + 16 * i, ks, lane); };
-    auto read_b = [&](auto h, int s, int ks, int j) { fb[h.value][ks][j] = LB::Lds::read16(at_b(h.value, s), 32 * wc + 16 * j, ks, lane); };
+    auto read_a = [&](int h, int s, int ks, int i) { fa[ks][i] = LA::Lds::read(at_a(h, s), 64 * wr + 16 * i, ks, lane); };
+    auto read_b = [&](auto h, int s, int ks, int j) { fb[h.value][ks][j] = LB::Lds::read(at_b(h.value, s), 32 * wc + 16 * j, ks, lane); };
     auto multiply = [&](auto ha, auto hb, int ks, int i) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            acc[ha.value][hb.value][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[hb.value][ks][j]), __builtin_bit_cast(bf16x8, fa[ks][i]),
-                                                                                    acc[ha.value][hb.value][i][j], 0, 0, 0);
+            acc[ha.value][hb.value][i][j] = mfma16(fb[hb.value][ks][j], fa[ks][i], acc[ha.value][hb.value][i][j]);
     };
     const std::integral_constant<int, 0> _0;
     const std::integral_constant<int, 1> _1;
