@@ -422,7 +422,7 @@ int cg_attn_bwd(const cg_attn_desc *d, const void *d_o, const void *q, const voi
 
 /* y[t] = scale * table[tokens[t]], table [vocab][cols] of `table_type`, y [tokens][cols] of `type`; a token outside
  * 0 .. vocab - 1 is none: its row of y is zero and it has no gradient.  tokens: device array.  vocab, cols >= 1; tokens = 0: fwd is a no-op.
- * tokens <= 2^28, tokens * ceil(cols / 8) < 2^30. */
+ * vocab, cols <= 2^31 - 2^16; tokens <= 2^28; tokens * ceil(cols / 8) < 2^30. */
 typedef struct { int table_type, type; int64_t vocab, cols, tokens; float scale; } cg_embedding_desc;
 int cg_embedding_fwd(const cg_embedding_desc *d, const int32_t *tokens, const void *table, int64_t table_ld, void *y, int64_t y_ld,
                      void *stream);
@@ -434,10 +434,10 @@ int cg_embedding_bwd(const cg_embedding_desc *d, const int32_t *tokens, const vo
 
 /* A tensor [rows][cols] in 8 bits: 32 neighbours of a row (the last block of a row may be shorter) share a power of two,
  *     x[r][c] ~ codes[r][c] * 2^(scales[r][c / 32] - 133),   codes rounded to the nearest (halves to even), -127 .. 127,
- * with the smallest power, 2^-133 or above, that the block's largest magnitude allows: it is off by 1/127 of that magnitude at
- * most, by 1/254 where it is least.  What is not finite has the code -128 and comes back as NaN; the others of its block are as if it were 0.
+ * with the smallest power, 2^-133 to 2^121, that the block's largest magnitude allows (above 127 * 2^121 the code is 127): it is off by
+ * 1/127 of that magnitude at most, by 1/254 where it is least.  What is not finite has the code -128 and comes back as NaN; the others of its block are as if it were 0.
  * Every value is a bf16 number.  *_ld: elements from a row to the next; no alignment is asked for.
- * rows * ceil(cols / 32) <= 2^29 - 2^16. */
+ * rows * ceil(cols / 32) <= 2^29 - 2^16, cols <= 2^31 - 2^16. */
 typedef struct { int8_t *codes; int64_t codes_ld; uint8_t *scales; int64_t scales_ld; } cg_packed8;
 int cg_pack8(int type, int64_t rows, int64_t cols, const void *x, int64_t x_ld, const cg_packed8 *p, void *stream);
 int cg_unpack8(int type, int64_t rows, int64_t cols, const cg_packed8 *p, void *y, int64_t y_ld, void *stream);

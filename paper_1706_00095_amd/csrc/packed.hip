@@ -21,10 +21,11 @@ struct PackArgs {
 
 // The exponent (biased) of the step 2^e at which the largest magnitude rounds to 64 .. 127: a number 1.m 2^k has the step 2^(k - 6), and the
 // next one where 64 (1.m) would round to 128, which is from 127.5 on.  Subnormal numbers have the step 2^-133, and the next from 127.5 of them on.
+// Above the last step's 127.5 the code stays 127.
 __device__ __forceinline__ uint32_t scale_of(uint32_t top)
 {
     const uint32_t e = top >> 23, m = top & 0x7fffffu;
-    return e + (m >= (e ? 0x7f0000u : 0x7f8000u));
+    return min(e + (m >= (e ? 0x7f0000u : 0x7f8000u)), (uint32_t)kPackTop);
 }
 
 template <class T> __global__ __launch_bounds__(256) void pack8_kernel(PackArgs a)
@@ -48,7 +49,7 @@ template <class T> __global__ __launch_bounds__(256) void pack8_kernel(PackArgs 
         for (int j = 0; j < 8; ++j) {
             const float f = elem(x, j);
             const bool finite = (__float_as_uint(f) & 0x7fffffffu) < 0x7f800000u;
-            const int q = finite ? (int)__builtin_rintf(__builtin_ldexpf(f, kPackBias - (int)e)) : -128;
+            const int q = finite ? min(max((int)__builtin_rintf(__builtin_ldexpf(f, kPackBias - (int)e)), -127), 127) : -128;
             w[j / 4] |= ((uint32_t)q & 0xffu) << (8 * (j & 3));
         }
         if (n > 0) {

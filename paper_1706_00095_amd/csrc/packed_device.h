@@ -1,15 +1,15 @@
 // Values in 8 bits (packed.hip writes them; linear_*.hip reads them).
 //
 // 32 neighbours of a row share a power of two, 2^(scale - 133): an element is code * 2^(scale - 133) with a code of -127 .. 127, or
-// no number (code -128).  133 lets 256 scales reach from the largest fp32 numbers (127 * 2^122 < 2^129) down to 2^-133, the smallest bf16
-// number, below which a finer step would be lost in a bf16 tensor.  A code has seven bits, so every value is a bf16 number exactly and
+// no number (code -128).  133 lets the scales reach from the largest fp32 numbers (254: 127 * 2^121 is the largest value; 64 * 2^122 would be
+// none) down to 2^-133, the smallest bf16 number, below which a finer step would be lost in a bf16 tensor.  A code has seven bits, so every value is a bf16 number exactly and
 // products of packed tensors are products of bf16 numbers.
 #pragma once
 #include "typed_device.h"
 
 namespace cg {
 
-constexpr int kPackBlock = 32, kPackBias = 133;
+constexpr int kPackBlock = 32, kPackBias = 133, kPackTop = 254;
 
 struct Packed {
     const int8_t *codes;

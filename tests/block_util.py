@@ -87,8 +87,8 @@ def linear_dw(dz, x):
 
 
 def packed(x):
-    """(codes, scales, values) of 8 bits, from the definition: the smallest power of two, 2^-133 or above, at which the block's largest
-    magnitude rounds to 127 or less.  x: float64, finite."""
+    """(codes, scales, values) of 8 bits, from the definition: the smallest power of two, 2^-133 to 2^121, at which the block's largest
+    magnitude rounds to 127 or less, or is above 127 * 2^121 and made that.  x: float64, finite."""
     rows, cols = x.shape
     blocks = (cols + 31) // 32
     v = torch.zeros(rows, blocks * 32, dtype=torch.float64)
@@ -96,10 +96,10 @@ def packed(x):
     v = v.view(rows, blocks, 32)
     top = v.abs().amax(2)
     scales = torch.zeros(rows, blocks, dtype=torch.int64)
-    for _ in range(256):
+    for _ in range(254):
         scales += (torch.round(top * torch.exp2(133.0 - scales.double())) > 127).long()
     step = torch.exp2(scales.double() - 133)[..., None]
-    codes = torch.round(v / step)
+    codes = torch.round(v / step).clamp(-127, 127)
     return codes.view(rows, -1)[:, :cols].to(torch.int8), scales.to(torch.uint8), (codes * step).view(rows, -1)[:, :cols]
 
 

@@ -61,6 +61,25 @@ def test_borders():
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_largest(dtype):
+    """The largest numbers of a type come back finite: off by 1/127 of the block's largest at most."""
+    cg, dt = _cg(), bu.DTYPES[dtype]
+    top = float(torch.finfo(dt).max)
+    x = torch.zeros(4, 33, dtype=torch.float64)
+    x[0, 3], x[1, 32], x[2, 0], x[3, :] = top, -top, 127.5 * 2.0 ** 121, 127 * 2.0 ** 121
+    x[0, 4], x[2, 1] = 0.3 * top, -63.4 * 2.0 ** 121
+    x = x.to(dt).double()
+    p = _pack(x.to(dt).cuda())
+    codes, scales, values = bu.packed(x)
+    assert torch.equal(p.scales.cpu(), scales) and torch.equal(p.codes.cpu(), codes)
+    for other in bu.DTYPES.values():
+        y = torch.empty(4, 33, dtype=other, device="cuda")
+        cg.cg_unpack8(p, y)
+        assert torch.equal(y.double().cpu(), values)
+    assert bool(((values - x).abs() <= x.abs().amax(1, keepdim=True) / 127).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_not_finite(dtype):
     cg, dt = _cg(), bu.DTYPES[dtype]
     x = bu.normal((3, 70), dt, 5)
