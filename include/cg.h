@@ -466,7 +466,7 @@ int cg_linear_bwd_data(const cg_linear_desc *d, const void *dz, int64_t dz_ld, c
 int cg_linear_bwd_weight(const cg_linear_desc *d, const void *dz, int64_t dz_ld, const void *x, int64_t x_ld, const cg_packed8 *x8, float *dw,
                          float *dbias, void *ws, size_t ws_bytes, void *stream);
 /* dz = dy * act'(z), z as a tensor or in 8 bits (the other NULL): the gradient through an activation whose output goes elsewhere than into
- * a linear layer.  rows * ceil(cols / 8) < 2^30. */
+ * a linear layer.  rows * ceil(cols / 8) < 2^30, cols <= 2^31 - 2^16. */
 int cg_act_bwd(int act, int type, int64_t rows, int64_t cols, const void *dy, int64_t dy_ld, const void *z, int64_t z_ld, const cg_packed8 *z8,
                void *dz, int64_t dz_ld, void *stream);
 

@@ -423,7 +423,7 @@ extern "C" int cg_act_bwd(int act, int type, int64_t rows, int64_t cols, const v
     if (rows == 0 || cols == 0) return CG_OK;
     if (!tensor_ok(dy, dy_ld, cols, type) || !tensor_ok(dz, dz_ld, cols, type) || !slope_ok(act, z, z_ld, z8, cols, type)) return CG_EINVAL;
     const int64_t chunks = (cols + 7) / 8;
-    if (!rows_fit(rows, cols) || rows * chunks > INT32_MAX / 2) return CG_EUNSUPPORTED;
+    if (rows > INT32_MAX || cols > INT32_MAX - 65535 || rows * chunks > INT32_MAX / 2) return CG_EUNSUPPORTED;
     EpiArgs e{};
     e.out = dz, e.out_ld = dz_ld;
     slope_args(e, act, z, z_ld, z8);

@@ -238,6 +238,37 @@ def test_act_bwd(dtype, act, rows, cols, pad):
         assert bool((whole_out[:, cols:] == 5.0).all())
 
 
+def test_act_bwd_of_many():
+    """More than 2^31 elements, in place."""
+    cg, rows, cols = _cg(), (1 << 16) + 3, (1 << 15) + 40
+    dy, z = bu.normal((40, cols), torch.bfloat16, 1), bu.normal((40, cols), torch.bfloat16, 2)
+    g, zd = (torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t, values in ((g, dy), (zd, z)):
+        t[:20], t[-20:] = values[:20].bfloat16().cuda(), values[20:].bfloat16().cuda()
+    p = cg.packed8_like(zd)
+    cg.cg_pack8(zd, p)
+    del zd
+    cg.cg_act_bwd("silu", g, p, g)
+    want = dy * bu.slope(bu.packed(z)[2], "silu")
+    bu.near(torch.cat([g[:20], g[-20:]]), want, bu.ACT * dy.abs() + (bu.half_step(torch.bfloat16) + bu.U) * want.abs(), "dz")
+    assert not g[20:-20].any()
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, a workspace each, that run beside each other: the bits of calls one after the other."""
+    layers = [Layer(t, 300, 520, 264, "gelu", "silu", True, True, seed=i) for i, t in enumerate(("bf16", "fp32"))]
+    want = [[*L.fwd(), L.dx(), *L.dw()] for L in layers]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in layers], [[], []]
+    for _ in range(5):
+        for i, L in enumerate(layers):
+            with torch.cuda.stream(streams[i]):
+                got[i] = [*L.fwd(), L.dx(), *L.dw()]
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 def test_gradients_by_differences():
     """dx and dw against central differences of a sum over y, in fp32 through the kernels themselves."""
     cg = _cg()
