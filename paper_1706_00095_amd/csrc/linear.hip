@@ -112,13 +112,20 @@ template <class T> __global__ __launch_bounds__(256) void gemm_join_kernel(const
     for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < count; i += gridDim.x * 256) {
         const int r = (int)fdiv(i, by_chunks), c = 8 * (int)(i - r * by_chunks.d), n = C - c;
         const float *p = part + (int64_t)r * C + c;
+        Raw8<float> bias = {};
+        if (e.bias) bias = load8(e.bias + c, n);
+        const EpiIn<T> in = {epi_load_add<T>(e, r, c, n), epi_load_z<EPI_EITHER, T>(e, r, c, n)};
         float v[8] = {};
-        for (int s = 0; s < splits; ++s, p += plane) {
-            const Raw8<float> x = load8(p, n);
+        for (int s = 0; s < splits; s += 4) {        // four parts on their way at a time
+            Raw8<float> x[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += elem(x, j);
+            for (int u = 0; u < 4; ++u) x[u] = load8(p + min(s + u, splits - 1) * plane, n);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += s + u < splits ? elem(x[u], j) : 0.f;
         }
-        finish8<T>(e, v, r, c, n);
+        epi_finish<EPI_EITHER, T>(e, v, bias, in, r, c, n);
     }
 }
 
