@@ -214,19 +214,27 @@ int desc_check(const cg_linear_desc *d)
 // Microseconds that `blocks` tiles of 128 x 128 take for `steps` steps of 64 values of k each, and that the join of a cut k takes: what was measured
 // on products of 64 to 9216 rows, columns and values of k.  A compute unit's second block costs less than its first, others as much
 // again.  bf16, 1024^3: 14 us uncut, 17 in two parts, 20 in four; 64 x 4096 x 4096: 15 in eight parts, 19 in sixteen, 17 in four.  fp32, 256 x
-// 9216 x 4096: 120 us in three parts, 186 uncut; 1500 x 771 x 515: 26 in four, 27 in seven, 38 uncut.
+// 9216 x 4096: 120 us in three parts, 186 uncut.
 double cost(int type, int64_t blocks, int64_t steps)
 {
     const int64_t each = (blocks + 255) / 256;
     const double of = type == CG_TYPE_FP32 ? each == 1 ? 2.8 : 2.4 * (double)each : each == 1 ? 0.55 : 0.4 * (double)each;
     return 4.0 + of * (double)steps;
 }
+// Tiles of 64 x 64 (fp32): a quarter of the work a tile in more than a quarter of the time, but four times the tiles, so that k need not be cut:
+// 1500 x 515 x 771 18 us (26 in four parts of tiles of 128), 1024^3 22 (30), 2048 x 1024 x 256 13 (18); 2048^3 118 (104), 256 x 4096 x 9216 136 (115).
+double small_cost(int64_t blocks, int64_t steps)
+{
+    const int64_t each = (blocks + 255) / 256;
+    return 4.0 + (each == 1 ? 1.06 : 0.87 * (double)each) * (double)steps + 1.2 * (double)(each - 1);
+}
 double join_cost(int64_t splits, int64_t R, int64_t C) { return 3.5 + (double)splits * (double)R * (double)C * 2e-6; }
 struct Plan {
     int R, C, K;              // of the product
     bool few;
+    bool small;               // tiles of 64 x 64 (fp32)
     bool large;               // tiles of 256 x 256, k uncut, where rows allow it (bf16)
-    int splits, chunk;        // of tiles of 128 x 128
+    int splits, chunk;        // of the others
 };
 Plan plan_of(const cg_linear_desc *d, int pass)
 {
@@ -237,16 +245,19 @@ Plan plan_of(const cg_linear_desc *d, int pass)
     p.K = pass == CG_PASS_FWD ? K : pass == CG_PASS_BWD_DATA ? N : M;
     p.few = pass == CG_PASS_FWD && M <= kFewTokens;
     p.splits = 1, p.chunk = p.K;
-    if (p.few) return p;
+    if (p.few || p.K == 0) return p;
     auto tiles = [&](int64_t t) { return ((p.R + t - 1) / t) * ((p.C + t - 1) / t); };
-    const int64_t n = tiles(128), pieces = (p.K + kGemmStep - 1) / kGemmStep;
-    double best = 0;
+    const int64_t pieces = (p.K + kGemmStep - 1) / kGemmStep;
+    double best = 1e30;
     const int64_t splits = (int64_t)p.R * p.C <= 1 << 28 ? kMostSplits : 1;       // of large outputs there are tiles enough
-    for (int64_t s = 1; s <= splits && s <= pieces; ++s) {
-        const int64_t per = (pieces + s - 1) / s, have = (pieces + per - 1) / per;
-        if (have != s || n * s > kMostBlocks) continue;
-        const double t = cost(d->type, n * s, per) + (s > 1 ? join_cost(s, p.R, p.C) : 0);
-        if (s == 1 || t < best) best = t, p.splits = (int)s, p.chunk = (int)(s > 1 ? per * kGemmStep : p.K);
+    for (int tile = 128; tile >= (d->type == CG_TYPE_FP32 ? 64 : 128); tile /= 2) {
+        const int64_t n = tiles(tile);
+        for (int64_t s = 1; s <= splits && s <= pieces; ++s) {
+            const int64_t per = (pieces + s - 1) / s, have = (pieces + per - 1) / per;
+            if (have != s || n * s > kMostBlocks) continue;
+            const double t = (tile == 64 ? small_cost(n * s, per) : cost(d->type, n * s, per)) + (s > 1 ? join_cost(s, p.R, p.C) : 0);
+            if (t < best) best = t, p.small = tile == 64, p.splits = (int)s, p.chunk = (int)(s > 1 ? per * kGemmStep : p.K);
+        }
     }
     // a block a compute unit: microseconds a step, and before and after the steps
     p.large = d->type == CG_TYPE_BF16 && (double)((tiles(256) + 255) / 256) * (9.0 + 1.0 * (double)pieces) < best + 4.0;
@@ -280,12 +291,12 @@ unsigned blocks_for(uint64_t n, unsigned most) { const uint64_t b = (n + 255) / 
 int product(const cg_linear_desc *d, int pass, const Plan &p, GemmArgs &a, bool packed, bool dma, void *ws, hipStream_t s)
 {
     const bool large = p.large && dma && !packed;
-    const int tile = large ? 256 : 128;
+    const int tile = large ? 256 : p.small ? 64 : 128;
     a.R = p.R, a.C = p.C, a.K = p.K;
     a.tiles_r = (p.R + tile - 1) / tile, a.tiles_c = (p.C + tile - 1) / tile;
     a.splits = large ? 1 : p.splits, a.chunk = large ? p.K : p.chunk;
     a.part = static_cast<float *>(ws);
-    if (int rc = gemm_launch({d->type, pass, packed, large, dma}, a, s)) return rc;
+    if (int rc = gemm_launch({d->type, pass, packed, tile, dma}, a, s)) return rc;
     if (a.splits == 1) return CG_OK;
     const uint32_t chunks = (uint32_t)((p.C + 7) / 8), count = chunks * (uint32_t)p.R;
     const dim3 grid(blocks_for(count, 4096));

@@ -31,9 +31,9 @@ struct GemmArgs {
     EpiArgs epi;
 };
 
-// linear_gemm.hip.  Which of its kernels: PASS_*; large: tiles of 256 x 256, else 128 x 128; dma: bf16 operands travel to LDS
-// without registers.
-struct GemmKind { int type, pass, packed, large, dma; };
+// linear_gemm.hip.  Which of its kernels: PASS_*; tiles of 128 x 128, of 256 x 256 (bf16) or of 64 x 64 (fp32); dma: bf16 operands travel to
+// LDS without registers.
+struct GemmKind { int type, pass, packed, tile, dma; };
 int gemm_launch(const GemmKind &kind, const GemmArgs &a, hipStream_t s);
 constexpr int kGemmStep = 64;         // chunks of k are multiples of it
 

@@ -21,10 +21,11 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 // same banks (64 of 4 bytes).
 template <bool ACROSS, int ROWS, int COLS, int NP> struct LdsTile {
     static constexpr int CH = COLS / 8, PLANE = ROWS * COLS * 2, BYTES = NP * PLANE;
-    static_assert(ACROSS ? COLS >= 128 : COLS == 64 || COLS == 32, "the exchange of chunks");
+    static_assert(ACROSS ? COLS >= 64 : COLS == 64 || COLS == 32, "the exchange of chunks");
     static __device__ __forceinline__ int swizzle(int row)
     {
-        if constexpr (ACROSS) return (row & 3) << 2 | (row >> 3 & 1) << 1;
+        if constexpr (ACROSS && COLS == 64) return (row >> 1 & 1) << 1 | (row >> 3 & 1) << 2;
+        else if constexpr (ACROSS) return (row & 3) << 2 | (row >> 3 & 1) << 1;
         else if constexpr (COLS == 64) return row >> 1 & 7;
         else return row >> 2 & 3;
     }
@@ -141,7 +142,8 @@ template <bool ACROSS> struct HalfLoader {
     }
 };
 
-// Otherwise through registers, at any alignment; fp32 is cut, and 8-bit numbers become bf16, on the way.
+// Otherwise through registers, at any alignment; fp32 is cut, and 8-bit numbers become bf16, on the way.  NT threads in a row load a tile; a block
+// may have several times as many, with a tile each.
 // inside(k): the step that begins at k may be loaded without bounds.  All of its values of k are there, and where rows lie across k another row
 // behind them, into which the last chunk of a row may reach; rows and chunks behind the last one are others again: what they give is not stored.
 template <class T> struct Source;
@@ -200,7 +202,7 @@ template <class T, bool ACROSS, int XT, int STEP, int NT> struct TileLoader<T, A
     {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int i = threadIdx.x + j * NT, x = x0 + (ACROSS ? 8 * (i % CH) : i / CH), k = kbeg + (ACROSS ? i / CH : 8 * (i % CH));
+            const int i = threadIdx.x % NT + j * NT, x = x0 + (ACROSS ? 8 * (i % CH) : i / CH), k = kbeg + (ACROSS ? i / CH : 8 * (i % CH));
             const int xc = ACROSS ? min(x, (count - 1) / 8 * 8) : min(x, count - 1);
             at[j] = ACROSS ? src.at(k, xc) : src.at(xc, k);
         }
@@ -211,14 +213,14 @@ template <class T, bool ACROSS, int XT, int STEP, int NT> struct TileLoader<T, A
     {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int i = threadIdx.x + j * NT, row = (ACROSS ? k : x0) + i / CH, c = (ACROSS ? x0 : k) + 8 * (i % CH);
+            const int i = threadIdx.x % NT + j * NT, row = (ACROSS ? k : x0) + i / CH, c = (ACROSS ? x0 : k) + 8 * (i % CH);
             if constexpr (INSIDE) r[j] = at[j].take(src, ACROSS ? STEP : 0, ACROSS ? 0 : STEP);
             else r[j] = src.load(row, c, row < (ACROSS ? kend : count) ? (ACROSS ? count : kend) - c : 0);
         }
     }
     __device__ __forceinline__ void finish_one(LdsByte *t, int j) const
     {
-        const int i = threadIdx.x + j * NT;
+        const int i = threadIdx.x % NT + j * NT;
         Lds::put(t, i / CH, i % CH, frag_of(r[j]));
     }
     __device__ __forceinline__ void finish(LdsByte *t) const
@@ -504,8 +506,99 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
         for (int i = 0; i < 2; ++i) store_bias(a, split, r0 + wr + 16 * i, lane, bias[i]);
     store_wave<float, 1, 2>(a, split, lds + wave * 32 * kEpiRow<2>, r0 + wr, c0 + wc, lane, acc);
 }
-template <class TB, bool AX, bool BX> int launch_cut(const GemmArgs &a, hipStream_t s)
+// Small fp32 products: tiles of 64 x 64, four waves for either half of a block's values of k, whose sums meet in LDS.  Bound by the latency of a
+// step's loads, cut and reads in turn (a step of either half 1.06 us where a compute unit has one block, 0.87 each where it has several, of which the
+// matrix instructions take 0.16): the halves fill each other's waits without a second launch that joins them.
+template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void gemm_cut_small_kernel(GemmArgs a)
 {
+    constexpr int STEP = 32, XT = 64;
+    using LA = TileLoader<float, AX, XT, STEP, 256, false>;
+    using LB = TileLoader<TB, BX, XT, STEP, 256, false>;
+    constexpr int NB = LB::NP, TILES = LA::Lds::BYTES + LB::Lds::BYTES, MINE = 32 * kEpiRow<1>;
+    __shared__ __align__(16) char smem[2 * TILES];
+    static_assert(4 * MINE <= 2 * TILES && MINE >= 64 * (4 * 16 + 2 * 4), "room for the epilogue, and for the sums of a wave");
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave >> 2, wr = (wave >> 1 & 1) * 32, wc = (wave & 1) * 32;
+    LdsByte *const lds = (LdsByte *)smem + half * TILES, *const mine = (LdsByte *)smem + (wave & 3) * MINE;
+    int tr, tc, split;
+    place_of(a, tr, tc, split);
+    const int r0 = tr * XT, c0 = tc * XT, k0 = split * a.chunk, k1 = min(a.K, k0 + a.chunk), each = (k1 - k0 + 2 * STEP - 1) / (2 * STEP);
+    const int kbeg = k0 + half * each * STEP, kend = min(k1, kbeg + each * STEP);
+
+    LA la(a.A, Packed{}, a.a_ld, r0, a.R, kbeg, kend, a.K);
+    LB lb(a.B, a.B8, a.b_ld, c0, a.C, kbeg, kend, a.K);
+    Sums<true, 2, 2> acc;
+    acc.zero();
+    const bool with_bias = AX && a.dbias && tc == 0 && wc == 0;
+    float bias[2] = {};
+    auto start = [&](int k) {
+        if (la.inside(k) && lb.inside(k)) {
+            la.template start<true>(k, lds);
+            lb.template start<true>(k, lds);
+        } else {
+            la.template start<false>(k, lds);
+            lb.template start<false>(k, lds);
+        }
+    };
+    if (kbeg < kend) start(kbeg);
+    for (int i = 0, k = kbeg; i < each; ++i, k += STEP) {
+        if (k < kend) {
+            la.finish(lds);
+            lb.finish(lds + LA::Lds::BYTES);
+        }
+        lds_barrier();
+        if (k + STEP < kend) start(k + STEP);
+        if (k < kend) {
+            u32x4 fa[3][2];
+#pragma unroll
+            for (int p = 2; p >= 0; --p)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) fa[p][t] = LA::Lds::read(lds, wr + 16 * t, 0, lane, p);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                u32x4 fb[NB];
+#pragma unroll
+                for (int p = NB - 1; p >= 0; --p) fb[p] = LB::Lds::read(lds + LA::Lds::BYTES, wc + 16 * j, 0, lane, p);
+#pragma unroll
+                for (int d = 2; d >= 0; --d)
+#pragma unroll
+                    for (int p = 0; p < 3; ++p)
+                        if (d - p >= 0 && d - p < NB) acc.mma(fa[p], fb[d - p < NB && d - p >= 0 ? d - p : 0], j, d == 0);
+            }
+            if (with_bias)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const u32x4 f[3] = {fa[0][t], fa[1][t], fa[2][t]};
+                    bias[t] += sum_of<3>(f);
+                }
+        }
+        lds_barrier();
+    }
+    if (half == 1) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) CG_LDS(u32x4, mine + (64 * t + lane) * 16) = acc.get(t >> 1, t & 1);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) CG_LDS(float, mine + 4096 + (64 * t + lane) * 4) = bias[t];
+    }
+    lds_barrier();
+    if (half == 1) return;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc.small[t >> 1][t & 1] += __builtin_bit_cast(v4f, CG_LDS(u32x4, mine + (64 * t + lane) * 16));
+    if (with_bias)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) store_bias(a, split, r0 + wr + 16 * t, lane, bias[t] + CG_LDS(float, mine + 4096 + (64 * t + lane) * 4));
+    __builtin_amdgcn_wave_barrier();
+    store_wave<float, 1, 1>(a, split, mine, r0 + wr, c0 + wc, lane, acc);
+}
+template <class TB, bool AX, bool BX> int launch_cut_small(const GemmArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((gemm_cut_small_kernel<TB, AX, BX>), dim3((unsigned)(a.tiles_r * a.tiles_c * a.splits)), dim3(512), 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
+template <class TB, bool AX, bool BX> int launch_cut(const GemmKind &k, const GemmArgs &a, hipStream_t s)
+{
+    if (k.tile == 64) return launch_cut_small<TB, AX, BX>(a, s);
     hipLaunchKernelGGL((gemm_cut_kernel<TB, AX, BX>), dim3((unsigned)(a.tiles_r * a.tiles_c * a.splits)), dim3(512), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
@@ -682,7 +775,7 @@ template <bool AX, bool BX, class TO> int launch_large(const GemmArgs &a, hipStr
 template <class TB, bool AX, bool BX, class TO> int launch_bf16(const GemmKind &k, const GemmArgs &a, hipStream_t s)
 {
     if constexpr (sizeof(TB) == 2)
-        if (k.large) return launch_large<AX, BX, TO>(a, s);
+        if (k.tile == 256) return launch_large<AX, BX, TO>(a, s);
     return k.dma ? launch<TB, AX, BX, true, TO>(a, s) : launch<TB, AX, BX, false, TO>(a, s);
 }
 
@@ -691,9 +784,9 @@ template <class TB, bool AX, bool BX, class TO> int launch_bf16(const GemmKind &
 int gemm_launch(const GemmKind &k, const GemmArgs &a, hipStream_t s)
 {
     if (k.type == CG_TYPE_FP32) {
-        if (k.pass == CG_PASS_FWD) return launch_cut<float, false, false>(a, s);
-        if (k.pass == CG_PASS_BWD_DATA) return launch_cut<float, false, true>(a, s);
-        return k.packed ? launch_cut<int8_t, true, true>(a, s) : launch_cut<float, true, true>(a, s);
+        if (k.pass == CG_PASS_FWD) return launch_cut<float, false, false>(k, a, s);
+        if (k.pass == CG_PASS_BWD_DATA) return launch_cut<float, false, true>(k, a, s);
+        return k.packed ? launch_cut<int8_t, true, true>(k, a, s) : launch_cut<float, true, true>(k, a, s);
     }
     if (k.pass == CG_PASS_FWD) return launch_bf16<bf16raw, false, false, bf16raw>(k, a, s);
     if (k.pass == CG_PASS_BWD_DATA) return launch_bf16<bf16raw, false, true, bf16raw>(k, a, s);
