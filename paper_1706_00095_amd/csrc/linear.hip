@@ -221,20 +221,22 @@ double cost(int type, int64_t blocks, int64_t steps)
     const double of = type == CG_TYPE_FP32 ? each == 1 ? 2.8 : 2.4 * (double)each : each == 1 ? 0.55 : 0.4 * (double)each;
     return 4.0 + of * (double)steps;
 }
-// Tiles of 64 x 64 (fp32): a quarter of the work a tile in more than a quarter of the time, but four times the tiles, so that k need not be cut:
-// 1500 x 515 x 771 18 us (26 in four parts of tiles of 128), 1024^3 22 (30), 2048 x 1024 x 256 13 (18); 2048^3 118 (104), 256 x 4096 x 9216 136 (115).
-double small_cost(int64_t blocks, int64_t steps)
+// The same of tiles of 64 x 64: a quarter of the work a tile in more than a quarter of the time, but four times the tiles, so that k need not be cut.
+// fp32: 1500 x 515 x 771 18 us (26 in four parts of tiles of 128), 1024^3 22 (30), 2048^3 118 (104), 256 x 4096 x 9216 136 (115).  bf16: 1024^3 8
+// (15), 1000 x 2048 x 2048 17 (25), 64 x 4096 x 4096 13 in four parts (15 in eight of tiles of 128), 2048^3 32 (27).
+double small_cost(int type, int64_t blocks, int64_t steps)
 {
     const int64_t each = (blocks + 255) / 256;
-    return 4.0 + (each == 1 ? 1.06 : 0.87 * (double)each) * (double)steps + 1.2 * (double)(each - 1);
+    const double of = type == CG_TYPE_FP32 ? each == 1 ? 1.06 : 0.87 * (double)each : each == 1 ? 0.3 : 0.19 * (double)each;
+    return 4.0 + of * (double)steps + 1.2 * (double)(each - 1);
 }
-double join_cost(int64_t splits, int64_t R, int64_t C) { return 3.5 + (double)splits * (double)R * (double)C * 2e-6; }
+double join_cost(int64_t splits, int64_t R, int64_t C) { return 4.5 + (double)splits * (double)R * (double)C * 2e-6; }
 struct Plan {
     int R, C, K;              // of the product
     bool few;
-    bool small;               // tiles of 64 x 64 (fp32)
+    bool small;               // tiles of 64 x 64, else 128 x 128
     bool large;               // tiles of 256 x 256, k uncut, where rows allow it (bf16)
-    int splits, chunk;        // of the others
+    int splits, chunk;        // of k, for tiles of 64 and 128
 };
 Plan plan_of(const cg_linear_desc *d, int pass)
 {
@@ -250,12 +252,12 @@ Plan plan_of(const cg_linear_desc *d, int pass)
     const int64_t pieces = (p.K + kGemmStep - 1) / kGemmStep;
     double best = 1e30;
     const int64_t splits = (int64_t)p.R * p.C <= 1 << 28 ? kMostSplits : 1;       // of large outputs there are tiles enough
-    for (int tile = 128; tile >= (d->type == CG_TYPE_FP32 ? 64 : 128); tile /= 2) {
+    for (int tile = 128; tile >= 64; tile /= 2) {
         const int64_t n = tiles(tile);
         for (int64_t s = 1; s <= splits && s <= pieces; ++s) {
             const int64_t per = (pieces + s - 1) / s, have = (pieces + per - 1) / per;
             if (have != s || n * s > kMostBlocks) continue;
-            const double t = (tile == 64 ? small_cost(n * s, per) : cost(d->type, n * s, per)) + (s > 1 ? join_cost(s, p.R, p.C) : 0);
+            const double t = (tile == 64 ? small_cost(d->type, n * s, per) : cost(d->type, n * s, per)) + (s > 1 ? join_cost(s, p.R, p.C) : 0);
             if (t < best) best = t, p.small = tile == 64, p.splits = (int)s, p.chunk = (int)(s > 1 ? per * kGemmStep : p.K);
         }
     }

@@ -31,7 +31,7 @@ struct GemmArgs {
     EpiArgs epi;
 };
 
-// linear_gemm.hip.  Which of its kernels: PASS_*; tiles of 128 x 128, of 256 x 256 (bf16) or of 64 x 64 (fp32); dma: bf16 operands travel to
+// linear_gemm.hip.  Which of its kernels: PASS_*; tiles of 64 x 64, of 128 x 128, or (bf16) of 256 x 256; dma: bf16 operands travel to
 // LDS without registers.
 struct GemmKind { int type, pass, packed, tile, dma; };
 int gemm_launch(const GemmKind &kind, const GemmArgs &a, hipStream_t s);

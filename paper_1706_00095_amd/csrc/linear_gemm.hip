@@ -71,7 +71,7 @@ template <bool ACROSS, int XT, int STEP, int NT> struct TileLoader<bf16raw, ACRO
             voff[j] = ACROSS && x0 + 8 * chunk >= count ? OOB_ROW : (uint32_t)((int64_t)row * ld * 2 + chunk * 16);
         }
     }
-    static __device__ __forceinline__ int at(int j) { return (j * WAVES + (int)(threadIdx.x >> 6)) * 1024 + (int)(threadIdx.x & 63) * 16; }
+    static __device__ __forceinline__ int at(int j) { return (j * WAVES + (int)(threadIdx.x >> 6) % WAVES) * 1024 + (int)(threadIdx.x & 63) * 16; }
     static __device__ __forceinline__ int row_of(int j) { return at(j) / (COLS * 2); }
     static __device__ __forceinline__ int chunk_of(int j) { return at(j) % (COLS * 2) / 16 ^ Lds::swizzle(row_of(j)); }
     __device__ __forceinline__ bool inside(int) const { return true; }
@@ -80,7 +80,7 @@ template <bool ACROSS, int XT, int STEP, int NT> struct TileLoader<bf16raw, ACRO
         const int row0 = ACROSS ? k : x0, col0 = ACROSS ? x0 : k, rows = (ACROSS ? kend : count) - row0, cols = (ACROSS ? count : kend) - col0;
         const BufferRsrc r = raw_buffer((uint64_t)reinterpret_cast<uintptr_t>(base) + (uint64_t)((row0 * ld + col0) * 2),
                                         (uint64_t)(rows - 1) * (uint64_t)ld * 2 + (uint64_t)cols * 2);
-        const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES;
         if (!ACROSS && cols < STEP) {        // the last step
 #pragma unroll
             for (int j = 0; j < N; ++j) dma16(r, lds + (j * WAVES + wave) * 1024, 8 * chunk_of(j) < cols ? voff[j] : OOB_ROW);
@@ -263,6 +263,7 @@ template <bool CUT, int MR, int MC> struct Sums {
             big[i][j] = mfma16(b, a[i], big[i][j]);
         }
     }
+    __device__ __forceinline__ v4f &of_join(int i, int j) { return CUT ? small[CUT ? i : 0][CUT ? j : 0] : big[i][j]; }      // what sums of another part are added to
     __device__ __forceinline__ u32x4 get(int i, int j) const
     {
         if constexpr (CUT) return __builtin_bit_cast(u32x4, big[i][j] + small[i][j]);
@@ -360,6 +361,28 @@ __device__ __forceinline__ void store_bias(const GemmArgs &a, int split, int row
     if (lane < 16 && row + lane < a.R) to[row + lane] = s;
 }
 
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }       // lets loads go on
+// The sums of the waves that have the same part of a tile in two halves of k meet in the first half's: through `mine`, the part's own.  false: nothing
+// is left for this wave to do.
+template <bool CUT> __device__ __forceinline__ bool join_halves(const GemmArgs &a, int split, int half, LdsByte *mine, int row, int lane, Sums<CUT, 2, 2> &acc, const float (&bias)[2], bool with_bias)
+{
+    if (half == 1) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) CG_LDS(u32x4, mine + (64 * t + lane) * 16) = acc.get(t >> 1, t & 1);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) CG_LDS(float, mine + 4096 + (64 * t + lane) * 4) = bias[t];
+    }
+    lds_barrier();
+    if (half == 1) return false;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc.of_join(t >> 1, t & 1) += __builtin_bit_cast(v4f, CG_LDS(u32x4, mine + (64 * t + lane) * 16));
+    if (with_bias)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) store_bias(a, split, row + 16 * t, lane, bias[t] + CG_LDS(float, mine + 4096 + (64 * t + lane) * 4));
+    __builtin_amdgcn_wave_barrier();
+    return true;
+}
+
 // Tiles of 128 x 128 of bf16 (and 8-bit) tensors, four waves, two steps in LDS; two blocks a compute unit.
 template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bounds__(256, 2) void gemm_kernel(GemmArgs a)
 {
@@ -437,8 +460,83 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> int launch(const GemmA
     return CG_OK;
 }
 
+// Small bf16 products: tiles of 64 x 64, four waves and two steps in LDS for either half of a block's values of k, whose sums meet in LDS.  Bound by the
+// latency of a step's loads (two steps, one of either half, 0.6 us where a compute unit has one block, 0.38 where it has several; the matrix
+// instructions of both take 0.12).
+template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bounds__(512, 4) void gemm_small_kernel(GemmArgs a)
+{
+    constexpr int STEP = 64, XT = 64;
+    using LA = TileLoader<bf16raw, AX, XT, STEP, 256, DMA>;
+    using LB = TileLoader<TB, BX, XT, STEP, 256, DMA && sizeof(TB) == 2>;
+    constexpr int STAGE = LA::Lds::BYTES + LB::Lds::BYTES, MINE = 32 * kEpiRow<1>;
+    __shared__ __align__(16) char smem[4 * STAGE];
+    static_assert(4 * MINE <= 4 * STAGE && MINE >= 64 * (4 * 16 + 2 * 4), "room for the epilogue, and for the sums of a wave");
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave >> 2, wr = (wave >> 1 & 1) * 32, wc = (wave & 1) * 32;
+    LdsByte *const lds = (LdsByte *)smem + half * 2 * STAGE, *const mine = (LdsByte *)smem + (wave & 3) * MINE;
+    int tr, tc, split;
+    place_of(a, tr, tc, split);
+    const int r0 = tr * XT, c0 = tc * XT, k0 = split * a.chunk, k1 = min(a.K, k0 + a.chunk), each = (k1 - k0 + 2 * STEP - 1) / (2 * STEP);
+    const int kbeg = k0 + half * each * STEP, kend = min(k1, kbeg + each * STEP);
+
+    LA la(a.A, Packed{}, a.a_ld, r0, a.R, kbeg, kend, a.K);
+    LB lb(a.B, a.B8, a.b_ld, c0, a.C, kbeg, kend, a.K);
+    Sums<false, 2, 2> acc;
+    acc.zero();
+    const bool with_bias = AX && a.dbias && tc == 0 && wc == 0;
+    float bias[2] = {};
+    auto start = [&](int k, LdsByte *at) {
+        if (la.inside(k) && lb.inside(k)) {
+            la.template start<true>(k, at);
+            lb.template start<true>(k, at + LA::Lds::BYTES);
+        } else {
+            la.template start<false>(k, at);
+            lb.template start<false>(k, at + LA::Lds::BYTES);
+        }
+    };
+    auto finish = [&](LdsByte *at) {
+        la.finish(at);
+        lb.finish(at + LA::Lds::BYTES);
+    };
+    if (kbeg < kend) {
+        start(kbeg, lds);
+        finish(lds);
+    }
+    for (int i = 0, k = kbeg; i < each; ++i, k += STEP) {
+        tile_sync();
+        LdsByte *const at = lds + (i & 1) * STAGE, *const next = lds + (~i & 1) * STAGE;
+        const bool more = k + STEP < kend;
+        if (more) start(k + STEP, next);
+        if (k < kend) {
+#pragma unroll
+            for (int ks = 0; ks < STEP / 32; ++ks) {
+                u32x4 fa[2], fb[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) fb[t] = LB::Lds::read(at + LA::Lds::BYTES, wc + 16 * t, ks, lane);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) fa[t] = LA::Lds::read(at, wr + 16 * t, ks, lane);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc.mma(fa, fb[j], j, true);
+                if (with_bias)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const u32x4 f[1] = {fa[t]};
+                        bias[t] += sum_of<1>(f);
+                    }
+            }
+        }
+        if (more) finish(next);
+    }
+    __syncthreads();
+    if (join_halves(a, split, half, mine, r0 + wr, lane, acc, bias, with_bias)) store_wave<TO, 1, 1>(a, split, mine, r0 + wr, c0 + wc, lane, acc);
+}
+template <class TB, bool AX, bool BX, bool DMA, class TO> int launch_small(const GemmArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((gemm_small_kernel<TB, AX, BX, DMA, TO>), dim3((unsigned)(a.tiles_r * a.tiles_c * a.splits)), dim3(512), 0, s, a);
+    CG_HIP_TRY(hipGetLastError());
+    return CG_OK;
+}
+
 // fp32 tensors: tiles of 128 x 128, eight waves, one step in LDS; two blocks a compute unit, one of which multiplies while the other cuts.
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }       // lets loads go on
 template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void gemm_cut_kernel(GemmArgs a)
 {
     constexpr int STEP = 32, XT = 128;
@@ -508,7 +606,7 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
 }
 // Small fp32 products: tiles of 64 x 64, four waves for either half of a block's values of k, whose sums meet in LDS.  Bound by the latency of a
 // step's loads, cut and reads in turn (a step of either half 1.06 us where a compute unit has one block, 0.87 each where it has several, of which the
-// matrix instructions take 0.16): the halves fill each other's waits without a second launch that joins them.
+// matrix instructions take 0.35): the halves fill each other's waits without a second launch that joins them.
 template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void gemm_cut_small_kernel(GemmArgs a)
 {
     constexpr int STEP = 32, XT = 64;
@@ -573,21 +671,7 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
         }
         lds_barrier();
     }
-    if (half == 1) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) CG_LDS(u32x4, mine + (64 * t + lane) * 16) = acc.get(t >> 1, t & 1);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) CG_LDS(float, mine + 4096 + (64 * t + lane) * 4) = bias[t];
-    }
-    lds_barrier();
-    if (half == 1) return;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) acc.small[t >> 1][t & 1] += __builtin_bit_cast(v4f, CG_LDS(u32x4, mine + (64 * t + lane) * 16));
-    if (with_bias)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) store_bias(a, split, r0 + wr + 16 * t, lane, bias[t] + CG_LDS(float, mine + 4096 + (64 * t + lane) * 4));
-    __builtin_amdgcn_wave_barrier();
-    store_wave<float, 1, 1>(a, split, mine, r0 + wr, c0 + wc, lane, acc);
+    if (join_halves(a, split, half, mine, r0 + wr, lane, acc, bias, with_bias)) store_wave<float, 1, 1>(a, split, mine, r0 + wr, c0 + wc, lane, acc);
 }
 template <class TB, bool AX, bool BX> int launch_cut_small(const GemmArgs &a, hipStream_t s)
 {
@@ -776,6 +860,7 @@ template <class TB, bool AX, bool BX, class TO> int launch_bf16(const GemmKind &
 {
     if constexpr (sizeof(TB) == 2)
         if (k.tile == 256) return launch_large<AX, BX, TO>(a, s);
+    if (k.tile == 64) return k.dma ? launch_small<TB, AX, BX, true, TO>(a, s) : launch_small<TB, AX, BX, false, TO>(a, s);
     return k.dma ? launch<TB, AX, BX, true, TO>(a, s) : launch<TB, AX, BX, false, TO>(a, s);
 }
 
