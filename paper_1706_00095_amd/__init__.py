@@ -486,9 +486,10 @@ def cg_attn_bwd(d, d_o, q, k, v, cu_q, cu_k, bias, o, o_rest, lse, dq, dk, dv, d
 
 def embedding_desc(table, y, scale=1.0):
     """Descriptor for a table [vocab][cols] and rows y [tokens][cols]; each in fp32 or bf16."""
-    if table.dim() != 2 or y.dim() != 2 or table.shape[1] != y.shape[1]:
+    t, n = table.shape, y.shape
+    if len(t) != 2 or len(n) != 2 or t[1] != n[1]:
         raise ValueError("expected a table [vocab][cols] and y [tokens][cols]")
-    return cg_embedding_desc(_type_of(table), _type_of(y), table.shape[0], table.shape[1], y.shape[0], scale)
+    return cg_embedding_desc(_type_of(table), _type_of(y), t[0], t[1], n[0], scale)
 
 
 def _tokens(t, n):
@@ -570,11 +571,12 @@ def cg_unpack8(p, y, stream=None):
 
 def linear_desc(x, w, act="none", act_in="none"):
     """Descriptor of a linear layer on x [M][K] with the weights w [N][K]; act, act_in: "none", "relu", "gelu" or "silu"."""
-    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
+    m, n = x.shape, w.shape
+    if len(m) != 2 or len(n) != 2 or m[1] != n[1]:
         raise ValueError("expected x [tokens][inputs] and w [outputs][inputs]")
     if x.dtype is not w.dtype:
         raise TypeError("x and w have to be of one type")
-    return cg_linear_desc(_type_of(x), x.shape[0], w.shape[0], x.shape[1], ACTS[act], ACTS[act_in])
+    return cg_linear_desc(_type_of(x), m[0], n[0], m[1], ACTS[act], ACTS[act_in])
 
 
 def cg_linear_workspace_bytes(d, which):

@@ -420,36 +420,58 @@ template <class T, int LANES, bool WIDE> __global__ __launch_bounds__(256) void 
     }
     if (now != none) store(behind == now);
 }
-// The runs that end in another chunk than they began in: what they left, added in order.
-template <int LANES, bool WIDE> __global__ __launch_bounds__(256) void join_runs_kernel(GradArgs a, int per_chunk, int64_t groups)
+// The runs that end in another chunk than they began in: what they left, added in order.  A block looks at a chunk's last run.  Its groups of lanes take
+// 16 of the chunks behind it each, the next block's worth after those, and their sums meet in LDS: bound by latency, which a frequent token's hundreds
+// of chunks would take one after the other (9663 places of 9 tokens, 8 columns: 44 us lookup and gradient with one group a run, XX so).
+template <int LANES, bool WIDE> __global__ __launch_bounds__(256) void join_runs_kernel(GradArgs a, int per_chunk)
 {
-    constexpr int AHEAD = 16;
-    const Group<LANES> g(a, per_chunk, groups);
-    if (!g.some || g.to >= a.n || g.c >= a.cols) return;
-    const uint32_t now = a.key[g.to - 1];
-    if (a.key[g.to] != now || now >= (uint32_t)a.vocab || (g.from > 0 && a.key[g.from - 1] == now)) return;
-    const Columns at(g.c, a.cols);
+    constexpr int AHEAD = 16, GROUPS = 256 / LANES;
+    __shared__ __align__(16) float lds[GROUPS][8 * LANES];
+    const int chunk = (int)blockIdx.x / per_chunk, from = chunk << a.chunk_shift, to = from + (1 << a.chunk_shift);
+    if (to >= a.n) return;
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     const int chunks = (int)(((int64_t)a.n + (1 << a.chunk_shift) - 1) >> a.chunk_shift);
-    float v[8];
-    const Raw8<float> first = load8(a.tail + (int64_t)g.chunk * a.cols + at.c, WIDE ? 8 : at.n);
+    auto key_at = [&](int q) { return q < chunks ? a.key[q << a.chunk_shift] : (uint32_t)a.vocab; };
+    // keys are asked for ahead of their use: of the next chunk, of this group's chunks, of the next round's
+    const uint32_t now = a.key[to - 1], behind = a.key[to], before = from > 0 ? a.key[from - 1] : (uint32_t)a.vocab;
+    uint32_t own = key_at(chunk + 1 + group * AHEAD), next = key_at(chunk + 1 + GROUPS * AHEAD);
+    if (behind != now || now >= (uint32_t)a.vocab || before == now) return;
+    const int c = ((int)blockIdx.x - chunk * per_chunk) * 8 * LANES + 8 * lane;
+    const Columns at(c < a.cols ? c : 0, a.cols);
+    float v[8] = {};
+    if (group == 0) {
+        const Raw8<float> first = load8(a.tail + (int64_t)chunk * a.cols + at.c, WIDE ? 8 : at.n);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = elem(first, j);
+        for (int j = 0; j < 8; ++j) v[j] = elem(first, j);
+    }
     bool more = true;
-    for (int q = g.chunk + 1; more; q += AHEAD) {
+    for (int q0 = chunk + 1; more; q0 += GROUPS * AHEAD) {
+        const int q = q0 + group * AHEAD;
+        const bool some = own == now;          // keys ascend: it is the run that chunk q begins with
+        more = next == now;
+        own = key_at(q + GROUPS * AHEAD), next = key_at(q0 + 2 * GROUPS * AHEAD);
+        if (!some) continue;
         bool mine[AHEAD];
         Raw8<float> x[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int r = min(q + u, chunks - 1);
-            mine[u] = q + u < chunks && a.key[r << a.chunk_shift] == now;      // keys ascend: it is the run that the chunk begins with
+            mine[u] = key_at(q + u) == now;
             x[u] = load8(a.head + (int64_t)r * a.cols + at.c, WIDE ? 8 : at.n);      // of other chunks: anything
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += mine[u] ? elem(x[u], j) : 0.f;
-        more = mine[AHEAD - 1];
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lds[group][8 * lane + j] = v[j];
+    __syncthreads();
+    if (group > 0 || c >= a.cols) return;
+#pragma unroll 8
+    for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += lds[g][8 * lane + j];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= a.scale;
     store8(a.dtable + (int64_t)now * a.cols + at.c, to_raw<float>(v), at.n);
@@ -508,7 +530,7 @@ template <class T, int LANES, bool WIDE> void runs_launch(const GradArgs &a, hip
     const int64_t chunks = ((int64_t)a.n + (1 << a.chunk_shift) - 1) >> a.chunk_shift, groups = chunks * per;
     const dim3 grid((unsigned)((groups + 256 / LANES - 1) / (256 / LANES)));
     hipLaunchKernelGGL((runs_kernel<T, LANES, WIDE>), grid, dim3(256), 0, s, a, per, groups);
-    if (chunks > 1) hipLaunchKernelGGL((join_runs_kernel<LANES, WIDE>), grid, dim3(256), 0, s, a, per, groups);
+    if (chunks > 1) hipLaunchKernelGGL((join_runs_kernel<LANES, WIDE>), dim3((unsigned)groups), dim3(256), 0, s, a, per);
 }
 template <class T> int grad_typed(const GradArgs &a, hipStream_t s)
 {
