@@ -60,7 +60,7 @@ template <class TT, class T, int AHEAD> __global__ __launch_bounds__(256) void l
 // those the wave has had before (counted in LDS).  Places without a token have the key `vocab` and come last.
 // A digit has up to 10 bits where a pass is one launch (a table of a million rows takes two passes), up to 8 beyond.  Six at least, so that a block's
 // threads share out the waves' counts of all digits in whole lines.
-constexpr int kDigits = 256, kMostDigits = 1024, kLeastBits = 6;
+constexpr int kDigits = 256, kMostDigits = 1 << 10, kLeastBits = 6;
 constexpr int kOneBlock = 1024, kOneItems = 4, kMostOne = kOneBlock * kOneItems;      // threads, places of a lane, of the block
 constexpr int kMostPass = 1 << 16;          // places up to which a pass is one launch
 constexpr int kTileBlock = 256, kItems = 16, kTile = kTileBlock * kItems;             // beyond: threads, places of a lane, of a block
@@ -92,6 +92,20 @@ template <int ITEMS> __device__ __forceinline__ void number_items(const uint32_t
             rank[j] = before + (uint32_t)__popcll(same & below);
         }
     }
+}
+// Counts of digits with an LDS atomic a place (whole numbers: in any order): in kMostDigits >> bits copies by lane, because places that share a digit wait
+// for each other, and few tokens or a frequent one make many of them (60000 places of 2 tokens, 16 columns: 36 us the gradient, 60 in one copy).
+__device__ __forceinline__ void count_digit(uint32_t *counts, uint32_t digit, int bits)
+{
+    const int copies = kMostDigits >> bits;
+    atomicAdd(&counts[(digit << (10 - bits)) + (threadIdx.x & (copies - 1))], 1u);
+}
+__device__ __forceinline__ uint32_t counted(const uint32_t *counts, int digit, int bits)
+{
+    uint32_t n = 0;
+    if (digit < 1 << bits)
+        for (int i = 0; i < kMostDigits >> bits; ++i) n += counts[(digit << (10 - bits)) + i];
+    return n;
 }
 // Exclusive sums over a block's threads; `lds`: one word a wave, free for use.
 template <int THREADS> __device__ __forceinline__ uint32_t block_before(uint32_t x, uint32_t *lds)
@@ -230,13 +244,13 @@ __global__ __launch_bounds__(kOneBlock) void sort_pass_kernel(SortArgs a)
 #pragma unroll
         for (int u = 0; u < 16; ++u) {
             const int j = j0 + u * kOneBlock;
-            if (j < all) atomicAdd(&(j < own ? ahead : rest)[k[u] >> a.shift & mask], 1u);       // whole numbers: in any order
+            if (j < all) count_digit(j < own ? ahead : rest, k[u] >> a.shift & mask, a.bits);
         }
     }
     number_items(key, 1, a.shift, a.bits, mine, rank);
     __syncthreads();
-    const uint32_t before = block_before<kOneBlock>(ahead[threadIdx.x] + rest[threadIdx.x], sums);
-    rest[threadIdx.x] = before + ahead[threadIdx.x];
+    const uint32_t earlier = counted(ahead, threadIdx.x, a.bits), before = block_before<kOneBlock>(earlier + counted(rest, threadIdx.x, a.bits), sums);
+    rest[threadIdx.x] = before + earlier;
     __syncthreads();
     places_of_waves(counts, a.bits, rest, sums);
     __syncthreads();
@@ -259,15 +273,16 @@ __device__ __forceinline__ void load_items(const SortArgs &a, uint32_t (&key)[kI
 __global__ __launch_bounds__(kTileBlock) void sort_count_kernel(SortArgs a)
 {
     if (fills(a.fill)) return;
-    __shared__ uint32_t counts[kDigits];
-    counts[threadIdx.x] = 0;
+    __shared__ uint32_t counts[kMostDigits];
+#pragma unroll
+    for (int j = 0; j < kMostDigits / kTileBlock; ++j) counts[threadIdx.x + j * kTileBlock] = 0;
     __syncthreads();
     uint32_t key[kItems], place[kItems];
     load_items(a, key, place);
 #pragma unroll
-    for (int j = 0; j < kItems; ++j) atomicAdd(&counts[key[j] >> a.shift & ((1u << a.bits) - 1)], 1u);       // whole numbers: in any order
+    for (int j = 0; j < kItems; ++j) count_digit(counts, key[j] >> a.shift & ((1u << a.bits) - 1), a.bits);
     __syncthreads();
-    a.counts[threadIdx.x * a.tiles + blockIdx.x] = counts[threadIdx.x];
+    a.counts[threadIdx.x * a.tiles + blockIdx.x] = counted(counts, threadIdx.x, a.bits);
 }
 __global__ __launch_bounds__(1024) void sort_sums_kernel(uint32_t *counts, int n)
 {
@@ -422,7 +437,7 @@ template <class T, int LANES, bool WIDE> __global__ __launch_bounds__(256) void 
 }
 // The runs that end in another chunk than they began in: what they left, added in order.  A block looks at a chunk's last run.  Its groups of lanes take
 // 16 of the chunks behind it each, the next block's worth after those, and their sums meet in LDS: bound by latency, which a frequent token's hundreds
-// of chunks would take one after the other (9663 places of 9 tokens, 8 columns: 44 us lookup and gradient with one group a run, XX so).
+// of chunks would take one after the other (9663 places of 9 tokens, 8 columns: 70 us the gradient with one group a run, 23 so).
 template <int LANES, bool WIDE> __global__ __launch_bounds__(256) void join_runs_kernel(GradArgs a, int per_chunk)
 {
     constexpr int AHEAD = 16, GROUPS = 256 / LANES;
