@@ -1,5 +1,5 @@
-// What the kernels that multiply tiles out of LDS on v_mfma_f32_32x32x16_bf16 share (attn_*.hip, linear_*.hip): operands in one bf16
-// number or three, accumulators, loads from memory into LDS.
+// What the kernels that multiply tiles out of LDS share (attn_*.hip, linear*.hip): operands in one bf16 number or three, accumulators of
+// v_mfma_f32_32x32x16_bf16 (attention), loads from memory into LDS.
 #pragma once
 #include "igemm_device.h"
 #include "typed_device.h"
