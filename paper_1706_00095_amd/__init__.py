@@ -537,19 +537,36 @@ class Packed8:
             raise ValueError(f"scales: expected the shape {(rows, (cols + 31) // 32)}, got {tuple(scales.shape)}")
         if (codes.stride(1) != 1 and cols > 1) or (scales.stride(1) != 1 and cols > 32):
             raise ValueError("the elements of a row have to lie next to each other")
-        self.codes, self.scales, self.shape = codes, scales, codes.shape
+        self._codes, self._scales, self.shape = codes, scales, codes.shape
         self.arg = cg_packed8(codes.data_ptr(), codes.stride(0) if rows > 1 else cols, scales.data_ptr(), scales.stride(0) if rows > 1 else (cols + 31) // 32)
 
 
+    @property
+    def codes(self):
+        if self._codes is None:
+            rows, cols = self.shape
+            self._codes = self._room[:rows * cols].view(rows, cols)
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            rows, blocks = self.shape[0], self.arg.scales_ld
+            self._scales = self._room[self._room.numel() - rows * blocks:].view(torch.uint8).view(rows, blocks)
+        return self._scales
+
+
 def packed8_like(x):
-    """Room for x [rows][cols] in 8 bits, on its device."""
+    """Room for x [rows][cols] in 8 bits, on its device: one allocation, which the codes and scales are views of."""
     if not x.is_cuda:
         raise TypeError("expected a device tensor")
-    rows, cols = x.shape
-    blocks, device = (cols + 31) // 32, x.device
+    rows, cols = shape = x.shape
+    blocks, at = (cols + 31) // 32, (rows * cols + 15) & ~15
     p = Packed8.__new__(Packed8)          # nothing to check
-    p.codes, p.scales, p.shape = torch.empty(rows, cols, dtype=torch.int8, device=device), torch.empty(rows, blocks, dtype=torch.uint8, device=device), x.shape
-    p.arg = cg_packed8(p.codes.data_ptr(), cols, p.scales.data_ptr(), blocks)
+    p._room = room = x.new_empty(at + rows * blocks, dtype=torch.int8)
+    p._codes, p._scales, p.shape = None, None, shape
+    start = room.data_ptr()
+    p.arg = cg_packed8(start, cols, start + at, blocks)
     return p
 
 

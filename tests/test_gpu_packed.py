@@ -113,6 +113,21 @@ def test_far_rows():
     assert torch.equal(x.double().cpu(), kept)
 
 
+def test_room():
+    """packed8_like: codes and scales are the rows that are written, whatever the sizes."""
+    cg = _cg()
+    for rows, cols in ((1, 1), (3, 33), (17, 100)):
+        x = bu.normal((rows, cols), torch.float32, rows)
+        p = cg.packed8_like(x.float().cuda())
+        cg.cg_pack8(x.float().cuda(), p)
+        codes, scales, _ = bu.packed(x)
+        assert torch.equal(p.codes.cpu(), codes) and torch.equal(p.scales.cpu(), scales)
+        again = cg.Packed8(p.codes, p.scales)
+        y = torch.empty(rows, cols, device="cuda")
+        cg.cg_unpack8(again, y)
+        assert torch.equal(y.double().cpu(), bu.packed(x)[2])
+
+
 def test_nothing():
     cg = _cg()
     for shape in ((0, 40), (3, 0)):
