@@ -364,21 +364,23 @@ __device__ __forceinline__ void store_bias(const GemmArgs &a, int split, int row
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }       // lets loads go on
 // The sums of the waves that have the same part of a tile in two halves of k meet in the first half's: through `mine`, the part's own.  false: nothing
 // is left for this wave to do.
-template <bool CUT> __device__ __forceinline__ bool join_halves(const GemmArgs &a, int split, int half, LdsByte *mine, int row, int lane, Sums<CUT, 2, 2> &acc, const float (&bias)[2], bool with_bias)
+template <int T> constexpr int kJoin = 64 * (T * T * 16 + T * 4);       // bytes of T x T tiles of 16 x 16, and of the bias
+template <bool CUT, int T>
+__device__ __forceinline__ bool join_halves(const GemmArgs &a, int split, int half, LdsByte *mine, int row, int lane, Sums<CUT, T, T> &acc, const float (&bias)[T], bool with_bias)
 {
     if (half == 1) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) CG_LDS(u32x4, mine + (64 * t + lane) * 16) = acc.get(t >> 1, t & 1);
+        for (int t = 0; t < T * T; ++t) CG_LDS(u32x4, mine + (64 * t + lane) * 16) = acc.get(t / T, t % T);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) CG_LDS(float, mine + 4096 + (64 * t + lane) * 4) = bias[t];
+        for (int t = 0; t < T; ++t) CG_LDS(float, mine + T * T * 1024 + (64 * t + lane) * 4) = bias[t];
     }
     lds_barrier();
     if (half == 1) return false;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) acc.of_join(t >> 1, t & 1) += __builtin_bit_cast(v4f, CG_LDS(u32x4, mine + (64 * t + lane) * 16));
+    for (int t = 0; t < T * T; ++t) acc.of_join(t / T, t % T) += __builtin_bit_cast(v4f, CG_LDS(u32x4, mine + (64 * t + lane) * 16));
     if (with_bias)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) store_bias(a, split, row + 16 * t, lane, bias[t] + CG_LDS(float, mine + 4096 + (64 * t + lane) * 4));
+        for (int t = 0; t < T; ++t) store_bias(a, split, row + 16 * t, lane, bias[t] + CG_LDS(float, mine + T * T * 1024 + (64 * t + lane) * 4));
     __builtin_amdgcn_wave_barrier();
     return true;
 }
@@ -460,18 +462,19 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> int launch(const GemmA
     return CG_OK;
 }
 
-// Small bf16 products: tiles of 64 x 64, four waves and two steps in LDS for either half of a block's values of k, whose sums meet in LDS.  Bound by the
-// latency of a step's loads (two steps, one of either half, 0.6 us where a compute unit has one block, 0.38 where it has several; the matrix
-// instructions of both take 0.12).
-template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bounds__(512, 4) void gemm_small_kernel(GemmArgs a)
+// The same with four waves and two steps in LDS for either half of a block's values of k, whose sums meet in LDS: small products, which the latency of a
+// step's loads bounds, in tiles of 64 x 64 (two steps, one of either half, 0.6 us where a compute unit has one block, 0.38 where it has several; the
+// matrix instructions of both take 0.12), and those that have a tile of 128 x 128 for each compute unit at most (1.2 us, of which LDS, written and read,
+// takes 0.7 and the matrix instructions 0.46).
+template <class TB, bool AX, bool BX, bool DMA, class TO, int XT> __global__ __launch_bounds__(512, XT == 64 ? 4 : 2) void gemm_halves_kernel(GemmArgs a)
 {
-    constexpr int STEP = 64, XT = 64;
+    constexpr int STEP = 64, T = XT / 32;
     using LA = TileLoader<bf16raw, AX, XT, STEP, 256, DMA>;
     using LB = TileLoader<TB, BX, XT, STEP, 256, DMA && sizeof(TB) == 2>;
-    constexpr int STAGE = LA::Lds::BYTES + LB::Lds::BYTES, MINE = 32 * kEpiRow<1>;
+    constexpr int STAGE = LA::Lds::BYTES + LB::Lds::BYTES, MINE = kJoin<T> > 32 * kEpiRow<T / 2> ? kJoin<T> : 32 * kEpiRow<T / 2>;
     __shared__ __align__(16) char smem[4 * STAGE];
-    static_assert(4 * MINE <= 4 * STAGE && MINE >= 64 * (4 * 16 + 2 * 4), "room for the epilogue, and for the sums of a wave");
-    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave >> 2, wr = (wave >> 1 & 1) * 32, wc = (wave & 1) * 32;
+    static_assert(MINE <= STAGE, "room for the epilogue, and for the sums of a wave");
+    const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave >> 2, wr = (wave >> 1 & 1) * XT / 2, wc = (wave & 1) * XT / 2;
     LdsByte *const lds = (LdsByte *)smem + half * 2 * STAGE, *const mine = (LdsByte *)smem + (wave & 3) * MINE;
     int tr, tc, split;
     place_of(a, tr, tc, split);
@@ -480,10 +483,10 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bo
 
     LA la(a.A, Packed{}, a.a_ld, r0, a.R, kbeg, kend, a.K);
     LB lb(a.B, a.B8, a.b_ld, c0, a.C, kbeg, kend, a.K);
-    Sums<false, 2, 2> acc;
+    Sums<false, T, T> acc;
     acc.zero();
     const bool with_bias = AX && a.dbias && tc == 0 && wc == 0;
-    float bias[2] = {};
+    float bias[T] = {};
     auto start = [&](int k, LdsByte *at) {
         if (la.inside(k) && lb.inside(k)) {
             la.template start<true>(k, at);
@@ -509,16 +512,16 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bo
         if (k < kend) {
 #pragma unroll
             for (int ks = 0; ks < STEP / 32; ++ks) {
-                u32x4 fa[2], fb[2];
+                u32x4 fa[T], fb[T];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) fb[t] = LB::Lds::read(at + LA::Lds::BYTES, wc + 16 * t, ks, lane);
+                for (int t = 0; t < T; ++t) fb[t] = LB::Lds::read(at + LA::Lds::BYTES, wc + 16 * t, ks, lane);
 #pragma unroll
-                for (int t = 0; t < 2; ++t) fa[t] = LA::Lds::read(at, wr + 16 * t, ks, lane);
+                for (int t = 0; t < T; ++t) fa[t] = LA::Lds::read(at, wr + 16 * t, ks, lane);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) acc.mma(fa, fb[j], j, true);
+                for (int j = 0; j < T; ++j) acc.mma(fa, fb[j], j, true);
                 if (with_bias)
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
+                    for (int t = 0; t < T; ++t) {
                         const u32x4 f[1] = {fa[t]};
                         bias[t] += sum_of<1>(f);
                     }
@@ -527,11 +530,11 @@ template <class TB, bool AX, bool BX, bool DMA, class TO> __global__ __launch_bo
         if (more) finish(next);
     }
     __syncthreads();
-    if (join_halves(a, split, half, mine, r0 + wr, lane, acc, bias, with_bias)) store_wave<TO, 1, 1>(a, split, mine, r0 + wr, c0 + wc, lane, acc);
+    if (join_halves(a, split, half, mine, r0 + wr, lane, acc, bias, with_bias)) store_wave<TO, T / 2, T / 2>(a, split, mine, r0 + wr, c0 + wc, lane, acc);
 }
-template <class TB, bool AX, bool BX, bool DMA, class TO> int launch_small(const GemmArgs &a, hipStream_t s)
+template <class TB, bool AX, bool BX, bool DMA, class TO, int XT> int launch_halves(const GemmArgs &a, hipStream_t s)
 {
-    hipLaunchKernelGGL((gemm_small_kernel<TB, AX, BX, DMA, TO>), dim3((unsigned)(a.tiles_r * a.tiles_c * a.splits)), dim3(512), 0, s, a);
+    hipLaunchKernelGGL((gemm_halves_kernel<TB, AX, BX, DMA, TO, XT>), dim3((unsigned)(a.tiles_r * a.tiles_c * a.splits)), dim3(512), 0, s, a);
     CG_HIP_TRY(hipGetLastError());
     return CG_OK;
 }
@@ -614,7 +617,7 @@ template <class TB, bool AX, bool BX> __global__ __launch_bounds__(512, 4) void 
     using LB = TileLoader<TB, BX, XT, STEP, 256, false>;
     constexpr int NB = LB::NP, TILES = LA::Lds::BYTES + LB::Lds::BYTES, MINE = 32 * kEpiRow<1>;
     __shared__ __align__(16) char smem[2 * TILES];
-    static_assert(4 * MINE <= 2 * TILES && MINE >= 64 * (4 * 16 + 2 * 4), "room for the epilogue, and for the sums of a wave");
+    static_assert(4 * MINE <= 2 * TILES && MINE >= kJoin<2>, "room for the epilogue, and for the sums of a wave");
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave >> 2, wr = (wave >> 1 & 1) * 32, wc = (wave & 1) * 32;
     LdsByte *const lds = (LdsByte *)smem + half * TILES, *const mine = (LdsByte *)smem + (wave & 3) * MINE;
     int tr, tc, split;
@@ -860,7 +863,9 @@ template <class TB, bool AX, bool BX, class TO> int launch_bf16(const GemmKind &
 {
     if constexpr (sizeof(TB) == 2)
         if (k.tile == 256) return launch_large<AX, BX, TO>(a, s);
-    if (k.tile == 64) return k.dma ? launch_small<TB, AX, BX, true, TO>(a, s) : launch_small<TB, AX, BX, false, TO>(a, s);
+    if (k.tile == 64) return k.dma ? launch_halves<TB, AX, BX, true, TO, 64>(a, s) : launch_halves<TB, AX, BX, false, TO, 64>(a, s);
+    // one block a compute unit: 2048^3 26 us (28 by four waves a block), 1024 x 4096 x 4096 42 (46)
+    if (a.tiles_r * a.tiles_c * a.splits <= 256) return k.dma ? launch_halves<TB, AX, BX, true, TO, 128>(a, s) : launch_halves<TB, AX, BX, false, TO, 128>(a, s);
     return k.dma ? launch<TB, AX, BX, true, TO>(a, s) : launch<TB, AX, BX, false, TO>(a, s);
 }
 

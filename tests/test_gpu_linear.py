@@ -109,7 +109,7 @@ def test_packed(dtype, M, K, N, pad, act_in):
 @pytest.mark.parametrize("dtype,M,K,N,pad,pack", [
     ("fp32", 2040, 250, 2044, 1, False), ("fp32", 2040, 2044, 250, 0, False), ("fp32", 250, 2044, 2040, 0, True), ("fp32", 256, 9216, 4096, 0, False),
     ("bf16", 2048, 2048, 2048, 0, False), ("bf16", 2048, 2048, 2048, 0, True), ("bf16", 2045, 2047, 2041, 3, False), ("bf16", 2045, 2047, 2041, 3, True),
-    ("bf16", 128, 8192, 6144, 0, False)])
+    ("bf16", 128, 8192, 6144, 0, False), ("bf16", 2100, 2111, 2077, 3, False), ("bf16", 2100, 2111, 2077, 0, True), ("bf16", 2104, 2112, 2080, 0, True)])
 def test_tiles_of_128(dtype, M, K, N, pad, pack):
     """Products for which tiles of 128 are taken, whole or with a k that is cut."""
     check(Layer(dtype, M, K, N, "gelu", "silu", True, True, pad, seed=11), pack)
