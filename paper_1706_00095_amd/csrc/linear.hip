@@ -8,7 +8,9 @@ namespace {
 
 // ---- few tokens -------------------------------------------------------------------------------------------------------------
 // Forward for up to 16 MT tokens: the weights are read once and that is all there is to do.  A block takes 16 rows of w, its eight waves every
-// eighth step along k; a step is a lane's 16 bytes of one row (4 lanes a row), AHEAD of them in flight.  w is the matrix instruction's first operand, the
+// eighth step along k; a step is a lane's 16 bytes of one row (4 lanes a row), AHEAD to 2 AHEAD of
+// them in flight (one token, 4096 -> 16384, weights out of HBM: 24.5 us, 5.5 TB/s; 26 with twice as many that all land before the next are asked
+// for, 28 with twice as many so).  w is the matrix instruction's first operand, the
 // tokens are the second; bf16: 16x16x32, fp32: 16x16x4 on the values as they are.  The waves' sums meet in LDS.
 constexpr int kFewWaves = 8, kFewRows = 16;
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -57,7 +59,7 @@ template <> struct FewStep<float> {
 template <class T, int MT> __global__ __launch_bounds__(64 * kFewWaves) void few_tokens_kernel(FewArgs a)
 {
     using S = FewStep<T>;
-    constexpr int STEP = 4 * S::PER, AHEAD = MT == 1 ? 8 : 4;
+    constexpr int STEP = 4 * S::PER, AHEAD = MT == 1 ? 4 : 2;
     __shared__ __align__(16) float sums[kFewWaves][MT * 16][kFewRows + 4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = lane & 15, k0 = (lane >> 4) * S::PER;
     const int n0 = blockIdx.x * kFewRows, row = n0 + at;
@@ -68,20 +70,33 @@ template <class T, int MT> __global__ __launch_bounds__(64 * kFewWaves) void few
     v4f acc[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[t] = v4f{};
-    // rows and tokens that are none read the first one's values, and their sums go nowhere
-    for (int s0 = wave * AHEAD * STEP; s0 < a.K; s0 += kFewWaves * AHEAD * STEP) {
-        u32x4 vw[AHEAD], vx[MT][AHEAD];
+    // rows and tokens that are none read the first one's values, and their sums go nowhere; the next AHEAD steps are asked for before these are multiplied
+    u32x4 vw[2][AHEAD], vx[2][MT][AHEAD];
+    auto ask = [&](int s0, auto half) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int k = s0 + u * STEP + k0;
-            vw[u] = S::load(w + k, a.K - k);
+            vw[half.value][u] = S::load(w + k, a.K - k);
 #pragma unroll
-            for (int t = 0; t < MT; ++t) vx[t][u] = S::load(x[t] + k, a.K - k);
+            for (int t = 0; t < MT; ++t) vx[half.value][t][u] = S::load(x[t] + k, a.K - k);
         }
+    };
+    auto multiply = [&](auto half) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-            for (int t = 0; t < MT; ++t) acc[t] = S::mma(vw[u], vx[t][u], acc[t]);
+            for (int t = 0; t < MT; ++t) acc[t] = S::mma(vw[half.value][u], vx[half.value][t][u], acc[t]);
+    };
+    constexpr int ALL = kFewWaves * AHEAD * STEP;
+    const std::integral_constant<int, 0> _0;
+    const std::integral_constant<int, 1> _1;
+    const int first = wave * AHEAD * STEP;
+    if (first < a.K) ask(first, _0);
+    for (int s0 = first; s0 < a.K; s0 += 2 * ALL) {
+        if (s0 + ALL < a.K) ask(s0 + ALL, _1);
+        multiply(_0);
+        if (s0 + 2 * ALL < a.K) ask(s0 + 2 * ALL, _0);
+        if (s0 + ALL < a.K) multiply(_1);
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) *reinterpret_cast<v4f *>(&sums[wave][16 * t + at][4 * (lane >> 4)]) = acc[t];
