@@ -102,6 +102,12 @@ int cg_debug_stream(void *dst, const void *src, const void *src2, size_t bytes, 
  * device pointer; the values mean nothing).  blocks in 1..65536, iters >= 1. */
 int cg_debug_mfma_loop(float *out, int blocks, int iters, void *stream);
 
+/* Test hook (host only, launches nothing): which kernels a pass of a linear layer takes.  tile: 16 (up to 32 tokens, forward), 64, 128 or 256
+ * rows and columns; parts: of k, joined by a launch of their own where there are several; halves: 1 where the waves of a block have
+ * half of k each, too.  whole: rows of bf16 tensors are whole 16 bytes at 16-byte addresses, not more than 2^21 elements apart;
+ * packed: backward-weight with x in 8 bits. */
+int cg_debug_linear_plan(const cg_linear_desc *d, int pass, int whole, int packed, int *tile, int *parts, int *halves);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,7 @@ EXPORTS = [
     "cg_conv_out_shape", "cg_conv_workspace_bytes", "cg_conv_fwd", "cg_conv_bwd_data", "cg_conv_bwd_weight", "cg_conv_bwd_weight_noalloc",
     "cg_conv_fwd_math", "cg_conv_bwd_data_math", "cg_conv_bwd_weight_math",
     "cg_grad_reduce_sgd", "cg_grad_reduce_sgd_multi", "cg_grad_reduce_sgd_tree", "cg_grad_reduce_sgd_tree_multi", "cg_net_create", "cg_net_destroy", "cg_net_param_count", "cg_net_layer_fused", "cg_net_bind",
-    "cg_net_workspace_bytes", "cg_train_step", "cg_net_tensor", "cg_net_tensor_image_stride", "cg_strerror", "cg_version", "cg_last_hip_error", "cg_debug_conv_operand", "cg_debug_copy", "cg_debug_stream", "cg_debug_mfma_loop", "cg_debug_launch_count", "cg_debug_fuse_lrn_pool", "cg_debug_patch_min_tiles", "cg_debug_resident_blocks", "cg_debug_band_kernel", "cg_debug_direct_kernel",
+    "cg_net_workspace_bytes", "cg_train_step", "cg_net_tensor", "cg_net_tensor_image_stride", "cg_strerror", "cg_version", "cg_last_hip_error", "cg_debug_conv_operand", "cg_debug_copy", "cg_debug_stream", "cg_debug_mfma_loop", "cg_debug_launch_count", "cg_debug_fuse_lrn_pool", "cg_debug_patch_min_tiles", "cg_debug_resident_blocks", "cg_debug_band_kernel", "cg_debug_direct_kernel", "cg_debug_linear_plan",
     "cg_profile_enable", "cg_profile_count", "cg_profile_get",
     "cg_dropout_fwd", "cg_dropout_bwd", "cg_layernorm_fwd", "cg_layernorm_workspace_bytes", "cg_layernorm_bwd",
     "cg_dropout_add_layernorm_fwd", "cg_dropout_add_layernorm_bwd",
@@ -170,6 +170,7 @@ def lib():
         L.cg_linear_fwd.argtypes = [lp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, sz, vp]
         L.cg_linear_bwd_data.argtypes = [lp, vp, i64, vp, i64, vp, i64, pp, vp, i64, vp, i64, vp, sz, vp]
         L.cg_linear_bwd_weight.argtypes = [lp, vp, i64, vp, i64, pp, vp, vp, vp, sz, vp]
+        L.cg_debug_linear_plan.argtypes = [lp, C.c_int, C.c_int, C.c_int, ip, ip, ip]
         L.cg_act_bwd.argtypes = [C.c_int, C.c_int, i64, i64, vp, i64, vp, i64, pp, vp, i64, vp]
         L.cg_strerror.argtypes = [C.c_int]
         L.cg_strerror.restype = C.c_char_p
@@ -647,6 +648,13 @@ def cg_debug_resident_blocks(blocks):
 
 def cg_debug_direct_kernel(on):
     _check(lib().cg_debug_direct_kernel(int(bool(on))), "cg_debug_direct_kernel")
+
+
+def cg_debug_linear_plan(d, which_pass, whole=True, packed=False):
+    """(tile, parts of k, whether the waves of a block have half of k each) of a pass of a linear layer."""
+    tile, parts, halves = C.c_int(), C.c_int(), C.c_int()
+    _check(lib().cg_debug_linear_plan(d, which_pass, int(whole), int(packed), C.byref(tile), C.byref(parts), C.byref(halves)), "cg_debug_linear_plan")
+    return tile.value, parts.value, bool(halves.value)
 
 
 def cg_debug_band_kernel(on):

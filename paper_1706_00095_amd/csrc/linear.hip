@@ -305,13 +305,19 @@ int ws_check(void *ws, size_t ws_bytes, size_t need)
 }
 unsigned blocks_for(uint64_t n, unsigned most) { const uint64_t b = (n + 255) / 256; return (unsigned)(b < most ? b : most); }
 
-int product(const cg_linear_desc *d, int pass, const Plan &p, GemmArgs &a, bool packed, bool dma, void *ws, hipStream_t s)
+// What a product takes of its plan, with operands as they are: its tile; a: its tiles and the parts of k.
+int tile_of(const Plan &p, bool packed, bool dma, GemmArgs &a)
 {
     const bool large = p.large && dma && !packed;
     const int tile = large ? 256 : p.small ? 64 : 128;
     a.R = p.R, a.C = p.C, a.K = p.K;
     a.tiles_r = (p.R + tile - 1) / tile, a.tiles_c = (p.C + tile - 1) / tile;
     a.splits = large ? 1 : p.splits, a.chunk = large ? p.K : p.chunk;
+    return tile;
+}
+int product(const cg_linear_desc *d, int pass, const Plan &p, GemmArgs &a, bool packed, bool dma, void *ws, hipStream_t s)
+{
+    const int tile = tile_of(p, packed, dma, a);
     a.part = static_cast<float *>(ws);
     if (int rc = gemm_launch({d->type, pass, packed, tile, dma}, a, s)) return rc;
     if (a.splits == 1) return CG_OK;
@@ -382,6 +388,19 @@ extern "C" size_t cg_linear_workspace_bytes(const cg_linear_desc *d, int pass)
     if (p.large && slice_bytes(d) > need) need = slice_bytes(d);
     if (unpacks(d, p) && unpacked_bytes(d) > need) need = unpacked_bytes(d);
     return need;
+}
+
+extern "C" int cg_debug_linear_plan(const cg_linear_desc *d, int pass, int whole, int packed, int *tile, int *parts, int *halves)
+{
+    if (int rc = desc_check(d)) return rc;
+    if ((pass != CG_PASS_FWD && pass != CG_PASS_BWD_DATA && pass != CG_PASS_BWD_WEIGHT) || !tile || !parts || !halves) return CG_EINVAL;
+    const Plan p = plan_of(d, pass);
+    const bool dma = whole && d->type == CG_TYPE_BF16;
+    GemmArgs a{};
+    *tile = p.few ? 16 : tile_of(p, packed && !(dma && unpacks(d, p)), dma, a);
+    *parts = p.few ? 1 : a.splits;
+    *halves = !p.few && gemm_halves(d->type, *tile, (int64_t)a.tiles_r * a.tiles_c * a.splits);
+    return CG_OK;
 }
 
 extern "C" int cg_linear_fwd(const cg_linear_desc *d, const void *x, int64_t x_ld, const void *w, int64_t w_ld, const float *bias,

@@ -35,6 +35,9 @@ struct GemmArgs {
 // LDS without registers.
 struct GemmKind { int type, pass, packed, tile, dma; };
 int gemm_launch(const GemmKind &kind, const GemmArgs &a, hipStream_t s);
+// Whether either half of a block's waves has half of its values of k: tiles of 64, and bf16 tiles of 128 that are one block a compute unit (2048^3 26 us,
+// 28 by four waves a block; 1024 x 4096 x 4096 42 and 46).
+inline bool gemm_halves(int type, int tile, int64_t blocks) { return tile == 64 || (type == CG_TYPE_BF16 && tile == 128 && blocks <= 256); }
 constexpr int kGemmStep = 64;         // chunks of k are multiples of it
 
 namespace {

@@ -863,9 +863,10 @@ template <class TB, bool AX, bool BX, class TO> int launch_bf16(const GemmKind &
 {
     if constexpr (sizeof(TB) == 2)
         if (k.tile == 256) return launch_large<AX, BX, TO>(a, s);
-    if (k.tile == 64) return k.dma ? launch_halves<TB, AX, BX, true, TO, 64>(a, s) : launch_halves<TB, AX, BX, false, TO, 64>(a, s);
-    // one block a compute unit: 2048^3 26 us (28 by four waves a block), 1024 x 4096 x 4096 42 (46)
-    if (a.tiles_r * a.tiles_c * a.splits <= 256) return k.dma ? launch_halves<TB, AX, BX, true, TO, 128>(a, s) : launch_halves<TB, AX, BX, false, TO, 128>(a, s);
+    if (gemm_halves(k.type, k.tile, (int64_t)a.tiles_r * a.tiles_c * a.splits)) {
+        if (k.tile == 64) return k.dma ? launch_halves<TB, AX, BX, true, TO, 64>(a, s) : launch_halves<TB, AX, BX, false, TO, 64>(a, s);
+        return k.dma ? launch_halves<TB, AX, BX, true, TO, 128>(a, s) : launch_halves<TB, AX, BX, false, TO, 128>(a, s);
+    }
     return k.dma ? launch<TB, AX, BX, true, TO>(a, s) : launch<TB, AX, BX, false, TO>(a, s);
 }
 
