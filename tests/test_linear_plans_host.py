@@ -1,4 +1,7 @@
 """CPU-only: the kernels that linear layers take, as the GPU tests that are named for them expect."""
+import math
+import random
+
 import pytest
 
 import linear_plan_util as lp
@@ -31,3 +34,27 @@ def test_what_is_refused():
     assert L.cg_debug_linear_plan(None, 0, 1, 0, *refs) == cg.CG_EINVAL and L.cg_debug_linear_plan(d, 3, 1, 0, *refs) == cg.CG_EINVAL
     for i in range(3):
         assert L.cg_debug_linear_plan(d, 0, 1, 0, *[None if i == j else r for j, r in enumerate(refs)]) == cg.CG_EINVAL
+
+
+@pytest.mark.parametrize("dtype,which,whole,packed,tile,cut,M,K,N", lp.CASES)
+def test_every_product(dtype, which, whole, packed, tile, cut, M, K, N):
+    got, parts, _ = cg.cg_debug_linear_plan(desc(dtype, M, K, N), which, whole, packed)
+    assert (got, parts > 1) == (tile, cut)
+
+
+def test_no_kernel_without_a_case():
+    """Sizes by chance take no kernel that no case takes (up to 32 tokens forward and tiles of 256 apart, which have tests of their own)."""
+    def kind(dtype, which, whole, packed, M, K, N):
+        tile, parts, halves = cg.cg_debug_linear_plan(desc(dtype, M, K, N), which, whole, packed)
+        return dtype, which, whole, packed, tile, parts > 1, halves
+
+    have = {kind(*c[:4], *c[6:]) for c in lp.CASES}
+    rng = random.Random(1)
+    for _ in range(20000):
+        M, K, N, whole, dtype = *(int(round(math.exp(rng.uniform(0, math.log(16384))))) for _ in range(3)), rng.random() < 0.5, rng.choice(["fp32", "bf16"])
+        if whole:
+            K, N, dtype = (K + 7) // 8 * 8, (N + 7) // 8 * 8, "bf16"
+        for which in PASSES:
+            for packed in (False, True) if which == cg.CG_PASS_BWD_WEIGHT else (False,):
+                k = kind(dtype, which, whole, packed, M, K, N)
+                assert k[4] in (16, 256) or k in have, (k, M, K, N)
