@@ -428,7 +428,8 @@ int cg_embedding_fwd(const cg_embedding_desc *d, const int32_t *tokens, const vo
                      void *stream);
 size_t cg_embedding_workspace_bytes(const cg_embedding_desc *d);      /* of the backward pass; 0 for an invalid descriptor */
 /* dtable[v] = scale * sum over t with tokens[t] = v, in order of t, of dy[t]; [vocab][cols] fp32, every row written (zeros where
- * there is none).  ws: 16-byte aligned. */
+ * there is none).  Of a token with many places, stretches of neighbouring ones are summed first and their sums then added, in order too; how
+ * they are cut follows from the tokens and the sizes alone.  ws: 16-byte aligned. */
 int cg_embedding_bwd(const cg_embedding_desc *d, const int32_t *tokens, const void *dy, int64_t dy_ld, float *dtable, void *ws,
                      size_t ws_bytes, void *stream);
 

@@ -3,7 +3,7 @@
 // The gradient is dense (the update takes whole buckets): row v is the sum of dy over the places that hold v, zero where there are none.
 // Places are sorted by token, stably, so that each row's sum is taken in the order of the places and results are the same bits run to
 // run.  A token that is frequent has thousands of places: the sorted places are cut into chunks, a wave each, and what runs that cross a
-// border leave in their chunks is added by a second kernel.  The table's gradient is filled with zeros by blocks beside those that sort,
+// border leave in their chunks is added by a second kernel, stretches of chunks first and then these, all of them in order.  The table's gradient is filled with zeros by blocks beside those that sort,
 // and the rows of tokens that occur are written over.
 #include <algorithm>
 #include "cg_internal.h"
@@ -436,12 +436,13 @@ template <class T, int LANES, bool WIDE> __global__ __launch_bounds__(256) void 
     if (now != none) store(behind == now);
 }
 // The runs that end in another chunk than they began in: what they left, added in order.  A block looks at a chunk's last run.  Its groups of lanes take
-// 16 of the chunks behind it each, the next block's worth after those, and their sums meet in LDS: bound by latency, which a frequent token's hundreds
-// of chunks would take one after the other (9663 places of 9 tokens, 8 columns: 70 us the gradient with one group a run, 23 so).
+// 16 of the chunks behind it each, whose sums meet neighbour by neighbour, in a wave and then in LDS, and so on with the next block's worth: places stay
+// in order, and a sum of n chunks takes the roundings of n / (16 GROUPS) additions and some 25 more.  Bound by latency, which a frequent token's hundreds
+// of chunks would take one after the other (9663 places of 9 tokens, 8 columns: 70 us the gradient with one group a run, 18 so).
 template <int LANES, bool WIDE> __global__ __launch_bounds__(256) void join_runs_kernel(GradArgs a, int per_chunk)
 {
-    constexpr int AHEAD = 16, GROUPS = 256 / LANES;
-    __shared__ __align__(16) float lds[GROUPS][8 * LANES];
+    constexpr int AHEAD = 16, GROUPS = 256 / LANES, WAVES = 4;
+    __shared__ __align__(16) float lds[2][WAVES][8 * LANES];
     const int chunk = (int)blockIdx.x / per_chunk, from = chunk << a.chunk_shift, to = from + (1 << a.chunk_shift);
     if (to >= a.n) return;
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
@@ -453,43 +454,57 @@ template <int LANES, bool WIDE> __global__ __launch_bounds__(256) void join_runs
     if (behind != now || now >= (uint32_t)a.vocab || before == now) return;
     const int c = ((int)blockIdx.x - chunk * per_chunk) * 8 * LANES + 8 * lane;
     const Columns at(c < a.cols ? c : 0, a.cols);
-    float v[8] = {};
+    float v[8] = {}, sum[8] = {};              // of this group's chunks; of the rounds before (group 0)
     if (group == 0) {
         const Raw8<float> first = load8(a.tail + (int64_t)chunk * a.cols + at.c, WIDE ? 8 : at.n);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = elem(first, j);
     }
     bool more = true;
-    for (int q0 = chunk + 1; more; q0 += GROUPS * AHEAD) {
+    for (int q0 = chunk + 1, buf = 0; more; q0 += GROUPS * AHEAD, buf ^= 1) {
         const int q = q0 + group * AHEAD;
         const bool some = own == now;          // keys ascend: it is the run that chunk q begins with
         more = next == now;
         own = key_at(q + GROUPS * AHEAD), next = key_at(q0 + 2 * GROUPS * AHEAD);
-        if (!some) continue;
-        bool mine[AHEAD];
-        Raw8<float> x[AHEAD];
+        if (some) {
+            bool mine[AHEAD];
+            Raw8<float> x[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int r = min(q + u, chunks - 1);
-            mine[u] = key_at(q + u) == now;
-            x[u] = load8(a.head + (int64_t)r * a.cols + at.c, WIDE ? 8 : at.n);      // of other chunks: anything
+            for (int u = 0; u < AHEAD; ++u) {
+                const int r = min(q + u, chunks - 1);
+                mine[u] = key_at(q + u) == now;
+                x[u] = load8(a.head + (int64_t)r * a.cols + at.c, WIDE ? 8 : at.n);      // of other chunks: anything
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += mine[u] ? elem(x[u], j) : 0.f;
+        }
+        // a wave's groups, then the waves: group 0 adds these while the others read the next round, whose sums go to the other half, which is free,
+        // because a round's barrier is behind group 0's additions of the round before
+#pragma unroll
+        for (int d = LANES; d < 64; d *= 2)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += __shfl_down(v[j], d);
+        if ((threadIdx.x & 63) < LANES)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) lds[buf][threadIdx.x >> 6][8 * lane + j] = v[j];
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += lds[buf][w][8 * lane + j];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += v[j];
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += mine[u] ? elem(x[u], j) : 0.f;
+        for (int j = 0; j < 8; ++j) v[j] = 0.f;
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) lds[group][8 * lane + j] = v[j];
-    __syncthreads();
     if (group > 0 || c >= a.cols) return;
-#pragma unroll 8
-    for (int g = 1; g < GROUPS; ++g)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += lds[g][8 * lane + j];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= a.scale;
-    store8(a.dtable + (int64_t)now * a.cols + at.c, to_raw<float>(v), at.n);
+    for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
+    store8(a.dtable + (int64_t)now * a.cols + at.c, to_raw<float>(sum), at.n);
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------------------

@@ -166,3 +166,19 @@ def test_graph_and_stream(n):
         assert torch.equal(y, want[i][0]) and torch.equal(dtable, want[i][1])
         held.copy_(tokens[1 - i])
         both()
+
+
+@pytest.mark.parametrize("cols", [5, 24, 100, 300])
+@pytest.mark.parametrize("tokens", [40000, 65536, 300000])
+def test_frequent_token_in_order(cols, tokens):
+    """A token of many chunks: two large numbers early on that cancel each other are gone before the second half of its places is added, whole numbers
+    whose sum is exact."""
+    cg = _cg()
+    dy = torch.zeros(tokens, cols, device="cuda")
+    dy[90], dy[1500], dy[tokens // 2:] = 2.0 ** 30, -2.0 ** 30, 1.0
+    t, dtable = torch.full((tokens,), 3, dtype=torch.int32, device="cuda"), torch.empty(7, cols, device="cuda")
+    d = cg.embedding_desc(dtable, dy)
+    cg.cg_embedding_bwd(d, t, dy, dtable, _ws(d))
+    want = torch.zeros_like(dtable)
+    want[3] = tokens - tokens // 2
+    assert torch.equal(dtable, want)
