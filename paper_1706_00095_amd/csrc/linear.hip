@@ -287,9 +287,14 @@ int column_slices(int64_t M, int64_t N)
     int64_t s = want < most ? want : most;
     return (int)(s < 1 ? 1 : s > 256 ? 256 : s);
 }
+// As far as rows may lie apart where a lane's offsets have 32 bits: what is sent out of range (2^31) stays out of it for 128 rows of 2 bytes an element.
+constexpr int64_t kMostDmaLd = 1 << 21;
 // Backward-weight in large tiles multiplies bf16 numbers: x in 8 bits is unpacked first.  Eight rows of tiles would each turn it into bf16 on
 // its way into LDS otherwise (8192 tokens, 8192 x 2048 weights: 521 us in tiles of 256 through registers, 812 in tiles of 128; 36 and 208 so).
-bool unpacks(const cg_linear_desc *d, const Plan &p) { return p.large && d->K % 8 == 0 && d->M * ((d->K + kPackBlock - 1) / kPackBlock) <= (INT32_MAX >> 2) - 65535; }
+bool unpacks(const cg_linear_desc *d, const Plan &p)
+{
+    return p.large && d->K % 8 == 0 && d->K <= kMostDmaLd && d->M * ((d->K + kPackBlock - 1) / kPackBlock) <= (INT32_MAX >> 2) - 65535;
+}
 size_t unpacked_bytes(const cg_linear_desc *d) { return (size_t)d->M * (size_t)d->K * 2; }
 size_t slice_bytes(const cg_linear_desc *d)
 {
@@ -297,7 +302,7 @@ size_t slice_bytes(const cg_linear_desc *d)
     return s > 1 ? (size_t)s * (size_t)d->N * sizeof(float) : 0;
 }
 
-bool dma_ok(const void *p, int64_t ld, int64_t cols) { return aligned16(p) && ld % 8 == 0 && cols % 8 == 0 && ld <= 1 << 21; }
+bool dma_ok(const void *p, int64_t ld, int64_t cols) { return aligned16(p) && ld % 8 == 0 && cols % 8 == 0 && ld <= kMostDmaLd; }
 int ws_check(void *ws, size_t ws_bytes, size_t need)
 {
     if (need && (!ws || !aligned16(ws))) return CG_EINVAL;

@@ -61,3 +61,20 @@ def test_in_a_graph(pack):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(first, results))
         into()
+
+
+@pytest.mark.parametrize("K", [1 << 21, (1 << 21) + 8])
+def test_widest_rows_in_8_bits(K):
+    """x in 8 bits with the widest rows that are unpacked, and the next: whole numbers, bit for bit where columns begin and end."""
+    cg, M, N = _cg(), 1024, 256
+    g = torch.Generator("cuda").manual_seed(3)
+    codes = torch.randint(-3, 4, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    x = cg.Packed8(codes, torch.full((M, (K + 31) // 32), 133, dtype=torch.uint8, device="cuda"))
+    dz = torch.randint(-3, 4, (M, N), generator=g, device="cuda").bfloat16()
+    d = cg.cg_linear_desc(cg.CG_TYPE_BF16, M, N, K, 0, 0)
+    dw, db = torch.full((N, K), 7.0, device="cuda"), torch.full((N,), 7.0, device="cuda")
+    cg.cg_linear_bwd_weight(d, dz, x, dw, db, _ws(cg.cg_linear_workspace_bytes(d, cg.CG_PASS_BWD_WEIGHT)))
+    h = dz.float().cpu()
+    assert torch.equal(db.cpu(), h.sum(0))
+    for part in (slice(0, 520), slice(K // 2 - 300, K // 2 + 300), slice(K - 520, K)):
+        assert torch.equal(dw[:, part].cpu(), h.T @ codes[:, part].float().cpu())

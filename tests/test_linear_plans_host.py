@@ -58,3 +58,14 @@ def test_no_kernel_without_a_case():
             for packed in (False, True) if which == cg.CG_PASS_BWD_WEIGHT else (False,):
                 k = kind(dtype, which, whole, packed, M, K, N)
                 assert k[4] in (16, 256) or k in have, (k, M, K, N)
+
+
+def test_rows_too_far_apart_are_not_unpacked():
+    """x in 8 bits becomes a dense tensor whose rows lie K apart: as far as tiles of 256 take them and no further."""
+    M, N = 1024, 256
+    for K, unpacked in ((1 << 21, True), ((1 << 21) + 8, False), (1 << 24, False)):
+        d = desc("bf16", M, K, N)
+        assert cg.cg_debug_linear_plan(d, cg.CG_PASS_BWD_WEIGHT) == (256, 1, False)
+        assert (cg.cg_debug_linear_plan(d, cg.CG_PASS_BWD_WEIGHT, packed=True)[0] == 256) == unpacked, K
+        n = cg.cg_linear_workspace_bytes(d, cg.CG_PASS_BWD_WEIGHT)
+        assert n == 2 * M * K if unpacked else n < 1 << 20, K
