@@ -65,3 +65,24 @@ def test_a_run_repeats(dtype, keep):
     losses = tb.main(["--steps", "30", "--dtype", dtype, "--keep", keep])
     assert all(math.isfinite(x) for x in losses)
     assert tb.main(["--steps", "10", "--dtype", dtype, "--keep", keep]) == losses[:10]
+
+
+@pytest.mark.parametrize("keep", ["8bit", "tensors"])
+def test_gradients_of_the_whole_block_in_bf16(keep):
+    """bf16: a gradient has passed at most twelve tensors that were rounded (x, h, z, a, r, the logits, their gradient, dr, dz, dh, dx and a weight), each
+    off by 2^-8 of its length at most, and a product with a random matrix makes an error at most twice as long as what it belongs to: 24 / 256
+    of a gradient's length.  8 bits add half a step, 1/128 of a block's largest, in the two kept tensors that a gradient reads (h or a, and z), whose
+    length is at least a third of that: 6 / 256 at most."""
+    block = tb.Block(torch.bfloat16, keep, seed=3)
+    g = torch.Generator("cuda").manual_seed(2)
+    for n in ("b1", "b2", "bo", "beta"):
+        block.w[n].normal_(0, 0.3, generator=g)
+    tokens, target = tb.batch(6)
+    loss = block.loss_and_gradients(tokens, target)
+    w = {k: (t.bfloat16() if k in ("w1", "w2", "wo") else t).double().cpu().requires_grad_() for k, t in block.w.items()}
+    ref = plain_loss(tokens.cpu(), target.cpu(), w, False)
+    ref.backward()
+    assert abs(float(loss) - float(ref.detach())) < 24 / 256 * float(ref.detach())
+    for name, got in block.grad.items():
+        want = w[name].grad
+        assert float((got.double().cpu() - want).norm()) < (30 if keep == "8bit" else 24) / 256 * float(want.norm()), name
