@@ -384,7 +384,8 @@ int cg_dropout_add_layernorm_bwd(const cg_layernorm_desc *d, const cg_drop *drop
  * Arithmetic: bf16 tensors are multiplied as they are, the probabilities and the gradients of the scores rounded to bf16 for
  * their products; in two bf16 numbers where the terms are few: dq of a sequence of 64 keys or fewer, dk and dv of one of 32 query rows
  * or fewer (tokens times the heads that share keys, without a bias; tokens with one).  fp32 tensors are multiplied as three bf16 numbers
- * in six products (CG_MATH_FP32 above).
+ * in six products (CG_MATH_FP32 above, but unscaled: an operand below 2^-110 is off by up to 2^-134, one of 2^128 - 2^119 and more counts as
+ * infinite).
  * Sequences that reach past Tq, Tk are cut there; rows of no sequence are neither read nor written.  With numbers that do not
  * ascend nothing outside the tensors is read or written either, but what the outputs hold is not defined.
  * A q, k or v that is not finite makes what sees it not finite; within its own sequence it may do so to rows that a causal mask
@@ -450,7 +451,8 @@ int cg_unpack8(int type, int64_t rows, int64_t cols, const cg_packed8 *p, void *
  * leaves the gradient of z_in, which is the dz of the layer that z_in came from; NONE: of x itself.  RELU'(0) = 0.
  * M >= 0, N, K >= 1, each at most 2^26; of the products of two of them, tiles of 128 x 128, 2^22 at most; tensors may exceed 2^31 bytes.
  * Arithmetic: bf16 tensors are multiplied as they are and summed in fp32.  fp32 tensors are multiplied as three bf16 numbers in six products
- * (CG_MATH_FP32 above), up to 32 tokens forward in fp32 multiply-adds; what meets an operand that is not finite is not finite, as NaN where
+ * (CG_MATH_FP32 above, but unscaled: an operand below 2^-110 is off by up to 2^-134, one of 2^128 - 2^119 and more counts as infinite), up to
+ * 32 tokens forward in fp32 multiply-adds; what meets an operand that is not finite is not finite, as NaN where
  * multiply-adds may give an infinity. */
 enum { CG_ACT_NONE = 0, CG_ACT_RELU = 1, CG_ACT_GELU = 2, CG_ACT_SILU = 3 };
 typedef struct { int type; int64_t M, N, K; int act, act_in; } cg_linear_desc;

@@ -366,3 +366,21 @@ def test_far_rows(M):
     assert torch.equal(dw.cpu(), (dz.T @ values).float())
     cg.cg_linear_bwd_data(d, dzd, wd, None, None, x, _ws(cg.cg_linear_workspace_bytes(d, 1)))
     assert torch.equal(x.cpu(), (dz @ w).bfloat16())
+
+
+@pytest.mark.parametrize("M,K,N", [(100, 70, 72), (300, 1500, 330), (20, 70, 72)])
+def test_ends_of_the_range(M, K, N):
+    """fp32 operands near the smallest numbers, off by half of 2^-133 where their third piece ends there, and up to where they count as infinite."""
+    L, most = Layer("fp32", M, K, N, bias=False), float.fromhex("0x1.fefffep127")
+
+    def near(size_x, size_w, off):
+        h = dict(L.h)
+        for k, size in (("x", size_x), ("dz", size_x), ("w", size_w)):
+            h[k] = (h[k] * size).clamp(-most, most).float().double()
+            L.d[k].copy_(h[k])
+        y, _ = L.fwd()
+        bu.near(y, h["x"] @ h["w"].T, bu.sum_error(h["x"], h["w"].T) + off * h["w"].abs().sum(1) + bu.U * (h["x"] @ h["w"].T).abs(), "y")
+        bu.near(L.dx(), h["dz"] @ h["w"], bu.sum_error(h["dz"], h["w"]) + off * h["w"].abs().sum(0) + bu.U * (h["dz"] @ h["w"]).abs(), "dx")
+
+    near(2.0 ** -122, 2.0 ** 30, 2.0 ** -134)
+    near(2.0 ** 127, 2.0 ** -30, 0.0)          # many are clamped to the largest that has three pieces
