@@ -541,7 +541,6 @@ class Packed8:
         self._codes, self._scales, self.shape = codes, scales, codes.shape
         self.arg = cg_packed8(codes.data_ptr(), codes.stride(0) if rows > 1 else cols, scales.data_ptr(), scales.stride(0) if rows > 1 else (cols + 31) // 32)
 
-
     @property
     def codes(self):
         if self._codes is None:

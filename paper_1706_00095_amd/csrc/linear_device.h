@@ -27,7 +27,7 @@ struct GemmArgs {
     int R, C, K;
     int tiles_r, tiles_c, splits, chunk;      // k is cut into `splits` chunks (a multiple of a step each)
     float *part;                      // [splits][R][C] where there are several, then [splits][R] for the bias
-    float *dbias;                     // backward-weight, tiles of 128: sums of A over k as well; NULL: not wanted
+    float *dbias;                     // backward-weight, all tiles but those of 256: sums of A over k as well; NULL: not wanted
     EpiArgs epi;
 };
 
@@ -63,7 +63,8 @@ __device__ __forceinline__ float tail_of_normal(float z, float &e)
     return p * t * e;
 }
 // For bf16 results, whose own rounding is 2^-9: Phi(-a) = 2^G(a) with a G of degree 7 fitted by iterated least squares on 0 <= a <= 9, off by 1.3e-6 |z| and
-// by 2.6e-5 of a result down to z = -5.5 (1e-2 at -9, where it is 1e-18).  Half as many instructions, which a tile's epilogue waits for (8192 x 4096
+// by 2.6e-5 of a result down to z = -5.5, 1.8e-4 to -7, 1e-2 to -9 (where it is 1e-18) and a fourth to -11 (2e-27): from -8.5 on more than its own
+// rounding, of numbers below 1e-16.  Half as many instructions, which a tile's epilogue waits for (8192 x 4096
 // -> 16384: 876 us, 857 so).  From 15 on Phi(-a) is 0 and a is taken as 15, so that an infinity stays one.
 __device__ __forceinline__ float gelu_bf16(float z)
 {

@@ -384,3 +384,16 @@ def test_ends_of_the_range(M, K, N):
 
     near(2.0 ** -122, 2.0 ** 30, 2.0 ** -134)
     near(2.0 ** 127, 2.0 ** -30, 0.0)          # many are clamped to the largest that has three pieces
+
+
+def test_gelu_far_down_in_bf16():
+    """gelu of a bf16 result relative to itself where it is small: its rounding and what its power of two is off by there."""
+    cg = _cg()
+    z = torch.linspace(-9, 9, 16 * 128).view(128, 16).bfloat16().cuda()
+    y = torch.empty_like(z)
+    eye = torch.eye(16, device="cuda").bfloat16()
+    cg.cg_linear_fwd(cg.linear_desc(z, eye, "gelu"), z, eye, None, None, y, None, _ws(cg.cg_linear_workspace_bytes(cg.linear_desc(z, eye, "gelu"), 0)))
+    v = z.double().cpu()
+    want = v * torch.erfc(-v / 2 ** 0.5) / 2          # as far down as 64 bits go
+    off = torch.where(v > -5.5, 2.6e-5, torch.where(v > -7, 1.8e-4, 1e-2)) + 4 * bu.U
+    bu.near(y, want, (off * (1 + bu.half_step(torch.bfloat16)) + bu.half_step(torch.bfloat16)) * want.abs(), "gelu")
